@@ -365,6 +365,173 @@ int moe_ovl_return_slots_static(int32_t device, int32_t num_src_ranks, int32_t t
                                 const int32_t *src_rank, const int32_t *src_token, int32_t *slot_out,
                                 int32_t *rows_per_rank_out, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators around the expert layer: the norm in front of it, the router that makes its expert ids and gates, and
+ * experts whose weights and activations are held in 8 bits.  They need no context: every call names its device, takes
+ * DEVICE pointers, enqueues its kernels on args->stream and returns; nothing is allocated, nothing is waited for, the
+ * calling thread's current device is left as it was, and a call can be captured in a CUDA graph.  Matrices are row-major
+ * with a stride between rows (in elements) of their own; columns lie next to each other.  Strides and pointers that are not
+ * multiples of 16 bytes are accepted unless stated otherwise; multiples of 16 are faster.  A call with no rows does
+ * nothing (moe_ovl_route still clears its counts, moe_ovl_add_norm_backward its weight gradient). */
+
+enum { MOE_OVL_BF16 = 0, MOE_OVL_F16 = 1, MOE_OVL_F32 = 2 };
+#define MOE_OVL_MAX_ROW 32768      /* widest row of the row operators (d, F) */
+#define MOE_OVL_MAX_ROUTED 1024    /* most experts of the router */
+#define MOE_OVL_MAX_TOP_K 32
+#define MOE_OVL_MAX_QUANT_K 131056 /* longest reduction of the 8-bit product: 131056 * 128 * 128 still fits 32 bits */
+
+/* RMS norm of a sum:  h = x + residual, rounded to the type of x (h = x without a residual);
+ *   rstd = 1 / sqrt(mean(h^2) + eps);  v = (h * rstd) * weight, in 32 bits.
+ * Any of: residual_out = h;  y = v rounded to the type of x;  q, scale = v in 8 bits, scale = max|v| / 127 of the row and
+ * q = v * 127 / max|v| to the nearest, ties to even, so v ~ q * scale (a row whose max|v| is below 2^-100 gives zeros);
+ * rstd, for the backward pass.  The norm is taken of the ROUNDED sum: it is what the next layer and the backward pass see.
+ * A row that holds a NaN or an infinity gets y and scale NaN where it must and q = 0.  residual_out may be
+ * residual or x itself, y may be x or residual: with the same stride. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, d;              /* 1 <= d <= MOE_OVL_MAX_ROW */
+    int32_t dtype;                /* MOE_OVL_BF16 ...: type of x, residual, residual_out, y */
+    int32_t weight_dtype;         /* that type, or MOE_OVL_F32 */
+    float eps;                    /* >= 0 */
+    uint32_t flags;               /* 0 */
+    const void *x;
+    const void *residual;         /* or NULL */
+    const void *weight;           /* [d] */
+    void *residual_out;           /* or NULL */
+    void *y;                      /* or NULL */
+    int8_t *q;                    /* or NULL, as scale */
+    float *scale;                 /* [rows] */
+    float *rstd;                  /* [rows] or NULL */
+    int64_t x_stride, residual_stride, residual_out_stride, y_stride, q_stride;
+    void *stream;
+} moe_ovl_norm_args;
+int moe_ovl_add_norm(const moe_ovl_norm_args *args);
+
+/* Its gradient.  With n = h * rstd and g = dy * weight:
+ *   dx = rstd * (g - n * mean(g * n)) (+ d_residual), the gradient of x and of the residual alike: d_residual is what
+ *        arrives at residual_out from the layers behind;
+ *   dweight = sum over the rows of dy * n, in 32 bits and in a fixed order (the same call gives the same bits).
+ * dx may be dy or d_residual itself with the same stride.  dweight (and then the workspace) may be NULL. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, d;
+    int32_t dtype;                /* of dy, h, d_residual, dx */
+    int32_t weight_dtype;
+    const void *dy;
+    const void *h;                /* what the forward pass normalised: residual_out, or x without a residual */
+    const void *weight;
+    const float *rstd;            /* [rows] from the forward pass */
+    const void *d_residual;       /* or NULL */
+    void *dx;
+    float *dweight;               /* [d] or NULL */
+    void *workspace;              /* DEVICE, 16-byte aligned; contents need not be kept or cleared */
+    size_t workspace_bytes;       /* >= moe_ovl_add_norm_workspace_bytes */
+    int64_t dy_stride, h_stride, d_residual_stride, dx_stride;
+    void *stream;
+} moe_ovl_norm_backward_args;
+int moe_ovl_add_norm_workspace_bytes(int32_t rows, int32_t d, size_t *bytes);
+int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *args);
+
+/* Gated activation between an expert's two products: v = g / (1 + exp(-g)) * u with g = gate_up[:, :F] and
+ * u = gate_up[:, F:2F] (the layout that w1 of moe_ovl_args gives), in 8 bits with a scale per row as above. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, f;              /* 1 <= f <= MOE_OVL_MAX_ROW */
+    int32_t dtype;                /* of gate_up */
+    uint32_t flags;               /* 0 */
+    const void *gate_up;          /* [rows, 2F] */
+    int8_t *q;                    /* [rows, F] */
+    float *scale;                 /* [rows] */
+    int64_t gate_up_stride, q_stride;
+    void *stream;
+} moe_ovl_swiglu_args;
+int moe_ovl_swiglu_quant(const moe_ovl_swiglu_args *args);
+
+/* Router: the top_k experts of every row of logits, and their gates.
+ *   score_i  = exp(l_i - max l) / sum_j exp(l_j - max l)   (MOE_OVL_SCORE_SOFTMAX)
+ *            = 1 / (1 + exp(-l_i))                         (MOE_OVL_SCORE_SIGMOID)
+ *   choice_i = score_i + bias_i: the bias balances the load and enters the choice only.
+ * With num_groups > 1 the experts form that many equal runs; a group's value is the sum of its group_best largest
+ * choices, and only the experts of the top_groups best groups can be chosen.  The top_k largest choices are taken in
+ * descending order; ties, between groups too, go to the lowest index.  Scores rise with their logits, so without a
+ * bias and with group_best = 1 the logits themselves are compared.
+ *   gate = gate_scale * score, or with renormalise gate_scale * score / (sum of the row's chosen scores)
+ *          (softmax: computed as the softmax of the chosen logits; 0 where that sum is 0).
+ * A logit (or a bias) that is -inf or NaN masks its expert: score 0, never chosen.  +inf counts as the largest finite value.
+ * Slots for which no expert is left hold expert -1 and gate 0. */
+enum { MOE_OVL_SCORE_SOFTMAX = 0, MOE_OVL_SCORE_SIGMOID = 1 };
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, num_experts;    /* 1 <= num_experts <= MOE_OVL_MAX_ROUTED */
+    int32_t top_k;                /* 1 .. min(num_experts, MOE_OVL_MAX_TOP_K) */
+    int32_t dtype;                /* of logits */
+    int32_t score;                /* MOE_OVL_SCORE_* */
+    int32_t num_groups;           /* >= 1, divides num_experts, at most 32 */
+    int32_t top_groups;           /* 1 .. num_groups */
+    int32_t group_best;           /* 1 or 2 */
+    int32_t renormalise;          /* 0 or 1 */
+    float gate_scale;
+    const void *logits;
+    const float *bias;            /* [num_experts] or NULL */
+    int32_t *expert;              /* [rows, top_k], contiguous */
+    float *gate;                  /* [rows, top_k], contiguous */
+    int32_t *counts;              /* [num_experts] or NULL: how often each expert was chosen; overwritten */
+    int64_t logits_stride;
+    void *stream;
+} moe_ovl_route_args;
+int moe_ovl_route(const moe_ovl_route_args *args);
+
+/* Its gradient: dlogits of sum(gate * dgate), the choice held fixed.  Slots with expert -1 (or outside the range) add nothing.
+ * dlogits is overwritten, zeros included; it may be logits itself with the same stride. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, num_experts, top_k, dtype, score, renormalise;
+    float gate_scale;
+    uint32_t flags;               /* 0 */
+    const void *logits;
+    const int32_t *expert;        /* [rows, top_k] of the forward pass */
+    const float *dgate;           /* [rows, top_k] */
+    void *dlogits;                /* type of logits */
+    int64_t logits_stride, dlogits_stride;
+    void *stream;
+} moe_ovl_route_backward_args;
+int moe_ovl_route_backward(const moe_ovl_route_backward_args *args);
+
+#define MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS 1u /* test hook: no tile is ever loaded, so the bounded waits run out */
+/* Product of 8-bit integers with a scale for each token and for each channel:
+ *   out[m][n] = (sum_k a[m][k] * b[e][n][k]) * a_scale[m] * b_scale[e][n]
+ * The sum is exact (32-bit integers), scaled in 32 bits and rounded once.  Without expert_counts there is one matrix b.
+ * With expert_counts the rows of a are grouped by expert as in moe_ovl_args: the first expert_counts[0] rows meet b[0],
+ * and so on; rows beyond their sum are left as they were, counts beyond `rows` are cut (negative ones count as 0).
+ * a and b: 16-byte aligned, strides multiples of 16, k a multiple of 16; otherwise MOE_OVL_ERR_UNSUPPORTED.
+ * status: [4] of DEVICE memory that the caller clears once and may share between calls on one stream; status[0] becomes
+ * MOE_OVL_ERR_TIMEOUT when a bounded wait inside a kernel gave up (the outputs are then unspecified, written in bounds, and
+ * later calls with the same status may give up early, until the caller clears it). */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, n, k;           /* 1 <= k <= MOE_OVL_MAX_QUANT_K */
+    int32_t num_experts;          /* 0: one matrix b [n, k]; else b [num_experts, n, k], at most 1024 */
+    int32_t out_dtype;
+    int32_t wait_timeout_us;      /* bound on every device-side wait; 0 = default (2 s) */
+    uint32_t flags;               /* 0, or MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS */
+    const int8_t *a;              /* [rows, k] */
+    const float *a_scale;         /* [rows] */
+    const int8_t *b;              /* expert e's row n starts at (e * n + its row) * b_stride */
+    const float *b_scale;         /* [max(num_experts, 1), n] */
+    const int32_t *expert_counts; /* [num_experts], NULL without experts */
+    void *out;                    /* [rows, n] */
+    int32_t *status;
+    int64_t a_stride, b_stride, out_stride;
+    void *stream;
+} moe_ovl_quant_matmul_args;
+int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *args);
+
 const char *moe_ovl_strerror(int code);
 /* cudaError_t of the last failing CUDA call made through this context (0 if none). */
 int moe_ovl_last_cuda_error(const moe_ovl_ctx *ctx);

@@ -36,6 +36,8 @@ EXPORTS = [
     "moe_ovl_expert_return_host", "moe_ovl_host_join", "moe_ovl_query_status", "moe_ovl_get_report", "moe_ovl_get_plan",
     "moe_ovl_get_sm_map", "moe_ovl_get_gemm_time", "moe_ovl_read_buffer", "moe_ovl_destroy", "moe_ovl_strerror", "moe_ovl_last_cuda_error",
     "moe_ovl_return_slots_static", "moe_ovl_get_trace",
+    "moe_ovl_add_norm", "moe_ovl_add_norm_workspace_bytes", "moe_ovl_add_norm_backward", "moe_ovl_swiglu_quant",
+    "moe_ovl_route", "moe_ovl_route_backward", "moe_ovl_quant_matmul",
 ]
 
 
@@ -140,6 +142,10 @@ def load(rebuild_if_stale: bool = True) -> C.CDLL:
     lib.moe_ovl_destroy.argtypes = [C.c_void_p]
     lib.moe_ovl_last_cuda_error.argtypes = [C.c_void_p]
     lib.moe_ovl_return_slots_static.argtypes = [C.c_int32] * 5 + [C.c_void_p] * 6
+    lib.moe_ovl_add_norm_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+    for name in ("moe_ovl_add_norm", "moe_ovl_add_norm_backward", "moe_ovl_swiglu_quant", "moe_ovl_route",
+                 "moe_ovl_route_backward", "moe_ovl_quant_matmul"):
+        getattr(lib, name).argtypes = [C.c_void_p]
     _lib = lib
     return lib
 

@@ -8,8 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe_ovl.so")
-SOURCES = ["moe_ovl.cu", "noalloc.cu"]
-HEADERS = ["common.cuh", "plan.cuh", "producer.cuh", "mover.cuh", os.path.join("..", "..", "include", "moe_ovl.h")]
+SOURCES = ["moe_ovl.cu", "noalloc.cu", "rowops.cu", "route.cu", "quant_matmul.cu"]
+HEADERS = ["common.cuh", "plan.cuh", "producer.cuh", "mover.cuh", "ptx.cuh", "opcommon.cuh", os.path.join("..", "..", "include", "moe_ovl.h")]
 
 
 def _nvcc() -> str:
@@ -31,7 +31,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     tmp = LIB + f".{os.getpid()}.tmp"
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
+    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "--threads", "0",
            "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]

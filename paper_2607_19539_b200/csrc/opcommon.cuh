@@ -1,0 +1,88 @@
+// Shared by the operators that need no context: element types, vectors of 16 bytes, reductions over the threads of a row,
+// and the guard that leaves the caller's current device as it was.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/moe_ovl.h"
+
+namespace moe_ovl {
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// VEC neighbouring elements; one load or store of 16 bytes where VEC * sizeof(T) is 16, in general of their size.
+template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
+
+template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_pack(const T *p)
+{
+    Pack<T, VEC> r;
+    if constexpr (sizeof(r) == 16) *reinterpret_cast<uint4 *>(&r) = *reinterpret_cast<const uint4 *>(p);
+    else r = *reinterpret_cast<const Pack<T, VEC> *>(p);
+    return r;
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_pack(T *p, const Pack<T, VEC> &r)
+{
+    if constexpr (sizeof(r) == 16) *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(&r);
+    else *reinterpret_cast<Pack<T, VEC> *>(p) = r;
+}
+
+// The larger of two; NaN where either is.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// Makes `device` current for one call and puts the caller's device back.
+struct DeviceGuard {
+    int before = -1;
+    bool ok = false;
+    explicit DeviceGuard(int device)
+    {
+        if (cudaGetDevice(&before) != cudaSuccess) return;
+        ok = before == device || cudaSetDevice(device) == cudaSuccess;
+        if (before == device) before = -1;
+    }
+    ~DeviceGuard()
+    {
+        if (before >= 0) cudaSetDevice(before);
+    }
+};
+
+inline int launched() { return cudaGetLastError() == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA; }
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline bool known_dtype(int t) { return t == MOE_OVL_BF16 || t == MOE_OVL_F16 || t == MOE_OVL_F32; }
+inline int dtype_bytes(int t) { return t == MOE_OVL_F32 ? 4 : 2; }
+
+// Calls f with a value of the element type.
+template <typename F> int with_dtype(int t, F f)
+{
+    if (t == MOE_OVL_BF16) return f(__nv_bfloat16());
+    if (t == MOE_OVL_F16) return f(__half());
+    return f(0.0f);
+}
+
+}  // namespace moe_ovl
