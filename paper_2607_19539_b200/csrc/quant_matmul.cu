@@ -93,9 +93,10 @@ template <int BN> struct QmShape {
 };
 
 // A give-up leaves copies in flight: they have to land before the CTA's shared memory goes.  Bounded.
-__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
 {
-    for (int i = 0; i < (1 << 20) && !mbar_try_wait(bar, parity); ++i) {}
+    const unsigned long long t0 = globaltimer_ns();
+    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 < limit_ns) {}
 }
 
 // One tile (128 channels x BN tokens) per cluster; the cluster's CTAs share its K.
@@ -151,7 +152,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
             if (issued < k1 - k0) {
                 // gave up
                 for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
-                    drain(bar_full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u);
+                    drain(bar_full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, p.timeout_ns);
             }
         } else if (warp == 1 && lane == 0) {
             int stage = 0;
@@ -226,6 +227,223 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     if (warp == 1) tmem_dealloc_self(tmem, TMEM_COLS);
 }
 
+// ------------------------------------------------------------------ large products: CTA pairs
+
+constexpr int QP_ROWS = 256;                 // channels per tile: 128 in each CTA of the pair
+constexpr int QP_TOKENS = 256;               // tokens per tile: each CTA loads half of them
+constexpr int QP_STAGE_BYTES = QM_A_BYTES + QP_TOKENS / 2 * QM_K;
+constexpr int QP_STAGES = 6;
+constexpr int QP_THREADS = 320;              // load warp, MMA warp, 8 epilogue warps
+constexpr int QP_GROUP = 16;                 // token tiles that are worked on side by side, see QpSchedule
+constexpr int QP_SMEM = QP_STAGES * QP_STAGE_BYTES + 1024 + 256;
+
+// Order of the tiles: experts one after the other; inside an expert up to QP_GROUP token tiles form a group, and for each tile
+// of channels all token tiles of the group come next to each other.  The CTA pairs that run side by side then share one
+// tile of weights in L2, and the weights are read from HBM once per group (4096 tokens).  Every pair takes every
+// gridDim/2-th tile, so a role only ever moves forward through the experts.
+struct QpSchedule {
+    const int *tile_start, *row_start;       // [experts + 1] token tiles and rows before each expert, in shared memory
+    int row_tiles, expert = 0;
+    struct Tile { int expert, channel0, row0, rows; };
+    __device__ long long total(int experts) const { return (long long)tile_start[experts] * row_tiles; }
+    __device__ Tile at(long long index)
+    {
+        while (index >= (long long)tile_start[expert + 1] * row_tiles) ++expert;
+        const int tiles = tile_start[expert + 1] - tile_start[expert];
+        const int i = (int)(index - (long long)tile_start[expert] * row_tiles);
+        const int group = i / (QP_GROUP * row_tiles), first = group * QP_GROUP, wide = min(QP_GROUP, tiles - first);
+        const int j = i - group * QP_GROUP * row_tiles;
+        const int row0 = row_start[expert] + (first + j % wide) * QP_TOKENS;
+        return {expert, j / wide * QP_ROWS, row0, min(QP_TOKENS, row_start[expert + 1] - row0)};
+    }
+};
+
+// One warp fills the schedule's tables; counts are cut so that no tile reaches beyond the rows there are.
+__device__ void fill_schedule(const QmP &p, int *tile_start, int *row_start, int lane)
+{
+    if (!p.counts) {
+        if (lane == 0) {
+            tile_start[0] = row_start[0] = 0;
+            tile_start[1] = (p.rows + QP_TOKENS - 1) / QP_TOKENS;
+            row_start[1] = p.rows;
+        }
+        return;
+    }
+    long long rows_before = 0;
+    int tiles_before = 0;
+    if (lane == 0) tile_start[0] = row_start[0] = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += 32) {
+        const int e = e0 + lane;
+        long long upto = e < p.experts ? max(p.counts[e], 0) : 0;
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const long long last = min(rows_before + upto, (long long)p.rows);
+        long long first = __shfl_up_sync(0xffffffffu, last, 1);
+        if (lane == 0) first = rows_before;
+        int tiles = ((int)(last - first) + QP_TOKENS - 1) / QP_TOKENS;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, tiles, o);
+            if (lane >= o) tiles += v;
+        }
+        if (e < p.experts) {
+            tile_start[e + 1] = tiles_before + tiles;
+            row_start[e + 1] = (int)last;
+        }
+        tiles_before += __shfl_sync(0xffffffffu, tiles, 31);
+        rows_before = __shfl_sync(0xffffffffu, last, 31);
+    }
+}
+
+// Persistent, one CTA per SM, pairs of CTAs share every matrix instruction (cta_group::2): 256 channels x 256 tokens, each CTA
+// holding its 128 channels and HALF of the tokens, which halves the operand bytes per SM against single CTAs -- at
+// 8 bits the tensor cores eat operands as fast as at 16, and that traffic out of L2 is what bounds the other kernel on large products.
+// Accumulators are double buffered (2 x 256 columns of tensor memory): a tile is scaled and stored while the next one runs.
+template <typename Out>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(QP_THREADS, 1)
+quant_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const QmP p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int s_tile_start[1025], s_row_start[1025];
+    __shared__ uint32_t s_tmem;
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bar_full = smem_base + QP_STAGES * QP_STAGE_BYTES, bar_empty = bar_full + 8 * QP_STAGES;
+    const uint32_t bar_tfull = bar_empty + 8 * QP_STAGES, bar_tempty = bar_tfull + 16, bar_drain = bar_tempty + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const uint32_t lead_full = map_to_cta(bar_full, 0), lead_tempty = map_to_cta(bar_tempty, 0);
+
+    if (warp == 0) {
+        fill_schedule(p, s_tile_start, s_row_start, lane);
+    } else if (warp == 1) {
+        tmem_alloc(smem_u32(&s_tmem), 512);
+    } else if (threadIdx.x == 64) {
+        for (int i = 0; i < QP_STAGES; ++i) {
+            mbar_init(bar_full + 8 * i, 1);           // the leader's load thread arrives, expecting both CTAs' bytes
+            mbar_init(bar_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_tfull + 8 * i, 1);
+            mbar_init(bar_tempty + 8 * i, 16);        // one arrival per epilogue warp of both CTAs
+        }
+        mbar_init(bar_drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    QpSchedule sched{s_tile_start, s_row_start, (p.n + QP_ROWS - 1) / QP_ROWS};
+    const long long total = sched.total(p.experts > 0 ? p.experts : 1);
+    const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    const int ksteps = (p.k + QM_K - 1) / QM_K;
+
+    if (warp == 0) {
+        if (lane == 0 && !p.no_loads) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            long long issued = 0;
+            for (long long t = first; ok && t < total; t += step) {
+                const QpSchedule::Tile tile = sched.at(t);
+                const int y_b = tile.expert * p.n + tile.channel0 + (int)rank * QM_ROWS;
+                const int y_a = tile.row0 + (int)rank * ((tile.rows + 31) / 32 * 16);       // second half of the tile's tokens
+                for (int k = 0; k < ksteps; ++k, ++issued) {
+                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, t)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t sa = smem_base + stage * QP_STAGE_BYTES, full = lead_full + 8 * stage;
+                    if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, 2 * QP_STAGE_BYTES);
+                    tma_load_2d(sa, &map_b, full, k * QM_K, y_b);
+                    tma_load_2d(sa + QM_A_BYTES, &map_a, full, k * QM_K, y_a);
+                    if (++stage == QP_STAGES) stage = 0, phase ^= 1u;
+                }
+            }
+            if (!ok && rank == 0) {
+                // gave up: wait for the copies of both CTAs (the peer stays until the cluster barrier at the end)
+                for (long long i = issued > QP_STAGES ? issued - QP_STAGES : 0; i < issued; ++i)
+                    drain(bar_full + 8 * (uint32_t)(i % QP_STAGES), (uint32_t)(i / QP_STAGES) & 1u, p.timeout_ns);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true;
+            for (long long t = first; ok && t < total; t += step) {
+                // fewer tokens than a full tile: a narrower instruction
+                const uint32_t idesc = umma_idesc_i8(2 * QM_ROWS, (sched.at(t).rows + 31) / 32 * 32);
+                ok = mbar_wait<true>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_QM_DONE, t);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)(acc * QP_TOKENS);
+                for (int k = 0; k < ksteps; ++k) {
+                    ok = mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, t);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_base + stage * QP_STAGE_BYTES;
+                    const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sa + QM_A_BYTES);
+#pragma unroll
+                    for (int i = 0; i < QM_K / 32; ++i)
+                        umma_i8<2>(d, da + (uint64_t)(i * 2), db + (uint64_t)(i * 2), idesc, (k | i) != 0 ? 1u : 0u);
+                    umma_commit_pair(bar_empty + 8 * stage);
+                    if (++stage == QP_STAGES) stage = 0, phase ^= 1u;
+                }
+                if (!ok) break;
+                umma_commit_pair(bar_tfull + 8 * acc);
+                if ((acc ^= 1) == 0) acc_phase ^= 1u;
+            }
+            umma_commit_self(bar_drain);                // every MMA has finished before tensor memory goes
+            drain(bar_drain, 0, p.timeout_ns);
+        }
+        __syncwarp();
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;          // lanes 32 * quarter .., every other 32 columns
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (long long t = first; t < total; t += step) {
+            const QpSchedule::Tile tile = sched.at(t);
+            const int ch = tile.channel0 + (int)rank * QM_ROWS + quarter * 32 + lane;
+            const bool in = ch < p.n;
+            const float bs = in ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
+            // a warp leaves the loop as one: what follows needs all of its lanes
+            if (!__all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * acc, acc_phase, p, SITE_QM_DONE, t))) break;
+            tc_fence_after();
+            for (int c = half * 32; c < tile.rows; c += 64) {
+                uint32_t v[32];
+                const float as_lane = c + lane < tile.rows ? p.a_scale[tile.row0 + c + lane] : 0.0f;
+                tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * QP_TOKENS + c), v);
+                tmem_ld_wait();
+                Out *out = static_cast<Out *>(p.out) + (long long)(tile.row0 + c) * p.out_stride + ch;
+                const int left = tile.rows - c;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float as = __shfl_sync(0xffffffffu, as_lane, j);
+                    if (in && j < left) store_scaled(out, (int)v[j], as, bs);
+                    out += p.out_stride;
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (rank == 0) mbar_arrive(bar_tempty + 8 * acc);
+                else mbar_arrive_cluster(lead_tempty + 8 * acc);
+            }
+            if ((acc ^= 1) == 0) acc_phase ^= 1u;
+        }
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();          // the peer no longer signals this CTA's barriers or reads its operands
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
@@ -267,6 +485,18 @@ template <typename K> bool allow_smem(K kernel, int bytes, int device, std::atom
     return true;
 }
 
+int sm_count(int device)
+{
+    static std::atomic<int> known[64];
+    if (device >= 64) return 148;
+    int n = known[device].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 2) return 2;
+        known[device].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 template <int BN, typename Out> int launch_split(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
 {
     constexpr int smem = QmShape<BN>::SMEM;
@@ -288,6 +518,14 @@ template <int BN, typename Out> int launch_split(const QmP &p, const CUtensorMap
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, quant_matmul_kernel<BN, Out>, b, a, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
+}
+
+template <typename Out> int launch_pair(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
+{
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(quant_matmul_pair_kernel<Out>, QP_SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    quant_matmul_pair_kernel<Out><<<sm_count(device) / 2 * 2, QP_THREADS, QP_SMEM, stream>>>(b, a, p);
+    return launched();
 }
 
 }  // namespace
@@ -320,11 +558,13 @@ extern "C" int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *a)
     // K is shared where the tiles alone would leave SMs idle
     const long long tiles = (long long)p.row_tiles * ((per_group + bn - 1) / bn) * std::max(1, std::min(a->num_experts, a->rows));
     while (p.splits < 8 && tiles * p.splits * 2 <= 296 && p.splits * 2 <= (a->k + QM_K - 1) / QM_K) p.splits *= 2;
+    const bool pair = per_group > 256;
     CUtensorMap map_b, map_a;
-    if (!encode_bytes(&map_b, a->b, b_rows, a->k, sb, QM_ROWS) || !encode_bytes(&map_a, a->a, a->rows, a->k, sa, bn)) return MOE_OVL_ERR_CUDA;
+    if (!encode_bytes(&map_b, a->b, b_rows, a->k, sb, QM_ROWS) || !encode_bytes(&map_a, a->a, a->rows, a->k, sa, pair ? QP_TOKENS / 2 : bn)) return MOE_OVL_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
     return with_dtype(a->out_dtype, [&](auto t) {
         using Out = decltype(t);
+        if (pair) return launch_pair<Out>(p, map_b, map_a, a->device, stream);
         switch (bn) {
         case 16: return launch_split<16, Out>(p, map_b, map_a, a->device, stream);
         case 32: return launch_split<32, Out>(p, map_b, map_a, a->device, stream);
