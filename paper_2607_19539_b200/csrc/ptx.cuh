@@ -186,6 +186,21 @@ __device__ __forceinline__ uint64_t umma_smem_desc(uint32_t saddr)
     return d;
 }
 
+// One lane of the (converged) warp, the same one every time.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+// A value that is the same in all lanes anyway, in a form from which the compiler can tell.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // ------------------------------------------------------------------ one CTA on its own (cta_group::1)
 
 __device__ __forceinline__ void tma_load_2d_self(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)

@@ -27,7 +27,6 @@ enum : long long { SITE_QM_EMPTY = 32, SITE_QM_FULL, SITE_QM_DONE };
 struct QmP {
     int rows, n, k, experts;                 // experts 0: one matrix
     int row_tiles;                           // tiles of QM_ROWS channels per expert
-    int splits;                              // CTAs of a cluster that share a tile's K
     const int *counts;
     const float *a_scale, *b_scale;
     void *out;
@@ -39,42 +38,51 @@ struct QmP {
 
 struct QmTile { int expert, row0, rows; };   // rows 0: beyond the last tile
 
-// The `index`-th tile of at most `height` tokens, experts in order.  One warp; every lane gets the answer.  Counts are
-// cut so that no tile reaches beyond the rows there are.
-__device__ QmTile find_tile(const QmP &p, int index, int height, int lane)
+// Inclusive sums over the lanes, none above `limit` (< 2^31; nor is v).  A loop, not unrolled: this runs once, before anything else
+// can, and every line of its code is fetched from memory then.
+__device__ __forceinline__ unsigned scan_up_to(unsigned v, unsigned limit, int lane)
+{
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned w = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v = min(v + w, limit);
+    }
+    return v;
+}
+
+// Rows of 32 experts from e0 on, one per lane: where each one's rows begin and end, given the rows before.  Counts are cut
+// so that no expert reaches beyond the rows there are.
+__device__ __forceinline__ void expert_rows(int count, unsigned limit, unsigned before, int lane, unsigned &first, unsigned &last)
+{
+    last = min(before + scan_up_to(min((unsigned)max(count, 0), limit), limit, lane), limit);
+    first = __shfl_up_sync(0xffffffffu, last, 1);
+    if (lane == 0) first = before;
+}
+__device__ __forceinline__ int count_of(const QmP &p, int e) { return p.counts && e < p.experts ? p.counts[e] : 0; }
+
+// The `index`-th tile of at most `height` tokens, experts in order.  One warp; every lane gets the answer.  `count`: count_of(lane).
+__device__ QmTile find_tile(const QmP &p, int index, int height, int count, int lane)
 {
     if (!p.counts) {
         const long long row0 = (long long)index * height;
         if (row0 >= p.rows) return {0, 0, 0};
         return {0, (int)row0, min(height, p.rows - (int)row0)};
     }
-    long long rows_before = 0;
-    int tiles_before = 0;
+    unsigned rows_before = 0, tiles_before = 0;
+#pragma unroll 1
     for (int e0 = 0; e0 < p.experts; e0 += 32) {
-        const int e = e0 + lane;
-        long long upto = e < p.experts ? max(p.counts[e], 0) : 0;      // inclusive sums over the lanes
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const long long last = min(rows_before + upto, (long long)p.rows);
-        long long first = __shfl_up_sync(0xffffffffu, last, 1);
-        if (lane == 0) first = rows_before;
-        const int mine = (int)(last - first), tiles = (mine + height - 1) / height;
-        int tiles_upto = tiles;
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, tiles_upto, o);
-            if (lane >= o) tiles_upto += v;
-        }
-        const int start = tiles_before + tiles_upto - tiles;
-        const unsigned hit = __ballot_sync(0xffffffffu, index >= start && index < start + tiles);
+        unsigned first, last;
+        expert_rows(e0 == 0 ? count : count_of(p, e0 + lane), (unsigned)p.rows, rows_before, lane, first, last);
+        const unsigned tiles = (last - first + height - 1) / height;
+        const unsigned start = tiles_before + scan_up_to(tiles, 0x7fffffffu, lane) - tiles;
+        const unsigned hit = __ballot_sync(0xffffffffu, (unsigned)index >= start && (unsigned)index < start + tiles);
         if (hit) {
             const int owner = __ffs(hit) - 1;
-            const int r = __shfl_sync(0xffffffffu, (int)first + (index - start) * height, owner);
-            const int end = __shfl_sync(0xffffffffu, (int)last, owner);
+            const int r = (int)__shfl_sync(0xffffffffu, first + (index - start) * height, owner);
+            const int end = (int)__shfl_sync(0xffffffffu, last, owner);
             return {e0 + owner, r, min(height, end - r)};
         }
-        tiles_before += __shfl_sync(0xffffffffu, tiles_upto, 31);
+        tiles_before = __shfl_sync(0xffffffffu, start + tiles, 31);
         rows_before = __shfl_sync(0xffffffffu, last, 31);
     }
     return {0, 0, 0};
@@ -99,8 +107,19 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned lo
     while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 < limit_ns) {}
 }
 
-// One tile (128 channels x BN tokens) per cluster; the cluster's CTAs share its K.
-template <int BN, typename Out>
+// A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const QmP &p, long long index, int lane)
+{
+    bool ok = true;
+    if (lane == 0) ok = mbar_wait(bar, parity, p, SITE_QM_DONE, index);
+    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    if (ok) mbar_try_wait(bar, parity);      // done already: this lane's own look, for the order of what it reads next
+    return ok;
+}
+
+// Few tiles: one tile (128 channels x BN tokens) per cluster, whose SPLITS CTAs share its K.  Each leaves its part in its shared
+// memory, and the tokens are dealt out for the sum and the scaling.
+template <int BN, int SPLITS, typename Out>
 __global__ void __launch_bounds__(QM_THREADS)
 quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const QmP p)
 {
@@ -110,13 +129,13 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     __shared__ uint32_t s_tmem;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar_full = smem_base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES, bar_done = bar_empty + 8 * STAGES;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)(blockIdx.x % (unsigned)p.splits);
-    const unsigned tile_index = blockIdx.x / (unsigned)p.splits;
+    const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
+    const int rank = (int)(blockIdx.x % SPLITS);
+    const unsigned tile_index = blockIdx.x / SPLITS;
     const int row_tile = (int)(tile_index % (unsigned)p.row_tiles);
 
     if (warp == 0) {
-        const QmTile t = find_tile(p, (int)(tile_index / (unsigned)p.row_tiles), BN, lane);
+        const QmTile t = find_tile(p, (int)(tile_index / (unsigned)p.row_tiles), BN, count_of(p, lane), lane);
         if (lane == 0) s_tile = t;
     } else if (warp == 1) {
         tmem_alloc_self(smem_u32(&s_tmem), TMEM_COLS);
@@ -131,22 +150,25 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const QmTile tile = s_tile;
-    const uint32_t tmem = s_tmem;
+    const QmTile tile = {uniform(s_tile.expert), uniform(s_tile.row0), uniform(s_tile.rows)};
+    const uint32_t tmem = uniform(s_tmem);
     const int steps_all = (p.k + QM_K - 1) / QM_K;
-    const int k0 = steps_all * rank / p.splits, k1 = steps_all * (rank + 1) / p.splits;
+    const int k0 = steps_all * rank / SPLITS, k1 = steps_all * (rank + 1) / SPLITS;
     if (tile.rows > 0) {
-        if (warp == 0 && lane == 0 && !p.no_loads) {
+        if (warp == 0 && !p.no_loads) {
+            const bool leader = elect_one();
             const int y_b = tile.expert * p.n + row_tile * QM_ROWS;
             int stage = 0;
             uint32_t phase = 0;
             int issued = 0;
             for (int k = k0; k < k1; ++k, ++issued) {
-                if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, k)) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, k))) break;
                 const uint32_t sa = smem_base + stage * STAGE_BYTES;
-                mbar_arrive_expect_tx(bar_full + 8 * stage, STAGE_BYTES);
-                tma_load_2d_self(sa, &map_b, bar_full + 8 * stage, k * QM_K, y_b);
-                tma_load_2d_self(sa + QM_A_BYTES, &map_a, bar_full + 8 * stage, k * QM_K, tile.row0);
+                if (leader) {
+                    mbar_arrive_expect_tx(bar_full + 8 * stage, STAGE_BYTES);
+                    tma_load_2d_self(sa, &map_b, bar_full + 8 * stage, k * QM_K, y_b);
+                    tma_load_2d_self(sa + QM_A_BYTES, &map_a, bar_full + 8 * stage, k * QM_K, tile.row0);
+                }
                 if (++stage == STAGES) stage = 0, phase ^= 1u;
             }
             if (issued < k1 - k0) {
@@ -154,94 +176,99 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
                 for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
                     drain(bar_full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, p.timeout_ns);
             }
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1) {
+            const bool leader = elect_one();
             int stage = 0;
             uint32_t phase = 0;
             for (int k = k0; k < k1; ++k) {
-                if (!mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k)) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k))) break;
                 tc_fence_after();
                 const uint32_t sa = smem_base + stage * STAGE_BYTES;
-                const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sa + QM_A_BYTES);
+                if (leader) {
+                    const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sa + QM_A_BYTES);
 #pragma unroll
-                for (int i = 0; i < QM_K / 32; ++i)
-                    umma_i8<1>(tmem, da + (uint64_t)(i * 2), db + (uint64_t)(i * 2), umma_idesc_i8(QM_ROWS, BN), (k > k0 || i > 0) ? 1u : 0u);
-                umma_commit_one(bar_empty + 8 * stage);
+                    for (int i = 0; i < QM_K / 32; ++i)
+                        umma_i8<1>(tmem, da + (uint64_t)(i * 2), db + (uint64_t)(i * 2), umma_idesc_i8(QM_ROWS, BN), (k > k0 || i > 0) ? 1u : 0u);
+                    umma_commit_one(bar_empty + 8 * stage);
+                }
                 if (++stage == STAGES) stage = 0, phase ^= 1u;
             }
-            umma_commit_one(bar_done);
+            if (leader) umma_commit_one(bar_done);
         }
     }
     __syncwarp();
     if (tile.rows > 0) {
         // everybody waits: nothing of the pipeline is in use behind this point, and its memory can hold the parts
-        mbar_wait(bar_done, 0, p, SITE_QM_DONE, tile.row0);
-        __syncwarp();
+        warp_wait(bar_done, 0, p, tile.row0, lane);
         tc_fence_after();
     }
     if (tile.rows > 0 && warp >= 2) {
         const int quarter = warp & 3;                       // a warp reads the lanes of its position among four
-        const int c = quarter * 32 + lane, ch = row_tile * QM_ROWS + c;
-        if (p.splits == 1) {
-            const float bs = ch < p.n ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
-            for (int t0 = 0; t0 < BN && t0 < tile.rows; t0 += 16) {
-                uint32_t v[16];
-                tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + t0, v);
-                tmem_ld_wait();
-                Out *out = static_cast<Out *>(p.out) + (long long)(tile.row0 + t0) * p.out_stride + ch;
+        const int c = quarter * 32 + lane;
+        for (int t0 = 0; t0 < BN && t0 < tile.rows; t0 += 16) {
+            uint32_t v[16];
+            tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + t0, v);
+            tmem_ld_wait();
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (t0 + j < tile.rows && ch < p.n)
-                        store_scaled(out + j * p.out_stride, (int)v[j], p.a_scale[tile.row0 + t0 + j], bs);
+            for (int j = 0; j < 16; ++j)
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem_base + 4u * (uint32_t)((t0 + j) * QM_ROWS + c)), "r"(v[j]) : "memory");
+        }
+    }
+    __syncwarp();
+    cluster_sync_all();
+    if (tile.rows > 0 && warp >= 2) {
+        const int c = (warp - 2) * 32 + lane, ch = row_tile * QM_ROWS + c;
+        const float bs = ch < p.n ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
+        // the parts of two tokens at a time: 2 * SPLITS loads in flight
+        for (int t = 2 * rank; t < tile.rows; t += 2 * SPLITS) {
+            uint32_t part[2][SPLITS];
+            const bool two = t + 1 < tile.rows;
+#pragma unroll
+            for (int s = 0; s < SPLITS; ++s) {
+                const uint32_t at = map_to_cta(smem_base + 4u * (uint32_t)(t * QM_ROWS + c), (uint32_t)s);
+                part[0][s] = ld_shared_cluster_u32(at);
+                part[1][s] = two ? ld_shared_cluster_u32(at + 4u * QM_ROWS) : 0u;
             }
-        } else {
-            for (int t0 = 0; t0 < BN && t0 < tile.rows; t0 += 16) {
-                uint32_t v[16];
-                tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + t0, v);
-                tmem_ld_wait();
+            uint32_t sum[2] = {0, 0};
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem_base + 4u * (uint32_t)((t0 + j) * QM_ROWS + c)), "r"(v[j]) : "memory");
+            for (int s = 0; s < SPLITS; ++s) {
+                sum[0] += part[0][s];
+                sum[1] += part[1][s];
+            }
+            if (ch < p.n) {
+                Out *out = static_cast<Out *>(p.out) + (long long)(tile.row0 + t) * p.out_stride + ch;
+                store_scaled(out, (int)sum[0], p.a_scale[tile.row0 + t], bs);
+                if (two) store_scaled(out + p.out_stride, (int)sum[1], p.a_scale[tile.row0 + t + 1], bs);
             }
         }
     }
-    if (p.splits > 1) {
-        __syncwarp();
-        cluster_sync_all();
-        if (tile.rows > 0 && warp >= 2) {
-            const int c = (warp - 2) * 32 + lane, ch = row_tile * QM_ROWS + c;
-            const float bs = ch < p.n ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
-            for (int t = rank; t < tile.rows; t += p.splits) {
-                int sum = 0;
-                for (int s = 0; s < p.splits; ++s)
-                    sum += (int)ld_shared_cluster_u32(map_to_cta(smem_base + 4u * (uint32_t)(t * QM_ROWS + c), (uint32_t)s));
-                if (ch < p.n)
-                    store_scaled(static_cast<Out *>(p.out) + (long long)(tile.row0 + t) * p.out_stride + ch, sum, p.a_scale[tile.row0 + t], bs);
-            }
-        }
-        __syncwarp();
-        cluster_sync_all();                                 // the parts stay until everybody has read them
-    }
+    __syncwarp();
+    cluster_sync_all();                                 // the parts stay until everybody has read them
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc_self(tmem, TMEM_COLS);
 }
 
-// ------------------------------------------------------------------ large products: CTA pairs
+// ------------------------------------------------------------------ enough tiles for every SM: persistent CTAs, alone or in pairs
 
-constexpr int QP_ROWS = 256;                 // channels per tile: 128 in each CTA of the pair
-constexpr int QP_TOKENS = 256;               // tokens per tile: each CTA loads half of them
-constexpr int QP_STAGE_BYTES = QM_A_BYTES + QP_TOKENS / 2 * QM_K;
-constexpr int QP_STAGES = 6;
 constexpr int QP_THREADS = 320;              // load warp, MMA warp, 8 epilogue warps
 constexpr int QP_GROUP = 16;                 // token tiles that are worked on side by side, see QpSchedule
-constexpr int QP_SMEM = QP_STAGES * QP_STAGE_BYTES + 1024 + 256;
+
+// CTAS CTAs work on a tile of 128 * CTAS channels x TOKENS tokens: each holds 128 channels and its share of the tokens.  What
+// is not needed for tokens deepens the pipeline: with few tokens the kernel streams weights, and the bytes in flight carry it.
+template <int CTAS, int TOKENS> struct QpShape {
+    static constexpr int STAGE_BYTES = QM_A_BYTES + TOKENS / CTAS * QM_K;
+    static constexpr int STAGES = 200 * 1024 / STAGE_BYTES;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 512;
+    static constexpr int ACC_COLS = TOKENS < 32 ? 32 : TOKENS;      // of tensor memory, per accumulator
+};
 
 // Order of the tiles: experts one after the other; inside an expert up to QP_GROUP token tiles form a group, and for each tile
-// of channels all token tiles of the group come next to each other.  The CTA pairs that run side by side then share one
-// tile of weights in L2, and the weights are read from HBM once per group (4096 tokens).  Every pair takes every
-// gridDim/2-th tile, so a role only ever moves forward through the experts.
-struct QpSchedule {
+// of channels all token tiles of the group come next to each other.  The CTAs that run side by side then share one
+// tile of weights in L2, and the weights are read from HBM once per group (4096 tokens of the largest tiles).  Every worker (a
+// CTA or a pair) takes every workers-th tile, so a role only ever moves forward through the experts.
+template <int CTAS, int TOKENS> struct QpSchedule {
     const int *tile_start, *row_start;       // [experts + 1] token tiles and rows before each expert, in shared memory
     int row_tiles, expert = 0;
     struct Tile { int expert, channel0, row0, rows; };
@@ -253,151 +280,182 @@ struct QpSchedule {
         const int i = (int)(index - (long long)tile_start[expert] * row_tiles);
         const int group = i / (QP_GROUP * row_tiles), first = group * QP_GROUP, wide = min(QP_GROUP, tiles - first);
         const int j = i - group * QP_GROUP * row_tiles;
-        const int row0 = row_start[expert] + (first + j % wide) * QP_TOKENS;
-        return {expert, j / wide * QP_ROWS, row0, min(QP_TOKENS, row_start[expert + 1] - row0)};
+        const int row0 = row_start[expert] + (first + j % wide) * TOKENS;
+        return {expert, j / wide * (CTAS * QM_ROWS), row0, min(TOKENS, row_start[expert + 1] - row0)};
     }
 };
 
-// One warp fills the schedule's tables; counts are cut so that no tile reaches beyond the rows there are.
-__device__ void fill_schedule(const QmP &p, int *tile_start, int *row_start, int lane)
+// One warp fills the schedule's tables.  `count`: count_of(lane), asked for early.
+template <int TOKENS> __device__ __forceinline__ void fill_schedule(const QmP &p, int *tile_start, int *row_start, int count, int lane)
 {
-    if (!p.counts) {
-        if (lane == 0) {
-            tile_start[0] = row_start[0] = 0;
-            tile_start[1] = (p.rows + QP_TOKENS - 1) / QP_TOKENS;
-            row_start[1] = p.rows;
-        }
-        return;
-    }
-    long long rows_before = 0;
-    int tiles_before = 0;
+    unsigned rows_before = 0, tiles_before = 0;
     if (lane == 0) tile_start[0] = row_start[0] = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += 32) {
+    const int experts = p.counts ? p.experts : 1;
+    if (!p.counts) count = lane == 0 ? p.rows : 0;
+#pragma unroll 1
+    for (int e0 = 0; e0 < experts; e0 += 32) {
         const int e = e0 + lane;
-        long long upto = e < p.experts ? max(p.counts[e], 0) : 0;
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const long long last = min(rows_before + upto, (long long)p.rows);
-        long long first = __shfl_up_sync(0xffffffffu, last, 1);
-        if (lane == 0) first = rows_before;
-        int tiles = ((int)(last - first) + QP_TOKENS - 1) / QP_TOKENS;
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, tiles, o);
-            if (lane >= o) tiles += v;
-        }
-        if (e < p.experts) {
-            tile_start[e + 1] = tiles_before + tiles;
+        unsigned first, last;
+        expert_rows(e0 == 0 ? count : count_of(p, e), (unsigned)p.rows, rows_before, lane, first, last);
+        const unsigned tiles = tiles_before + scan_up_to((last - first + TOKENS - 1) / TOKENS, 0x7fffffffu, lane);
+        if (e < experts) {
+            tile_start[e + 1] = (int)tiles;
             row_start[e + 1] = (int)last;
         }
-        tiles_before += __shfl_sync(0xffffffffu, tiles, 31);
+        tiles_before = __shfl_sync(0xffffffffu, tiles, 31);
         rows_before = __shfl_sync(0xffffffffu, last, 31);
     }
+    __syncwarp();
 }
 
-// Persistent, one CTA per SM, pairs of CTAs share every matrix instruction (cta_group::2): 256 channels x 256 tokens, each CTA
-// holding its 128 channels and HALF of the tokens, which halves the operand bytes per SM against single CTAs -- at
-// 8 bits the tensor cores eat operands as fast as at 16, and that traffic out of L2 is what bounds the other kernel on large products.
-// Accumulators are double buffered (2 x 256 columns of tensor memory): a tile is scaled and stored while the next one runs.
-template <typename Out>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(QP_THREADS, 1)
-quant_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const QmP p)
+// The load warp's place in its sequence of stages.  The whole warp runs the loop, with everything in it the same in all lanes, and
+// one elected lane issues: tile copies take their operands from uniform registers, and where the compiler cannot tell that a
+// value is uniform (one lane's branch, values out of shared memory) it gathers them anew for every copy.
+template <int CTAS, int TOKENS> struct QpLoader {
+    using Shape = QpShape<CTAS, TOKENS>;
+    QpSchedule<CTAS, TOKENS> sched;
+    long long t, total, step, issued = 0;
+    int ksteps, k = 0, stage = 0, y_b = 0, y_a = 0;
+    uint32_t phase = 0;
+    // Issues stages until `most` have been issued; false: a wait gave up.
+    __device__ __forceinline__ bool run(const QmP &p, const CUtensorMap &map_b, const CUtensorMap &map_a, uint32_t smem_base, uint32_t bar_full,
+                                        uint32_t bar_empty, uint32_t lead_full, uint32_t rank, long long most, bool leader)
+    {
+        while (t < total && issued < most) {
+            if (k == 0) {
+                const auto tile = sched.at(t);
+                y_b = uniform(tile.expert * p.n + tile.channel0 + (int)rank * QM_ROWS);
+                // a pair's CTAs hold the halves of the instruction's N side
+                y_a = uniform(tile.row0 + (int)rank * ((tile.rows + 31) / 32 * 16));
+            }
+            if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, t))) return false;
+            const uint32_t sa = smem_base + stage * Shape::STAGE_BYTES;
+            if (leader) {
+                if (CTAS == 1) {
+                    mbar_arrive_expect_tx(bar_full + 8 * stage, Shape::STAGE_BYTES);
+                    tma_load_2d_self(sa, &map_b, bar_full + 8 * stage, k * QM_K, y_b);
+                    tma_load_2d_self(sa + QM_A_BYTES, &map_a, bar_full + 8 * stage, k * QM_K, y_a);
+                } else {
+                    if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, 2 * Shape::STAGE_BYTES);
+                    tma_load_2d(sa, &map_b, lead_full + 8 * stage, k * QM_K, y_b);
+                    tma_load_2d(sa + QM_A_BYTES, &map_a, lead_full + 8 * stage, k * QM_K, y_a);
+                }
+            }
+            if (++stage == Shape::STAGES) stage = 0, phase ^= 1u;
+            ++issued;
+            if (++k == ksteps) k = 0, t += step;
+        }
+        return true;
+    }
+};
+
+// Persistent, one CTA per SM.
+// CTAS = 2: pairs of CTAs share every matrix instruction (cta_group::2), 256 channels x TOKENS tokens, each CTA holding
+// its 128 channels and HALF of the tokens, which halves the operand bytes per SM against single CTAs -- at 8 bits the tensor
+// cores eat operands as fast as at 16, and that traffic out of L2 is what would bound large products (single CTAs: 1.32 ms at 7919 x 28672 x 4096, pairs 0.58 ms).
+// CTAS = 1: for few tokens, where the weights' way from HBM is all that counts: nothing waits for a second CTA, and the first
+// loads are under way before the rest of the block is set up.
+// Accumulators are double buffered (2 x 256 columns of tensor memory at most): a tile is scaled and stored while the next one runs.
+template <int CTAS, int TOKENS, typename Out>
+__global__ void __launch_bounds__(QP_THREADS, 1)
+quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const QmP p)
 {
+    using Shape = QpShape<CTAS, TOKENS>;
+    constexpr int STAGES = Shape::STAGES, STAGE_BYTES = Shape::STAGE_BYTES, ACC_COLS = Shape::ACC_COLS;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
     __shared__ uint32_t s_tmem;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bar_full = smem_base + QP_STAGES * QP_STAGE_BYTES, bar_empty = bar_full + 8 * QP_STAGES;
-    const uint32_t bar_tfull = bar_empty + 8 * QP_STAGES, bar_tempty = bar_tfull + 16, bar_drain = bar_tempty + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_ctarank();
-    const uint32_t lead_full = map_to_cta(bar_full, 0), lead_tempty = map_to_cta(bar_tempty, 0);
+    const uint32_t bar_full = smem_base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES;
+    const uint32_t bar_tfull = bar_empty + 8 * STAGES, bar_tempty = bar_tfull + 16, bar_drain = bar_tempty + 16;
+    const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
+    const uint32_t rank = CTAS == 1 ? 0 : cluster_ctarank();
+    const uint32_t lead_full = CTAS == 1 ? bar_full : map_to_cta(bar_full, 0);
+    const uint32_t lead_tempty = CTAS == 1 ? bar_tempty : map_to_cta(bar_tempty, 0);
+    const int ksteps = (p.k + QM_K - 1) / QM_K, experts = p.experts > 0 ? p.experts : 1;
+    QpSchedule<CTAS, TOKENS> sched{s_tile_start, s_row_start, (p.n + CTAS * QM_ROWS - 1) / (CTAS * QM_ROWS)};
+    const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    QpLoader<CTAS, TOKENS> loader{sched, first, 0, step, 0, ksteps};
+    bool ok = true;
 
     if (warp == 0) {
-        fill_schedule(p, s_tile_start, s_row_start, lane);
+        const int count = count_of(p, lane);
+        if (lane == 0) {
+#pragma unroll 1
+            for (int i = 0; i < STAGES; ++i) {
+                mbar_init(bar_full + 8 * i, 1);           // the leader's load thread arrives, expecting all CTAs' bytes
+                mbar_init(bar_empty + 8 * i, 1);
+            }
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(bar_tfull + 8 * i, 1);
+                mbar_init(bar_tempty + 8 * i, 8 * CTAS);  // one arrival per epilogue warp
+            }
+            mbar_init(bar_drain, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        fill_schedule<TOKENS>(p, s_tile_start, s_row_start, count, lane);
+        loader.total = sched.total(experts);
+        if (CTAS == 1 && !p.no_loads)
+            ok = loader.run(p, map_b, map_a, smem_base, bar_full, bar_empty, lead_full, rank, STAGES, elect_one());
     } else if (warp == 1) {
-        tmem_alloc(smem_u32(&s_tmem), 512);
-    } else if (threadIdx.x == 64) {
-        for (int i = 0; i < QP_STAGES; ++i) {
-            mbar_init(bar_full + 8 * i, 1);           // the leader's load thread arrives, expecting both CTAs' bytes
-            mbar_init(bar_empty + 8 * i, 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(bar_tfull + 8 * i, 1);
-            mbar_init(bar_tempty + 8 * i, 16);        // one arrival per epilogue warp of both CTAs
-        }
-        mbar_init(bar_drain, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (CTAS == 1) tmem_alloc_self(smem_u32(&s_tmem), 2 * ACC_COLS);
+        else tmem_alloc(smem_u32(&s_tmem), 2 * ACC_COLS);
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();
+    if (CTAS == 2) cluster_sync_all();
     tc_fence_after();
-    const uint32_t tmem = s_tmem;
-    QpSchedule sched{s_tile_start, s_row_start, (p.n + QP_ROWS - 1) / QP_ROWS};
-    const long long total = sched.total(p.experts > 0 ? p.experts : 1);
-    const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
-    const int ksteps = (p.k + QM_K - 1) / QM_K;
+    const uint32_t tmem = uniform(s_tmem);
+    const long long total = sched.total(experts);
 
     if (warp == 0) {
-        if (lane == 0 && !p.no_loads) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            long long issued = 0;
-            for (long long t = first; ok && t < total; t += step) {
-                const QpSchedule::Tile tile = sched.at(t);
-                const int y_b = tile.expert * p.n + tile.channel0 + (int)rank * QM_ROWS;
-                const int y_a = tile.row0 + (int)rank * ((tile.rows + 31) / 32 * 16);       // second half of the tile's tokens
-                for (int k = 0; k < ksteps; ++k, ++issued) {
-                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, t)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t sa = smem_base + stage * QP_STAGE_BYTES, full = lead_full + 8 * stage;
-                    if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, 2 * QP_STAGE_BYTES);
-                    tma_load_2d(sa, &map_b, full, k * QM_K, y_b);
-                    tma_load_2d(sa + QM_A_BYTES, &map_a, full, k * QM_K, y_a);
-                    if (++stage == QP_STAGES) stage = 0, phase ^= 1u;
-                }
-            }
+        if (!p.no_loads) {
+            ok = ok && loader.run(p, map_b, map_a, smem_base, bar_full, bar_empty, lead_full, rank, 0x7fffffffffffffffll, elect_one());
             if (!ok && rank == 0) {
-                // gave up: wait for the copies of both CTAs (the peer stays until the cluster barrier at the end)
-                for (long long i = issued > QP_STAGES ? issued - QP_STAGES : 0; i < issued; ++i)
-                    drain(bar_full + 8 * (uint32_t)(i % QP_STAGES), (uint32_t)(i / QP_STAGES) & 1u, p.timeout_ns);
+                // gave up: wait for the copies of all CTAs (a peer stays until the cluster barrier at the end)
+                for (long long i = loader.issued > STAGES ? loader.issued - STAGES : 0; i < loader.issued; ++i)
+                    drain(bar_full + 8 * (uint32_t)(i % STAGES), (uint32_t)(i / STAGES) & 1u, p.timeout_ns);
             }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
+            const bool leader = elect_one();
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
-            bool ok = true;
             for (long long t = first; ok && t < total; t += step) {
                 // fewer tokens than a full tile: a narrower instruction
-                const uint32_t idesc = umma_idesc_i8(2 * QM_ROWS, (sched.at(t).rows + 31) / 32 * 32);
-                ok = mbar_wait<true>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_QM_DONE, t);
+                const uint32_t idesc = uniform(umma_idesc_i8(CTAS * QM_ROWS, (sched.at(t).rows + 16 * CTAS - 1) / (16 * CTAS) * (16 * CTAS)));
+                ok = __all_sync(0xffffffffu, mbar_wait<CTAS == 2>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_QM_DONE, t));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t d = tmem + (uint32_t)(acc * QP_TOKENS);
+                const uint32_t d = tmem + (uint32_t)(acc * ACC_COLS);
                 for (int k = 0; k < ksteps; ++k) {
-                    ok = mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, t);
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, t));
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t sa = smem_base + stage * QP_STAGE_BYTES;
-                    const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sa + QM_A_BYTES);
+                    const uint32_t sa = smem_base + stage * STAGE_BYTES;
+                    if (leader) {
+                        const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sa + QM_A_BYTES);
 #pragma unroll
-                    for (int i = 0; i < QM_K / 32; ++i)
-                        umma_i8<2>(d, da + (uint64_t)(i * 2), db + (uint64_t)(i * 2), idesc, (k | i) != 0 ? 1u : 0u);
-                    umma_commit_pair(bar_empty + 8 * stage);
-                    if (++stage == QP_STAGES) stage = 0, phase ^= 1u;
+                        for (int i = 0; i < QM_K / 32; ++i)
+                            umma_i8<CTAS>(d, da + (uint64_t)(i * 2), db + (uint64_t)(i * 2), idesc, (k | i) != 0 ? 1u : 0u);
+                        if (CTAS == 1) umma_commit_one(bar_empty + 8 * stage);
+                        else umma_commit_pair(bar_empty + 8 * stage);
+                    }
+                    if (++stage == STAGES) stage = 0, phase ^= 1u;
                 }
                 if (!ok) break;
-                umma_commit_pair(bar_tfull + 8 * acc);
+                if (leader) {
+                    if (CTAS == 1) umma_commit_one(bar_tfull + 8 * acc);
+                    else umma_commit_pair(bar_tfull + 8 * acc);
+                }
                 if ((acc ^= 1) == 0) acc_phase ^= 1u;
             }
-            umma_commit_self(bar_drain);                // every MMA has finished before tensor memory goes
+            if (leader) {
+                if (CTAS == 1) umma_commit_one(bar_drain);      // every MMA has finished before tensor memory goes
+                else umma_commit_self(bar_drain);
+            }
             drain(bar_drain, 0, p.timeout_ns);
         }
         __syncwarp();
@@ -406,17 +464,17 @@ quant_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid
         int acc = 0;
         uint32_t acc_phase = 0;
         for (long long t = first; t < total; t += step) {
-            const QpSchedule::Tile tile = sched.at(t);
+            const auto tile = sched.at(t);
             const int ch = tile.channel0 + (int)rank * QM_ROWS + quarter * 32 + lane;
             const bool in = ch < p.n;
             const float bs = in ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
             // a warp leaves the loop as one: what follows needs all of its lanes
-            if (!__all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * acc, acc_phase, p, SITE_QM_DONE, t))) break;
+            if (!warp_wait(bar_tfull + 8 * acc, acc_phase, p, t, lane)) break;
             tc_fence_after();
             for (int c = half * 32; c < tile.rows; c += 64) {
                 uint32_t v[32];
                 const float as_lane = c + lane < tile.rows ? p.a_scale[tile.row0 + c + lane] : 0.0f;
-                tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * QP_TOKENS + c), v);
+                tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * ACC_COLS + c), v);
                 tmem_ld_wait();
                 Out *out = static_cast<Out *>(p.out) + (long long)(tile.row0 + c) * p.out_stride + ch;
                 const int left = tile.rows - c;
@@ -439,9 +497,12 @@ quant_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();          // the peer no longer signals this CTA's barriers or reads its operands
+    if (CTAS == 2) cluster_sync_all();          // the peer no longer signals this CTA's barriers or reads its operands
     tc_fence_after();
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    if (warp == 1) {
+        if (CTAS == 1) tmem_dealloc_self(tmem, 2 * ACC_COLS);
+        else tmem_dealloc(tmem, 2 * ACC_COLS);
+    }
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -497,35 +558,85 @@ int sm_count(int device)
     return n;
 }
 
-template <int BN, typename Out> int launch_split(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
+template <typename K>
+int launch(K kernel, unsigned blocks, int threads, int smem, int cluster, const QmP &p, const CUtensorMap &b, const CUtensorMap &a, cudaStream_t stream)
 {
-    constexpr int smem = QmShape<BN>::SMEM;
-    static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(quant_matmul_kernel<BN, Out>, smem, device, allowed)) return MOE_OVL_ERR_CUDA;
-    // most token tiles that any counts can give
-    const long long tiles = p.counts ? p.rows / BN + std::min(p.experts, p.rows) : (p.rows + BN - 1) / BN;
-    const long long blocks = tiles * p.row_tiles * p.splits;
-    if (blocks > 0x7fffffffll) return MOE_OVL_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(QM_THREADS);
-    cfg.dynamicSmemBytes = smem;
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.splits;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, quant_matmul_kernel<BN, Out>, b, a, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, b, a, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
 }
 
-template <typename Out> int launch_pair(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
+template <int BN, int SPLITS, typename Out>
+int launch_split(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
 {
     static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(quant_matmul_pair_kernel<Out>, QP_SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
-    quant_matmul_pair_kernel<Out><<<sm_count(device) / 2 * 2, QP_THREADS, QP_SMEM, stream>>>(b, a, p);
-    return launched();
+    const auto kernel = quant_matmul_kernel<BN, SPLITS, Out>;
+    if (!allow_smem(kernel, QmShape<BN>::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    // most token tiles that any counts can give
+    const long long tiles = p.counts ? p.rows / BN + std::min(p.experts, p.rows) : (p.rows + BN - 1) / BN;
+    const long long blocks = tiles * p.row_tiles * SPLITS;
+    if (blocks > 0x7fffffffll) return MOE_OVL_ERR_UNSUPPORTED;
+    return launch(kernel, (unsigned)blocks, QM_THREADS, QmShape<BN>::SMEM, SPLITS, p, b, a, stream);
+}
+
+template <int CTAS, int TOKENS, typename Out>
+int launch_tiles(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
+{
+    static std::atomic<unsigned long long> allowed{0};
+    const auto kernel = quant_matmul_tiles_kernel<CTAS, TOKENS, Out>;
+    if (!allow_smem(kernel, QpShape<CTAS, TOKENS>::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    return launch(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), QP_THREADS, QpShape<CTAS, TOKENS>::SMEM, CTAS, p, b, a, stream);
+}
+
+template <int N> struct Number { static constexpr int value = N; };
+
+// ctas 0: a cluster of `splits` CTAs per tile; 1, 2: persistent CTAs, alone or in pairs.
+struct QmChoice { int ctas, tokens, splits; };
+
+// The kernel goes by the tiles there are (with the experts' rows taken as even: the counts are on the device).  W(channels, tokens):
+// waves of such tiles over the 148 CTAs or 74 pairs.  Measured, us:
+//   few tiles leave SMs idle, so they share their K: 1 token, n = k = 4096 (32 tiles) 7.4 split by 4, 10.2 unsplit; n = 8192,
+//     k = 2048 (64 tiles) 7.2 and 7.9; 256 tokens, n = 1024, k = 8192 (32 tiles of 64 tokens) 10.3 and 14.6; 128 tokens, n = 4096, k = 14336
+//     (64 such tiles) 18.3 and 22; with k = 4096 10.5 and 10.2: more of them take a long K to pay;
+//   up to 64 tokens per expert, or where tiles of 64 fit one wave, single CTAs: 16 experts of 64 tokens 48.4 against 49.4 in pairs (of 128:
+//     61.1 against 55.8); 256 tokens, n = k = 4096 10.3 against 11.8;
+//   pairs take 128 or 256 tokens, whose tiles cost about 8 : 13: 512 tokens, n = k = 4096 (one wave each) 12.3 and 17.5; 2048 tokens
+//     (four waves, two) 28.9 and 26.9.
+QmChoice choose(const QmP &p)
+{
+    const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows + groups - 1) / groups;
+    auto tiles = [&](int channels, int tokens) {
+        return (long long)((p.n + channels - 1) / channels) * groups * ((per_group + tokens - 1) / tokens);
+    };
+    const int ksteps = (p.k + QM_K - 1) / QM_K;
+    auto split = [&](int tokens) {
+        // two CTAs per SM at most, a step of K for each, eight where there are as many CTAs as that
+        const long long t = tiles(QM_ROWS, tokens);
+        int n = 1;
+        while (n < 8 && t * n * 2 <= 296 && n * 2 <= ksteps && (n < 4 || ksteps >= 64)) n *= 2;
+        return QmChoice{0, tokens, n};
+    };
+    QmChoice c = {1, per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64, 1};
+    if (per_group <= 64) {
+        if (tiles(QM_ROWS, std::min(c.tokens, 32)) <= 74) c = split(std::min(c.tokens, 32));
+    } else if (tiles(QM_ROWS, 64) <= (ksteps >= 64 ? 74 : 37)) {
+        c = split(64);
+    } else if (tiles(QM_ROWS, 64) > 148) {
+        const long long w128 = (tiles(2 * QM_ROWS, 128) + 73) / 74, w256 = (tiles(2 * QM_ROWS, 256) + 73) / 74;
+        c = {2, per_group <= 128 || 8 * w128 <= 13 * w256 ? 128 : 256, 1};
+    }
+    // a K of one step cannot be shared
+    if (c.ctas == 0 && c.splits == 1) c.ctas = 1;
+    return c;
 }
 
 }  // namespace
@@ -550,26 +661,41 @@ extern "C" int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *a)
     if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 16 != 0 || sb % 16 != 0) return MOE_OVL_ERR_UNSUPPORTED;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
-    QmP p = {a->rows, a->n, a->k, a->num_experts, (a->n + QM_ROWS - 1) / QM_ROWS, 1, a->expert_counts, a->a_scale, a->b_scale,
-             a->out, a->out_stride, a->status,
-             a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : QM_TIMEOUT_NS, (a->flags & MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS) != 0};
-    const int per_group = a->num_experts ? (a->rows + a->num_experts - 1) / a->num_experts : a->rows;
-    const int bn = per_group <= 16 ? 16 : per_group <= 32 ? 32 : per_group <= 64 ? 64 : 128;
-    // K is shared where the tiles alone would leave SMs idle
-    const long long tiles = (long long)p.row_tiles * ((per_group + bn - 1) / bn) * std::max(1, std::min(a->num_experts, a->rows));
-    while (p.splits < 8 && tiles * p.splits * 2 <= 296 && p.splits * 2 <= (a->k + QM_K - 1) / QM_K) p.splits *= 2;
-    const bool pair = per_group > 256;
+    const QmP p = {a->rows, a->n, a->k, a->num_experts, (a->n + QM_ROWS - 1) / QM_ROWS, a->expert_counts, a->a_scale, a->b_scale, a->out,
+                   a->out_stride, a->status, a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : QM_TIMEOUT_NS,
+                   (a->flags & MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS) != 0};
+    const QmChoice c = choose(p);
     CUtensorMap map_b, map_a;
-    if (!encode_bytes(&map_b, a->b, b_rows, a->k, sb, QM_ROWS) || !encode_bytes(&map_a, a->a, a->rows, a->k, sa, pair ? QP_TOKENS / 2 : bn)) return MOE_OVL_ERR_CUDA;
+    if (!encode_bytes(&map_b, a->b, b_rows, a->k, sb, QM_ROWS) || !encode_bytes(&map_a, a->a, a->rows, a->k, sa, c.ctas == 2 ? c.tokens / 2 : c.tokens))
+        return MOE_OVL_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
     return with_dtype(a->out_dtype, [&](auto t) {
         using Out = decltype(t);
-        if (pair) return launch_pair<Out>(p, map_b, map_a, a->device, stream);
-        switch (bn) {
-        case 16: return launch_split<16, Out>(p, map_b, map_a, a->device, stream);
-        case 32: return launch_split<32, Out>(p, map_b, map_a, a->device, stream);
-        case 64: return launch_split<64, Out>(p, map_b, map_a, a->device, stream);
-        default: return launch_split<128, Out>(p, map_b, map_a, a->device, stream);
+        if (c.ctas == 1) {
+            switch (c.tokens) {
+            case 16: return launch_tiles<1, 16, Out>(p, map_b, map_a, a->device, stream);
+            case 32: return launch_tiles<1, 32, Out>(p, map_b, map_a, a->device, stream);
+            default: return launch_tiles<1, 64, Out>(p, map_b, map_a, a->device, stream);
+            }
+        }
+        if (c.ctas == 2) {
+            switch (c.tokens) {
+            case 128: return launch_tiles<2, 128, Out>(p, map_b, map_a, a->device, stream);
+            default: return launch_tiles<2, 256, Out>(p, map_b, map_a, a->device, stream);
+            }
+        }
+        auto split = [&](auto n) {
+            constexpr int BN = decltype(n)::value;
+            switch (c.splits) {
+            case 2: return launch_split<BN, 2, Out>(p, map_b, map_a, a->device, stream);
+            case 4: return launch_split<BN, 4, Out>(p, map_b, map_a, a->device, stream);
+            default: return launch_split<BN, 8, Out>(p, map_b, map_a, a->device, stream);
+            }
+        };
+        switch (c.tokens) {
+        case 16: return split(Number<16>());
+        case 32: return split(Number<32>());
+        default: return split(Number<64>());
         }
     });
 }
