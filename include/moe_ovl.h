@@ -371,7 +371,7 @@ int moe_ovl_return_slots_static(int32_t device, int32_t num_src_ranks, int32_t t
  * DEVICE pointers, enqueues its kernels on args->stream and returns; nothing is allocated, nothing is waited for, the
  * calling thread's current device is left as it was, and a call can be captured in a CUDA graph.  Matrices are row-major
  * with a stride between rows (in elements) of their own; columns lie next to each other.  Strides and pointers that are not
- * multiples of 16 bytes are accepted unless stated otherwise; multiples of 16 are faster.  A call with no rows does
+ * multiples of 16 bytes are accepted unless stated otherwise (multiples of 16 are faster); a stride of 2^31 or more is refused.  A call with no rows does
  * nothing (moe_ovl_route still clears its counts, moe_ovl_add_norm_backward its weight gradient). */
 
 enum { MOE_OVL_BF16 = 0, MOE_OVL_F16 = 1, MOE_OVL_F32 = 2 };

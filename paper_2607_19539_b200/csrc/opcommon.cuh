@@ -35,11 +35,69 @@ template <typename T, int VEC> __device__ __forceinline__ void store_pack(T *p, 
     else *reinterpret_cast<Pack<T, VEC> *>(p) = r;
 }
 
-// The larger of two; NaN where either is.
-__device__ __forceinline__ float max_nan(float a, float b)
+// Two neighbouring values as floats, and back with one rounding each.
+__device__ __forceinline__ float2 to_f32x2(const float *p) { return make_float2(p[0], p[1]); }
+__device__ __forceinline__ float2 to_f32x2(const __nv_bfloat16 *p)
+{
+    const uint32_t u = *reinterpret_cast<const uint32_t *>(p);
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+__device__ __forceinline__ float2 to_f32x2(const __half *p) { return __half22float2(*reinterpret_cast<const __half2 *>(p)); }
+__device__ __forceinline__ void from_f32x2(float *p, float2 v) { p[0] = v.x, p[1] = v.y; }
+__device__ __forceinline__ void from_f32x2(__nv_bfloat16 *p, float2 v) { *reinterpret_cast<__nv_bfloat162 *>(p) = __float22bfloat162_rn(v); }
+__device__ __forceinline__ void from_f32x2(__half *p, float2 v) { *reinterpret_cast<__half2 *>(p) = __float22half2_rn(v); }
+// a + b, rounded once to the type
+__device__ __forceinline__ void add_round2(float *a, const float *b) { a[0] += b[0], a[1] += b[1]; }
+__device__ __forceinline__ void add_round2(__nv_bfloat16 *a, const __nv_bfloat16 *b)
+{
+    __nv_bfloat162 *p = reinterpret_cast<__nv_bfloat162 *>(a);
+    *p = __hadd2(*p, *reinterpret_cast<const __nv_bfloat162 *>(b));
+}
+__device__ __forceinline__ void add_round2(__half *a, const __half *b)
+{
+    __half2 *p = reinterpret_cast<__half2 *>(a);
+    *p = __hadd2(*p, *reinterpret_cast<const __half2 *>(b));
+}
+
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+        : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)),
+          "l"(*reinterpret_cast<unsigned long long *>(&c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+        : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+        : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+    return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// The largest magnitude; NaN where any is.
+__device__ __forceinline__ float max_abs(float a, float b)
 {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+__device__ __forceinline__ float max_abs(float a, float2 b)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b.x), "f"(b.y));
     return r;
 }
 
@@ -49,11 +107,12 @@ __device__ __forceinline__ float warp_sum(float v)
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+// Largest value over the warp; NaN where any is.
 __device__ __forceinline__ float warp_max(float v)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 // Makes `device` current for one call and puts the caller's device back.

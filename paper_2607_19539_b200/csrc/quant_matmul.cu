@@ -654,8 +654,9 @@ extern "C" int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *a)
     const int es = dtype_bytes(a->out_dtype);
     if (!a->a || !a->a_scale || !a->b || !a->b_scale || !a->out || !a->status || !aligned(a->a_scale, 4) || !aligned(a->b_scale, 4) ||
         !aligned(a->out, es) || !aligned(a->status, 4) || !aligned(a->expert_counts, 4) || (a->rows > 1 && (a->a_stride < a->k || a->out_stride < a->n)) ||
-        (b_rows > 1 && a->b_stride < a->k) || a->a_stride >= (1ll << 39) || a->b_stride >= (1ll << 39) || a->out_stride >= (1ll << 40))
+        (b_rows > 1 && a->b_stride < a->k))
         return MOE_OVL_ERR_INVALID_ARG;
+    if (std::max(std::max(a->a_stride, a->b_stride), a->out_stride) > 0x7fffffff) return MOE_OVL_ERR_UNSUPPORTED;
     // a single row's stride is never used; the tensor map wants one that holds the row
     const long long sa = a->rows > 1 ? a->a_stride : a->k, sb = b_rows > 1 ? a->b_stride : a->k;
     if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 16 != 0 || sb % 16 != 0) return MOE_OVL_ERR_UNSUPPORTED;

@@ -1,24 +1,31 @@
 // Router of the expert layer and its gradient (moe_ovl_route, moe_ovl_route_backward in include/moe_ovl.h).
 //
-// One warp per row.  A lane holds NR logits in registers, V neighbours at a time, so a row is read once.  Choices are
-// compared as 32-bit keys whose unsigned order is the order of the floats (0 = masked): the largest key over the warp
-// is one reduction instruction, and the lowest index among the lanes that hold it is a second one, which is what makes
-// ties go to the lowest index.
+// G lanes share a row, NR neighbouring logits each (8 up to 256 experts), so a warp works on 32 / G rows at once and what it does
+// once per row -- the reductions, the rounds of the choice -- is shared by all of them.  Choices are compared as 32-bit keys whose
+// unsigned order is that of the floats (0 = masked).  Every lane sorts its keys once, stably; a round then is the largest head
+// over the G lanes, the first lane that holds it (its experts are the lowest: ties go to the lowest index), and a shift
+// of that lane's list.  Where the logits themselves are compared and have 16 bits, a key holds the expert too, in its lower half
+// and descending, so that the largest key alone is the round's answer.  Bound by instructions: at 65521 x 64, bf16, 6 chosen, a warp per
+// row with a search through its keys in every round takes 45 us, G lanes with sorted lists 22 us, with the expert in the key
+// 16.5 us, 4 of them for the counts (clearing them and adding up the blocks').
 #include <algorithm>
+#include <type_traits>
 
 #include "opcommon.cuh"
+#include "ptx.cuh"
 
 using namespace moe_ovl;
 
 namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr int ROUTE_WARPS = 8;
-constexpr int ROUTE_BLOCKS = 148 * 8;      // every SM full of warps
+constexpr int ROUTE_THREADS = 256;
+constexpr int ROUTE_BLOCKS = 148 * 4;      // what the registers allow; more of them only add counts to add up
 
 struct RouteP {
     int rows, experts, k, groups, per_group, top_groups, group_best;
     bool sigmoid, renormalise, by_score;   // by_score: choices are scores (+ bias); else the logits themselves
+    bool cluster;                          // the whole grid is one cluster, whose first block writes the counts
     float gate_scale;
     const void *logits;
     const float *bias;
@@ -41,139 +48,319 @@ __device__ __forceinline__ float value_of(unsigned key)
 // A logit as it is used: +inf is the largest finite value, a NaN is -inf.
 __device__ __forceinline__ float usable(float v) { return v != v ? -INFINITY : fminf(v, 3.402823466e+38f); }
 __device__ __forceinline__ float sigmoid_of(float v) { return 1.0f / (1.0f + expf(-v)); }
+// exp(l - m) with l = -inf giving 0 also where the whole row is masked
+__device__ __forceinline__ float exp_from(float l, float m) { return l > -INFINITY ? expf(l - m) : 0.0f; }
 
-// Index of a lane's r-th logit.
-template <int V> __device__ __forceinline__ int expert_at(int r, int lane) { return (r / V) * (32 * V) + lane * V + r % V; }
+// Over the G lanes of a row.
+template <int G> __device__ __forceinline__ unsigned group_max(unsigned v)
+{
+    if constexpr (G == 32) {
+        v = __reduce_max_sync(FULL, v);
+    } else {
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(FULL, v, o));
+    }
+    return v;
+}
+template <int G> __device__ __forceinline__ float group_max(float v)
+{
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
+    return v;
+}
+template <int G> __device__ __forceinline__ float group_sum(float v)
+{
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    return v;
+}
 
+// NR neighbouring logits from expert e0 on, V at a time; what lies beyond the last expert is masked.
 template <typename T, int NR, int V>
-__device__ __forceinline__ void load_row(const T *row, int experts, int lane, float (&l)[NR])
+__device__ __forceinline__ void load_logits(const T *row, int experts, int e0, T (&l)[NR])
 {
 #pragma unroll
     for (int r = 0; r < NR; r += V) {
-        const int e = expert_at<V>(r, lane);
-        if (e < experts) {
-            const Pack<T, V> a = load_pack<T, V>(row + e);
+        if (e0 + r < experts) {
+            const Pack<T, V> a = load_pack<T, V>(row + e0 + r);
 #pragma unroll
-            for (int j = 0; j < V; ++j) l[r + j] = usable(to_f32(a.v[j]));
+            for (int j = 0; j < V; ++j) l[r + j] = a.v[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) l[r + j] = -INFINITY;
+            for (int j = 0; j < V; ++j) l[r + j] = from_f32<T>(-INFINITY);
         }
     }
 }
 
-// exp(l - m) with l = -inf giving 0 also where the whole row is masked
-__device__ __forceinline__ float exp_from(float l, float m) { return l > -INFINITY ? expf(l - m) : 0.0f; }
-
-template <typename T, int NR, int V, bool GROUPS>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(const RouteP p)
+// Keys of 16-bit logits: the logit's order above, the expert below, so that of two equal logits the earlier has the larger key.
+__device__ __forceinline__ unsigned bits_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
+__device__ __forceinline__ unsigned bits_of(__half v) { return __half_as_ushort(v); }
+template <typename T> __device__ __forceinline__ T from_bits(unsigned u)
 {
-    extern __shared__ int histogram[];
-    const int lane = threadIdx.x & 31;
-    if (p.counts) {
-        for (int i = threadIdx.x; i < p.experts; i += blockDim.x) histogram[i] = 0;
-        __syncthreads();
-    }
-    int group[GROUPS ? NR : 1];
-    if (GROUPS) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) group[r] = expert_at<V>(r, lane) / p.per_group;   // beyond the last: >= groups
-    }
-    for (int row = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); row < p.rows; row += gridDim.x * ROUTE_WARPS) {
-        const T *logits = static_cast<const T *>(p.logits) + row * p.stride;
-        float l[NR];
-        load_row<T, NR, V>(logits, p.experts, lane, l);
-        float top = -INFINITY, total = 0.0f;            // softmax over the row
-        if (!p.sigmoid && (p.by_score || !p.renormalise)) {
-#pragma unroll
-            for (int r = 0; r < NR; ++r) top = fmaxf(top, l[r]);
-            top = warp_max(top);
-#pragma unroll
-            for (int r = 0; r < NR; ++r) total += exp_from(l[r], top);
-            total = warp_sum(total);
-        }
-        unsigned key[NR];
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) return __ushort_as_bfloat16((unsigned short)u);
+    else if constexpr (std::is_same<T, __half>::value) return __ushort_as_half((unsigned short)u);
+    else return 0.0f;
+}
+template <typename T> __device__ __forceinline__ unsigned packed_key(T v, int e)
+{
+    constexpr unsigned INF = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+    unsigned u = bits_of(v);
+    const bool masked = (u & 0x7fffu) > INF || u == (0x8000u | INF);
+    u = u == 0x8000u ? 0u : u;                              // both zeros are one
+    u = (u & 0x8000u) ? ~u : u | 0x8000u;
+    return masked ? 0u : (u << 16) | (unsigned)(0xffff - e);
+}
+template <typename T> __device__ __forceinline__ float packed_value(unsigned key)
+{
+    const unsigned u = key >> 16;
+    return usable(to_f32(from_bits<T>((u & 0x8000u) ? u & 0x7fffu : ~u & 0xffffu)));
+}
+__device__ __forceinline__ int packed_expert(unsigned key) { return 0xffff - (int)(key & 0xffffu); }
+
+// Eight keys in descending order, none equal to another but masked ones: 19 exchanges.
+__device__ __forceinline__ void sort_eight(unsigned (&k)[8])
+{
+    auto order = [&](int a, int b) {
+        const unsigned x = max(k[a], k[b]), y = min(k[a], k[b]);
+        k[a] = x, k[b] = y;
+    };
+    order(0, 2), order(1, 3), order(4, 6), order(5, 7);
+    order(0, 4), order(1, 5), order(2, 6), order(3, 7);
+    order(0, 1), order(2, 3), order(4, 5), order(6, 7);
+    order(2, 4), order(3, 5);
+    order(1, 4), order(3, 6);
+    order(1, 2), order(3, 4), order(5, 6);
+}
+
+// Masks the keys of the experts outside the row's best groups.
+template <int G, int NR>
+__device__ __forceinline__ void keep_groups(const RouteP &p, unsigned (&key)[NR], int lane)
+{
+    const int at = lane & (G - 1), base = lane & ~(G - 1), e0 = at * NR;
+    const int lanes = p.per_group / NR;                 // per group, where each holds one group's experts only
+    if (p.per_group % NR == 0 && (lanes & (lanes - 1)) == 0) {
+        unsigned first = 0, second = 0;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            float c = l[r];
-            if (p.by_score && c > -INFINITY) {
-                const int e = expert_at<V>(r, lane);
-                c = p.sigmoid ? sigmoid_of(c) : expf(c - top) / total;
-                if (p.bias) c += p.bias[e];
-            }
-            key[r] = key_of(c);
+            second = max(second, min(first, key[r]));
+            first = max(first, key[r]);
         }
-        if (GROUPS) {
-            float mine = -INFINITY;                     // value of group `lane`
-            for (int g = 0; g < p.groups; ++g) {
-                unsigned first = 0, second = 0;
-#pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                    const unsigned x = group[r] == g ? key[r] : 0u;
-                    second = max(second, min(first, x));
-                    first = max(first, x);
-                }
-                const unsigned best = __reduce_max_sync(FULL, first);
-                float v = best ? value_of(best) : -INFINITY;
-                if (p.group_best == 2) {
-                    const int owner = __ffs(__ballot_sync(FULL, first == best)) - 1;
-                    const unsigned next = __reduce_max_sync(FULL, lane == owner ? second : first);
-                    if (next) v += value_of(next);
-                }
-                if (lane == g) mine = v;
-            }
-            int before = 0;                             // groups that come first: larger, or equal with a lower index
-            for (int g = 0; g < p.groups; ++g) {
-                const float v = __shfl_sync(FULL, mine, g);
-                before += v > mine || (v == mine && g < lane);
-            }
-            const unsigned taken = __ballot_sync(FULL, lane < p.groups && before < p.top_groups);
-#pragma unroll
-            for (int r = 0; r < NR; ++r)
-                if (group[r] >= 32 || !(taken >> group[r] & 1u)) key[r] = 0;
+        for (int o = 1; o < lanes; o <<= 1) {
+            const unsigned f = __shfl_xor_sync(FULL, first, o), s = __shfl_xor_sync(FULL, second, o);
+            second = max(min(first, f), max(second, s));
+            first = max(first, f);
         }
-        int chosen = -1;                                // of slot `lane`
-        for (int j = 0; j < p.k; ++j) {
-            unsigned best = 0;
-#pragma unroll
-            for (int r = 0; r < NR; ++r) best = max(best, key[r]);
-            best = __reduce_max_sync(FULL, best);
-            if (best == 0) break;                       // uniform: nothing is left
-            unsigned at = 0xffffffffu;
-#pragma unroll
-            for (int r = NR - 1; r >= 0; --r)
-                if (key[r] == best) at = expert_at<V>(r, lane);
-            at = __reduce_min_sync(FULL, at);
-#pragma unroll
-            for (int r = 0; r < NR; ++r)
-                if (expert_at<V>(r, lane) == (int)at) key[r] = 0;
-            if (lane == j) chosen = (int)at;
+        float mine = first ? value_of(first) : -INFINITY;
+        if (p.group_best == 2 && second) mine += value_of(second);
+        const int group = at / lanes;
+        int before = 0;                                 // groups that come first: larger, or equal with a lower index
+        for (int g = 0; g < p.groups; ++g) {
+            const float v = __shfl_sync(FULL, mine, base + g * lanes);
+            before += v > mine || (v == mine && g < group);
         }
-        const float x = chosen >= 0 ? usable(to_f32(logits[chosen])) : -INFINITY;
-        float g = 0.0f;
-        if (p.sigmoid) {
-            g = chosen >= 0 ? sigmoid_of(x) : 0.0f;
-        } else if (p.renormalise) {
-            g = exp_from(x, warp_max(x));
+        if (before >= p.top_groups) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) key[r] = 0;
+        }
+        return;
+    }
+    // groups that begin inside a lane's run: their values one after the other, then each key's group is looked up
+    unsigned taken = 0;
+    for (int g = 0; g < p.groups; ++g) {
+        float v = -INFINITY, mine = -INFINITY;
+        int before = 0;
+        for (int h = -1; h < p.groups; ++h) {           // h = -1: this group's own value
+            const int which = h < 0 ? g : h, lo = which * p.per_group, hi = lo + p.per_group;
+            unsigned first = 0, second = 0;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const unsigned x = e0 + r >= lo && e0 + r < hi ? key[r] : 0u;
+                second = max(second, min(first, x));
+                first = max(first, x);
+            }
+#pragma unroll
+            for (int o = G / 2; o > 0; o >>= 1) {
+                const unsigned f = __shfl_xor_sync(FULL, first, o), s = __shfl_xor_sync(FULL, second, o);
+                second = max(min(first, f), max(second, s));
+                first = max(first, f);
+            }
+            v = first ? value_of(first) : -INFINITY;
+            if (p.group_best == 2 && second) v += value_of(second);
+            if (h < 0) mine = v;
+            else before += v > mine || (v == mine && h < g);
+        }
+        if (before < p.top_groups) taken |= 1u << g;
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int g = (e0 + r) / p.per_group;
+        if (g >= p.groups || !(taken >> g & 1u)) key[r] = 0;
+    }
+}
+
+// PACKED: 16-bit logits that are compared themselves, without groups.
+template <typename T, int G, int NR, int V, bool PACKED>
+__global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteP p)
+{
+    constexpr int SLOTS = G >= 32 ? 1 : (32 / G < NR ? 32 / G : NR);     // slots of the choice per lane: slot j is lane j % G's
+    constexpr int ROWS = ROUTE_THREADS / G;                             // per block at once
+    extern __shared__ int histogram[];
+    const int lane = threadIdx.x & 31, at = lane & (G - 1), base = lane & ~(G - 1), e0 = at * NR;
+    if (p.counts) {
+        for (int i = threadIdx.x; i < p.experts; i += ROUTE_THREADS) histogram[i] = 0;
+        __syncthreads();
+    }
+    // a warp's rows come and go together: the loop ends when its first row is beyond the last
+    for (int row0 = blockIdx.x * ROWS + (threadIdx.x / 32) * (32 / G); row0 < p.rows; row0 += gridDim.x * ROWS) {
+        const int row = row0 + lane / G;
+        const bool live = row < p.rows;
+        const T *logits = static_cast<const T *>(p.logits) + (long long)row * p.stride;
+        T raw[NR];
+        load_logits<T, NR, V>(logits, live ? p.experts : 0, e0, raw);
+        float top = -INFINITY, total = 0.0f;                // softmax over the row
+        if (!p.sigmoid && (p.by_score || !p.renormalise)) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) top = fmaxf(top, usable(to_f32(raw[r])));
+            top = group_max<G>(top);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) total += exp_from(usable(to_f32(raw[r])), top);
+            total = group_sum<G>(total);
+        }
+        unsigned key[NR];
+        unsigned order = 0;                                 // 4 bits each: which of the lane's eight logits
+        if constexpr (PACKED) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) key[r] = packed_key(raw[r], e0 + r);
+            if constexpr (NR == 8) sort_eight(key);
         } else {
-            g = exp_from(x, top) / total;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                float c = usable(to_f32(raw[r]));
+                if (p.by_score && c > -INFINITY) {
+                    c = p.sigmoid ? sigmoid_of(c) : expf(c - top) / total;
+                    if (p.bias) c += p.bias[e0 + r];
+                }
+                key[r] = key_of(c);
+            }
+            if (p.groups > 1) keep_groups<G, NR>(p, key, lane);
+            if constexpr (NR == 8) {
+                // descending, equal keys in the order of their experts: neighbours are exchanged only where the later one is larger
+                int idx[NR];
+#pragma unroll
+                for (int r = 0; r < NR; ++r) idx[r] = r;
+#pragma unroll
+                for (int pass = 0; pass < NR; ++pass)
+#pragma unroll
+                    for (int r = pass & 1; r + 1 < NR; r += 2) {
+                        const bool swap = key[r + 1] > key[r];
+                        const unsigned a = key[r], b = key[r + 1];
+                        key[r] = max(a, b), key[r + 1] = min(a, b);
+                        const int i = idx[r], j = idx[r + 1];
+                        idx[r] = swap ? j : i, idx[r + 1] = swap ? i : j;
+                    }
+#pragma unroll
+                for (int r = 0; r < NR; ++r) order |= (unsigned)idx[r] << (4 * r);
+            }
         }
-        if (p.renormalise) {
-            const float sum = warp_sum(g);
-            g = sum > 0.0f ? g / sum : 0.0f;
+        int chosen[SLOTS];
+        unsigned chosen_key[SLOTS];
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            chosen[s] = -1;
+            chosen_key[s] = 0;
+            for (int t = 0; t < G && s * G + t < p.k; ++t) {
+                unsigned head = key[0];
+                if constexpr (NR > 8) {
+#pragma unroll
+                    for (int r = 1; r < NR; ++r) head = max(head, key[r]);
+                }
+                const unsigned best = group_max<G>(head);
+                if constexpr (PACKED) {
+                    if constexpr (NR == 8) {
+                        if (head == best) {
+#pragma unroll
+                            for (int r = 0; r + 1 < NR; ++r) key[r] = key[r + 1];
+                            key[NR - 1] = 0;
+                        }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < NR; ++r) key[r] = key[r] == best ? 0u : key[r];
+                    }
+                    if (at == t) chosen_key[s] = best;
+                } else {
+                    const unsigned holders = __ballot_sync(FULL, head == best) >> base;
+                    const int owner = __ffs(G == 32 ? holders : holders & ((1u << (G & 31)) - 1u)) - 1;
+                    int e = e0;
+                    if constexpr (NR == 8) {
+                        e += (int)(order & 15u);
+                        if (at == owner) {
+#pragma unroll
+                            for (int r = 0; r + 1 < NR; ++r) key[r] = key[r + 1];
+                            key[NR - 1] = 0;
+                            order >>= 4;
+                        }
+                    } else {
+                        bool found = at != owner;
+#pragma unroll
+                        for (int r = 0; r < NR; ++r) {
+                            const bool hit = !found && key[r] == best;
+                            if (hit) e = e0 + r, key[r] = 0;
+                            found = found || hit;
+                        }
+                    }
+                    e = __shfl_sync(FULL, e, base + owner);
+                    if (at == t && best) {
+                        chosen[s] = e;
+                        chosen_key[s] = best;
+                    }
+                }
+            }
+            if (PACKED && chosen_key[s]) chosen[s] = packed_expert(chosen_key[s]);
         }
-        if (lane < p.k) {
-            p.expert[(long long)row * p.k + lane] = chosen;
-            p.gate[(long long)row * p.k + lane] = chosen >= 0 ? p.gate_scale * g : 0.0f;
-            if (p.counts && chosen >= 0) atomicAdd(&histogram[chosen], 1);
+        // slots beyond the k-th belong to nobody (s * G >= p.k for all lanes alike)
+        float g[SLOTS], sum = 0.0f, most = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            if (s * G >= p.k) continue;
+            g[s] = -INFINITY;                               // the chosen logit
+            if (chosen[s] >= 0)
+                g[s] = PACKED ? packed_value<T>(chosen_key[s]) : p.by_score ? usable(to_f32(logits[chosen[s]])) : value_of(chosen_key[s]);
+            most = fmaxf(most, g[s]);
+        }
+        if (!p.sigmoid && p.renormalise) top = group_max<G>(most);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            if (s * G >= p.k) continue;
+            if (p.sigmoid) g[s] = chosen[s] >= 0 ? sigmoid_of(g[s]) : 0.0f;
+            else g[s] = p.renormalise ? exp_from(g[s], top) : exp_from(g[s], top) / total;
+            sum += chosen[s] >= 0 ? g[s] : 0.0f;
+        }
+        if (p.renormalise) sum = group_sum<G>(sum);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const int j = s * G + at;
+            if (s * G >= p.k || !live || j >= p.k) continue;
+            float v = 0.0f;
+            if (chosen[s] >= 0 && (!p.renormalise || sum > 0.0f)) v = p.gate_scale * (p.renormalise ? g[s] / sum : g[s]);
+            p.expert[(long long)row * p.k + j] = chosen[s];
+            p.gate[(long long)row * p.k + j] = v;
+            if (p.counts && chosen[s] >= 0) atomicAdd(&histogram[chosen[s]], 1);
         }
     }
-    if (p.counts) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < p.experts; i += blockDim.x) {
-            if (gridDim.x == 1) p.counts[i] = histogram[i];
-            else if (histogram[i]) atomicAdd(&p.counts[i], histogram[i]);      // whole numbers: any order
-        }
+    if (!p.counts) return;
+    __syncthreads();
+    if (p.cluster) {
+        cluster_sync_all();
+        if (blockIdx.x == 0)
+            for (int i = threadIdx.x; i < p.experts; i += ROUTE_THREADS) {
+                int n = 0;
+                for (unsigned b = 0; b < gridDim.x; ++b) n += (int)ld_shared_cluster_u32(map_to_cta(smem_u32(&histogram[i]), b));
+                p.counts[i] = n;
+            }
+        cluster_sync_all();                                 // the histograms stay until they have been read
+    } else {
+        for (int i = threadIdx.x; i < p.experts; i += ROUTE_THREADS)
+            if (histogram[i]) atomicAdd(&p.counts[i], histogram[i]);      // whole numbers: any order
     }
 }
 
@@ -193,91 +380,127 @@ struct RouteBackP {
 //   softmax, renormalised w_j (c dgate_j - sum c dgate w)    the chosen ones, 0 elsewhere
 //   sigmoid              c dgate_j s_j (1 - s_j)
 //   sigmoid, renormalised w_j (1 - s_j) (c dgate_j - sum c dgate w)
-template <typename T, int NR, int V>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_kernel(const RouteBackP p)
+// Every expert's value is written first, as if it were not chosen, and then the chosen ones' over it.  The softmax over the
+// whole row takes the approximate power of two (relative error about 2^-22 + |l - max| 2^-23).
+template <typename T, int G, int NR, int V>
+__global__ void __launch_bounds__(ROUTE_THREADS) route_backward_kernel(const RouteBackP p)
 {
-    const int lane = threadIdx.x & 31;
-    for (int row = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); row < p.rows; row += gridDim.x * ROUTE_WARPS) {
-        const T *logits = static_cast<const T *>(p.logits) + row * p.stride;
-        T *out = static_cast<T *>(p.dlogits) + row * p.out_stride;
-        int e = -1;
-        float d = 0.0f;
-        if (lane < p.k) {
-            e = p.expert[(long long)row * p.k + lane];
-            d = p.gate_scale * p.dgate[(long long)row * p.k + lane];
-            if (e < 0 || e >= p.experts) e = -1, d = 0.0f;
+    constexpr int SLOTS = G >= 32 ? 1 : (32 / G < NR ? 32 / G : NR);
+    constexpr int ROWS = ROUTE_THREADS / G;
+    constexpr float LOG2E = 1.4426950408889634f;
+    const int lane = threadIdx.x & 31, at = lane & (G - 1), e0 = at * NR;
+    for (int row0 = blockIdx.x * ROWS + (threadIdx.x / 32) * (32 / G); row0 < p.rows; row0 += gridDim.x * ROWS) {
+        const int row = row0 + lane / G;
+        const bool live = row < p.rows;
+        const T *logits = static_cast<const T *>(p.logits) + (long long)row * p.stride;
+        T *out = static_cast<T *>(p.dlogits) + (long long)row * p.out_stride;
+        int e[SLOTS];
+        float d[SLOTS], x[SLOTS];
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const int j = s * G + at;
+            e[s] = -1, d[s] = 0.0f, x[s] = -INFINITY;
+            if (live && j < p.k) {
+                const int chosen = p.expert[(long long)row * p.k + j];
+                const float dg = p.dgate[(long long)row * p.k + j];
+                if (chosen >= 0 && chosen < p.experts) {
+                    e[s] = chosen;
+                    x[s] = usable(to_f32(logits[chosen]));
+                    d[s] = x[s] > -INFINITY ? p.gate_scale * dg : 0.0f;
+                }
+            }
         }
-        float x = e >= 0 ? usable(to_f32(logits[e])) : -INFINITY;
-        if (!(x > -INFINITY)) d = 0.0f;
-        float dense[NR];                                // what an expert that was not chosen gets
+        float dense[NR];                                    // what an expert that was not chosen gets
 #pragma unroll
         for (int r = 0; r < NR; ++r) dense[r] = 0.0f;
-        float mine;
+        float mine[SLOTS] = {}, dot = 0.0f;
         if (!p.sigmoid && !p.renormalise) {
-            float l[NR];
-            load_row<T, NR, V>(logits, p.experts, lane, l);
-            float top = -INFINITY, total = 0.0f;
+            T raw[NR];
+            float l[NR], top = -INFINITY, total = 0.0f;
+            load_logits<T, NR, V>(logits, live ? p.experts : 0, e0, raw);
 #pragma unroll
-            for (int r = 0; r < NR; ++r) top = fmaxf(top, l[r]);
-            top = warp_max(top);
+            for (int r = 0; r < NR; ++r) top = fmaxf(top, l[r] = usable(to_f32(raw[r])));
+            top = group_max<G>(top);
+            const float shift = top > -INFINITY ? -top * LOG2E : 0.0f;
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
-                dense[r] = exp_from(l[r], top);
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(dense[r]) : "f"(fmaf(l[r], LOG2E, shift)));
                 total += dense[r];
             }
-            total = warp_sum(total);
+            total = group_sum<G>(total);
             const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-            const float s = exp_from(x, top) * inv;
-            const float dot = warp_sum(d * s);
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                if (s * G >= p.k) continue;
+                float v;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(v) : "f"(fmaf(x[s], LOG2E, shift)));
+                mine[s] = v * inv;
+                dot = fmaf(d[s], mine[s], dot);
+            }
+            dot = group_sum<G>(dot);
 #pragma unroll
             for (int r = 0; r < NR; ++r) dense[r] *= -inv * dot;
-            mine = s * (d - dot);
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) mine[s] *= d[s] - dot;
         } else {
-            const float s = p.sigmoid ? (x > -INFINITY ? sigmoid_of(x) : 0.0f) : exp_from(x, warp_max(x));
-            float w = s, dot = 0.0f;
-            if (p.renormalise) {
-                const float sum = warp_sum(s);
-                w = sum > 0.0f ? s / sum : 0.0f;
-                dot = warp_sum(d * w);
+            float most = -INFINITY, sum = 0.0f, slope[SLOTS] = {};
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) most = fmaxf(most, x[s]);
+            if (!p.sigmoid) most = group_max<G>(most);
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                if (s * G >= p.k) continue;
+                mine[s] = p.sigmoid ? (x[s] > -INFINITY ? sigmoid_of(x[s]) : 0.0f) : exp_from(x[s], most);
+                slope[s] = p.sigmoid ? 1.0f - mine[s] : 1.0f;
+                sum += mine[s];
             }
-            mine = w * (d - dot) * (p.sigmoid ? 1.0f - s : 1.0f);
+            if (p.renormalise) {
+                sum = group_sum<G>(sum);
+#pragma unroll
+                for (int s = 0; s < SLOTS; ++s) {
+                    if (s * G >= p.k) continue;
+                    mine[s] = sum > 0.0f ? mine[s] / sum : 0.0f;
+                    dot = fmaf(d[s], mine[s], dot);
+                }
+                dot = group_sum<G>(dot);
+            }
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) mine[s] = mine[s] * (d[s] - dot) * slope[s];
         }
-        __syncwarp();                                   // every logit of the row has been read: out may be logits
+        __syncwarp();                                       // every logit of the row has been read: out may be logits
 #pragma unroll
         for (int r = 0; r < NR; r += V) {
-            const int at = expert_at<V>(r, lane);
-            if (at < p.experts) {
+            if (live && e0 + r < p.experts) {
                 Pack<T, V> o;
 #pragma unroll
                 for (int j = 0; j < V; ++j) o.v[j] = from_f32<T>(dense[r + j]);
-                store_pack<T, V>(out + at, o);
+                store_pack<T, V>(out + e0 + r, o);
             }
         }
-        __syncwarp();                                   // the chosen ones' values come after the others'
-        if (e >= 0) out[e] = from_f32<T>(mine);
+        __syncwarp();                                       // the chosen ones' values come after the others'
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (e[s] >= 0) out[e[s]] = from_f32<T>(mine[s]);
     }
 }
 
-template <int A, int B> struct Pair { static constexpr int nr = A, v = B; };
-// Calls f with the logits per lane and, where rows allow it, as many neighbours as 16 bytes hold.
+template <int A, int B, int C> struct Shape { static constexpr int g = A, nr = B, v = C; };
+// Calls f with the lanes per row, the logits per lane and how many of them a load takes: 16 bytes where the rows allow it.
 template <typename T, typename F> int with_row(int experts, bool wide, F f)
 {
     constexpr int W = 16 / (int)sizeof(T);
-    if (experts <= 32) return f(Pair<1, 1>());
-    if (experts <= 64) return wide ? f(Pair<2, 2>()) : f(Pair<2, 1>());
-    if (experts <= 128) return wide ? f(Pair<4, 4>()) : f(Pair<4, 1>());
-    if (experts <= 256) return wide ? f(Pair<8, W>()) : f(Pair<8, 1>());
-    if (experts <= 512) return wide ? f(Pair<16, W>()) : f(Pair<16, 1>());
-    return wide ? f(Pair<32, W>()) : f(Pair<32, 1>());
-}
-// Neighbours per load that with_row takes for a wide row.
-template <typename T> int wide_of(int experts)
-{
-    const int w = 16 / (int)sizeof(T);
-    return experts <= 32 ? 1 : experts <= 64 ? 2 : experts <= 128 ? std::min(4, w) : w;
+    auto by_width = [&](auto s) { return wide ? f(Shape<decltype(s)::g, decltype(s)::nr, W>()) : f(Shape<decltype(s)::g, decltype(s)::nr, 1>()); };
+    if (experts <= 8) return by_width(Shape<1, 8, 1>());
+    if (experts <= 16) return by_width(Shape<2, 8, 1>());
+    if (experts <= 32) return by_width(Shape<4, 8, 1>());
+    if (experts <= 64) return by_width(Shape<8, 8, 1>());
+    if (experts <= 128) return by_width(Shape<16, 8, 1>());
+    if (experts <= 256) return by_width(Shape<32, 8, 1>());
+    if (experts <= 512) return by_width(Shape<32, 16, 1>());
+    return by_width(Shape<32, 32, 1>());
 }
 
-int blocks_for(int rows) { return std::min((rows + ROUTE_WARPS - 1) / ROUTE_WARPS, ROUTE_BLOCKS); }
+int blocks_for(int rows, int lanes) { return (int)std::min(((long long)rows * lanes + ROUTE_THREADS - 1) / ROUTE_THREADS, (long long)ROUTE_BLOCKS); }
 
 }  // namespace
 
@@ -291,29 +514,45 @@ extern "C" int moe_ovl_route(const moe_ovl_route_args *a)
     if (a->num_experts > MOE_OVL_MAX_ROUTED || a->top_k > MOE_OVL_MAX_TOP_K || a->num_groups > 32) return MOE_OVL_ERR_UNSUPPORTED;
     const int es = dtype_bytes(a->dtype);
     if (a->rows > 0 && (!a->logits || !a->expert || !a->gate || !aligned(a->logits, es) || !aligned(a->expert, 4) || !aligned(a->gate, 4) ||
-                        a->logits_stride >= (1ll << 40) || (a->rows > 1 && a->logits_stride < a->num_experts)))
+                        (a->rows > 1 && a->logits_stride < a->num_experts)))
         return MOE_OVL_ERR_INVALID_ARG;
+    if (a->logits_stride > 0x7fffffff) return MOE_OVL_ERR_UNSUPPORTED;
     if (!aligned(a->bias, 4) || !aligned(a->counts, 4)) return MOE_OVL_ERR_INVALID_ARG;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
-    const int blocks = blocks_for(a->rows);
-    // one block stores its counts; several add to them
-    if (a->counts && blocks != 1 && cudaMemsetAsync(a->counts, 0, (size_t)a->num_experts * 4, stream) != cudaSuccess) return MOE_OVL_ERR_CUDA;
-    if (a->rows == 0) return MOE_OVL_OK;
+    if (a->rows == 0)
+        return !a->counts || cudaMemsetAsync(a->counts, 0, (size_t)a->num_experts * 4, stream) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
     RouteP p = {a->rows, a->num_experts, a->top_k, a->num_groups, a->num_experts / a->num_groups, a->top_groups, a->group_best,
                 a->score == MOE_OVL_SCORE_SIGMOID, a->renormalise != 0, a->bias != nullptr || (a->num_groups > 1 && a->group_best == 2),
-                a->gate_scale, a->logits, a->bias, a->expert, a->gate, a->counts, a->logits_stride};
+                false, a->gate_scale, a->logits, a->bias, a->expert, a->gate, a->counts, a->logits_stride};
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        const int v = wide_of<T>(p.experts);
-        const bool wide = p.experts % v == 0 && p.stride % v == 0 && aligned(p.logits, v * sizeof(T));
+        constexpr int W = 16 / (int)sizeof(T);
+        const bool wide = p.experts % W == 0 && p.stride % W == 0 && aligned(p.logits, 16);
         return with_row<T>(p.experts, wide, [&](auto c) {
-            constexpr int NR = decltype(c)::nr, V = std::min(decltype(c)::v, 16 / (int)sizeof(T));
-            const size_t smem = p.counts ? (size_t)p.experts * 4 : 0;
-            if (p.groups > 1) route_kernel<T, NR, V, true><<<blocks, 32 * ROUTE_WARPS, smem, stream>>>(p);
-            else route_kernel<T, NR, V, false><<<blocks, 32 * ROUTE_WARPS, smem, stream>>>(p);
-            return launched();
+            using C = decltype(c);
+            const bool packed = sizeof(T) == 2 && !p.by_score && p.groups == 1;
+            const auto kernel = packed ? route_kernel<T, C::g, C::nr, C::v, sizeof(T) == 2> : route_kernel<T, C::g, C::nr, C::v, false>;
+            const int blocks = blocks_for(p.rows, C::g);
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)blocks);
+            cfg.blockDim = dim3(ROUTE_THREADS);
+            cfg.dynamicSmemBytes = p.counts ? (size_t)p.experts * 4 : 0;
+            cfg.stream = stream;
+            cudaLaunchAttribute attr[1];
+            if (p.counts && blocks <= 8) {
+                // a few blocks add their counts up among themselves; more of them add to memory that has been cleared
+                p.cluster = true;
+                attr[0].id = cudaLaunchAttributeClusterDimension;
+                attr[0].val.clusterDim.x = (unsigned)blocks;
+                attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+                cfg.attrs = attr;
+                cfg.numAttrs = 1;
+            } else if (p.counts && cudaMemsetAsync(p.counts, 0, (size_t)p.experts * 4, stream) != cudaSuccess) {
+                return MOE_OVL_ERR_CUDA;
+            }
+            return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
         });
     });
 }
@@ -328,21 +567,21 @@ extern "C" int moe_ovl_route_backward(const moe_ovl_route_backward_args *a)
     if (a->rows == 0) return MOE_OVL_OK;
     const int es = dtype_bytes(a->dtype);
     if (!a->logits || !a->expert || !a->dgate || !a->dlogits || !aligned(a->logits, es) || !aligned(a->dlogits, es) || !aligned(a->expert, 4) ||
-        !aligned(a->dgate, 4) || a->logits_stride >= (1ll << 40) || a->dlogits_stride >= (1ll << 40) ||
-        (a->rows > 1 && (a->logits_stride < a->num_experts || a->dlogits_stride < a->num_experts)))
+        !aligned(a->dgate, 4) || (a->rows > 1 && (a->logits_stride < a->num_experts || a->dlogits_stride < a->num_experts)))
         return MOE_OVL_ERR_INVALID_ARG;
+    if (std::max(a->logits_stride, a->dlogits_stride) > 0x7fffffff) return MOE_OVL_ERR_UNSUPPORTED;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
     RouteBackP p = {a->rows, a->num_experts, a->top_k, a->score == MOE_OVL_SCORE_SIGMOID, a->renormalise != 0, a->gate_scale,
                     a->logits, a->expert, a->dgate, a->dlogits, a->logits_stride, a->dlogits_stride};
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        const int v = wide_of<T>(p.experts);
-        const bool wide = p.experts % v == 0 && p.stride % v == 0 && p.out_stride % v == 0 && aligned(p.logits, v * sizeof(T)) &&
-                          aligned(p.dlogits, v * sizeof(T));
+        constexpr int W = 16 / (int)sizeof(T);
+        const bool wide = p.experts % W == 0 && p.stride % W == 0 && p.out_stride % W == 0 && aligned(p.logits, 16) && aligned(p.dlogits, 16);
         return with_row<T>(p.experts, wide, [&](auto c) {
-            constexpr int NR = decltype(c)::nr, V = std::min(decltype(c)::v, 16 / (int)sizeof(T));
-            route_backward_kernel<T, NR, V><<<blocks_for(p.rows), 32 * ROUTE_WARPS, 0, static_cast<cudaStream_t>(a->stream)>>>(p);
+            using C = decltype(c);
+            route_backward_kernel<T, C::g, C::nr, C::v>
+                <<<blocks_for(p.rows, C::g), ROUTE_THREADS, 0, static_cast<cudaStream_t>(a->stream)>>>(p);
             return launched();
         });
     });

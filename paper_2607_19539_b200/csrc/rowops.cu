@@ -3,7 +3,13 @@
 //
 // All of them read each element once, need one reduction over the row, and write once: they are bound by HBM.  A row is
 // held in registers between the two (NV packs of VEC elements per thread), so nothing is read twice.  The row's
-// threads are one block, or one warp where the row is short (several rows per block then, and no block barrier).
+// threads are one block, or one warp where the row is short (several rows per block then, and no block barrier).  Blocks
+// stay and take rows at a fixed distance, and what belongs to a column (weights, the weight gradient's sums) stays in registers.
+// The next row's loads are under way while a row is reduced and written: in registers, and in the gradient's kernel, which has
+// three matrices to read and sums to keep, in shared memory up to four rows deep (struct Feed).
+#include <algorithm>
+#include <atomic>
+
 #include "opcommon.cuh"
 
 using namespace moe_ovl;
@@ -15,17 +21,25 @@ constexpr float QUANT_TINY = 7.8886090522101181e-31f;      // 2^-100
 constexpr int NORM_PARTIALS = 592;                          // most partial rows of the weight gradient: 148 SMs x 4
 
 // Threads a block of a kernel with so many values per thread may have: the row lives in registers.
-constexpr int max_threads(int values) { return values <= 16 ? 1024 : 512; }
+constexpr int max_threads(int values) { return values <= 8 ? 1024 : 512; }
+constexpr int swiglu_threads(int values) { return values <= 16 ? 1024 : 512; }     // 14336 columns fit a block of 896 threads, a row in 64 registers each
 
-// Sum / largest magnitude over the threads of one row.  `buf`: 32 floats that no thread of the block still reads.
+// Sums and largest values over the threads of one row.  `buf`: values of the row's warps, that no thread of the block still reads.
+// In the second step every warp adds up all warps' values.
+__device__ __forceinline__ float sum_of_warps(float v, int lane)
+{
+    const int warps = blockDim.x >> 5;
+    v = lane < warps ? v : 0.0f;
+    for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return __shfl_sync(0xffffffffu, v, 0);
+}
 __device__ __forceinline__ float row_sum(float v, float *buf)
 {
     v = warp_sum(v);
     if (blockDim.x == 32) return v;
     if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return warp_sum(lane < (int)(blockDim.x >> 5) ? buf[lane] : 0.0f);
+    return sum_of_warps(buf[threadIdx.x & 31], threadIdx.x & 31);
 }
 __device__ __forceinline__ float row_max(float v, float *buf)
 {
@@ -44,123 +58,221 @@ __device__ __forceinline__ void row_sum_max(float &s, float &m, float2 *buf)
     if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = make_float2(s, m);
     __syncthreads();
     const int lane = threadIdx.x & 31;
-    const float2 t = lane < (int)(blockDim.x >> 5) ? buf[lane] : make_float2(0.0f, 0.0f);
-    s = warp_sum(t.x);
-    m = warp_max(t.y);
+    const float2 t = buf[lane];
+    s = sum_of_warps(t.x, lane);
+    m = warp_max(lane < (int)(blockDim.x >> 5) ? t.y : 0.0f);
 }
 
 // scale = most / 127 and the factor that takes a value to its 8 bits; a row of (almost) nothing gives zeros.
 __device__ __forceinline__ float2 quant_scale(float most)
 {
     if (most < QUANT_TINY) return make_float2(0.0f, 0.0f);
-    return make_float2(most / QUANT_MAX, QUANT_MAX / most);
+    return make_float2(most * (1.0f / QUANT_MAX), QUANT_MAX / most);
 }
-// To the nearest whole number, ties to even; a NaN gives 0.
-__device__ __forceinline__ int8_t quant(float v, float inverse)
+// VEC values in 8 bits: v * factor to the nearest whole number, ties to even.  Adding 1.5 * 2^23 rounds to a whole number and leaves it,
+// as two's complement, in the float's low byte (|v * factor| <= 127 (1 + 2^-22): nothing to clamp); the conversion instruction has a
+// fraction of that rate.  A row that holds a NaN or an infinity gives zeros: `keep` is 0 then.
+template <int VEC> __device__ __forceinline__ void store_quant(int8_t *q, const float *v, float factor, uint32_t keep)
 {
-    const int i = __float2int_rn(v * inverse);
-    return (int8_t)max(-127, min(127, i));
+    if constexpr (VEC == 1) {
+        *q = (int8_t)(__float_as_uint(fmaf(v[0], factor, 12582912.0f)) & keep);
+    } else if constexpr (VEC == 2) {
+        const float2 t = fma2(make_float2(v[0], v[1]), both(factor), both(12582912.0f));
+        *reinterpret_cast<uint16_t *>(q) = (uint16_t)(__byte_perm(__float_as_uint(t.x), __float_as_uint(t.y), 0x0040) & keep);
+    } else {
+        uint32_t b[VEC], w[VEC / 4];
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) {
+            const float2 t = fma2(make_float2(v[j], v[j + 1]), both(factor), both(12582912.0f));
+            b[j] = __float_as_uint(t.x), b[j + 1] = __float_as_uint(t.y);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC / 4; ++j)
+            w[j] = __byte_perm(__byte_perm(b[4 * j], b[4 * j + 1], 0x0040), __byte_perm(b[4 * j + 2], b[4 * j + 3], 0x0040), 0x5410) & keep;
+        if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(q) = w[0];
+    }
 }
+__device__ __forceinline__ uint32_t keep_mask(float most) { return most <= 3.402823466e+38f ? 0xffffffffu : 0u; }
+
+// Where row `row` of a matrix begins for a thread whose first column is c.
+template <typename T> __device__ __forceinline__ T *at_row(T *base, int row, int stride, int c) { return base + ((long long)row * stride + c); }
+
+// Rows on their way from global to shared memory.  Every thread copies, waits for and reads its own packs only (asynchronous
+// copies of 16 or 4 bytes), so no thread waits for another.  `depth` rows are on their way; 0: the packs are loaded when they are
+// needed (elements of two bytes, which such copies do not know, always are).
+template <typename T, int VEC, int NV, int ARRAYS> struct Feed {
+    static constexpr int BYTES = VEC * (int)sizeof(T);
+    static constexpr bool ASYNC = BYTES >= 4;
+    uint32_t base, stride;                      // this thread's first pack, bytes from pack to pack
+    int depth, put = 0, take = 0;
+    __device__ Feed(int depth_) : depth(ASYNC ? depth_ : 0)
+    {
+        extern __shared__ __align__(16) uint8_t feed_memory[];
+        base = (uint32_t)__cvta_generic_to_shared(feed_memory) + (threadIdx.y * blockDim.x + threadIdx.x) * BYTES;
+        stride = blockDim.x * blockDim.y * BYTES;
+    }
+    // Asks for a row: `at[k]` its start for this thread in matrix k (NULL: none), `width` columns from there on, `across` from pack to pack.
+    __device__ __forceinline__ void ask(const T *const (&at)[ARRAYS], bool any, int width, int across)
+    {
+        if constexpr (ASYNC) {
+            if (any) {
+#pragma unroll
+                for (int k = 0; k < ARRAYS; ++k)
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        if (at[k] && i * across < width) {
+                            const uint32_t to = base + ((put * ARRAYS + k) * NV + i) * stride;
+                            if constexpr (BYTES == 16)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at[k] + i * across) : "memory");
+                            else
+                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(at[k] + i * across) : "memory");
+                        }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++put == depth) put = 0;
+        }
+    }
+    // Waits for the oldest row asked for.
+    __device__ __forceinline__ void wait()
+    {
+        if (depth == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    __device__ __forceinline__ Pack<T, VEC> got(int k, int i) const
+    {
+        Pack<T, VEC> r = {};
+        const uint32_t from = base + ((take * ARRAYS + k) * NV + i) * stride;
+        if constexpr (BYTES == 16) {
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+            *reinterpret_cast<uint4 *>(&r) = v;
+        } else if constexpr (BYTES == 4) {
+            uint32_t v;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
+            *reinterpret_cast<uint32_t *>(&r) = v;
+        }
+        return r;
+    }
+    __device__ __forceinline__ void next()
+    {
+        if (++take == depth) take = 0;
+    }
+};
 
 struct NormP {
     int rows, d;
-    float eps;
+    float per_d, eps;                           // per_d: 1 / d
     const void *x, *residual, *weight;
     void *residual_out, *y;
     int8_t *q;
     float *scale, *rstd;
-    long long x_stride, residual_stride, residual_out_stride, y_stride, q_stride;
+    int x_stride, residual_stride, residual_out_stride, y_stride, q_stride;
 };
 
-// One row per block (or warp).  The row's sum of squares and the largest |h * weight| come out of ONE reduction: rstd is
-// a positive factor of the whole row, so the scale of the 8-bit output needs no second pass over the normed values.
+// The row's sum of squares and the largest |h * weight| come out of ONE reduction: rstd is a positive factor of the whole row,
+// so the scale of the 8-bit output needs no second pass over the normed values.
 template <typename T, typename W, int VEC, int NV>
 __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const NormP p)
 {
-    __shared__ float2 buf[32];
-    const int row = blockIdx.x * blockDim.y + threadIdx.y;
-    if (row >= p.rows) return;                  // whole warps: rows share a block only as one warp each
-    const T *x = static_cast<const T *>(p.x) + row * p.x_stride;
-    const T *res = p.residual ? static_cast<const T *>(p.residual) + row * p.residual_stride : nullptr;
-    T *h_out = p.residual_out ? static_cast<T *>(p.residual_out) + row * p.residual_out_stride : nullptr;
+    __shared__ float2 buf[2][32];
+    const int step = gridDim.x * blockDim.y;
     const W *w = static_cast<const W *>(p.weight);
+    int row = blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= p.rows) return;                  // whole warps: rows share a block only as one warp each
+    const int c0 = threadIdx.x * VEC, across = blockDim.x * VEC;
     Pack<T, VEC> a[NV], b[NV];
+    auto load = [&](int r) {
+        const T *x = at_row(static_cast<const T *>(p.x), r, p.x_stride, c0), *res = at_row(static_cast<const T *>(p.residual), r, p.residual_stride, c0);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        if (c < p.d) {
-            a[i] = load_pack<T, VEC>(x + c);
-            if (res) b[i] = load_pack<T, VEC>(res + c);
-        }
-    }
-    float v[NV * VEC];                          // h, then h * weight
-    float sum = 0.0f, most = 0.0f;
+        for (int i = 0; i < NV; ++i)
+            if (c0 + i * across < p.d) {
+                a[i] = load_pack<T, VEC>(x + i * across);
+                if (p.residual) b[i] = load_pack<T, VEC>(res + i * across);
+            }
+    };
+    load(row);
+    Pack<W, VEC> wv[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        if (c >= p.d) {
+    for (int i = 0; i < NV; ++i)
+        if (c0 + i * across < p.d) wv[i] = load_pack<W, VEC>(w + c0 + i * across);
+    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+        float v[NV * VEC];                      // h * weight
+        float most = 0.0f;
+        float2 sum = both(0.0f);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[i * VEC + j] = 0.0f;
-            continue;
-        }
-        const Pack<W, VEC> wv = load_pack<W, VEC>(w + c);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
+        for (int i = 0; i < NV; ++i) {
+            if (c0 + i * across >= p.d) continue;
             // the sum is rounded to the type it is stored in: the norm is that of the stored value
-            const T h = res ? from_f32<T>(to_f32(a[i].v[j]) + to_f32(b[i].v[j])) : a[i].v[j];
-            a[i].v[j] = h;
-            const float hf = to_f32(h);
-            sum = fmaf(hf, hf, sum);
-            const float t = hf * to_f32(wv.v[j]);
-            v[i * VEC + j] = t;
-            most = max_nan(most, fabsf(t));
+            if constexpr (VEC == 1) {
+                if (p.residual) a[i].v[0] = from_f32<T>(to_f32(a[i].v[0]) + to_f32(b[i].v[0]));
+                const float h = to_f32(a[i].v[0]);
+                sum.x = fmaf(h, h, sum.x);
+                v[i] = h * to_f32(wv[i].v[0]);
+                most = max_abs(most, v[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 2) {
+                    if (p.residual) add_round2(&a[i].v[j], &b[i].v[j]);
+                    const float2 h = to_f32x2(&a[i].v[j]);
+                    sum = fma2(h, h, sum);
+                    const float2 t = mul2(h, to_f32x2(&wv[i].v[j]));
+                    v[i * VEC + j] = t.x, v[i * VEC + j + 1] = t.y;
+                    most = max_abs(most, t);
+                }
+            }
+            if (p.residual_out) store_pack<T, VEC>(at_row(static_cast<T *>(p.residual_out), row, p.residual_out_stride, c0) + i * across, a[i]);
         }
-        if (h_out) store_pack<T, VEC>(h_out + c, a[i]);
-    }
-    row_sum_max(sum, most, buf);
-    const float rstd = 1.0f / sqrtf(sum / (float)p.d + p.eps);
-    if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
-    if (p.y) {
-        T *y = static_cast<T *>(p.y) + row * p.y_stride;
+        if (row + step < p.rows) load(row + step);
+        float total = sum.x + sum.y;
+        row_sum_max(total, most, buf[turn]);
+        const float rstd = rsqrtf(fmaf(total, p.per_d, p.eps));
+        if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
+        if (p.y) {
+            T *y = at_row(static_cast<T *>(p.y), row, p.y_stride, c0);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
-            if (c < p.d) {
-                Pack<T, VEC> o;
+            for (int i = 0; i < NV; ++i) {
+                if (c0 + i * across < p.d) {
+                    Pack<T, VEC> o;
+                    if constexpr (VEC == 1) {
+                        o.v[0] = from_f32<T>(v[i] * rstd);
+                    } else {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) o.v[j] = from_f32<T>(v[i * VEC + j] * rstd);
-                store_pack<T, VEC>(y + c, o);
+                        for (int j = 0; j < VEC; j += 2)
+                            from_f32x2(&o.v[j], mul2(make_float2(v[i * VEC + j], v[i * VEC + j + 1]), both(rstd)));
+                    }
+                    store_pack<T, VEC>(y + i * across, o);
+                }
             }
         }
-    }
-    if (p.q) {
-        const float2 s = quant_scale(most * rstd);
-        if (threadIdx.x == 0) p.scale[row] = s.x;
-        int8_t *q = p.q + row * p.q_stride;
+        if (p.q) {
+            int8_t *q = at_row(p.q, row, p.q_stride, c0);
+            most *= rstd;
+            const float2 s = quant_scale(most);
+            if (threadIdx.x == 0) p.scale[row] = s.x;
+            const float factor = rstd * s.y;
+            const uint32_t keep = keep_mask(most);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
-            if (c < p.d) {
-                Pack<int8_t, VEC> o;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) o.v[j] = quant(v[i * VEC + j] * rstd, s.y);
-                store_pack<int8_t, VEC>(q + c, o);
-            }
+            for (int i = 0; i < NV; ++i)
+                if (c0 + i * across < p.d) store_quant<VEC>(q + i * across, v + i * VEC, factor, keep);
         }
     }
 }
 
 struct NormBackP {
-    int rows, d;
+    int rows, d, depth;
+    float per_d;
     const void *dy, *h, *weight, *d_residual;
     const float *rstd;
     void *dx;
-    float *partial;                             // [gridDim.x * blockDim.y][d] sums of dy * n, or NULL
-    long long dy_stride, h_stride, d_residual_stride, dx_stride;
+    float *partial;                             // [gridDim.x][d] sums of dy * n, or NULL
+    int dy_stride, h_stride, d_residual_stride, dx_stride;
 };
 
-// Every block (or warp) takes rows at a fixed distance and keeps its columns' share of the weight gradient in registers
-// over all of them; the partial rows are added up in a fixed order by reduce_partials_kernel: no atomics, same bits.
+// Every block (or warp) keeps its columns' share of the weight gradient over all of its rows; the partial rows are
+// added up in a fixed order by reduce_partials_kernel: no atomics, the same bits every time.
 template <typename T, typename W, int VEC, int NV>
 __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel(const NormBackP p)
 {
@@ -170,80 +282,151 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel
     for (int i = 0; i < NV * VEC; ++i) acc[i] = 0.0f;
     const int first = blockIdx.x * blockDim.y + threadIdx.y, step = gridDim.x * blockDim.y;
     const W *w = static_cast<const W *>(p.weight);
+    const int c0 = threadIdx.x * VEC, across = blockDim.x * VEC;
+    auto start = [&](int r, const T *(&at)[3]) {
+        at[0] = at_row(static_cast<const T *>(p.dy), r, p.dy_stride, c0);
+        at[1] = at_row(static_cast<const T *>(p.h), r, p.h_stride, c0);
+        at[2] = p.d_residual ? at_row(static_cast<const T *>(p.d_residual), r, p.d_residual_stride, c0) : nullptr;
+    };
+    Feed<T, VEC, NV, 3> feed(p.depth);
+    auto ask = [&](int r) {
+        const T *at[3];
+        start(r, at);
+        feed.ask(at, r < p.rows, p.d - c0, across);
+    };
+    for (int i = 0; i < feed.depth; ++i) ask(first + i * step);
+    Pack<W, VEC> wv[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (c0 + i * across < p.d) wv[i] = load_pack<W, VEC>(w + c0 + i * across);
     int turn = 0;
     for (int row = first; row < p.rows; row += step, turn ^= 1) {
-        const T *dy = static_cast<const T *>(p.dy) + row * p.dy_stride;
-        const T *h = static_cast<const T *>(p.h) + row * p.h_stride;
-        const T *dr = p.d_residual ? static_cast<const T *>(p.d_residual) + row * p.d_residual_stride : nullptr;
-        T *dx = static_cast<T *>(p.dx) + row * p.dx_stride;
         const float rstd = p.rstd[row];
-        Pack<T, VEC> a[NV], b[NV], r[NV];
+        // the row stays as it was loaded for the second half (n = h * rstd and g = dy * weight would take twice the registers)
+        Pack<T, VEC> dy[NV], h[NV], add[NV];
+        if (feed.depth > 0) {
+            feed.wait();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (c0 + i * across < p.d) {
+                    dy[i] = feed.got(0, i);
+                    h[i] = feed.got(1, i);
+                    if (p.d_residual) add[i] = feed.got(2, i);
+                }
+            feed.next();
+        } else {
+            const T *at[3];
+            start(row, at);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (c0 + i * across < p.d) {
+                    dy[i] = load_pack<T, VEC>(at[0] + i * across);
+                    h[i] = load_pack<T, VEC>(at[1] + i * across);
+                    if (p.d_residual) add[i] = load_pack<T, VEC>(at[2] + i * across);
+                }
+        }
+        float2 dot = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
-            if (c < p.d) {
-                a[i] = load_pack<T, VEC>(dy + c);
-                b[i] = load_pack<T, VEC>(h + c);
-                if (dr) r[i] = load_pack<T, VEC>(dr + c);
+            if (c0 + i * across >= p.d) continue;
+            if constexpr (VEC == 1) {
+                const float t = to_f32(dy[i].v[0]), n = to_f32(h[i].v[0]) * rstd;
+                acc[i] = fmaf(t, n, acc[i]);
+                dot.x = fmaf(t * to_f32(wv[i].v[0]), n, dot.x);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 2) {
+                    const int k = i * VEC + j;
+                    const float2 t = to_f32x2(&dy[i].v[j]), n = mul2(to_f32x2(&h[i].v[j]), both(rstd));
+                    const float2 s = fma2(t, n, make_float2(acc[k], acc[k + 1]));
+                    acc[k] = s.x, acc[k + 1] = s.y;
+                    dot = fma2(mul2(t, to_f32x2(&wv[i].v[j])), n, dot);
+                }
             }
         }
-        float dot = 0.0f;
+        if (feed.depth > 0) ask(row + feed.depth * step);
+        // dx = rstd * (g - n * mean) = dy * (weight * rstd) - h * (rstd^2 * mean)
+        const float mean = row_sum(dot.x + dot.y, buf[turn]) * p.per_d, back = -rstd * rstd * mean;
+        T *dx = at_row(static_cast<T *>(p.dx), row, p.dx_stride, c0);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
-            if (c >= p.d) continue;
-            const Pack<W, VEC> wv = load_pack<W, VEC>(w + c);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float n = to_f32(b[i].v[j]) * rstd, t = to_f32(a[i].v[j]);
-                acc[i * VEC + j] = fmaf(t, n, acc[i * VEC + j]);
-                dot = fmaf(t * to_f32(wv.v[j]), n, dot);
-            }
-        }
-        const float mean = row_sum(dot, buf[turn]) / (float)p.d;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
-            if (c >= p.d) continue;
-            const Pack<W, VEC> wv = load_pack<W, VEC>(w + c);
+            if (c0 + i * across >= p.d) continue;
             Pack<T, VEC> o;
+            if constexpr (VEC == 1) {
+                float v = fmaf(to_f32(dy[i].v[0]), to_f32(wv[i].v[0]) * rstd, to_f32(h[i].v[0]) * back);
+                if (p.d_residual) v += to_f32(add[i].v[0]);
+                o.v[0] = from_f32<T>(v);
+            } else {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float n = to_f32(b[i].v[j]) * rstd, g = to_f32(a[i].v[j]) * to_f32(wv.v[j]);
-                float v = rstd * (g - n * mean);
-                if (dr) v += to_f32(r[i].v[j]);
-                o.v[j] = from_f32<T>(v);
+                for (int j = 0; j < VEC; j += 2) {
+                    float2 v = mul2(to_f32x2(&h[i].v[j]), both(back));
+                    if (p.d_residual) v = add2(v, to_f32x2(&add[i].v[j]));
+                    from_f32x2(&o.v[j], fma2(to_f32x2(&dy[i].v[j]), mul2(to_f32x2(&wv[i].v[j]), both(rstd)), v));
+                }
             }
-            store_pack<T, VEC>(dx + c, o);
+            store_pack<T, VEC>(dx + i * across, o);
         }
     }
     if (!p.partial) return;
-    float *out = p.partial + (long long)first * p.d;
+    // the sums of a block's rows first meet in shared memory, in the order of the warps: one partial row per block
+    extern __shared__ __align__(16) uint8_t feed_memory[];
+    float *sums = reinterpret_cast<float *>(feed_memory);
+    if (blockDim.y > 1) {
+        asm volatile("cp.async.wait_all;" ::: "memory");        // nothing is on its way into that memory any more
+        __syncthreads();
+        if (threadIdx.y > 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) sums[((threadIdx.y - 1) * NV * VEC + i * VEC + j) * 32 + threadIdx.x] = acc[i * VEC + j];
+        }
+        __syncthreads();
+        if (threadIdx.y > 0) return;
+        for (int y = 1; y < blockDim.y; ++y)
+#pragma unroll
+            for (int i = 0; i < NV * VEC; ++i) acc[i] += sums[((y - 1) * NV * VEC + i) * 32 + threadIdx.x];
+    }
+    float *out = p.partial + (long long)blockIdx.x * p.d + c0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        if (c < p.d) {
+        if (c0 + i * across < p.d) {
+            Pack<float, VEC> o;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) out[c + j] = acc[i * VEC + j];
+            for (int j = 0; j < VEC; ++j) o.v[j] = acc[i * VEC + j];
+            if (p.d % 4 == 0) {
+                store_pack<float, VEC>(out + i * across, o);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) out[i * across + j] = o.v[j];
+            }
         }
     }
 }
 
-// dweight[c] = sum of the partial rows, each column by 16 threads and then in one tree: a fixed order.
-__global__ void __launch_bounds__(512) reduce_partials_kernel(const float *partial, int count, int d, float *dweight)
+// dweight[c] = sum of the partial rows: 32 columns per block, each by 32 threads with several loads in flight and then in one
+// tree -- a fixed order.
+__global__ void __launch_bounds__(1024) reduce_partials_kernel(const float *partial, int count, int d, float *dweight)
 {
-    __shared__ float buf[16][33];
+    __shared__ float buf[32][33];
     const int c = blockIdx.x * 32 + threadIdx.x;
-    float s = 0.0f;
-    if (c < d)
-        for (int i = threadIdx.y; i < count; i += 16) s += partial[(long long)i * d + c];
-    buf[threadIdx.y][threadIdx.x] = s;
-    __syncthreads();
-    for (int o = 8; o > 0; o >>= 1) {
-        if (threadIdx.y < o) buf[threadIdx.y][threadIdx.x] += buf[threadIdx.y + o][threadIdx.x];
-        __syncthreads();
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < d) {
+        int i = threadIdx.y;
+        for (; i + 224 < count; i += 256) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = partial[(long long)(i + 32 * j) * d + c];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j & 3] += v[j];
+        }
+#pragma unroll 4
+        for (; i < count; i += 32) s[0] += partial[(long long)i * d + c];
     }
-    if (threadIdx.y == 0 && c < d) dweight[c] = buf[0][threadIdx.x];
+    buf[threadIdx.y][threadIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    const float t = warp_sum(buf[threadIdx.x][threadIdx.y]);      // a warp per column
+    const int out = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && out < d) dweight[out] = t;
 }
 
 struct SwigluP {
@@ -251,52 +434,70 @@ struct SwigluP {
     const void *x;
     int8_t *q;
     float *scale;
-    long long x_stride, q_stride;
+    int x_stride, q_stride;
 };
 
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(max_threads(VEC *NV)) swiglu_quant_kernel(const SwigluP p)
+// g / (1 + exp(-g)) by the approximate power of two and reciprocal: relative error about 2^-22 + |g| 2^-24 before the rounding to
+// 8 bits (a row with g < -75 throughout is zeros anyway).  The full exponential and division take 20 instructions more per element,
+// and the kernel would be bound by them, not by HBM.  exp(-g) = inf gives g * 0.
+__device__ __forceinline__ float2 silu2(float2 g)
 {
-    __shared__ float buf[32];
-    const int row = blockIdx.x * blockDim.y + threadIdx.y;
+    const float2 p = mul2(g, both(-1.4426950408889634f));
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(p.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(p.y));
+    e = add2(e, both(1.0f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+    return mul2(g, r);
+}
+
+template <typename T, int VEC, int NV>
+__global__ void __launch_bounds__(swiglu_threads(VEC *NV)) swiglu_quant_kernel(const SwigluP p)
+{
+    __shared__ float buf[2][32];
+    const int step = gridDim.x * blockDim.y;
+    int row = blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= p.rows) return;
-    const T *g = static_cast<const T *>(p.x) + row * p.x_stride, *u = g + p.f;
+    const int c0 = threadIdx.x * VEC, across = blockDim.x * VEC;
     Pack<T, VEC> a[NV], b[NV];
+    auto load = [&](int r) {
+        const T *g = at_row(static_cast<const T *>(p.x), r, p.x_stride, c0), *u = g + p.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        if (c < p.f) {
-            a[i] = load_pack<T, VEC>(g + c);
-            b[i] = load_pack<T, VEC>(u + c);
-        }
-    }
-    float v[NV * VEC], most = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            float t = 0.0f;
-            if (c < p.f) {
-                const float gf = to_f32(a[i].v[j]);
-                t = gf / (1.0f + expf(-gf)) * to_f32(b[i].v[j]);
+        for (int i = 0; i < NV; ++i)
+            if (c0 + i * across < p.f) {
+                a[i] = load_pack<T, VEC>(g + i * across);
+                b[i] = load_pack<T, VEC>(u + i * across);
             }
-            v[i * VEC + j] = t;
-            most = max_nan(most, fabsf(t));
+    };
+    load(row);
+    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+        float v[NV * VEC], most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (c0 + i * across >= p.f) continue;
+            if constexpr (VEC == 1) {
+                const float2 t = silu2(both(to_f32(a[i].v[0])));
+                v[i] = t.x * to_f32(b[i].v[0]);
+                most = max_abs(most, v[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 2) {
+                    const float2 t = mul2(silu2(to_f32x2(&a[i].v[j])), to_f32x2(&b[i].v[j]));
+                    v[i * VEC + j] = t.x, v[i * VEC + j + 1] = t.y;
+                    most = max_abs(most, t);
+                }
+            }
         }
-    }
-    most = row_max(most, buf);
-    const float2 s = quant_scale(most);
-    if (threadIdx.x == 0) p.scale[row] = s.x;
-    int8_t *q = p.q + row * p.q_stride;
+        if (row + step < p.rows) load(row + step);
+        most = row_max(most, buf[turn]);
+        const float2 s = quant_scale(most);
+        if (threadIdx.x == 0) p.scale[row] = s.x;
+        const uint32_t keep = keep_mask(most);
+        int8_t *q = at_row(p.q, row, p.q_stride, c0);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        if (c < p.f) {
-            Pack<int8_t, VEC> o;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) o.v[j] = quant(v[i * VEC + j], s.y);
-            store_pack<int8_t, VEC>(q + c, o);
+        for (int i = 0; i < NV; ++i) {
+            if (c0 + i * across < p.f) store_quant<VEC>(q + i * across, v + i * VEC, s.y, keep);
         }
     }
 }
@@ -304,43 +505,106 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) swiglu_quant_kernel(cons
 // How a row of `width` elements is spread: threads per row, packs per thread, rows per block.
 struct RowShape { int threads, packs, rows_per_block; };
 
-RowShape row_shape(int rows, int width, int vec, int want_packs)
+template <int VEC> RowShape row_shape(int rows, int width, int want_values, int (*most_threads)(int))
 {
-    RowShape s;
-    const int packs = (width + vec - 1) / vec;
-    // few rows leave SMs idle whatever the block is: the latency of one row counts, so a thread takes one pack
-    const int want = rows <= 296 ? 1 : want_packs;
-    int nv = 1;
-    while (nv < want && packs > 32 * nv) nv *= 2;
-    // a pack more per thread until the block is small enough for the registers
+    const int packs = (width + VEC - 1) / VEC;
+    // few rows leave SMs idle whatever the block is: the latency of one row counts, so a thread takes few values
+    const int want = rows <= 296 ? 8 : want_values;
     auto threads = [&](int n) { return ((packs + n - 1) / n + 31) / 32 * 32; };
-    while (threads(nv) > max_threads(vec * nv)) nv *= 2;
-    s.packs = nv;
-    s.threads = threads(nv);
-    s.rows_per_block = s.threads == 32 ? 4 : 1;
+    auto next = [](int n) { return VEC >= 4 || n >= 32 ? 2 * n : 4 * n; };
+    int nv = VEC >= 4 ? 1 : 2;
+    while ((next(nv) * VEC <= want && packs > 32 * nv) || threads(nv) > most_threads(VEC * nv)) nv = next(nv);
+    RowShape s = {threads(nv), nv, 1};
+    if (s.threads == 32) s.rows_per_block = 8;
     return s;
 }
 
+int sm_count(int device)
+{
+    static std::atomic<int> known[64];
+    std::atomic<int> &have = known[device & 63];
+    int n = have.load(std::memory_order_relaxed);
+    if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess && device < 64) have.store(n, std::memory_order_relaxed);
+    return std::max(n, 1);
+}
+
+// As many blocks as the device holds at once, or as the rows need.  0: a CUDA call failed.
+template <typename K> int resident(K kernel, int threads, int smem, int blocks, int device)
+{
+    if (blocks <= sm_count(device)) return blocks;
+    int per_sm = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess) return 0;
+    return std::min(blocks, per_sm * sm_count(device));
+}
+
+template <typename K, typename P> int launch_rows(K kernel, const P &p, const RowShape &s, int device, cudaStream_t stream)
+{
+    const int blocks = resident(kernel, s.threads * s.rows_per_block, 0, (p.rows + s.rows_per_block - 1) / s.rows_per_block, device);
+    if (blocks < 1) return MOE_OVL_ERR_CUDA;
+    kernel<<<blocks, dim3(s.threads, s.rows_per_block), 0, stream>>>(p);
+    return launched();
+}
+
+// The gradient's kernel: as many rows on their way per block as shared memory has room for (four at most; a block less per SM where
+// there would not be three).  Where every SM has a block at most, nothing is to come.  `allowed`: whether this kernel has been allowed
+// its shared memory on each device.
+template <int VEC, int NV, typename T, typename K>
+int launch_backward(K kernel, std::atomic<int> *allowed, NormBackP &p, const RowShape &s, int device, cudaStream_t stream, int &blocks)
+{
+    constexpr int ROOM = 200 * 1024;
+    const int threads = s.threads * s.rows_per_block, sms = sm_count(device);
+    int smem = (s.rows_per_block - 1) * VEC * NV * 32 * 4;
+    blocks = std::min((p.rows + s.rows_per_block - 1) / s.rows_per_block, NORM_PARTIALS);
+    p.depth = 0;
+    if (blocks > sms) {
+        int per_sm = 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) return MOE_OVL_ERR_CUDA;
+        if (VEC * sizeof(T) >= 4) {
+            const int row_bytes = 3 * NV * VEC * (int)sizeof(T) * threads;
+            while (per_sm > 1 && ROOM / per_sm / row_bytes < 3) --per_sm;
+            p.depth = std::min(4, ROOM / per_sm / row_bytes);
+            smem = std::max(p.depth * row_bytes, smem);
+        }
+        blocks = std::min(blocks, per_sm * sms);
+    }
+    if (smem > 46 * 1024 && (device > 63 || allowed[device].load(std::memory_order_relaxed) == 0)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM) != cudaSuccess) return MOE_OVL_ERR_CUDA;
+        if (device <= 63) allowed[device].store(1, std::memory_order_relaxed);
+    }
+    kernel<<<blocks, dim3(s.threads, s.rows_per_block), smem, stream>>>(p);
+    return launched();
+}
+
 template <int N> struct Count { static constexpr int value = N; };
-// Calls f with the number of packs as a constant: 1, 2, 4 ... up to 64 / VEC values' worth.
+// Calls f with the number of packs as a constant.
 template <int VEC, typename F> int with_packs(int packs, F f)
 {
-    if (packs <= 1) return f(Count<1>());
+    if constexpr (VEC >= 4) {
+        if (packs == 1) return f(Count<1>());
+        if (packs == 4) return f(Count<4>());
+        if constexpr (VEC == 4) if (packs == 16) return f(Count<16>());
+    }
     if (packs == 2) return f(Count<2>());
-    if (packs == 4) return f(Count<4>());
-    if constexpr (VEC <= 8) if (packs == 8) return f(Count<8>());
-    if constexpr (VEC <= 4) if (packs == 16) return f(Count<16>());
-    if constexpr (VEC <= 1) if (packs == 32) return f(Count<32>());
-    if constexpr (VEC <= 1) if (packs == 64) return f(Count<64>());
+    if (packs == 8) return f(Count<8>());
+    if constexpr (VEC <= 2) if (packs == 32) return f(Count<32>());
+    if constexpr (VEC == 1) if (packs == 64) return f(Count<64>());
     return MOE_OVL_ERR_UNSUPPORTED;
 }
 
-template <typename T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
+// Calls f with the widest pack that the matrices allow: 16 bytes, a pair of 16-bit values, or one value.
+template <typename T, typename F> int with_vec(bool wide, bool pairs, F f)
+{
+    if (wide) return f(Count<16 / (int)sizeof(T)>());
+    if constexpr (sizeof(T) == 2) if (pairs) return f(Count<2>());
+    return f(Count<1>());
+}
 
 bool rows_ok(const void *p, int64_t stride, int vec, int bytes) { return aligned(p, (size_t)vec * bytes) && stride % vec == 0; }
 
-// A matrix whose rows do not overlap (or that has one row) and whose offsets stay within 63 bits.
-bool stride_ok(int64_t stride, int rows, int width) { return (rows <= 1 || stride >= width) && stride >= 0 && stride < (1ll << 40); }
+// Rows that do not overlap (or one row).
+bool stride_ok(int64_t stride, int rows, int width) { return (rows <= 1 || stride >= width) && stride >= 0; }
+// Kernels take strides of 31 bits (offsets are 64 bits wide).
+bool fits_int(int64_t a, int64_t b = 0, int64_t c = 0, int64_t d = 0, int64_t e = 0) { return std::max({a, b, c, d, e}) <= 0x7fffffff; }
 
 }  // namespace
 
@@ -355,6 +619,7 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
         (a->residual_out && !stride_ok(a->residual_out_stride, a->rows, a->d)) ||
         (a->y && !stride_ok(a->y_stride, a->rows, a->d)) || (a->q && !stride_ok(a->q_stride, a->rows, a->d)))
         return MOE_OVL_ERR_INVALID_ARG;
+    if (!fits_int(a->x_stride, a->residual_stride, a->residual_out_stride, a->y_stride, a->q_stride)) return MOE_OVL_ERR_UNSUPPORTED;
     if (a->rows == 0) return MOE_OVL_OK;
     const int es = dtype_bytes(a->dtype), ws = dtype_bytes(a->weight_dtype);
     if (!a->x || !a->weight || !aligned(a->x, es) || !aligned(a->residual, es) || !aligned(a->residual_out, es) || !aligned(a->y, es) ||
@@ -362,28 +627,26 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
         return MOE_OVL_ERR_INVALID_ARG;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
-    NormP p = {a->rows, a->d, a->eps, a->x, a->residual, a->weight, a->residual_out, a->y, a->q, a->scale, a->rstd,
-               a->x_stride, a->residual_stride, a->residual_out_stride, a->y_stride, a->q_stride};
-    const int vec = 16 / es;
-    const bool wide = a->d % vec == 0 && rows_ok(a->x, a->x_stride, vec, es) && aligned(a->weight, (size_t)vec * ws) &&
-                      (!a->residual || rows_ok(a->residual, a->residual_stride, vec, es)) &&
-                      (!a->residual_out || rows_ok(a->residual_out, a->residual_out_stride, vec, es)) &&
-                      (!a->y || rows_ok(a->y, a->y_stride, vec, es)) && (!a->q || rows_ok(a->q, a->q_stride, vec, 1));
+    const NormP p = {a->rows, a->d, 1.0f / (float)a->d, a->eps, a->x, a->residual, a->weight, a->residual_out, a->y, a->q, a->scale, a->rstd,
+                     (int)a->x_stride, (int)a->residual_stride, (int)a->residual_out_stride, (int)a->y_stride, (int)a->q_stride};
+    auto fits = [&](int vec) {
+        return a->d % vec == 0 && rows_ok(a->x, a->x_stride, vec, es) && aligned(a->weight, (size_t)vec * ws) &&
+               (!a->residual || rows_ok(a->residual, a->residual_stride, vec, es)) &&
+               (!a->residual_out || rows_ok(a->residual_out, a->residual_out_stride, vec, es)) &&
+               (!a->y || rows_ok(a->y, a->y_stride, vec, es)) && (!a->q || rows_ok(a->q, a->q_stride, vec, 1));
+    };
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto w, auto v) {
             using W = decltype(w);
             constexpr int VEC = decltype(v)::value;
-            const RowShape s = row_shape(p.rows, p.d, VEC, VEC == 1 ? 8 : 2);
+            const RowShape s = row_shape<VEC>(p.rows, p.d, VEC >= 4 ? VEC : 8, max_threads);
             return with_packs<VEC>(s.packs, [&](auto n) {
-                const int blocks = (p.rows + s.rows_per_block - 1) / s.rows_per_block;
-                add_norm_kernel<T, W, VEC, decltype(n)::value>
-                    <<<blocks, dim3(s.threads, s.rows_per_block), 0, static_cast<cudaStream_t>(a->stream)>>>(p);
-                return launched();
+                constexpr int NV = decltype(n)::value;
+                return launch_rows(add_norm_kernel<T, W, VEC, NV>, p, s, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
-        auto by_weight = [&](auto v) { return a->weight_dtype == a->dtype ? launch(T(), v) : launch(0.0f, v); };
-        return wide ? by_weight(Count<vec_of<T>()>()) : by_weight(Count<1>());
+        return with_vec<T>(fits(16 / es), fits(2), [&](auto v) { return a->weight_dtype == a->dtype ? launch(T(), v) : launch(0.0f, v); });
     });
 }
 
@@ -403,6 +666,7 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
     if (!stride_ok(a->dy_stride, a->rows, a->d) || !stride_ok(a->h_stride, a->rows, a->d) || !stride_ok(a->dx_stride, a->rows, a->d) ||
         (a->d_residual && !stride_ok(a->d_residual_stride, a->rows, a->d)))
         return MOE_OVL_ERR_INVALID_ARG;
+    if (!fits_int(a->dy_stride, a->h_stride, a->d_residual_stride, a->dx_stride)) return MOE_OVL_ERR_UNSUPPORTED;
     const int es = dtype_bytes(a->dtype), ws = dtype_bytes(a->weight_dtype);
     if (a->rows > 0 && (!a->dy || !a->h || !a->weight || !a->rstd || !a->dx || !aligned(a->dy, es) || !aligned(a->h, es) ||
                         !aligned(a->d_residual, es) || !aligned(a->dx, es) || !aligned(a->weight, ws) || !aligned(a->rstd, 4)))
@@ -418,34 +682,31 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
         if (!a->dweight) return MOE_OVL_OK;
         return cudaMemsetAsync(a->dweight, 0, (size_t)a->d * 4, stream) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
     }
-    NormBackP p = {a->rows, a->d, a->dy, a->h, a->weight, a->d_residual, a->rstd, a->dx,
-                   a->dweight ? static_cast<float *>(a->workspace) : nullptr, a->dy_stride, a->h_stride, a->d_residual_stride, a->dx_stride};
-    const int vec = 16 / es;
-    const bool wide = a->d % vec == 0 && rows_ok(a->dy, a->dy_stride, vec, es) && rows_ok(a->h, a->h_stride, vec, es) &&
-                      rows_ok(a->dx, a->dx_stride, vec, es) && aligned(a->weight, (size_t)vec * ws) &&
-                      (!a->d_residual || rows_ok(a->d_residual, a->d_residual_stride, vec, es));
+    NormBackP p = {a->rows, a->d, 0, 1.0f / (float)a->d, a->dy, a->h, a->weight, a->d_residual, a->rstd, a->dx,
+                   a->dweight ? static_cast<float *>(a->workspace) : nullptr, (int)a->dy_stride, (int)a->h_stride,
+                   (int)a->d_residual_stride, (int)a->dx_stride};
+    auto fits = [&](int vec) {
+        return a->d % vec == 0 && rows_ok(a->dy, a->dy_stride, vec, es) && rows_ok(a->h, a->h_stride, vec, es) &&
+               rows_ok(a->dx, a->dx_stride, vec, es) && aligned(a->weight, (size_t)vec * ws) &&
+               (!a->d_residual || rows_ok(a->d_residual, a->d_residual_stride, vec, es));
+    };
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto w, auto v) {
             using W = decltype(w);
             constexpr int VEC = decltype(v)::value;
-            const RowShape s = row_shape(p.rows, p.d, VEC, VEC == 1 ? 8 : 1);
+            const RowShape s = row_shape<VEC>(p.rows, p.d, 8, max_threads);
             return with_packs<VEC>(s.packs, [&](auto n) {
-                // rows_per_block rows at a time; at most NORM_PARTIALS partial rows in all
-                int blocks = (p.rows + s.rows_per_block - 1) / s.rows_per_block;
-                blocks = blocks < NORM_PARTIALS / s.rows_per_block ? blocks : NORM_PARTIALS / s.rows_per_block;
-                int rows_per_block = s.rows_per_block;
-                if (p.rows < rows_per_block) rows_per_block = p.rows, blocks = 1;
-                if (blocks * rows_per_block > p.rows) blocks = p.rows / rows_per_block;
-                add_norm_backward_kernel<T, W, VEC, decltype(n)::value>
-                    <<<blocks, dim3(s.threads, rows_per_block), 0, stream>>>(p);
-                if (p.partial)
-                    reduce_partials_kernel<<<(p.d + 31) / 32, dim3(32, 16), 0, stream>>>(p.partial, blocks * rows_per_block, p.d, a->dweight);
+                constexpr int NV = decltype(n)::value;
+                int blocks = 0;
+                static std::atomic<int> allowed[64];
+                const int rc = launch_backward<VEC, NV, T>(add_norm_backward_kernel<T, W, VEC, NV>, allowed, p, s, a->device, stream, blocks);
+                if (rc != MOE_OVL_OK || !p.partial) return rc;
+                reduce_partials_kernel<<<(p.d + 31) / 32, dim3(32, 32), 0, stream>>>(p.partial, blocks, p.d, a->dweight);
                 return launched();
             });
         };
-        auto by_weight = [&](auto v) { return a->weight_dtype == a->dtype ? launch(T(), v) : launch(0.0f, v); };
-        return wide ? by_weight(Count<vec_of<T>()>()) : by_weight(Count<1>());
+        return with_vec<T>(fits(16 / es), fits(2), [&](auto v) { return a->weight_dtype == a->dtype ? launch(T(), v) : launch(0.0f, v); });
     });
 }
 
@@ -455,26 +716,24 @@ extern "C" int moe_ovl_swiglu_quant(const moe_ovl_swiglu_args *a)
     if (!known_dtype(a->dtype)) return MOE_OVL_ERR_INVALID_ARG;
     if (a->f > MOE_OVL_MAX_ROW) return MOE_OVL_ERR_UNSUPPORTED;
     if (!stride_ok(a->gate_up_stride, a->rows, 2 * a->f) || !stride_ok(a->q_stride, a->rows, a->f)) return MOE_OVL_ERR_INVALID_ARG;
+    if (!fits_int(a->gate_up_stride, a->q_stride)) return MOE_OVL_ERR_UNSUPPORTED;
     if (a->rows == 0) return MOE_OVL_OK;
     const int es = dtype_bytes(a->dtype);
     if (!a->gate_up || !a->q || !a->scale || !aligned(a->gate_up, es) || !aligned(a->scale, 4)) return MOE_OVL_ERR_INVALID_ARG;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
-    const SwigluP p = {a->rows, a->f, a->gate_up, a->q, a->scale, a->gate_up_stride, a->q_stride};
-    const int vec = 16 / es;
-    const bool wide = a->f % vec == 0 && rows_ok(a->gate_up, a->gate_up_stride, vec, es) && rows_ok(a->q, a->q_stride, vec, 1);
+    const SwigluP p = {a->rows, a->f, a->gate_up, a->q, a->scale, (int)a->gate_up_stride, (int)a->q_stride};
+    auto fits = [&](int vec) { return a->f % vec == 0 && rows_ok(a->gate_up, a->gate_up_stride, vec, es) && rows_ok(a->q, a->q_stride, vec, 1); };
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto v) {
             constexpr int VEC = decltype(v)::value;
-            const RowShape s = row_shape(p.rows, p.f, VEC, VEC == 1 ? 8 : 2);
+            const RowShape s = row_shape<VEC>(p.rows, p.f, 16, swiglu_threads);
             return with_packs<VEC>(s.packs, [&](auto n) {
-                const int blocks = (p.rows + s.rows_per_block - 1) / s.rows_per_block;
-                swiglu_quant_kernel<T, VEC, decltype(n)::value>
-                    <<<blocks, dim3(s.threads, s.rows_per_block), 0, static_cast<cudaStream_t>(a->stream)>>>(p);
-                return launched();
+                constexpr int NV = decltype(n)::value;
+                return launch_rows(swiglu_quant_kernel<T, VEC, NV>, p, s, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
-        return wide ? launch(Count<vec_of<T>()>()) : launch(Count<1>());
+        return with_vec<T>(fits(16 / es), fits(2), launch);
     });
 }
