@@ -9,7 +9,7 @@ of the tensors' device, or to `stream`; tensors used on a stream that is not the
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional
+import struct
 
 import torch
 
@@ -26,9 +26,17 @@ _u32, _i32, _i64, _f32, _ptr = C.c_uint32, C.c_int32, C.c_int64, C.c_float, C.c_
 
 
 def _struct(name, text):
+    """The C structure that `text` spells out, and in `pack` the same layout as bytes: a call builds its arguments with that,
+    which takes a third of the time of filling the structure."""
     kinds = {"u": _u32, "i": _i32, "l": _i64, "f": _f32, "p": _ptr, "z": C.c_size_t}
-    fields = [(f, kinds[part[0]]) for part in text.split(";") for f in part[1:].replace(",", " ").split()]
-    return type(name, (C.Structure,), {"_fields_": fields})
+    codes = {"u": "I", "i": "i", "l": "q", "f": "f", "p": "P", "z": "N"}
+    fields = [(f, part[0]) for part in text.split(";") for f in part[1:].replace(",", " ").split()]
+    t = type(name, (C.Structure,), {"_fields_": [(f, kinds[k]) for f, k in fields]})
+    packer = struct.Struct("@" + "".join(codes[k] for _, k in fields) + "0q")
+    assert packer.size == C.sizeof(t)
+    t.pack = packer.pack
+    t.bytes = packer.size
+    return t
 
 
 NormArgs = _struct("NormArgs", "u struct_size;i device,rows,d,dtype,weight_dtype;f eps;u flags;"
@@ -49,9 +57,10 @@ def _refuse(where: str, what: str):
 
 
 def _device(where, t) -> int:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    device = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if device < 0:
         _refuse(where, "tensors have to be on a CUDA device")
-    return t.device.index
+    return device
 
 
 def _dtype(where, name, t) -> int:
@@ -61,11 +70,14 @@ def _dtype(where, name, t) -> int:
     return d
 
 
-def _matrix(where, name, t, rows, cols, dtype, device) -> int:
-    """Row stride of a [rows, cols] tensor whose columns lie next to each other."""
-    if t.shape != (rows, cols) or t.dtype is not dtype or not t.is_cuda or t.device.index != device:
-        _refuse(where, f"{name} has to be [{rows}, {cols}] {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
+def _matrix(where, name, t, shape, dtype, device) -> int:
+    """Row stride of a tensor of two dimensions whose columns lie next to each other."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _refuse(where, f"{name} has to be {list(shape)} {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
     s0, s1 = t.stride()
+    if s1 == 1 and s0 >= shape[1]:
+        return s0
+    rows, cols = shape
     if (s1 != 1 and cols > 1) or s0 < 0:
         _refuse(where, f"{name}: the columns of a row have to lie next to each other (strides {t.stride()})")
     if rows > 1 and s0 < cols:
@@ -74,15 +86,15 @@ def _matrix(where, name, t, rows, cols, dtype, device) -> int:
 
 
 def _vector(where, name, t, shape, dtype, device) -> None:
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or t.device.index != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         _refuse(where, f"{name} has to be a contiguous {list(shape)} {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
 
 
-def _at(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
+def _at(t) -> int:
+    return 0 if t is None else t.data_ptr()
 
 
-def _stream(device: int, stream, tensors) -> int:
+def _stream(device: int, stream, *tensors) -> int:
     current = torch._C._cuda_getCurrentRawStream(device)
     if stream is None or stream.cuda_stream == current:
         return current
@@ -99,6 +111,14 @@ def _done(rc: int, where: str) -> None:
         raise MoeOvlError(rc, where)
 
 
+def _call(where: str, function, kind, *values) -> None:
+    try:
+        args = kind.pack(kind.bytes, *values)
+    except struct.error as e:           # a number that its field does not hold
+        _refuse(where, str(e))
+    _done(function(args), where)
+
+
 def moe_ovl_add_norm(*, x, weight, eps: float = 1e-6, residual=None, residual_out=None, y=None, q=None, scale=None, rstd=None,
                      stream=None) -> None:
     """RMS norm of x + residual, rounded to x's type: h -> residual_out; h * rstd * weight -> y and / or, in 8 bits with a
@@ -107,23 +127,23 @@ def moe_ovl_add_norm(*, x, weight, eps: float = 1e-6, residual=None, residual_ou
     dev, dt = _device(where, x), _dtype(where, "x", x)
     if x.dim() != 2:
         _refuse(where, "x has to be [rows, d]")
-    rows, d = x.shape
-    sx = _matrix(where, "x", x, rows, d, x.dtype, dev)
-    if weight.dtype is not x.dtype and weight.dtype is not torch.float32:
-        _refuse(where, f"weight has to be {x.dtype} or float32, not {weight.dtype}")
-    _vector(where, "weight", weight, (d,), weight.dtype, dev)
-    sr = _matrix(where, "residual", residual, rows, d, x.dtype, dev) if residual is not None else 0
-    so = _matrix(where, "residual_out", residual_out, rows, d, x.dtype, dev) if residual_out is not None else 0
-    sy = _matrix(where, "y", y, rows, d, x.dtype, dev) if y is not None else 0
-    sq = _matrix(where, "q", q, rows, d, torch.int8, dev) if q is not None else 0
+    shape, kind, wkind = x.shape, x.dtype, weight.dtype
+    rows, d = shape
+    sx = _matrix(where, "x", x, shape, kind, dev)
+    if wkind is not kind and wkind is not torch.float32:
+        _refuse(where, f"weight has to be {kind} or float32, not {wkind}")
+    _vector(where, "weight", weight, (d,), wkind, dev)
+    sr = _matrix(where, "residual", residual, shape, kind, dev) if residual is not None else 0
+    so = _matrix(where, "residual_out", residual_out, shape, kind, dev) if residual_out is not None else 0
+    sy = _matrix(where, "y", y, shape, kind, dev) if y is not None else 0
+    sq = _matrix(where, "q", q, shape, torch.int8, dev) if q is not None else 0
     if scale is not None:
         _vector(where, "scale", scale, (rows,), torch.float32, dev)
     if rstd is not None:
         _vector(where, "rstd", rstd, (rows,), torch.float32, dev)
-    a = NormArgs(C.sizeof(NormArgs), dev, rows, d, dt, DTYPES[weight.dtype], eps, 0, x.data_ptr(), _at(residual), weight.data_ptr(),
-                 _at(residual_out), _at(y), _at(q), _at(scale), _at(rstd), sx, sr, so, sy, sq,
-                 _stream(dev, stream, (x, weight, residual, residual_out, y, q, scale, rstd)))
-    _done(B.load().moe_ovl_add_norm(C.byref(a)), where)
+    _call(where, B.load().moe_ovl_add_norm, NormArgs, dev, rows, d, dt, DTYPES[wkind], eps, 0, x.data_ptr(), _at(residual), weight.data_ptr(),
+          _at(residual_out), _at(y), _at(q), _at(scale), _at(rstd), sx, sr, so, sy, sq,
+          _stream(dev, stream, x, weight, residual, residual_out, y, q, scale, rstd))
 
 
 def moe_ovl_add_norm_workspace_bytes(rows: int, d: int) -> int:
@@ -139,11 +159,12 @@ def moe_ovl_add_norm_backward(*, dy, h, weight, rstd, dx, dweight=None, d_residu
     dev, dt = _device(where, dy), _dtype(where, "dy", dy)
     if dy.dim() != 2:
         _refuse(where, "dy has to be [rows, d]")
-    rows, d = dy.shape
-    sy = _matrix(where, "dy", dy, rows, d, dy.dtype, dev)
-    sh = _matrix(where, "h", h, rows, d, dy.dtype, dev)
-    sx = _matrix(where, "dx", dx, rows, d, dy.dtype, dev)
-    sr = _matrix(where, "d_residual", d_residual, rows, d, dy.dtype, dev) if d_residual is not None else 0
+    shape = dy.shape
+    rows, d = shape
+    sy = _matrix(where, "dy", dy, shape, dy.dtype, dev)
+    sh = _matrix(where, "h", h, shape, dy.dtype, dev)
+    sx = _matrix(where, "dx", dx, shape, dy.dtype, dev)
+    sr = _matrix(where, "d_residual", d_residual, shape, dy.dtype, dev) if d_residual is not None else 0
     if weight.dtype is not dy.dtype and weight.dtype is not torch.float32:
         _refuse(where, f"weight has to be {dy.dtype} or float32, not {weight.dtype}")
     _vector(where, "weight", weight, (d,), weight.dtype, dev)
@@ -155,10 +176,9 @@ def moe_ovl_add_norm_backward(*, dy, h, weight, rstd, dx, dweight=None, d_residu
         if not workspace.is_cuda or workspace.device.index != dev or not workspace.is_contiguous():
             _refuse(where, f"workspace has to be contiguous on cuda:{dev}")
         nbytes = workspace.numel() * workspace.element_size()
-    a = NormBackwardArgs(C.sizeof(NormBackwardArgs), dev, rows, d, dt, DTYPES[weight.dtype], dy.data_ptr(), h.data_ptr(), weight.data_ptr(),
-                         rstd.data_ptr(), _at(d_residual), dx.data_ptr(), _at(dweight), _at(workspace), nbytes, sy, sh, sr, sx,
-                         _stream(dev, stream, (dy, h, weight, rstd, d_residual, dx, dweight, workspace)))
-    _done(B.load().moe_ovl_add_norm_backward(C.byref(a)), where)
+    _call(where, B.load().moe_ovl_add_norm_backward, NormBackwardArgs, dev, rows, d, dt, DTYPES[weight.dtype], dy.data_ptr(), h.data_ptr(),
+          weight.data_ptr(), rstd.data_ptr(), _at(d_residual), dx.data_ptr(), _at(dweight), _at(workspace), nbytes, sy, sh, sr, sx,
+          _stream(dev, stream, dy, h, weight, rstd, d_residual, dx, dweight, workspace))
 
 
 def moe_ovl_swiglu_quant(*, gate_up, q, scale, stream=None) -> None:
@@ -168,12 +188,11 @@ def moe_ovl_swiglu_quant(*, gate_up, q, scale, stream=None) -> None:
     if gate_up.dim() != 2 or gate_up.shape[1] % 2:
         _refuse(where, "gate_up has to be [rows, 2F]")
     rows, f = gate_up.shape[0], gate_up.shape[1] // 2
-    sg = _matrix(where, "gate_up", gate_up, rows, 2 * f, gate_up.dtype, dev)
-    sq = _matrix(where, "q", q, rows, f, torch.int8, dev)
+    sg = _matrix(where, "gate_up", gate_up, gate_up.shape, gate_up.dtype, dev)
+    sq = _matrix(where, "q", q, (rows, f), torch.int8, dev)
     _vector(where, "scale", scale, (rows,), torch.float32, dev)
-    a = SwigluArgs(C.sizeof(SwigluArgs), dev, rows, f, dt, 0, gate_up.data_ptr(), q.data_ptr(), scale.data_ptr(), sg, sq,
-                   _stream(dev, stream, (gate_up, q, scale)))
-    _done(B.load().moe_ovl_swiglu_quant(C.byref(a)), where)
+    _call(where, B.load().moe_ovl_swiglu_quant, SwigluArgs, dev, rows, f, dt, 0, gate_up.data_ptr(), q.data_ptr(), scale.data_ptr(), sg, sq,
+          _stream(dev, stream, gate_up, q, scale))
 
 
 def moe_ovl_route(*, logits, expert, gate, counts=None, bias=None, score: int = SCORE_SOFTMAX, num_groups: int = 1, top_groups: int = 1,
@@ -185,17 +204,15 @@ def moe_ovl_route(*, logits, expert, gate, counts=None, bias=None, score: int = 
         _refuse(where, "logits have to be [rows, experts], expert [rows, top_k]")
     rows, e = logits.shape
     k = expert.shape[1]
-    sl = _matrix(where, "logits", logits, rows, e, logits.dtype, dev)
+    sl = _matrix(where, "logits", logits, logits.shape, logits.dtype, dev)
     _vector(where, "expert", expert, (rows, k), torch.int32, dev)
-    _vector(where, "gate", gate, (rows, k), torch.float32, dev)
+    _vector(where, "gate", gate, expert.shape, torch.float32, dev)
     if bias is not None:
         _vector(where, "bias", bias, (e,), torch.float32, dev)
     if counts is not None:
         _vector(where, "counts", counts, (e,), torch.int32, dev)
-    a = RouteArgs(C.sizeof(RouteArgs), dev, rows, e, k, dt, score, num_groups, top_groups, group_best, 1 if renormalise else 0, gate_scale,
-                  logits.data_ptr(), _at(bias), expert.data_ptr(), gate.data_ptr(), _at(counts), sl,
-                  _stream(dev, stream, (logits, expert, gate, bias, counts)))
-    _done(B.load().moe_ovl_route(C.byref(a)), where)
+    _call(where, B.load().moe_ovl_route, RouteArgs, dev, rows, e, k, dt, score, num_groups, top_groups, group_best, 1 if renormalise else 0, gate_scale,
+          logits.data_ptr(), _at(bias), expert.data_ptr(), gate.data_ptr(), _at(counts), sl, _stream(dev, stream, logits, expert, gate, bias, counts))
 
 
 def moe_ovl_route_backward(*, logits, expert, dgate, dlogits, score: int = SCORE_SOFTMAX, renormalise: bool = True, gate_scale: float = 1.0,
@@ -207,14 +224,12 @@ def moe_ovl_route_backward(*, logits, expert, dgate, dlogits, score: int = SCORE
         _refuse(where, "logits have to be [rows, experts], expert [rows, top_k]")
     rows, e = logits.shape
     k = expert.shape[1]
-    sl = _matrix(where, "logits", logits, rows, e, logits.dtype, dev)
-    so = _matrix(where, "dlogits", dlogits, rows, e, logits.dtype, dev)
+    sl = _matrix(where, "logits", logits, logits.shape, logits.dtype, dev)
+    so = _matrix(where, "dlogits", dlogits, logits.shape, logits.dtype, dev)
     _vector(where, "expert", expert, (rows, k), torch.int32, dev)
-    _vector(where, "dgate", dgate, (rows, k), torch.float32, dev)
-    a = RouteBackwardArgs(C.sizeof(RouteBackwardArgs), dev, rows, e, k, dt, score, 1 if renormalise else 0, gate_scale, 0,
-                          logits.data_ptr(), expert.data_ptr(), dgate.data_ptr(), dlogits.data_ptr(), sl, so,
-                          _stream(dev, stream, (logits, expert, dgate, dlogits)))
-    _done(B.load().moe_ovl_route_backward(C.byref(a)), where)
+    _vector(where, "dgate", dgate, expert.shape, torch.float32, dev)
+    _call(where, B.load().moe_ovl_route_backward, RouteBackwardArgs, dev, rows, e, k, dt, score, 1 if renormalise else 0, gate_scale, 0,
+          logits.data_ptr(), expert.data_ptr(), dgate.data_ptr(), dlogits.data_ptr(), sl, so, _stream(dev, stream, logits, expert, dgate, dlogits))
 
 
 def moe_ovl_quant_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=None, wait_timeout_us: int = 0, flags: int = 0,
@@ -237,20 +252,17 @@ def moe_ovl_quant_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=N
     elif b.dim() == 3 and b.shape[0] != 1:
         _refuse(where, "several experts need expert_counts")
     n = b.shape[-2]
-    sa = _matrix(where, "a", a, rows, k, torch.int8, dev)
-    if b.shape[-1] != k or b.dtype is not torch.int8 or not b.is_cuda or b.device.index != dev or b.stride(-1) != 1:
+    sa = _matrix(where, "a", a, a.shape, torch.int8, dev)
+    if b.shape[-1] != k or b.dtype is not torch.int8 or b.get_device() != dev or b.stride(-1) != 1:
         _refuse(where, f"b has to be [..., {n}, {k}] int8 on cuda:{dev} with its columns next to each other")
     sb = b.stride(-2)
     if sb < k or (experts > 1 and b.stride(0) != n * sb):
         _refuse(where, "the rows of b have to lie at one distance, across experts too")
     dt = _dtype(where, "out", out)
-    so = _matrix(where, "out", out, rows, n, out.dtype, dev)
+    so = _matrix(where, "out", out, (rows, n), out.dtype, dev)
     _vector(where, "a_scale", a_scale, (rows,), torch.float32, dev)
-    if b_scale.shape != b.shape[:-1] or b_scale.dtype is not torch.float32 or not b_scale.is_cuda or b_scale.device.index != dev \
-            or not b_scale.is_contiguous():
-        _refuse(where, f"b_scale has to be a contiguous {list(b.shape[:-1])} float32 on cuda:{dev}")
+    _vector(where, "b_scale", b_scale, b.shape[:-1], torch.float32, dev)
     _vector(where, "status", status, (4,), torch.int32, dev)
-    args = QuantMatmulArgs(C.sizeof(QuantMatmulArgs), dev, rows, n, k, experts, dt, wait_timeout_us, flags, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(),
-                           b_scale.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, so,
-                           _stream(dev, stream, (a, a_scale, b, b_scale, expert_counts, out, status)))
-    _done(B.load().moe_ovl_quant_matmul(C.byref(args)), where)
+    _call(where, B.load().moe_ovl_quant_matmul, QuantMatmulArgs, dev, rows, n, k, experts, dt, wait_timeout_us, flags, a.data_ptr(), a_scale.data_ptr(),
+          b.data_ptr(), b_scale.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, so,
+          _stream(dev, stream, a, a_scale, b, b_scale, expert_counts, out, status))
