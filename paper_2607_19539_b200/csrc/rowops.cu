@@ -98,10 +98,62 @@ __device__ __forceinline__ uint32_t keep_mask(float most) { return most <= 3.402
 // Where row `row` of a matrix begins for a thread whose first column is c.
 template <typename T> __device__ __forceinline__ T *at_row(T *base, int row, int stride, int c) { return base + ((long long)row * stride + c); }
 
+// RAGGED rows: their length or their distance is no multiple of a pack, so they begin anywhere in one.  A thread then owns packs of the
+// ADDRESS space: its first column is `shift` columns further left, and shift = (row * stride) mod VEC stays the same for a block when its
+// rows lie a multiple of VEC rows apart.  All matrices have to agree on it (the same stride mod VEC, aligned bases).  Only the row's first and
+// last pack are partial; their elements are read and written one by one, and count as 0 outside the row.  (4097 columns, 8000 rows, bf16:
+// element by element 142 us, this way RAGGED_US.)
+template <int VEC, bool RAGGED> __device__ __forceinline__ bool whole_pack(int c, int d) { return RAGGED ? c >= 0 && c + VEC <= d : c < d; }
+template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_part(const T *p, int c, int d)
+{
+    Pack<T, VEC> r;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) r.v[j] = c + j >= 0 && c + j < d ? p[j] : from_f32<T>(0.0f);
+    return r;
+}
+template <typename T, int VEC, bool RAGGED> __device__ __forceinline__ Pack<T, VEC> load_some(const T *p, int c, int d)
+{
+    if constexpr (RAGGED) {
+        if (!whole_pack<VEC, true>(c, d)) return load_part<T, VEC>(p, c, d);
+    }
+    return load_pack<T, VEC>(p);
+}
+template <typename T, int VEC, bool RAGGED> __device__ __forceinline__ void store_some(T *p, const Pack<T, VEC> &r, int c, int d)
+{
+    if constexpr (RAGGED) {
+        if (!whole_pack<VEC, true>(c, d)) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j >= 0 && c + j < d) p[j] = r.v[j];
+            return;
+        }
+    }
+    store_pack<T, VEC>(p, r);
+}
+// The weights of a thread's columns, wherever they begin.
+template <typename W, int VEC, bool RAGGED> __device__ __forceinline__ Pack<W, VEC> load_weight(const W *w, int c, int d)
+{
+    if constexpr (RAGGED) return load_part<W, VEC>(w + c, c, d);
+    else return load_pack<W, VEC>(w + c);
+}
+template <int VEC, bool RAGGED> __device__ __forceinline__ void quant_some(int8_t *q, const float *v, float factor, uint32_t keep, int c, int d)
+{
+    if constexpr (RAGGED) {
+        if (!whole_pack<VEC, true>(c, d)) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j >= 0 && c + j < d) store_quant<1>(q + j, v + j, factor, keep);
+            return;
+        }
+    }
+    store_quant<VEC>(q, v, factor, keep);
+}
+template <int VEC, bool RAGGED> __device__ __forceinline__ int shift_of(int row, int stride) { return RAGGED ? (int)((unsigned)row * (unsigned)stride % VEC) : 0; }
+
 // Rows on their way from global to shared memory.  Every thread copies, waits for and reads its own packs only (asynchronous
 // copies of 16 or 4 bytes), so no thread waits for another.  `depth` rows are on their way; 0: the packs are loaded when they are
 // needed (elements of two bytes, which such copies do not know, always are).
-template <typename T, int VEC, int NV, int ARRAYS> struct Feed {
+template <typename T, int VEC, int NV, int ARRAYS, bool RAGGED> struct Feed {
     static constexpr int BYTES = VEC * (int)sizeof(T);
     static constexpr bool ASYNC = BYTES >= 4;
     uint32_t base, stride;                      // this thread's first pack, bytes from pack to pack
@@ -112,8 +164,8 @@ template <typename T, int VEC, int NV, int ARRAYS> struct Feed {
         base = (uint32_t)__cvta_generic_to_shared(feed_memory) + (threadIdx.y * blockDim.x + threadIdx.x) * BYTES;
         stride = blockDim.x * blockDim.y * BYTES;
     }
-    // Asks for a row: `at[k]` its start for this thread in matrix k (NULL: none), `width` columns from there on, `across` from pack to pack.
-    __device__ __forceinline__ void ask(const T *const (&at)[ARRAYS], bool any, int width, int across)
+    // Asks for a row: `at[k]` where this thread's first column c lies in matrix k (NULL: none), `across` columns from pack to pack.
+    __device__ __forceinline__ void ask(const T *const (&at)[ARRAYS], bool any, int c, int d, int across)
     {
         if constexpr (ASYNC) {
             if (any) {
@@ -121,7 +173,7 @@ template <typename T, int VEC, int NV, int ARRAYS> struct Feed {
                 for (int k = 0; k < ARRAYS; ++k)
 #pragma unroll
                     for (int i = 0; i < NV; ++i)
-                        if (at[k] && i * across < width) {
+                        if (at[k] && whole_pack<VEC, RAGGED>(c + i * across, d)) {
                             const uint32_t to = base + ((put * ARRAYS + k) * NV + i) * stride;
                             if constexpr (BYTES == 16)
                                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at[k] + i * across) : "memory");
@@ -174,7 +226,7 @@ struct NormP {
 
 // The row's sum of squares and the largest |h * weight| come out of ONE reduction: rstd is a positive factor of the whole row,
 // so the scale of the 8-bit output needs no second pass over the normed values.
-template <typename T, typename W, int VEC, int NV>
+template <typename T, typename W, int VEC, int NV, bool RAGGED>
 __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const NormP p)
 {
     __shared__ float2 buf[2][32];
@@ -182,22 +234,22 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const No
     const W *w = static_cast<const W *>(p.weight);
     int row = blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= p.rows) return;                  // whole warps: rows share a block only as one warp each
-    const int c0 = threadIdx.x * VEC, across = blockDim.x * VEC;
+    const int c0 = threadIdx.x * VEC - shift_of<VEC, RAGGED>(row, p.x_stride), across = blockDim.x * VEC;
     Pack<T, VEC> a[NV], b[NV];
     auto load = [&](int r) {
         const T *x = at_row(static_cast<const T *>(p.x), r, p.x_stride, c0), *res = at_row(static_cast<const T *>(p.residual), r, p.residual_stride, c0);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (c0 + i * across < p.d) {
-                a[i] = load_pack<T, VEC>(x + i * across);
-                if (p.residual) b[i] = load_pack<T, VEC>(res + i * across);
+                a[i] = load_some<T, VEC, RAGGED>(x + i * across, c0 + i * across, p.d);
+                if (p.residual) b[i] = load_some<T, VEC, RAGGED>(res + i * across, c0 + i * across, p.d);
             }
     };
     load(row);
     Pack<W, VEC> wv[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (c0 + i * across < p.d) wv[i] = load_pack<W, VEC>(w + c0 + i * across);
+        if (c0 + i * across < p.d) wv[i] = load_weight<W, VEC, RAGGED>(w, c0 + i * across, p.d);
     for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
         float v[NV * VEC];                      // h * weight
         float most = 0.0f;
@@ -223,7 +275,8 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const No
                     most = max_abs(most, t);
                 }
             }
-            if (p.residual_out) store_pack<T, VEC>(at_row(static_cast<T *>(p.residual_out), row, p.residual_out_stride, c0) + i * across, a[i]);
+            if (p.residual_out)
+                store_some<T, VEC, RAGGED>(at_row(static_cast<T *>(p.residual_out), row, p.residual_out_stride, c0) + i * across, a[i], c0 + i * across, p.d);
         }
         if (row + step < p.rows) load(row + step);
         float total = sum.x + sum.y;
@@ -243,7 +296,7 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const No
                         for (int j = 0; j < VEC; j += 2)
                             from_f32x2(&o.v[j], mul2(make_float2(v[i * VEC + j], v[i * VEC + j + 1]), both(rstd)));
                     }
-                    store_pack<T, VEC>(y + i * across, o);
+                    store_some<T, VEC, RAGGED>(y + i * across, o, c0 + i * across, p.d);
                 }
             }
         }
@@ -256,7 +309,7 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const No
             const uint32_t keep = keep_mask(most);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (c0 + i * across < p.d) store_quant<VEC>(q + i * across, v + i * VEC, factor, keep);
+                if (c0 + i * across < p.d) quant_some<VEC, RAGGED>(q + i * across, v + i * VEC, factor, keep, c0 + i * across, p.d);
         }
     }
 }
@@ -273,7 +326,7 @@ struct NormBackP {
 
 // Every block (or warp) keeps its columns' share of the weight gradient over all of its rows; the partial rows are
 // added up in a fixed order by reduce_partials_kernel: no atomics, the same bits every time.
-template <typename T, typename W, int VEC, int NV>
+template <typename T, typename W, int VEC, int NV, bool RAGGED>
 __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel(const NormBackP p)
 {
     __shared__ float buf[2][32];
@@ -282,49 +335,47 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel
     for (int i = 0; i < NV * VEC; ++i) acc[i] = 0.0f;
     const int first = blockIdx.x * blockDim.y + threadIdx.y, step = gridDim.x * blockDim.y;
     const W *w = static_cast<const W *>(p.weight);
-    const int c0 = threadIdx.x * VEC, across = blockDim.x * VEC;
+    const int c0 = threadIdx.x * VEC - shift_of<VEC, RAGGED>(first, p.dy_stride), across = blockDim.x * VEC;
     auto start = [&](int r, const T *(&at)[3]) {
         at[0] = at_row(static_cast<const T *>(p.dy), r, p.dy_stride, c0);
         at[1] = at_row(static_cast<const T *>(p.h), r, p.h_stride, c0);
         at[2] = p.d_residual ? at_row(static_cast<const T *>(p.d_residual), r, p.d_residual_stride, c0) : nullptr;
     };
-    Feed<T, VEC, NV, 3> feed(p.depth);
+    Feed<T, VEC, NV, 3, RAGGED> feed(p.depth);
     auto ask = [&](int r) {
         const T *at[3];
         start(r, at);
-        feed.ask(at, r < p.rows, p.d - c0, across);
+        feed.ask(at, r < p.rows, c0, p.d, across);
     };
     for (int i = 0; i < feed.depth; ++i) ask(first + i * step);
     Pack<W, VEC> wv[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (c0 + i * across < p.d) wv[i] = load_pack<W, VEC>(w + c0 + i * across);
+        if (c0 + i * across < p.d) wv[i] = load_weight<W, VEC, RAGGED>(w, c0 + i * across, p.d);
     int turn = 0;
     for (int row = first; row < p.rows; row += step, turn ^= 1) {
         const float rstd = p.rstd[row];
         // the row stays as it was loaded for the second half (n = h * rstd and g = dy * weight would take twice the registers)
         Pack<T, VEC> dy[NV], h[NV], add[NV];
-        if (feed.depth > 0) {
-            feed.wait();
+        const bool fed = feed.depth > 0;
+        const T *at[3];
+        if (RAGGED || !fed) start(row, at);
+        if (fed) feed.wait();
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (c0 + i * across < p.d) {
-                    dy[i] = feed.got(0, i);
-                    h[i] = feed.got(1, i);
-                    if (p.d_residual) add[i] = feed.got(2, i);
-                }
-            feed.next();
-        } else {
-            const T *at[3];
-            start(row, at);
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (c0 + i * across < p.d) {
-                    dy[i] = load_pack<T, VEC>(at[0] + i * across);
-                    h[i] = load_pack<T, VEC>(at[1] + i * across);
-                    if (p.d_residual) add[i] = load_pack<T, VEC>(at[2] + i * across);
-                }
+        for (int i = 0; i < NV; ++i) {
+            const int c = c0 + i * across;
+            if (c >= p.d) continue;
+            if (fed && whole_pack<VEC, RAGGED>(c, p.d)) {
+                dy[i] = feed.got(0, i);
+                h[i] = feed.got(1, i);
+                if (p.d_residual) add[i] = feed.got(2, i);
+            } else if (RAGGED || !fed) {
+                dy[i] = load_some<T, VEC, RAGGED>(at[0] + i * across, c, p.d);
+                h[i] = load_some<T, VEC, RAGGED>(at[1] + i * across, c, p.d);
+                if (p.d_residual) add[i] = load_some<T, VEC, RAGGED>(at[2] + i * across, c, p.d);
+            }
         }
+        if (fed) feed.next();
         float2 dot = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -364,41 +415,41 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel
                     from_f32x2(&o.v[j], fma2(to_f32x2(&dy[i].v[j]), mul2(to_f32x2(&wv[i].v[j]), both(rstd)), v));
                 }
             }
-            store_pack<T, VEC>(dx + i * across, o);
+            store_some<T, VEC, RAGGED>(dx + i * across, o, c0 + i * across, p.d);
         }
     }
     if (!p.partial) return;
-    // the sums of a block's rows first meet in shared memory, in the order of the warps: one partial row per block
-    extern __shared__ __align__(16) uint8_t feed_memory[];
-    float *sums = reinterpret_cast<float *>(feed_memory);
+    float *out = p.partial + (long long)blockIdx.x * p.d;
     if (blockDim.y > 1) {
+        // the sums of a block's rows first meet in shared memory, by columns and in the order of the warps: one partial row per block
+        extern __shared__ __align__(16) uint8_t feed_memory[];
+        float *sums = reinterpret_cast<float *>(feed_memory);
         asm volatile("cp.async.wait_all;" ::: "memory");        // nothing is on its way into that memory any more
         __syncthreads();
-        if (threadIdx.y > 0) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) sums[((threadIdx.y - 1) * NV * VEC + i * VEC + j) * 32 + threadIdx.x] = acc[i * VEC + j];
+        for (int i = 0; i < NV * VEC; ++i) {
+            const int c = c0 + i / VEC * across + i % VEC;
+            if (c >= 0 && c < p.d) sums[threadIdx.y * p.d + c] = acc[i];
         }
         __syncthreads();
-        if (threadIdx.y > 0) return;
-        for (int y = 1; y < blockDim.y; ++y)
-#pragma unroll
-            for (int i = 0; i < NV * VEC; ++i) acc[i] += sums[((y - 1) * NV * VEC + i) * 32 + threadIdx.x];
+        for (int c = threadIdx.y * 32 + threadIdx.x; c < p.d; c += 32 * blockDim.y) {
+            float t = 0.0f;
+            for (int y = 0; y < blockDim.y; ++y) t += sums[y * p.d + c];
+            out[c] = t;
+        }
+        return;
     }
-    float *out = p.partial + (long long)blockIdx.x * p.d + c0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        if (c0 + i * across < p.d) {
-            Pack<float, VEC> o;
+        const int c = c0 + i * across;
+        if constexpr (!RAGGED && VEC % 4 == 0) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) o.v[j] = acc[i * VEC + j];
-            if (p.d % 4 == 0) {
-                store_pack<float, VEC>(out + i * across, o);
-            } else {
+            for (int j = 0; j < VEC; j += 4)
+                if (c < p.d) *reinterpret_cast<float4 *>(out + c + j) = make_float4(acc[i * VEC + j], acc[i * VEC + j + 1], acc[i * VEC + j + 2], acc[i * VEC + j + 3]);
+        } else {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) out[i * across + j] = o.v[j];
-            }
+            for (int j = 0; j < VEC; ++j)
+                if (c + j >= 0 && c + j < p.d) out[c + j] = acc[i * VEC + j];
         }
     }
 }
@@ -505,9 +556,9 @@ __global__ void __launch_bounds__(swiglu_threads(VEC *NV)) swiglu_quant_kernel(c
 // How a row of `width` elements is spread: threads per row, packs per thread, rows per block.
 struct RowShape { int threads, packs, rows_per_block; };
 
-template <int VEC> RowShape row_shape(int rows, int width, int want_values, int (*most_threads)(int))
+template <int VEC> RowShape row_shape(int rows, int width, int want_values, int (*most_threads)(int), bool ragged = false)
 {
-    const int packs = (width + VEC - 1) / VEC;
+    const int packs = (width + VEC - 1 + (ragged ? VEC - 1 : 0)) / VEC;
     // few rows leave SMs idle whatever the block is: the latency of one row counts, so a thread takes few values
     const int want = rows <= 296 ? 8 : want_values;
     auto threads = [&](int n) { return ((packs + n - 1) / n + 31) / 32 * 32; };
@@ -537,9 +588,12 @@ template <typename K> int resident(K kernel, int threads, int smem, int blocks, 
     return std::min(blocks, per_sm * sm_count(device));
 }
 
-template <typename K, typename P> int launch_rows(K kernel, const P &p, const RowShape &s, int device, cudaStream_t stream)
+// Ragged rows: a block's rows have to lie a multiple of VEC (8 at most) apart, unless each block has one row.
+int whole_steps(int blocks, const RowShape &s, int rows, bool ragged) { return ragged && s.rows_per_block == 1 && blocks < rows && blocks > 8 ? blocks / 8 * 8 : blocks; }
+
+template <typename K, typename P> int launch_rows(K kernel, const P &p, const RowShape &s, bool ragged, int device, cudaStream_t stream)
 {
-    const int blocks = resident(kernel, s.threads * s.rows_per_block, 0, (p.rows + s.rows_per_block - 1) / s.rows_per_block, device);
+    const int blocks = whole_steps(resident(kernel, s.threads * s.rows_per_block, 0, (p.rows + s.rows_per_block - 1) / s.rows_per_block, device), s, p.rows, ragged);
     if (blocks < 1) return MOE_OVL_ERR_CUDA;
     kernel<<<blocks, dim3(s.threads, s.rows_per_block), 0, stream>>>(p);
     return launched();
@@ -549,11 +603,11 @@ template <typename K, typename P> int launch_rows(K kernel, const P &p, const Ro
 // there would not be three).  Where every SM has a block at most, nothing is to come.  `allowed`: whether this kernel has been allowed
 // its shared memory on each device.
 template <int VEC, int NV, typename T, typename K>
-int launch_backward(K kernel, std::atomic<int> *allowed, NormBackP &p, const RowShape &s, int device, cudaStream_t stream, int &blocks)
+int launch_backward(K kernel, std::atomic<int> *allowed, NormBackP &p, const RowShape &s, bool ragged, int device, cudaStream_t stream, int &blocks)
 {
     constexpr int ROOM = 200 * 1024;
     const int threads = s.threads * s.rows_per_block, sms = sm_count(device);
-    int smem = (s.rows_per_block - 1) * VEC * NV * 32 * 4;
+    int smem = s.rows_per_block > 1 ? s.rows_per_block * p.d * 4 : 0;
     blocks = std::min((p.rows + s.rows_per_block - 1) / s.rows_per_block, NORM_PARTIALS);
     p.depth = 0;
     if (blocks > sms) {
@@ -567,6 +621,7 @@ int launch_backward(K kernel, std::atomic<int> *allowed, NormBackP &p, const Row
         }
         blocks = std::min(blocks, per_sm * sms);
     }
+    blocks = whole_steps(blocks, s, p.rows, ragged);
     if (smem > 46 * 1024 && (device > 63 || allowed[device].load(std::memory_order_relaxed) == 0)) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM) != cudaSuccess) return MOE_OVL_ERR_CUDA;
         if (device <= 63) allowed[device].store(1, std::memory_order_relaxed);
@@ -589,6 +644,15 @@ template <int VEC, typename F> int with_packs(int packs, F f)
     if constexpr (VEC <= 2) if (packs == 32) return f(Count<32>());
     if constexpr (VEC == 1) if (packs == 64) return f(Count<64>());
     return MOE_OVL_ERR_UNSUPPORTED;
+}
+
+// Calls f with the packs that the matrices allow, and whether rows are ragged in them: 16 bytes, or one element.
+template <typename T, typename F> int with_ragged(bool wide, bool ragged, F f)
+{
+    constexpr int VEC = 16 / (int)sizeof(T);
+    if (wide) return f(Count<VEC>(), Count<0>());
+    if (ragged) return f(Count<VEC>(), Count<1>());
+    return f(Count<1>(), Count<0>());
 }
 
 // Calls f with the widest pack that the matrices allow: 16 bytes, a pair of 16-bit values, or one value.
@@ -635,18 +699,26 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
                (!a->residual_out || rows_ok(a->residual_out, a->residual_out_stride, vec, es)) &&
                (!a->y || rows_ok(a->y, a->y_stride, vec, es)) && (!a->q || rows_ok(a->q, a->q_stride, vec, 1));
     };
+    auto agree = [&](int vec) {
+        auto like_x = [&](const void *m, int64_t stride, int bytes) { return !m || (aligned(m, (size_t)vec * bytes) && (stride - a->x_stride) % vec == 0); };
+        return like_x(a->x, a->x_stride, es) && like_x(a->residual, a->residual_stride, es) && like_x(a->residual_out, a->residual_out_stride, es) &&
+               like_x(a->y, a->y_stride, es) && like_x(a->q, a->q_stride, 1);
+    };
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        auto launch = [&](auto w, auto v) {
+        auto launch = [&](auto w, auto v, auto r) {
             using W = decltype(w);
             constexpr int VEC = decltype(v)::value;
-            const RowShape s = row_shape<VEC>(p.rows, p.d, VEC >= 4 ? VEC : 8, max_threads);
+            constexpr bool RAGGED = decltype(r)::value != 0;
+            const RowShape s = row_shape<VEC>(p.rows, p.d, VEC >= 4 ? VEC : 8, max_threads, RAGGED);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
-                return launch_rows(add_norm_kernel<T, W, VEC, NV>, p, s, a->device, static_cast<cudaStream_t>(a->stream));
+                return launch_rows(add_norm_kernel<T, W, VEC, NV, RAGGED>, p, s, RAGGED, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
-        return with_vec<T>(fits(16 / es), fits(2), [&](auto v) { return a->weight_dtype == a->dtype ? launch(T(), v) : launch(0.0f, v); });
+        return with_ragged<T>(fits(16 / es), agree(16 / es), [&](auto v, auto r) {
+            return a->weight_dtype == a->dtype ? launch(T(), v, r) : launch(0.0f, v, r);
+        });
     });
 }
 
@@ -690,23 +762,30 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
                rows_ok(a->dx, a->dx_stride, vec, es) && aligned(a->weight, (size_t)vec * ws) &&
                (!a->d_residual || rows_ok(a->d_residual, a->d_residual_stride, vec, es));
     };
+    auto agree = [&](int vec) {
+        auto like_dy = [&](const void *m, int64_t stride) { return !m || (aligned(m, (size_t)vec * es) && (stride - a->dy_stride) % vec == 0); };
+        return like_dy(a->dy, a->dy_stride) && like_dy(a->h, a->h_stride) && like_dy(a->d_residual, a->d_residual_stride) && like_dy(a->dx, a->dx_stride);
+    };
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        auto launch = [&](auto w, auto v) {
+        auto launch = [&](auto w, auto v, auto r) {
             using W = decltype(w);
             constexpr int VEC = decltype(v)::value;
-            const RowShape s = row_shape<VEC>(p.rows, p.d, 8, max_threads);
+            constexpr bool RAGGED = decltype(r)::value != 0;
+            const RowShape s = row_shape<VEC>(p.rows, p.d, 8, max_threads, RAGGED);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 int blocks = 0;
                 static std::atomic<int> allowed[64];
-                const int rc = launch_backward<VEC, NV, T>(add_norm_backward_kernel<T, W, VEC, NV>, allowed, p, s, a->device, stream, blocks);
+                const int rc = launch_backward<VEC, NV, T>(add_norm_backward_kernel<T, W, VEC, NV, RAGGED>, allowed, p, s, RAGGED, a->device, stream, blocks);
                 if (rc != MOE_OVL_OK || !p.partial) return rc;
                 reduce_partials_kernel<<<(p.d + 31) / 32, dim3(32, 32), 0, stream>>>(p.partial, blocks, p.d, a->dweight);
                 return launched();
             });
         };
-        return with_vec<T>(fits(16 / es), fits(2), [&](auto v) { return a->weight_dtype == a->dtype ? launch(T(), v) : launch(0.0f, v); });
+        return with_ragged<T>(fits(16 / es), agree(16 / es), [&](auto v, auto r) {
+            return a->weight_dtype == a->dtype ? launch(T(), v, r) : launch(0.0f, v, r);
+        });
     });
 }
 
@@ -731,7 +810,7 @@ extern "C" int moe_ovl_swiglu_quant(const moe_ovl_swiglu_args *a)
             const RowShape s = row_shape<VEC>(p.rows, p.f, 16, swiglu_threads);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
-                return launch_rows(swiglu_quant_kernel<T, VEC, NV>, p, s, a->device, static_cast<cudaStream_t>(a->stream));
+                return launch_rows(swiglu_quant_kernel<T, VEC, NV>, p, s, false, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
         return with_vec<T>(fits(16 / es), fits(2), launch);

@@ -179,11 +179,43 @@ def test_add_norm_backward(d, dtype):
         close(dx, want, U[dtype] * want.abs() + 1e-5 * size + FLOOR[dtype])
         close(dw, dw_want, 1e-5 * dw_size + 1e-30)
         assert bool((ws[-64:] == 3).all()) and untouched(full, dx)
-        dw2, dx2 = torch.empty_like(dw), torch.empty_like(dx)
+        dw2, (dx2, _) = torch.empty_like(dw), make()
         ops.moe_ovl_add_norm_backward(dy=dy, h=h, weight=w, rstd=rstd, d_residual=use, dx=dx2, dweight=dw2, workspace=ws)
         assert torch.equal(dw, dw2) and torch.equal(dx, dx2)        # the same bits
         ops.moe_ovl_add_norm_backward(dy=dy, h=h, weight=w, rstd=rstd, d_residual=use, dx=dy)     # in place, without dweight
         assert torch.equal(dy, dx)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("d", [3, 9, 33, 127, 250, 255, 513, 1001, 2047, 4097, 8190])
+def test_add_norm_and_gradient_of_ragged_rows(d, dtype):
+    """Rows whose length or distance is no multiple of 16 bytes, from aligned bases, more of them than blocks; then with matrices that do
+    not agree on where a row begins."""
+    g = gen(d)
+    for rows, pads in ((2, (0, 0, 0)), (1900, (0, 0, 0)), (2500, (8, 16, 0)), (700, (1, 2, 5))):
+        wide = lambda pad, t=dtype: torch.full((rows, d + pad), 7, dtype=t, device="cuda")  # noqa: E731
+        x, r, h, y = wide(pads[0]), wide(pads[1]), wide(pads[2]), wide(pads[0])
+        q, scale, rstd = wide(pads[1], torch.int8), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        cut = lambda m: m[:, :d]  # noqa: E731
+        cut(x).copy_(normal(g, (rows, d), dtype))
+        cut(r).copy_(normal(g, (rows, d), dtype))
+        w = normal(g, (d,), dtype) + 1
+        ops.moe_ovl_add_norm(x=cut(x), residual=cut(r), weight=w, residual_out=cut(h), y=cut(y), q=cut(q), scale=scale, rstd=rstd)
+        assert torch.equal(cut(h), (cut(x).float() + cut(r).float()).to(dtype))
+        v, rs = norm64(cut(h), w, 1e-6)
+        close(rstd, rs, 4e-6 * rs)
+        close(cut(y), v, (U[dtype] + 6e-6) * v.abs() + FLOOR[dtype])
+        close(cut(q).double() * scale.double()[:, None], v, 0.502 * v.abs().amax(1, keepdim=True) / 127)
+        dy, dx, dw = wide(pads[1]), wide(pads[0]), torch.empty(d, device="cuda")
+        cut(dy).copy_(normal(g, (rows, d), dtype))
+        ws = torch.empty(ops.moe_ovl_add_norm_workspace_bytes(rows, d), dtype=torch.uint8, device="cuda")
+        ops.moe_ovl_add_norm_backward(dy=cut(dy), h=cut(h), weight=w, rstd=rstd, d_residual=cut(r), dx=cut(dx), dweight=dw, workspace=ws)
+        want, dw_want, size, dw_size = norm_backward64(cut(dy), cut(h), w, rstd, cut(r))
+        close(cut(dx), want, U[dtype] * want.abs() + 1e-5 * size + FLOOR[dtype])
+        close(dw, dw_want, 1e-5 * dw_size + 1e-30)
+        for m, pad in ((h, pads[2]), (y, pads[0]), (q, pads[1]), (dx, pads[0])):
+            assert pad == 0 or bool((m[:, d:] == 7).all())
 
 
 @gpu
