@@ -5,8 +5,8 @@
 // held in registers between the two (NV packs of VEC elements per thread), so nothing is read twice.  The row's
 // threads are one block, or one warp where the row is short (several rows per block then, and no block barrier).  Blocks
 // stay and take rows at a fixed distance, and what belongs to a column (weights, the weight gradient's sums) stays in registers.
-// The next row's loads are under way while a row is reduced and written: in registers, and in the gradient's kernel, which has
-// three matrices to read and sums to keep, in shared memory up to four rows deep (struct Feed).
+// The next row's loads are under way while a row is reduced and written: into registers, and in the gradient's kernel, which has
+// three matrices to read and sums to keep, into shared memory (struct Feed).
 #include <algorithm>
 #include <atomic>
 
@@ -18,7 +18,7 @@ namespace {
 
 constexpr float QUANT_MAX = 127.0f;
 constexpr float QUANT_TINY = 7.8886090522101181e-31f;      // 2^-100
-constexpr int NORM_PARTIALS = 592;                          // most partial rows of the weight gradient: 148 SMs x 4
+constexpr int NORM_PARTIALS = 888;                          // most partial rows of the weight gradient: 148 SMs x 6
 
 // Threads a block of a kernel with so many values per thread may have: the row lives in registers.
 constexpr int max_threads(int values) { return values <= 8 ? 1024 : 512; }
@@ -102,7 +102,7 @@ template <typename T> __device__ __forceinline__ T *at_row(T *base, int row, int
 // ADDRESS space: its first column is `shift` columns further left, and shift = (row * stride) mod VEC stays the same for a block when its
 // rows lie a multiple of VEC rows apart.  All matrices have to agree on it (the same stride mod VEC, aligned bases).  Only the row's first and
 // last pack are partial; their elements are read and written one by one, and count as 0 outside the row.  (4097 columns, 8000 rows, bf16:
-// element by element 142 us, this way RAGGED_US.)
+// element by element 142 us, this way 75 us.)
 template <int VEC, bool RAGGED> __device__ __forceinline__ bool whole_pack(int c, int d) { return RAGGED ? c >= 0 && c + VEC <= d : c < d; }
 template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_part(const T *p, int c, int d)
 {
@@ -150,67 +150,54 @@ template <int VEC, bool RAGGED> __device__ __forceinline__ void quant_some(int8_
 }
 template <int VEC, bool RAGGED> __device__ __forceinline__ int shift_of(int row, int stride) { return RAGGED ? (int)((unsigned)row * (unsigned)stride % VEC) : 0; }
 
-// Rows on their way from global to shared memory.  Every thread copies, waits for and reads its own packs only (asynchronous
-// copies of 16 or 4 bytes), so no thread waits for another.  `depth` rows are on their way; 0: the packs are loaded when they are
-// needed (elements of two bytes, which such copies do not know, always are).
+// Two rows in shared memory, one in use and one on its way from global memory.  Every thread copies, waits for and reads its own
+// packs only (asynchronous copies of 16 or 4 bytes), so no thread waits for another.  Partial packs are not copied.
 template <typename T, int VEC, int NV, int ARRAYS, bool RAGGED> struct Feed {
     static constexpr int BYTES = VEC * (int)sizeof(T);
-    static constexpr bool ASYNC = BYTES >= 4;
     uint32_t base, stride;                      // this thread's first pack, bytes from pack to pack
-    int depth, put = 0, take = 0;
-    __device__ Feed(int depth_) : depth(ASYNC ? depth_ : 0)
+    int slot = 0;
+    __device__ Feed()
     {
         extern __shared__ __align__(16) uint8_t feed_memory[];
         base = (uint32_t)__cvta_generic_to_shared(feed_memory) + (threadIdx.y * blockDim.x + threadIdx.x) * BYTES;
         stride = blockDim.x * blockDim.y * BYTES;
     }
-    // Asks for a row: `at[k]` where this thread's first column c lies in matrix k (NULL: none), `across` columns from pack to pack.
+    // Asks for a row into the slot that is not in use: `at[k]` where this thread's first column c lies in matrix k (NULL: none),
+    // `across` columns from pack to pack.
     __device__ __forceinline__ void ask(const T *const (&at)[ARRAYS], bool any, int c, int d, int across)
     {
-        if constexpr (ASYNC) {
-            if (any) {
+        if (any) {
 #pragma unroll
-                for (int k = 0; k < ARRAYS; ++k)
+            for (int k = 0; k < ARRAYS; ++k)
 #pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (at[k] && whole_pack<VEC, RAGGED>(c + i * across, d)) {
-                            const uint32_t to = base + ((put * ARRAYS + k) * NV + i) * stride;
-                            if constexpr (BYTES == 16)
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at[k] + i * across) : "memory");
-                            else
-                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(at[k] + i * across) : "memory");
-                        }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (++put == depth) put = 0;
+                for (int i = 0; i < NV; ++i)
+                    if (at[k] && whole_pack<VEC, RAGGED>(c + i * across, d)) {
+                        const uint32_t to = base + (((slot ^ 1) * ARRAYS + k) * NV + i) * stride;
+                        if constexpr (BYTES == 16)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at[k] + i * across) : "memory");
+                        else
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(at[k] + i * across) : "memory");
+                    }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // Waits for the oldest row asked for.
-    __device__ __forceinline__ void wait()
-    {
-        if (depth == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-        else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-        else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    }
+    __device__ __forceinline__ void turn() { slot ^= 1; }
+    // The row of the slot in use is here; the one asked for last may not be.
+    __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
     __device__ __forceinline__ Pack<T, VEC> got(int k, int i) const
     {
-        Pack<T, VEC> r = {};
-        const uint32_t from = base + ((take * ARRAYS + k) * NV + i) * stride;
+        Pack<T, VEC> r;
+        const uint32_t from = base + ((slot * ARRAYS + k) * NV + i) * stride;
         if constexpr (BYTES == 16) {
             uint4 v;
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
             *reinterpret_cast<uint4 *>(&r) = v;
-        } else if constexpr (BYTES == 4) {
+        } else {
             uint32_t v;
             asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
             *reinterpret_cast<uint32_t *>(&r) = v;
         }
         return r;
-    }
-    __device__ __forceinline__ void next()
-    {
-        if (++take == depth) take = 0;
     }
 };
 
@@ -315,7 +302,7 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const No
 }
 
 struct NormBackP {
-    int rows, d, depth;
+    int rows, d;
     float per_d;
     const void *dy, *h, *weight, *d_residual;
     const float *rstd;
@@ -324,11 +311,21 @@ struct NormBackP {
     int dy_stride, h_stride, d_residual_stride, dx_stride;
 };
 
+// What the gradient's kernel asks of shared memory per row, where it takes rows through it: not for elements of two bytes, which the
+// copies do not know, nor for rows of which no two fit.
+template <typename T, int VEC, int NV> struct BackFeed {
+    static constexpr int THREAD_BYTES = 3 * NV * VEC * (int)sizeof(T);
+    static constexpr bool ON = VEC * sizeof(T) >= 4 && 2 * THREAD_BYTES * max_threads(VEC * NV) <= 200 * 1024;
+};
+
 // Every block (or warp) keeps its columns' share of the weight gradient over all of its rows; the partial rows are
-// added up in a fixed order by reduce_partials_kernel: no atomics, the same bits every time.
+// added up in a fixed order by reduce_partials_kernel: no atomics, the same bits every time.  A row is read from shared memory twice, before
+// and after its reduction, so that few registers are in use across the barrier: blocks per SM carry this kernel (12289 x 2048,
+// bf16: 84, 49, 40, 36 us with 1, 2, 3, 4 of them), not how many rows are on their way (one to four: the same).
 template <typename T, typename W, int VEC, int NV, bool RAGGED>
 __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel(const NormBackP p)
 {
+    constexpr bool FED = BackFeed<T, VEC, NV>::ON;
     __shared__ float buf[2][32];
     float acc[NV * VEC];
 #pragma unroll
@@ -341,13 +338,13 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel
         at[1] = at_row(static_cast<const T *>(p.h), r, p.h_stride, c0);
         at[2] = p.d_residual ? at_row(static_cast<const T *>(p.d_residual), r, p.d_residual_stride, c0) : nullptr;
     };
-    Feed<T, VEC, NV, 3, RAGGED> feed(p.depth);
+    Feed<T, VEC, NV, 3, RAGGED> feed;
     auto ask = [&](int r) {
         const T *at[3];
         start(r, at);
         feed.ask(at, r < p.rows, c0, p.d, across);
     };
-    for (int i = 0; i < feed.depth; ++i) ask(first + i * step);
+    if constexpr (FED) ask(first);
     Pack<W, VEC> wv[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -355,64 +352,68 @@ __global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel
     int turn = 0;
     for (int row = first; row < p.rows; row += step, turn ^= 1) {
         const float rstd = p.rstd[row];
-        // the row stays as it was loaded for the second half (n = h * rstd and g = dy * weight would take twice the registers)
-        Pack<T, VEC> dy[NV], h[NV], add[NV];
-        const bool fed = feed.depth > 0;
         const T *at[3];
-        if (RAGGED || !fed) start(row, at);
-        if (fed) feed.wait();
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = c0 + i * across;
-            if (c >= p.d) continue;
-            if (fed && whole_pack<VEC, RAGGED>(c, p.d)) {
-                dy[i] = feed.got(0, i);
-                h[i] = feed.got(1, i);
-                if (p.d_residual) add[i] = feed.got(2, i);
-            } else if (RAGGED || !fed) {
-                dy[i] = load_some<T, VEC, RAGGED>(at[0] + i * across, c, p.d);
-                h[i] = load_some<T, VEC, RAGGED>(at[1] + i * across, c, p.d);
-                if (p.d_residual) add[i] = load_some<T, VEC, RAGGED>(at[2] + i * across, c, p.d);
-            }
+        if constexpr (FED) {
+            feed.turn();
+            ask(row + step);
+            feed.wait();
         }
-        if (fed) feed.next();
+        if (RAGGED || !FED) start(row, at);
+        Pack<T, VEC> own[3][FED ? 1 : NV] = {};     // without the feed a row stays in registers
+        auto pack = [&](int k, int i) -> Pack<T, VEC> {
+            if constexpr (!FED) return own[k][i];
+            const int c = c0 + i * across;
+            if constexpr (RAGGED) {
+                if (!whole_pack<VEC, true>(c, p.d)) return load_part<T, VEC>(at[k] + i * across, c, p.d);
+            }
+            return feed.got(k, i);
+        };
+        if constexpr (!FED) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (c0 + i * across < p.d && at[k]) own[k][i] = load_some<T, VEC, RAGGED>(at[k] + i * across, c0 + i * across, p.d);
+        }
         float2 dot = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (c0 + i * across >= p.d) continue;
+            const Pack<T, VEC> dy = pack(0, i), h = pack(1, i);
             if constexpr (VEC == 1) {
-                const float t = to_f32(dy[i].v[0]), n = to_f32(h[i].v[0]) * rstd;
+                const float t = to_f32(dy.v[0]), n = to_f32(h.v[0]) * rstd;
                 acc[i] = fmaf(t, n, acc[i]);
                 dot.x = fmaf(t * to_f32(wv[i].v[0]), n, dot.x);
             } else {
 #pragma unroll
                 for (int j = 0; j < VEC; j += 2) {
                     const int k = i * VEC + j;
-                    const float2 t = to_f32x2(&dy[i].v[j]), n = mul2(to_f32x2(&h[i].v[j]), both(rstd));
+                    const float2 t = to_f32x2(&dy.v[j]), n = mul2(to_f32x2(&h.v[j]), both(rstd));
                     const float2 s = fma2(t, n, make_float2(acc[k], acc[k + 1]));
                     acc[k] = s.x, acc[k + 1] = s.y;
                     dot = fma2(mul2(t, to_f32x2(&wv[i].v[j])), n, dot);
                 }
             }
         }
-        if (feed.depth > 0) ask(row + feed.depth * step);
         // dx = rstd * (g - n * mean) = dy * (weight * rstd) - h * (rstd^2 * mean)
         const float mean = row_sum(dot.x + dot.y, buf[turn]) * p.per_d, back = -rstd * rstd * mean;
         T *dx = at_row(static_cast<T *>(p.dx), row, p.dx_stride, c0);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (c0 + i * across >= p.d) continue;
-            Pack<T, VEC> o;
+            const Pack<T, VEC> dy = pack(0, i), h = pack(1, i);
+            Pack<T, VEC> add, o;
+            if (p.d_residual) add = pack(2, i);
             if constexpr (VEC == 1) {
-                float v = fmaf(to_f32(dy[i].v[0]), to_f32(wv[i].v[0]) * rstd, to_f32(h[i].v[0]) * back);
-                if (p.d_residual) v += to_f32(add[i].v[0]);
+                float v = fmaf(to_f32(dy.v[0]), to_f32(wv[i].v[0]) * rstd, to_f32(h.v[0]) * back);
+                if (p.d_residual) v += to_f32(add.v[0]);
                 o.v[0] = from_f32<T>(v);
             } else {
 #pragma unroll
                 for (int j = 0; j < VEC; j += 2) {
-                    float2 v = mul2(to_f32x2(&h[i].v[j]), both(back));
-                    if (p.d_residual) v = add2(v, to_f32x2(&add[i].v[j]));
-                    from_f32x2(&o.v[j], fma2(to_f32x2(&dy[i].v[j]), mul2(to_f32x2(&wv[i].v[j]), both(rstd)), v));
+                    float2 v = mul2(to_f32x2(&h.v[j]), both(back));
+                    if (p.d_residual) v = add2(v, to_f32x2(&add.v[j]));
+                    from_f32x2(&o.v[j], fma2(to_f32x2(&dy.v[j]), mul2(to_f32x2(&wv[i].v[j]), both(rstd)), v));
                 }
             }
             store_some<T, VEC, RAGGED>(dx + i * across, o, c0 + i * across, p.d);
@@ -599,33 +600,19 @@ template <typename K, typename P> int launch_rows(K kernel, const P &p, const Ro
     return launched();
 }
 
-// The gradient's kernel: as many rows on their way per block as shared memory has room for (four at most; a block less per SM where
-// there would not be three).  Where every SM has a block at most, nothing is to come.  `allowed`: whether this kernel has been allowed
-// its shared memory on each device.
+// `allowed`: whether this kernel has been allowed its shared memory on each device.
 template <int VEC, int NV, typename T, typename K>
-int launch_backward(K kernel, std::atomic<int> *allowed, NormBackP &p, const RowShape &s, bool ragged, int device, cudaStream_t stream, int &blocks)
+int launch_backward(K kernel, std::atomic<int> *allowed, const NormBackP &p, const RowShape &s, bool ragged, int device, cudaStream_t stream, int &blocks)
 {
-    constexpr int ROOM = 200 * 1024;
-    const int threads = s.threads * s.rows_per_block, sms = sm_count(device);
-    int smem = s.rows_per_block > 1 ? s.rows_per_block * p.d * 4 : 0;
-    blocks = std::min((p.rows + s.rows_per_block - 1) / s.rows_per_block, NORM_PARTIALS);
-    p.depth = 0;
-    if (blocks > sms) {
-        int per_sm = 0;
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) return MOE_OVL_ERR_CUDA;
-        if (VEC * sizeof(T) >= 4) {
-            const int row_bytes = 3 * NV * VEC * (int)sizeof(T) * threads;
-            while (per_sm > 1 && ROOM / per_sm / row_bytes < 3) --per_sm;
-            p.depth = std::min(4, ROOM / per_sm / row_bytes);
-            smem = std::max(p.depth * row_bytes, smem);
-        }
-        blocks = std::min(blocks, per_sm * sms);
-    }
-    blocks = whole_steps(blocks, s, p.rows, ragged);
+    const int threads = s.threads * s.rows_per_block;
+    const int smem = std::max(BackFeed<T, VEC, NV>::ON ? 2 * BackFeed<T, VEC, NV>::THREAD_BYTES * threads : 0, s.rows_per_block > 1 ? s.rows_per_block * p.d * 4 : 0);
     if (smem > 46 * 1024 && (device > 63 || allowed[device].load(std::memory_order_relaxed) == 0)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROOM) != cudaSuccess) return MOE_OVL_ERR_CUDA;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) return MOE_OVL_ERR_CUDA;
         if (device <= 63) allowed[device].store(1, std::memory_order_relaxed);
     }
+    blocks = resident(kernel, threads, smem, std::min((p.rows + s.rows_per_block - 1) / s.rows_per_block, NORM_PARTIALS), device);
+    if (blocks < 1) return MOE_OVL_ERR_CUDA;
+    blocks = whole_steps(blocks, s, p.rows, ragged);
     kernel<<<blocks, dim3(s.threads, s.rows_per_block), smem, stream>>>(p);
     return launched();
 }
@@ -754,7 +741,7 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
         if (!a->dweight) return MOE_OVL_OK;
         return cudaMemsetAsync(a->dweight, 0, (size_t)a->d * 4, stream) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
     }
-    NormBackP p = {a->rows, a->d, 0, 1.0f / (float)a->d, a->dy, a->h, a->weight, a->d_residual, a->rstd, a->dx,
+    const NormBackP p = {a->rows, a->d, 1.0f / (float)a->d, a->dy, a->h, a->weight, a->d_residual, a->rstd, a->dx,
                    a->dweight ? static_cast<float *>(a->workspace) : nullptr, (int)a->dy_stride, (int)a->h_stride,
                    (int)a->d_residual_stride, (int)a->dx_stride};
     auto fits = [&](int vec) {
