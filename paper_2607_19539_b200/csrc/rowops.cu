@@ -213,8 +213,9 @@ struct NormP {
 
 // The row's sum of squares and the largest |h * weight| come out of ONE reduction: rstd is a positive factor of the whole row,
 // so the scale of the 8-bit output needs no second pass over the normed values.
-template <typename T, typename W, int VEC, int NV, bool RAGGED>
-__global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const NormP p)
+// REGS: what a thread may have where it holds 8 values at most (a block of 1024 threads has room for 64).
+template <typename T, typename W, int VEC, int NV, bool RAGGED, int REGS>
+__global__ void __maxnreg__(VEC *NV <= 8 ? REGS : 128) add_norm_kernel(const NormP p)
 {
     __shared__ float2 buf[2][32];
     const int step = gridDim.x * blockDim.y;
@@ -322,8 +323,9 @@ template <typename T, int VEC, int NV> struct BackFeed {
 // added up in a fixed order by reduce_partials_kernel: no atomics, the same bits every time.  A row is read from shared memory twice, before
 // and after its reduction, so that few registers are in use across the barrier: blocks per SM carry this kernel (12289 x 2048,
 // bf16: 84, 49, 40, 36 us with 1, 2, 3, 4 of them), not how many rows are on their way (one to four: the same).
+// In 64 registers (48, 40: 37, 46 us); ragged rows in 48, where 544 threads fit an SM twice (8000 x 4097: 93 us, in 64 142 us).
 template <typename T, typename W, int VEC, int NV, bool RAGGED>
-__global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel(const NormBackP p)
+__global__ void __maxnreg__(VEC *NV <= 8 ? (RAGGED ? 48 : 64) : 128) add_norm_backward_kernel(const NormBackP p)
 {
     constexpr bool FED = BackFeed<T, VEC, NV>::ON;
     __shared__ float buf[2][32];
@@ -700,7 +702,10 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
             const RowShape s = row_shape<VEC>(p.rows, p.d, VEC >= 4 ? VEC : 8, max_threads, RAGGED);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
-                return launch_rows(add_norm_kernel<T, W, VEC, NV, RAGGED>, p, s, RAGGED, a->device, static_cast<cudaStream_t>(a->stream));
+                // An 8-bit output alone: blocks per SM count (16384 x 4096: 72 us in 40 registers, 80 us in 64).  With an output in the type of x the
+                // writes are what bounds it, and fewer blocks write better (87 us in 64, 92 us in 40).
+                const auto kernel = p.q && !p.y ? add_norm_kernel<T, W, VEC, NV, RAGGED, 40> : add_norm_kernel<T, W, VEC, NV, RAGGED, 64>;
+                return launch_rows(kernel, p, s, RAGGED, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
         return with_ragged<T>(fits(16 / es), agree(16 / es), [&](auto v, auto r) {
