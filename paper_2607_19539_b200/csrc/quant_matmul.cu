@@ -290,8 +290,8 @@ template <int TOKENS> __device__ __forceinline__ void fill_schedule(const QmP &p
 {
     unsigned rows_before = 0, tiles_before = 0;
     if (lane == 0) tile_start[0] = row_start[0] = 0;
-    const int experts = p.counts ? p.experts : 1;
-    if (!p.counts) count = lane == 0 ? p.rows : 0;
+    if (!p.counts && lane == 0) tile_start[1] = (p.rows + TOKENS - 1) / TOKENS, row_start[1] = p.rows;
+    const int experts = p.counts ? p.experts : 0;
 #pragma unroll 1
     for (int e0 = 0; e0 < experts; e0 += 32) {
         const int e = e0 + lane;
@@ -310,25 +310,20 @@ template <int TOKENS> __device__ __forceinline__ void fill_schedule(const QmP &p
 
 // The load warp's place in its sequence of stages.  The whole warp runs the loop, with everything in it the same in all lanes, and
 // one elected lane issues: tile copies take their operands from uniform registers, and where the compiler cannot tell that a
-// value is uniform (one lane's branch, values out of shared memory) it gathers them anew for every copy.
+// value is uniform (one lane's branch, values out of shared memory) it gathers them anew for every copy.  The loop of the stages is kept
+// short: one warp's instructions follow each other slowly, and 64-bit counters in it cost a tenth of the streaming rate.
 template <int CTAS, int TOKENS> struct QpLoader {
     using Shape = QpShape<CTAS, TOKENS>;
-    QpSchedule<CTAS, TOKENS> sched;
-    long long t, total, step, issued = 0;
-    int ksteps, k = 0, stage = 0, y_b = 0, y_a = 0;
+    uint32_t smem_base, bar_full, bar_empty, lead_full;
+    int rank, stage = 0, issued = 0;         // issued: no further than a whole ring
     uint32_t phase = 0;
-    // Issues stages until `most` have been issued; false: a wait gave up.
-    __device__ __forceinline__ bool run(const QmP &p, const CUtensorMap &map_b, const CUtensorMap &map_a, uint32_t smem_base, uint32_t bar_full,
-                                        uint32_t bar_empty, uint32_t lead_full, uint32_t rank, long long most, bool leader)
+    bool leader;
+    // Issues stages k .. k1 - 1 of a tile; false: a wait gave up.  FRESH: the stages have never been used.
+    template <bool FRESH>
+    __device__ __forceinline__ bool run(const QmP &p, const CUtensorMap &map_b, const CUtensorMap &map_a, int y_b, int y_a, int k, int k1)
     {
-        while (t < total && issued < most) {
-            if (k == 0) {
-                const auto tile = sched.at(t);
-                y_b = uniform(tile.expert * p.n + tile.channel0 + (int)rank * QM_ROWS);
-                // a pair's CTAs hold the halves of the instruction's N side
-                y_a = uniform(tile.row0 + (int)rank * ((tile.rows + 31) / 32 * 16));
-            }
-            if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, t))) return false;
+        for (; k < k1; ++k) {
+            if (!FRESH && !__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, y_b))) return false;
             const uint32_t sa = smem_base + stage * Shape::STAGE_BYTES;
             if (leader) {
                 if (CTAS == 1) {
@@ -342,10 +337,21 @@ template <int CTAS, int TOKENS> struct QpLoader {
                 }
             }
             if (++stage == Shape::STAGES) stage = 0, phase ^= 1u;
-            ++issued;
-            if (++k == ksteps) k = 0, t += step;
+            if (issued < Shape::STAGES) ++issued;
         }
         return true;
+    }
+    // After a give-up: the copies still in flight have to land.
+    __device__ void drain_all(const QmP &p)
+    {
+        // the last fills, newest first: the phase of a stage's last fill ends when it has landed
+        int s = stage;
+        uint32_t ph = phase;
+        for (int i = 0; i < issued; ++i) {
+            if (s == 0) s = Shape::STAGES, ph ^= 1u;
+            --s;
+            drain(bar_full + 8 * s, ph, p.timeout_ns);
+        }
     }
 };
 
@@ -375,28 +381,37 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     const int ksteps = (p.k + QM_K - 1) / QM_K, experts = p.experts > 0 ? p.experts : 1;
     QpSchedule<CTAS, TOKENS> sched{s_tile_start, s_row_start, (p.n + CTAS * QM_ROWS - 1) / (CTAS * QM_ROWS)};
     const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
-    QpLoader<CTAS, TOKENS> loader{sched, first, 0, step, 0, ksteps};
+    QpLoader<CTAS, TOKENS> loader{smem_base, bar_full, bar_empty, lead_full, (int)rank};
+    int early = 0;                          // stages of the first tile that are issued before the block is set up
     bool ok = true;
+    // where a tile's operands begin; a pair's CTAs hold the halves of the instruction's N side
+    auto rows_of = [&](long long t, int &y_b, int &y_a) {
+        const auto tile = sched.at(t);
+        y_b = uniform(tile.expert * p.n + tile.channel0 + (int)rank * QM_ROWS);
+        y_a = uniform(tile.row0 + (int)rank * ((tile.rows + 31) / 32 * 16));
+    };
 
     if (warp == 0) {
         const int count = count_of(p, lane);
-        if (lane == 0) {
-#pragma unroll 1
-            for (int i = 0; i < STAGES; ++i) {
-                mbar_init(bar_full + 8 * i, 1);           // the leader's load thread arrives, expecting all CTAs' bytes
-                mbar_init(bar_empty + 8 * i, 1);
-            }
-            for (int i = 0; i < 2; ++i) {
-                mbar_init(bar_tfull + 8 * i, 1);
-                mbar_init(bar_tempty + 8 * i, 8 * CTAS);  // one arrival per epilogue warp
-            }
-            mbar_init(bar_drain, 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        static_assert(STAGES <= 27, "a lane per barrier");
+        if (lane < STAGES) {
+            mbar_init(bar_full + 8 * lane, 1);            // the leader's load thread arrives, expecting all CTAs' bytes
+            mbar_init(bar_empty + 8 * lane, 1);
+        } else if (lane >= 27) {
+            // lanes 27 .. 31: accumulators full, accumulators empty (one arrival per epilogue warp), drained
+            const int i = lane - 27;
+            mbar_init(i < 2 ? bar_tfull + 8 * i : i < 4 ? bar_tempty + 8 * (i - 2) : bar_drain, i < 2 || i == 4 ? 1 : 8 * CTAS);
         }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        __syncwarp();
         fill_schedule<TOKENS>(p, s_tile_start, s_row_start, count, lane);
-        loader.total = sched.total(experts);
-        if (CTAS == 1 && !p.no_loads)
-            ok = loader.run(p, map_b, map_a, smem_base, bar_full, bar_empty, lead_full, rank, STAGES, elect_one());
+        loader.leader = elect_one();
+        if (CTAS == 1 && !p.no_loads && first < sched.total(experts)) {
+            int y_b, y_a;
+            rows_of(first, y_b, y_a);
+            early = min(ksteps, STAGES);
+            loader.template run<true>(p, map_b, map_a, y_b, y_a, 0, early);
+        }
     } else if (warp == 1) {
         if (CTAS == 1) tmem_alloc_self(smem_u32(&s_tmem), 2 * ACC_COLS);
         else tmem_alloc(smem_u32(&s_tmem), 2 * ACC_COLS);
@@ -410,17 +425,19 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
 
     if (warp == 0) {
         if (!p.no_loads) {
-            ok = ok && loader.run(p, map_b, map_a, smem_base, bar_full, bar_empty, lead_full, rank, 0x7fffffffffffffffll, elect_one());
-            if (!ok && rank == 0) {
-                // gave up: wait for the copies of all CTAs (a peer stays until the cluster barrier at the end)
-                for (long long i = loader.issued > STAGES ? loader.issued - STAGES : 0; i < loader.issued; ++i)
-                    drain(bar_full + 8 * (uint32_t)(i % STAGES), (uint32_t)(i / STAGES) & 1u, p.timeout_ns);
+            for (long long t = first; ok && t < total; t += step) {
+                int y_b, y_a;
+                rows_of(t, y_b, y_a);
+                ok = loader.template run<false>(p, map_b, map_a, y_b, y_a, early, ksteps);
+                early = 0;
             }
+            if (!ok && rank == 0) loader.drain_all(p);      // the peer stays until the cluster barrier at the end
         }
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
             const bool leader = elect_one();
+            const uint64_t desc_b = umma_smem_desc(smem_base);      // of stage 0; addresses are below 2^18, in units of 16 bytes
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             for (long long t = first; ok && t < total; t += step) {
@@ -431,12 +448,11 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(acc * ACC_COLS);
                 for (int k = 0; k < ksteps; ++k) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, t));
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k));
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t sa = smem_base + stage * STAGE_BYTES;
                     if (leader) {
-                        const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sa + QM_A_BYTES);
+                        const uint64_t da = desc_b + (uint32_t)stage * (STAGE_BYTES / 16), db = da + QM_A_BYTES / 16;
 #pragma unroll
                         for (int i = 0; i < QM_K / 32; ++i)
                             umma_i8<CTAS>(d, da + (uint64_t)(i * 2), db + (uint64_t)(i * 2), idesc, (k | i) != 0 ? 1u : 0u);
@@ -575,9 +591,19 @@ int launch(K kernel, unsigned blocks, int threads, int smem, int cluster, const 
     return cudaLaunchKernelEx(&cfg, kernel, b, a, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
 }
 
-template <int BN, int SPLITS, typename Out>
-int launch_split(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
+// The operands as the tensor maps need them.  A map's box and the kernel's tile come from the same constant, in the two functions below.
+struct QmOperands { const void *a, *b; long long b_rows, a_stride, b_stride; };
+
+bool encode_operands(const QmP &p, const QmOperands &o, int token_rows, CUtensorMap *a, CUtensorMap *b)
 {
+    return encode_bytes(b, o.b, o.b_rows, p.k, o.b_stride, QM_ROWS) && encode_bytes(a, o.a, p.rows, p.k, o.a_stride, token_rows);
+}
+
+template <int BN, int SPLITS, typename Out>
+int launch_split(const QmP &p, const QmOperands &o, int device, cudaStream_t stream)
+{
+    CUtensorMap a, b;
+    if (!encode_operands(p, o, BN, &a, &b)) return MOE_OVL_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
     const auto kernel = quant_matmul_kernel<BN, SPLITS, Out>;
     if (!allow_smem(kernel, QmShape<BN>::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
@@ -589,8 +615,10 @@ int launch_split(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int d
 }
 
 template <int CTAS, int TOKENS, typename Out>
-int launch_tiles(const QmP &p, const CUtensorMap &b, const CUtensorMap &a, int device, cudaStream_t stream)
+int launch_tiles(const QmP &p, const QmOperands &o, int device, cudaStream_t stream)
 {
+    CUtensorMap a, b;
+    if (!encode_operands(p, o, TOKENS / CTAS, &a, &b)) return MOE_OVL_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
     const auto kernel = quant_matmul_tiles_kernel<CTAS, TOKENS, Out>;
     if (!allow_smem(kernel, QpShape<CTAS, TOKENS>::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
@@ -602,41 +630,34 @@ template <int N> struct Number { static constexpr int value = N; };
 // ctas 0: a cluster of `splits` CTAs per tile; 1, 2: persistent CTAs, alone or in pairs.
 struct QmChoice { int ctas, tokens, splits; };
 
-// The kernel goes by the tiles there are (with the experts' rows taken as even: the counts are on the device).  W(channels, tokens):
-// waves of such tiles over the 148 CTAs or 74 pairs.  Measured, us:
-//   few tiles leave SMs idle, so they share their K: 1 token, n = k = 4096 (32 tiles) 7.4 split by 4, 10.2 unsplit; n = 8192,
-//     k = 2048 (64 tiles) 7.2 and 7.9; 256 tokens, n = 1024, k = 8192 (32 tiles of 64 tokens) 10.3 and 14.6; 128 tokens, n = 4096, k = 14336
-//     (64 such tiles) 18.3 and 22; with k = 4096 10.5 and 10.2: more of them take a long K to pay;
-//   up to 64 tokens per expert, or where tiles of 64 fit one wave, single CTAs: 16 experts of 64 tokens 48.4 against 49.4 in pairs (of 128:
-//     61.1 against 55.8); 256 tokens, n = k = 4096 10.3 against 11.8;
-//   pairs take 128 or 256 tokens, whose tiles cost about 8 : 13: 512 tokens, n = k = 4096 (one wave each) 12.3 and 17.5; 2048 tokens
-//     (four waves, two) 28.9 and 26.9.
+// The kernel goes by the tiles there are (with the experts' rows taken as even: the counts are on the device).  Measured, us:
+//   few tiles leave SMs idle, so they share their K: 1 token, n = k = 4096 (32 tiles) 7.3 split by 4, 8.0 unsplit; n = 1024, k = 8192 5.4 split
+//     by 8, 11.7; 128 tokens, n = 4096, k = 14336 (64 tiles) 18.1 and 20.9.  A step of K takes a CTA about 0.15 us; sharing costs about 1.2 us, and
+//     0.03 us per token of the tile, whose parts have to be added up.  With more tiles it does not pay: n = 8192, k = 2048 (64) 7.3 and 6.8;
+//   up to 64 tokens per expert, or where tiles of 64 fit one wave of the 148 CTAs, single CTAs: 16 experts of 64 tokens 48.4 against 49.4 in
+//     pairs (of 128: 61.1 against 55.8); 256 tokens, n = k = 4096 9.4 against 11.7.  Tiles of 32 where those fit the wave: 64 tokens, n = k = 4096
+//     8.5 against 9.2;
+//   pairs take 128 or 256 tokens, whose tiles cost about 8 : 13: 512 tokens, n = k = 4096 (one wave of the 74 pairs each) 12.2 and 17.2; 2048
+//     tokens (four waves, two) 28.9 and 26.9.
 QmChoice choose(const QmP &p)
 {
     const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows + groups - 1) / groups;
     auto tiles = [&](int channels, int tokens) {
         return (long long)((p.n + channels - 1) / channels) * groups * ((per_group + tokens - 1) / tokens);
     };
-    const int ksteps = (p.k + QM_K - 1) / QM_K;
-    auto split = [&](int tokens) {
-        // two CTAs per SM at most, a step of K for each, eight where there are as many CTAs as that
-        const long long t = tiles(QM_ROWS, tokens);
-        int n = 1;
-        while (n < 8 && t * n * 2 <= 296 && n * 2 <= ksteps && (n < 4 || ksteps >= 64)) n *= 2;
-        return QmChoice{0, tokens, n};
-    };
-    QmChoice c = {1, per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64, 1};
-    if (per_group <= 64) {
-        if (tiles(QM_ROWS, std::min(c.tokens, 32)) <= 74) c = split(std::min(c.tokens, 32));
-    } else if (tiles(QM_ROWS, 64) <= (ksteps >= 64 ? 74 : 37)) {
-        c = split(64);
-    } else if (tiles(QM_ROWS, 64) > 148) {
-        const long long w128 = (tiles(2 * QM_ROWS, 128) + 73) / 74, w256 = (tiles(2 * QM_ROWS, 256) + 73) / 74;
-        c = {2, per_group <= 128 || 8 * w128 <= 13 * w256 ? 128 : 256, 1};
+    const long long ksteps = (p.k + QM_K - 1) / QM_K;
+    QmChoice c = {0, per_group <= 16 ? 16 : per_group <= 64 ? 32 : 64, 1};
+    const long long shared = tiles(QM_ROWS, c.tokens);
+    if (shared <= (ksteps >= 64 ? 74 : 40)) {
+        // two CTAs per SM at most, a step of K for each, eight of them only for a long K
+        while (c.splits < 8 && shared * c.splits * 2 <= 296 && c.splits * 2 <= ksteps && (c.splits < 4 || ksteps >= 64)) c.splits *= 2;
+        if (ksteps * (c.splits - 1) * 15 > c.splits * (120 + 3 * std::min(c.tokens, per_group))) return c;
     }
-    // a K of one step cannot be shared
-    if (c.ctas == 0 && c.splits == 1) c.ctas = 1;
-    return c;
+    if (per_group <= 16) return {1, 16, 1};
+    if (per_group <= 32 || tiles(QM_ROWS, 32) <= 148) return {1, 32, 1};
+    if (per_group <= 64 || tiles(QM_ROWS, 64) <= 148) return {1, 64, 1};
+    const long long w128 = (tiles(2 * QM_ROWS, 128) + 73) / 74, w256 = (tiles(2 * QM_ROWS, 256) + 73) / 74;
+    return {2, per_group <= 128 || 8 * w128 <= 13 * w256 ? 128 : 256, 1};
 }
 
 }  // namespace
@@ -666,31 +687,29 @@ extern "C" int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *a)
                    a->out_stride, a->status, a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : QM_TIMEOUT_NS,
                    (a->flags & MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS) != 0};
     const QmChoice c = choose(p);
-    CUtensorMap map_b, map_a;
-    if (!encode_bytes(&map_b, a->b, b_rows, a->k, sb, QM_ROWS) || !encode_bytes(&map_a, a->a, a->rows, a->k, sa, c.ctas == 2 ? c.tokens / 2 : c.tokens))
-        return MOE_OVL_ERR_CUDA;
+    const QmOperands o = {a->a, a->b, b_rows, sa, sb};
     const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
     return with_dtype(a->out_dtype, [&](auto t) {
         using Out = decltype(t);
         if (c.ctas == 1) {
             switch (c.tokens) {
-            case 16: return launch_tiles<1, 16, Out>(p, map_b, map_a, a->device, stream);
-            case 32: return launch_tiles<1, 32, Out>(p, map_b, map_a, a->device, stream);
-            default: return launch_tiles<1, 64, Out>(p, map_b, map_a, a->device, stream);
+            case 16: return launch_tiles<1, 16, Out>(p, o, a->device, stream);
+            case 32: return launch_tiles<1, 32, Out>(p, o, a->device, stream);
+            default: return launch_tiles<1, 64, Out>(p, o, a->device, stream);
             }
         }
         if (c.ctas == 2) {
             switch (c.tokens) {
-            case 128: return launch_tiles<2, 128, Out>(p, map_b, map_a, a->device, stream);
-            default: return launch_tiles<2, 256, Out>(p, map_b, map_a, a->device, stream);
+            case 128: return launch_tiles<2, 128, Out>(p, o, a->device, stream);
+            default: return launch_tiles<2, 256, Out>(p, o, a->device, stream);
             }
         }
         auto split = [&](auto n) {
             constexpr int BN = decltype(n)::value;
             switch (c.splits) {
-            case 2: return launch_split<BN, 2, Out>(p, map_b, map_a, a->device, stream);
-            case 4: return launch_split<BN, 4, Out>(p, map_b, map_a, a->device, stream);
-            default: return launch_split<BN, 8, Out>(p, map_b, map_a, a->device, stream);
+            case 2: return launch_split<BN, 2, Out>(p, o, a->device, stream);
+            case 4: return launch_split<BN, 4, Out>(p, o, a->device, stream);
+            default: return launch_split<BN, 8, Out>(p, o, a->device, stream);
             }
         };
         switch (c.tokens) {
