@@ -213,9 +213,8 @@ struct NormP {
 
 // The row's sum of squares and the largest |h * weight| come out of ONE reduction: rstd is a positive factor of the whole row,
 // so the scale of the 8-bit output needs no second pass over the normed values.
-// REGS: what a thread may have where it holds 8 values at most (a block of 1024 threads has room for 64).
-template <typename T, typename W, int VEC, int NV, bool RAGGED, int REGS>
-__global__ void __maxnreg__(VEC *NV <= 8 ? REGS : 128) add_norm_kernel(const NormP p)
+template <typename T, typename W, int VEC, int NV, bool RAGGED>
+__device__ __forceinline__ void add_norm_rows(const NormP &p)
 {
     __shared__ float2 buf[2][32];
     const int step = gridDim.x * blockDim.y;
@@ -302,6 +301,12 @@ __global__ void __maxnreg__(VEC *NV <= 8 ? REGS : 128) add_norm_kernel(const Nor
     }
 }
 
+template <typename T, typename W, int VEC, int NV, bool RAGGED>
+__global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_kernel(const NormP p) { add_norm_rows<T, W, VEC, NV, RAGGED>(p); }
+// The same in fewer registers.
+template <typename T, typename W, int VEC, int NV, bool RAGGED>
+__global__ void __maxnreg__(VEC *NV <= 8 ? 40 : 128) add_norm_lean_kernel(const NormP p) { add_norm_rows<T, W, VEC, NV, RAGGED>(p); }
+
 struct NormBackP {
     int rows, d;
     float per_d;
@@ -323,9 +328,8 @@ template <typename T, int VEC, int NV> struct BackFeed {
 // added up in a fixed order by reduce_partials_kernel: no atomics, the same bits every time.  A row is read from shared memory twice, before
 // and after its reduction, so that few registers are in use across the barrier: blocks per SM carry this kernel (12289 x 2048,
 // bf16: 84, 49, 40, 36 us with 1, 2, 3, 4 of them), not how many rows are on their way (one to four: the same).
-// In 64 registers (48, 40: 37, 46 us); ragged rows in 48, where 544 threads fit an SM twice (8000 x 4097: 93 us, in 64 142 us).
 template <typename T, typename W, int VEC, int NV, bool RAGGED>
-__global__ void __maxnreg__(VEC *NV <= 8 ? (RAGGED ? 48 : 64) : 128) add_norm_backward_kernel(const NormBackP p)
+__device__ __forceinline__ void add_norm_backward_rows(const NormBackP &p)
 {
     constexpr bool FED = BackFeed<T, VEC, NV>::ON;
     __shared__ float buf[2][32];
@@ -456,6 +460,13 @@ __global__ void __maxnreg__(VEC *NV <= 8 ? (RAGGED ? 48 : 64) : 128) add_norm_ba
         }
     }
 }
+
+// In up to 64 registers (48, 40: 37, 46 us).
+template <typename T, typename W, int VEC, int NV>
+__global__ void __launch_bounds__(max_threads(VEC *NV)) add_norm_backward_kernel(const NormBackP p) { add_norm_backward_rows<T, W, VEC, NV, false>(p); }
+// Ragged rows in 48, where 544 threads fit an SM twice (8000 x 4097: 93 us, in 64 142 us).
+template <typename T, typename W, int VEC, int NV>
+__global__ void __maxnreg__(VEC *NV <= 8 ? 48 : 128) add_norm_backward_ragged_kernel(const NormBackP p) { add_norm_backward_rows<T, W, VEC, NV, true>(p); }
 
 // dweight[c] = sum of the partial rows: 32 columns per block, each by 32 threads with several loads in flight and then in one
 // tree -- a fixed order.
@@ -704,7 +715,7 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
                 constexpr int NV = decltype(n)::value;
                 // An 8-bit output alone: blocks per SM count (16384 x 4096: 72 us in 40 registers, 80 us in 64).  With an output in the type of x the
                 // writes are what bounds it, and fewer blocks write better (87 us in 64, 92 us in 40).
-                const auto kernel = p.q && !p.y ? add_norm_kernel<T, W, VEC, NV, RAGGED, 40> : add_norm_kernel<T, W, VEC, NV, RAGGED, 64>;
+                const auto kernel = p.q && !p.y ? add_norm_lean_kernel<T, W, VEC, NV, RAGGED> : add_norm_kernel<T, W, VEC, NV, RAGGED>;
                 return launch_rows(kernel, p, s, RAGGED, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
@@ -769,7 +780,10 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
                 constexpr int NV = decltype(n)::value;
                 int blocks = 0;
                 static std::atomic<int> allowed[64];
-                const int rc = launch_backward<VEC, NV, T>(add_norm_backward_kernel<T, W, VEC, NV, RAGGED>, allowed, p, s, RAGGED, a->device, stream, blocks);
+                void (*kernel)(NormBackP);
+                if constexpr (RAGGED) kernel = add_norm_backward_ragged_kernel<T, W, VEC, NV>;
+                else kernel = add_norm_backward_kernel<T, W, VEC, NV>;
+                const int rc = launch_backward<VEC, NV, T>(kernel, allowed, p, s, RAGGED, a->device, stream, blocks);
                 if (rc != MOE_OVL_OK || !p.partial) return rc;
                 reduce_partials_kernel<<<(p.d + 31) / 32, dim3(32, 32), 0, stream>>>(p.partial, blocks, p.d, a->dweight);
                 return launched();
