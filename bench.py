@@ -40,8 +40,8 @@ FALLBACK_PEAKS = {"hbm_gbs": 6650.0, "bf16_tflops": 1590.0, "bf16_tflops_sustain
 # ncu capture; valid only for the kernel source it was taken from (sha1 of csrc/producer.cuh, first 12 digits).
 # A changed kernel makes the figure stale: it is then reported as null with the reason.
 NCU_PRODUCER_TRAFFIC = {
-    "mixtral": {"bytes": 2770726000 + 382985984, "kernel_sha1": "925db34cd702",
-                "capture": "ncu --set full, one launch of the GEMM kernel at full size, non-overlap mode"},
+    "mixtral": {"bytes": 2777206000 + 382403328, "kernel_sha1": "b43f127217fa",
+                "capture": "ncu (DRAM bytes, one pass), one launch of the GEMM kernel at full size, non-overlap mode"},
 }
 PREHEAT_S = 1.0      # untimed steps before the timed ones, so that the timed steps see the GPU's sustained state
 
