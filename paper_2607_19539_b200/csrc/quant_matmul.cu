@@ -135,6 +135,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     const int row_tile = (int)(tile_index % (unsigned)p.row_tiles);
 
     if (warp == 0) {
+        after_previous();
         const QmTile t = find_tile(p, (int)(tile_index / (unsigned)p.row_tiles), BN, count_of(p, lane), lane);
         if (lane == 0) s_tile = t;
     } else if (warp == 1) {
@@ -148,7 +149,9 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tc_fence_before();
+    after_previous();
     __syncthreads();
+    may_follow();
     tc_fence_after();
     const QmTile tile = {uniform(s_tile.expert), uniform(s_tile.row0), uniform(s_tile.rows)};
     const uint32_t tmem = uniform(s_tmem);
@@ -392,7 +395,6 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     };
 
     if (warp == 0) {
-        const int count = count_of(p, lane);
         static_assert(STAGES <= 27, "a lane per barrier");
         if (lane < STAGES) {
             mbar_init(bar_full + 8 * lane, 1);            // the leader's load thread arrives, expecting all CTAs' bytes
@@ -404,7 +406,8 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         __syncwarp();
-        fill_schedule<TOKENS>(p, s_tile_start, s_row_start, count, lane);
+        after_previous();
+        fill_schedule<TOKENS>(p, s_tile_start, s_row_start, count_of(p, lane), lane);
         loader.leader = elect_one();
         if (CTAS == 1 && !p.no_loads && first < sched.total(experts)) {
             int y_b, y_a;
@@ -417,8 +420,10 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
         else tmem_alloc(smem_u32(&s_tmem), 2 * ACC_COLS);
     }
     tc_fence_before();
+    after_previous();
     __syncthreads();
     if (CTAS == 2) cluster_sync_all();
+    may_follow();
     tc_fence_after();
     const uint32_t tmem = uniform(s_tmem);
     const long long total = sched.total(experts);
@@ -574,23 +579,6 @@ int sm_count(int device)
     return n;
 }
 
-template <typename K>
-int launch(K kernel, unsigned blocks, int threads, int smem, int cluster, const QmP &p, const CUtensorMap &b, const CUtensorMap &a, cudaStream_t stream)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, b, a, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
-}
-
 // The operands as the tensor maps need them.  A map's box and the kernel's tile come from the same constant, in the two functions below.
 struct QmOperands { const void *a, *b; long long b_rows, a_stride, b_stride; };
 
@@ -611,7 +599,7 @@ int launch_split(const QmP &p, const QmOperands &o, int device, cudaStream_t str
     const long long tiles = p.counts ? p.rows / BN + std::min(p.experts, p.rows) : (p.rows + BN - 1) / BN;
     const long long blocks = tiles * p.row_tiles * SPLITS;
     if (blocks > 0x7fffffffll) return MOE_OVL_ERR_UNSUPPORTED;
-    return launch(kernel, (unsigned)blocks, QM_THREADS, QmShape<BN>::SMEM, SPLITS, p, b, a, stream);
+    return launch_behind(kernel, (unsigned)blocks, dim3(QM_THREADS), QmShape<BN>::SMEM, SPLITS, stream, b, a, p);
 }
 
 template <int CTAS, int TOKENS, typename Out>
@@ -622,7 +610,7 @@ int launch_tiles(const QmP &p, const QmOperands &o, int device, cudaStream_t str
     static std::atomic<unsigned long long> allowed{0};
     const auto kernel = quant_matmul_tiles_kernel<CTAS, TOKENS, Out>;
     if (!allow_smem(kernel, QpShape<CTAS, TOKENS>::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
-    return launch(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), QP_THREADS, QpShape<CTAS, TOKENS>::SMEM, CTAS, p, b, a, stream);
+    return launch_behind(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), dim3(QP_THREADS), QpShape<CTAS, TOKENS>::SMEM, CTAS, stream, b, a, p);
 }
 
 template <int N> struct Number { static constexpr int value = N; };

@@ -217,6 +217,8 @@ template <typename T, typename W, int VEC, int NV, bool RAGGED>
 __device__ __forceinline__ void add_norm_rows(const NormP &p)
 {
     __shared__ float2 buf[2][32];
+    after_previous();
+    may_follow();
     const int step = gridDim.x * blockDim.y;
     const W *w = static_cast<const W *>(p.weight);
     int row = blockIdx.x * blockDim.y + threadIdx.y;
@@ -333,6 +335,8 @@ __device__ __forceinline__ void add_norm_backward_rows(const NormBackP &p)
 {
     constexpr bool FED = BackFeed<T, VEC, NV>::ON;
     __shared__ float buf[2][32];
+    after_previous();
+    may_follow();
     float acc[NV * VEC];
 #pragma unroll
     for (int i = 0; i < NV * VEC; ++i) acc[i] = 0.0f;
@@ -521,6 +525,8 @@ template <typename T, int VEC, int NV>
 __global__ void __launch_bounds__(swiglu_threads(VEC *NV)) swiglu_quant_kernel(const SwigluP p)
 {
     __shared__ float buf[2][32];
+    after_previous();
+    may_follow();
     const int step = gridDim.x * blockDim.y;
     int row = blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= p.rows) return;
@@ -609,8 +615,7 @@ template <typename K, typename P> int launch_rows(K kernel, const P &p, const Ro
 {
     const int blocks = whole_steps(resident(kernel, s.threads * s.rows_per_block, 0, (p.rows + s.rows_per_block - 1) / s.rows_per_block, device), s, p.rows, ragged);
     if (blocks < 1) return MOE_OVL_ERR_CUDA;
-    kernel<<<blocks, dim3(s.threads, s.rows_per_block), 0, stream>>>(p);
-    return launched();
+    return launch_behind(kernel, (unsigned)blocks, dim3(s.threads, s.rows_per_block), 0, 1, stream, p);
 }
 
 // `allowed`: whether this kernel has been allowed its shared memory on each device.
@@ -626,8 +631,7 @@ int launch_backward(K kernel, std::atomic<int> *allowed, const NormBackP &p, con
     blocks = resident(kernel, threads, smem, std::min((p.rows + s.rows_per_block - 1) / s.rows_per_block, NORM_PARTIALS), device);
     if (blocks < 1) return MOE_OVL_ERR_CUDA;
     blocks = whole_steps(blocks, s, p.rows, ragged);
-    kernel<<<blocks, dim3(s.threads, s.rows_per_block), smem, stream>>>(p);
-    return launched();
+    return launch_behind(kernel, (unsigned)blocks, dim3(s.threads, s.rows_per_block), smem, 1, stream, p);
 }
 
 template <int N> struct Count { static constexpr int value = N; };
