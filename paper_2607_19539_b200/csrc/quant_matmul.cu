@@ -625,6 +625,9 @@ struct QmChoice { int ctas, tokens, splits; };
 //   up to 64 tokens per expert, or where tiles of 64 fit one wave of the 148 CTAs, single CTAs: 16 experts of 64 tokens 48.4 against 49.4 in
 //     pairs (of 128: 61.1 against 55.8); 256 tokens, n = k = 4096 9.4 against 11.7.  Tiles of 32 where those fit the wave: 64 tokens, n = k = 4096
 //     8.5 against 9.2;
+//   experts' rows are never even, and a second tile reads an expert's weights anew, so their tiles are taken wider, where the mean is above 4
+//     rows (64 experts of 15 rows, the busiest 65, n = 224, k = 3312: 17.6 with tiles of 16, 14.0 of 32, 14.8 of 64; 16 experts of 32, the busiest
+//     158, n = 8192, k = 2048: 49.2 with 32, 45.8 with 64; one row each, n = 5104, k = 3088: 33.4 with 16, 35.7 with 32, 42.9 with 64);
 //   pairs take 128 or 256 tokens, whose tiles cost about 8 : 13: 512 tokens, n = k = 4096 (one wave of the 74 pairs each) 12.2 and 17.2; 2048
 //     tokens (four waves, two) 28.9 and 26.9.
 QmChoice choose(const QmP &p)
@@ -641,6 +644,7 @@ QmChoice choose(const QmP &p)
         while (c.splits < 8 && shared * c.splits * 2 <= 296 && c.splits * 2 <= ksteps && (c.splits < 4 || ksteps >= 64)) c.splits *= 2;
         if (ksteps * (c.splits - 1) * 15 > c.splits * (120 + 3 * std::min(c.tokens, per_group))) return c;
     }
+    if (p.experts && per_group > 4 && per_group <= 64) return {1, per_group <= 16 ? 32 : 64, 1};
     if (per_group <= 16) return {1, 16, 1};
     if (per_group <= 32 || tiles(QM_ROWS, 32) <= 148) return {1, 32, 1};
     if (per_group <= 64 || tiles(QM_ROWS, 64) <= 148) return {1, 64, 1};
