@@ -63,27 +63,31 @@ __device__ __forceinline__ void row_sum_max(float &s, float &m, float2 *buf)
     m = warp_max(lane < (int)(blockDim.x >> 5) ? t.y : 0.0f);
 }
 
-// scale = most / 127 and the factor that takes a value to its 8 bits; a row of (almost) nothing gives zeros.
-__device__ __forceinline__ float2 quant_scale(float most)
+// The scale of a row whose largest magnitude is `most`, and the factor that takes its values to 8 bits; a row of (almost) nothing gives zeros.
+// most / 127 is rounded once: the remainder of a first quotient is exact and brings it to within 2^-22 of a unit in the last place, while no
+// quotient of 24 bits by 127 is nearer than 1/254 of one to the middle between two floats (Brisebarre and Muller, division by a constant).
+__device__ __forceinline__ float quant_scale(float most)
 {
-    if (most < QUANT_TINY) return make_float2(0.0f, 0.0f);
-    return make_float2(most * (1.0f / QUANT_MAX), QUANT_MAX / most);
+    const float first = most * (1.0f / QUANT_MAX), rest = fmaf(-first, QUANT_MAX, most);
+    return most < QUANT_TINY ? 0.0f : most < INFINITY ? fmaf(rest, 1.0f / QUANT_MAX, first) : most;
 }
-// VEC values in 8 bits: v * factor to the nearest whole number, ties to even.  Adding 1.5 * 2^23 rounds to a whole number and leaves it,
-// as two's complement, in the float's low byte (|v * factor| <= 127 (1 + 2^-22): nothing to clamp); the conversion instruction has a
-// fraction of that rate.  A row that holds a NaN or an infinity gives zeros: `keep` is 0 then.
+__device__ __forceinline__ float quant_factor(float most) { return most < QUANT_TINY ? 0.0f : QUANT_MAX / most; }
+// VEC values in 8 bits: v * factor to the nearest whole number, ties to even.  The product is rounded first, as a value of its own: half
+// of a row's largest value then meets 63.5 where the factor is exact, and not one side of it or the other.  Adding 1.5 * 2^23 rounds to a
+// whole number and leaves it, as two's complement, in the float's low byte (|v * factor| <= 127 (1 + 2^-22): nothing to clamp); the
+// conversion instruction has a fraction of that rate.  A row that holds a NaN or an infinity gives zeros: `keep` is 0 then.
 template <int VEC> __device__ __forceinline__ void store_quant(int8_t *q, const float *v, float factor, uint32_t keep)
 {
     if constexpr (VEC == 1) {
-        *q = (int8_t)(__float_as_uint(fmaf(v[0], factor, 12582912.0f)) & keep);
+        *q = (int8_t)(__float_as_uint(__fadd_rn(__fmul_rn(v[0], factor), 12582912.0f)) & keep);
     } else if constexpr (VEC == 2) {
-        const float2 t = fma2(make_float2(v[0], v[1]), both(factor), both(12582912.0f));
+        const float2 t = add2(mul2(make_float2(v[0], v[1]), both(factor)), both(12582912.0f));
         *reinterpret_cast<uint16_t *>(q) = (uint16_t)(__byte_perm(__float_as_uint(t.x), __float_as_uint(t.y), 0x0040) & keep);
     } else {
         uint32_t b[VEC], w[VEC / 4];
 #pragma unroll
         for (int j = 0; j < VEC; j += 2) {
-            const float2 t = fma2(make_float2(v[j], v[j + 1]), both(factor), both(12582912.0f));
+            const float2 t = add2(mul2(make_float2(v[j], v[j + 1]), both(factor)), both(12582912.0f));
             b[j] = __float_as_uint(t.x), b[j + 1] = __float_as_uint(t.y);
         }
 #pragma unroll
@@ -291,11 +295,11 @@ __device__ __forceinline__ void add_norm_rows(const NormP &p)
         }
         if (p.q) {
             int8_t *q = at_row(p.q, row, p.q_stride, c0);
-            most *= rstd;
-            const float2 s = quant_scale(most);
-            if (threadIdx.x == 0) p.scale[row] = s.x;
-            const float factor = rstd * s.y;
-            const uint32_t keep = keep_mask(most);
+            // rstd cancels out of a value over the row's largest
+            const float value = most * rstd;
+            if (threadIdx.x == 0) p.scale[row] = quant_scale(value);
+            const float factor = value < QUANT_TINY ? 0.0f : QUANT_MAX / most;
+            const uint32_t keep = keep_mask(value);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (c0 + i * across < p.d) quant_some<VEC, RAGGED>(q + i * across, v + i * VEC, factor, keep, c0 + i * across, p.d);
@@ -562,13 +566,13 @@ __global__ void __launch_bounds__(swiglu_threads(VEC *NV)) swiglu_quant_kernel(c
         }
         if (row + step < p.rows) load(row + step);
         most = row_max(most, buf[turn]);
-        const float2 s = quant_scale(most);
-        if (threadIdx.x == 0) p.scale[row] = s.x;
+        const float factor = quant_factor(most);
+        if (threadIdx.x == 0) p.scale[row] = quant_scale(most);
         const uint32_t keep = keep_mask(most);
         int8_t *q = at_row(p.q, row, p.q_stride, c0);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (c0 + i * across < p.f) store_quant<VEC>(q + i * across, v + i * VEC, s.y, keep);
+            if (c0 + i * across < p.f) store_quant<VEC>(q + i * across, v + i * VEC, factor, keep);
         }
     }
 }
