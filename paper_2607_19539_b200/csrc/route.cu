@@ -392,7 +392,8 @@ struct RouteBackP {
 //   sigmoid              c dgate_j s_j (1 - s_j)
 //   sigmoid, renormalised w_j (1 - s_j) (c dgate_j - sum c dgate w)
 // Every expert's value is written first, as if it were not chosen, and then the chosen ones' over it.  The softmax over the
-// whole row takes the approximate power of two (relative error about 2^-22 + |l - max| 2^-23).
+// whole row takes the approximate power of two (relative error about 2^-22 + |l - max| 2^-23) of the difference to the row's largest logit:
+// the difference of two logits near each other is exact, wherever in the type's range they lie, while products of theirs need not be finite.
 // Bound by the rows in flight: their loads hang on one another.  At 65521 x 64, bf16, out of HBM, 4 blocks per SM that go from row to
 // row take 11.1 us, a block for every 32 rows 10.0, with 32 registers (8 blocks per SM) 9.1, with the next launch under way 8.2; fewer than 8
 // lanes per row need more registers for their share of the choice.
@@ -437,11 +438,14 @@ __global__ void __launch_bounds__(ROUTE_THREADS, NR == 8 && G >= 8 ? 8 : 1) rout
 #pragma unroll
             for (int r = 0; r < NR; ++r) top = fmaxf(top, l[r] = usable(to_f32(raw[r])));
             top = group_max<G>(top);
-            const float shift = top > -INFINITY ? -top * LOG2E : 0.0f;
+            if (!(top > -INFINITY)) top = 0.0f;             // a row that is masked throughout
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(dense[r]) : "f"(fmaf(l[r], LOG2E, shift)));
+            for (int r = 0; r < NR; r += 2) {
+                const float2 t = mul2(add2(make_float2(l[r], l[r + 1]), both(-top)), both(LOG2E));
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(dense[r]) : "f"(t.x));
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(dense[r + 1]) : "f"(t.y));
                 total += dense[r];
+                total += dense[r + 1];
             }
             total = group_sum<G>(total);
             const float inv = total > 0.0f ? 1.0f / total : 0.0f;
@@ -449,7 +453,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, NR == 8 && G >= 8 ? 8 : 1) rout
             for (int s = 0; s < SLOTS; ++s) {
                 if (s * G >= p.k) continue;
                 float v;
-                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(v) : "f"(fmaf(x[s], LOG2E, shift)));
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(v) : "f"((x[s] - top) * LOG2E));
                 mine[s] = v * inv;
                 dot = fmaf(d[s], mine[s], dot);
             }

@@ -39,3 +39,80 @@ def test_quantised_halves_and_scales(d, dtype):
     assert torch.equal(q.sign(), torch.where(q == 0, 0, x.float().sign()).to(torch.int8))
     most = power.squeeze(1) * rstd                          # exact: a power of two
     assert torch.equal(scale, (most.double() / 127).float())
+
+
+def usable64(logits):
+    """Logits as the router uses them, in 64 bits: +inf is the largest finite value, NaN is -inf."""
+    z = logits.double()
+    return torch.where(z.isnan(), -math.inf, z).clamp_max(3.4028234663852886e38)
+
+
+@gpu
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("e,k", [(40, 6), (5, 2), (300, 8), (1024, 4)])
+def test_route_gradient_of_rows_at_the_ends_of_the_type(e, k, dtype, score, renorm):
+    """Rows that a mask fills with the type's lowest value, far-away rows, ties of infinities, rows with nothing left."""
+    g = gen(e + k)
+    low, inf = torch.finfo(dtype).min, math.inf
+    far = -1e4 if dtype is F16 else -1e10
+    z = normal(g, (16, e), dtype)
+    z[0] = low
+    z[1] = far
+    z[2, 1] = z[2, 3] = inf
+    z[3] = -inf
+    z[4] = float("nan")
+    z[5, 2:] = low
+    z[6, 2:] = -inf
+    z[7] = -low
+    z[8] = -far
+    z[9] = far + normal(g, (e,), F32, abs(far) * 1e-2).to(dtype)
+    z[10, ::2] = low
+    z[11, 4] = -low
+    z[12, 0] = inf
+    z[12, 1:] = -inf
+    expert, gate, _ = call_route(z, k, score=score, renorm=renorm)
+    assert bool(gate.isfinite().all())
+    dgate = torch.randn((16, k), generator=g, device="cuda")
+    out = torch.empty_like(z)
+    ops.moe_ovl_route_backward(logits=z, expert=expert, dgate=dgate, dlogits=out, score=ops.SCORES[score], renormalise=renorm)
+    # the definition, with rows that are masked throughout giving 0
+    u = usable64(z)
+    live = expert >= 0
+    at = expert.long().clamp_min(0)
+    if score == "softmax":
+        top = u.amax(1, keepdim=True)
+        p = torch.where(u > -inf, torch.exp(u - torch.where(top > -inf, top, 0.0)), 0.0)
+        total = p.sum(1, keepdim=True)
+        p = torch.where(total > 0, p / total, 0.0)
+        slope = torch.ones_like(p)
+    else:
+        p, slope = torch.sigmoid(u), torch.sigmoid(-u)
+    s, d = torch.where(live, p.gather(1, at), 0.0), dgate.double()
+    if renorm:
+        if score == "softmax":                              # of the chosen logits
+            c = torch.where(live, u.gather(1, at), -inf)
+            top = c.amax(1, keepdim=True)
+            s = torch.where(c > -inf, torch.exp(c - torch.where(top > -inf, top, 0.0)), 0.0)
+        # scores that 32 bits do not hold are 0, and gates of a row without a sum are 0
+        s = torch.where(s < 2.0 ** -126, 0.0, s)
+        total = s.sum(1, keepdim=True)
+        s = torch.where(total > 0, s / total, 0.0)
+    dot = (d * s).sum(1, keepdim=True) if renorm or score == "softmax" else 0.0
+    mine = s * (d - dot) * slope.gather(1, at)
+    want = torch.where(live, mine, 0.0)
+    dense = torch.zeros_like(u)
+    if score == "softmax" and not renorm:
+        dense = -p * dot
+    for j in range(k):
+        rows = live[:, j].nonzero().squeeze(1)
+        dense[rows, at[rows, j]] = want[rows, j]
+    size = (d.abs() * s).sum(1, keepdim=True)
+    bound = 1e-5 * (p * size if score == "softmax" and not renorm else torch.zeros_like(p))
+    reach = 1e-5 * s * (d.abs() + size) * slope.gather(1, at)
+    for j in range(k):
+        rows = live[:, j].nonzero().squeeze(1)
+        bound[rows, at[rows, j]] += reach[rows, j]
+    assert bool(out.isfinite().all())
+    close(out, dense, U[dtype] * dense.abs() + bound + FLOOR[dtype] + 1e-37)   # 1e-37: scores below the normal range
