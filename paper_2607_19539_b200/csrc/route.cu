@@ -470,8 +470,10 @@ __global__ void __launch_bounds__(ROUTE_THREADS, NR == 8 && G >= 8 ? 8 : 1) rout
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s) {
                 if (s * G >= p.k) continue;
-                mine[s] = p.sigmoid ? (x[s] > -INFINITY ? sigmoid_of(x[s]) : 0.0f) : exp_from(x[s], most);
-                slope[s] = p.sigmoid ? 1.0f - mine[s] : 1.0f;
+                const float t = expf(p.sigmoid ? -x[s] : x[s] - most);
+                mine[s] = x[s] > -INFINITY ? (p.sigmoid ? 1.0f / (1.0f + t) : t) : 0.0f;
+                // 1 - s as exp(-l) s: the difference loses its digits where s is near 1
+                slope[s] = p.sigmoid && mine[s] > 0.0f ? t * mine[s] : 1.0f;
                 sum += mine[s];
             }
             if (p.renormalise) {

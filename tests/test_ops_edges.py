@@ -116,3 +116,30 @@ def test_route_gradient_of_rows_at_the_ends_of_the_type(e, k, dtype, score, reno
         bound[rows, at[rows, j]] += reach[rows, j]
     assert bool(out.isfinite().all())
     close(out, dense, U[dtype] * dense.abs() + bound + FLOOR[dtype] + 1e-37)   # 1e-37: scores below the normal range
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_route_sigmoid_gradient_of_large_logits(dtype, renorm):
+    """s (1 - s) of logits from -30 to 30 to its own relative accuracy.  Both factors come of one exp to 2 ulp, a sum, a quotient and a product; with
+    the quotient by the sum of up to 8 scores, the sum over them and four products less than 60 roundings of 2^-24 = 3.6e-6, of the
+    magnitudes (1 - s) w (|d| + sum |d| w); 1e-5 as in test_ops."""
+    g = gen(13)
+    for e, k in ((5, 2), (64, 8), (300, 4)):
+        z = ((torch.rand((50, e), generator=g, device="cuda") * 60 - 30)).to(dtype)
+        expert = torch.stack([torch.randperm(e, generator=g, device="cuda")[:k] for _ in range(50)]).to(torch.int32)
+        dgate = torch.randn((50, k), generator=g, device="cuda")
+        out = torch.empty_like(z)
+        ops.moe_ovl_route_backward(logits=z, expert=expert, dgate=dgate, dlogits=out, score=ops.SCORE_SIGMOID, renormalise=renorm)
+        at, d = expert.long(), dgate.double()
+        l = z.double().gather(1, at)
+        w, slope = torch.sigmoid(l), torch.sigmoid(-l)
+        dot = size = torch.zeros((50, 1), dtype=torch.float64, device="cuda")
+        if renorm:
+            w = w / w.sum(1, keepdim=True)
+            dot, size = (w * d).sum(1, keepdim=True), (w * d).abs().sum(1, keepdim=True)
+        want, bound = torch.zeros_like(z, dtype=torch.float64), torch.zeros_like(z, dtype=torch.float64)
+        want.scatter_(1, at, w * (d - dot) * slope)
+        bound.scatter_(1, at, w * (d.abs() + size) * slope)
+        close(out, want, U[dtype] * want.abs() + 1e-5 * bound + 1e-37)
