@@ -143,3 +143,21 @@ def test_route_sigmoid_gradient_of_large_logits(dtype, renorm):
         want.scatter_(1, at, w * (d - dot) * slope)
         bound.scatter_(1, at, w * (d.abs() + size) * slope)
         close(out, want, U[dtype] * want.abs() + 1e-5 * bound + 1e-37)
+
+
+@gpu
+def test_route_gradient_of_a_softmax_in_32_bits():
+    """Two experts far apart, the nearer one chosen: dlogits of the other is -s0 s1 d with s0 = exp(l0 - l1) to 2 ulp (2.4e-7), s1 = 1 and at most six
+    roundings of 2^-24 (3.6e-7); 8e-7.  The difference is exact: both logits are multiples of 1/8."""
+    rows = 640
+    z = torch.zeros((rows, 2), device="cuda")
+    z[:, 0] = -torch.arange(rows, device="cuda") / 8
+    expert = torch.ones((rows, 1), dtype=torch.int32, device="cuda")
+    dgate = 1 + torch.rand((rows, 1), generator=gen(3), device="cuda")
+    out = torch.empty_like(z)
+    ops.moe_ovl_route_backward(logits=z, expert=expert, dgate=dgate, dlogits=out, renormalise=False)
+    p = torch.softmax(z.double(), 1)
+    far = p[:, 0] < 2.0 ** -25                              # there s1 rounds to 1
+    want = -p[:, 0] * p[:, 1] * dgate.double()[:, 0]
+    close(out[far, 0], want[far], 8e-7 * want[far].abs())
+    close(out[far, 1], -want[far], 1.2e-7 * dgate.double()[far, 0])
