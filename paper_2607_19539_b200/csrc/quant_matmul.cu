@@ -100,11 +100,12 @@ template <int BN> struct QmShape {
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
 };
 
-// A give-up leaves copies in flight: they have to land before the CTA's shared memory goes.  Bounded.
-__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
+// A wait that gives up, in whichever warp, leaves tile copies and matrix instructions under way: they have to land before the CTA's shared and
+// tensor memory go to somebody else.  This wait has a limit of its own, which neither a caller's short one nor an aborted status shortens.
+constexpr unsigned long long QM_LANDING_NS = 2000000000ull;
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long since)
 {
-    const unsigned long long t0 = globaltimer_ns();
-    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 < limit_ns) {}
+    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - since < QM_LANDING_NS) {}
 }
 
 // A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
@@ -126,7 +127,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     constexpr int STAGES = QmShape<BN>::STAGES, STAGE_BYTES = QmShape<BN>::STAGE_BYTES, TMEM_COLS = BN < 32 ? 32 : BN;
     extern __shared__ uint8_t smem_raw[];
     __shared__ QmTile s_tile;
-    __shared__ uint32_t s_tmem;
+    __shared__ uint32_t s_tmem, s_gave_up;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar_full = smem_base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES, bar_done = bar_empty + 8 * STAGES;
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
@@ -146,6 +147,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
             mbar_init(bar_empty + 8 * i, 1);
         }
         mbar_init(bar_done, 1);
+        s_gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tc_fence_before();
@@ -157,13 +159,13 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     const uint32_t tmem = uniform(s_tmem);
     const int steps_all = (p.k + QM_K - 1) / QM_K;
     const int k0 = steps_all * rank / SPLITS, k1 = steps_all * (rank + 1) / SPLITS;
+    int issued = 0;                         // warp 0: stages
     if (tile.rows > 0) {
         if (warp == 0 && !p.no_loads) {
             const bool leader = elect_one();
             const int y_b = tile.expert * p.n + row_tile * QM_ROWS;
             int stage = 0;
             uint32_t phase = 0;
-            int issued = 0;
             for (int k = k0; k < k1; ++k, ++issued) {
                 if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, k))) break;
                 const uint32_t sa = smem_base + stage * STAGE_BYTES;
@@ -174,17 +176,16 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
                 }
                 if (++stage == STAGES) stage = 0, phase ^= 1u;
             }
-            if (issued < k1 - k0) {
-                // gave up
-                for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
-                    drain(bar_full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, p.timeout_ns);
-            }
+            if (issued < k1 - k0) s_gave_up = 1;
         } else if (warp == 1) {
             const bool leader = elect_one();
             int stage = 0;
             uint32_t phase = 0;
             for (int k = k0; k < k1; ++k) {
-                if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k))) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k))) {
+                    s_gave_up = 1;
+                    break;
+                }
                 tc_fence_after();
                 const uint32_t sa = smem_base + stage * STAGE_BYTES;
                 if (leader) {
@@ -200,9 +201,18 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
         }
     }
     __syncwarp();
+    // scales of this lane's channel and of tokens `lane`, `lane` + 32, ..: here before they are needed
+    const int own = (warp - 2) * 32 + lane, ch = row_tile * QM_ROWS + own;
+    float b_scale = 0.0f, a_scale[(BN + 31) / 32] = {};
+    if (tile.rows > 0 && warp >= 2) {
+        if (ch < p.n) b_scale = p.b_scale[(long long)tile.expert * p.n + ch];
+#pragma unroll
+        for (int i = 0; i < (BN + 31) / 32; ++i)
+            if (i * 32 + lane < tile.rows) a_scale[i] = p.a_scale[tile.row0 + i * 32 + lane];
+    }
     if (tile.rows > 0) {
         // everybody waits: nothing of the pipeline is in use behind this point, and its memory can hold the parts
-        warp_wait(bar_done, 0, p, tile.row0, lane);
+        if (!warp_wait(bar_done, 0, p, tile.row0, lane)) s_gave_up = 1;
         tc_fence_after();
     }
     if (tile.rows > 0 && warp >= 2) {
@@ -220,15 +230,13 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     __syncwarp();
     cluster_sync_all();
     if (tile.rows > 0 && warp >= 2) {
-        const int c = (warp - 2) * 32 + lane, ch = row_tile * QM_ROWS + c;
-        const float bs = ch < p.n ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
         // the parts of two tokens at a time: 2 * SPLITS loads in flight
         for (int t = 2 * rank; t < tile.rows; t += 2 * SPLITS) {
             uint32_t part[2][SPLITS];
             const bool two = t + 1 < tile.rows;
 #pragma unroll
             for (int s = 0; s < SPLITS; ++s) {
-                const uint32_t at = map_to_cta(smem_base + 4u * (uint32_t)(t * QM_ROWS + c), (uint32_t)s);
+                const uint32_t at = map_to_cta(smem_base + 4u * (uint32_t)(t * QM_ROWS + own), (uint32_t)s);
                 part[0][s] = ld_shared_cluster_u32(at);
                 part[1][s] = two ? ld_shared_cluster_u32(at + 4u * QM_ROWS) : 0u;
             }
@@ -238,10 +246,14 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
                 sum[0] += part[0][s];
                 sum[1] += part[1][s];
             }
+            float mine = a_scale[0];
+#pragma unroll
+            for (int i = 1; i < (BN + 31) / 32; ++i) mine = t >= 32 * i ? a_scale[i] : mine;
+            const float a0 = __shfl_sync(0xffffffffu, mine, t & 31), a1 = __shfl_sync(0xffffffffu, mine, (t + 1) & 31);
             if (ch < p.n) {
                 Out *out = static_cast<Out *>(p.out) + (long long)(tile.row0 + t) * p.out_stride + ch;
-                store_scaled(out, (int)sum[0], p.a_scale[tile.row0 + t], bs);
-                if (two) store_scaled(out + p.out_stride, (int)sum[1], p.a_scale[tile.row0 + t + 1], bs);
+                store_scaled(out, (int)sum[0], a0, b_scale);
+                if (two) store_scaled(out + p.out_stride, (int)sum[1], a1, b_scale);
             }
         }
     }
@@ -249,6 +261,16 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     cluster_sync_all();                                 // the parts stay until everybody has read them
     tc_fence_before();
     __syncthreads();
+    if (s_gave_up) {
+        if (threadIdx.x == 0) {
+            // the last fill of every stage, and the matrix instructions
+            const unsigned long long t0 = globaltimer_ns();
+            for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
+                drain(bar_full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, t0);
+            drain(bar_done, 0, t0);
+        }
+        __syncthreads();
+    }
     tc_fence_after();
     if (warp == 1) tmem_dealloc_self(tmem, TMEM_COLS);
 }
@@ -318,15 +340,16 @@ template <int TOKENS> __device__ __forceinline__ void fill_schedule(const QmP &p
 template <int CTAS, int TOKENS> struct QpLoader {
     using Shape = QpShape<CTAS, TOKENS>;
     uint32_t smem_base, bar_full, bar_empty, lead_full;
-    int rank, stage = 0, issued = 0;         // issued: no further than a whole ring
-    uint32_t phase = 0;
+    int rank, stage = 0;
+    uint32_t phase = 0, issued = 0;          // issued: stages, all in all
     bool leader;
-    // Issues stages k .. k1 - 1 of a tile; false: a wait gave up.  FRESH: the stages have never been used.
+    // Issues stages k0 .. k1 - 1 of a tile; false: a wait gave up.  FRESH: the stages have never been used.
     template <bool FRESH>
-    __device__ __forceinline__ bool run(const QmP &p, const CUtensorMap &map_b, const CUtensorMap &map_a, int y_b, int y_a, int k, int k1)
+    __device__ __forceinline__ bool run(const QmP &p, const CUtensorMap &map_b, const CUtensorMap &map_a, int y_b, int y_a, int k0, int k1)
     {
+        int k = k0;
         for (; k < k1; ++k) {
-            if (!FRESH && !__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, y_b))) return false;
+            if (!FRESH && !__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, y_b))) break;
             const uint32_t sa = smem_base + stage * Shape::STAGE_BYTES;
             if (leader) {
                 if (CTAS == 1) {
@@ -340,23 +363,29 @@ template <int CTAS, int TOKENS> struct QpLoader {
                 }
             }
             if (++stage == Shape::STAGES) stage = 0, phase ^= 1u;
-            if (issued < Shape::STAGES) ++issued;
         }
-        return true;
-    }
-    // After a give-up: the copies still in flight have to land.
-    __device__ void drain_all(const QmP &p)
-    {
-        // the last fills, newest first: the phase of a stage's last fill ends when it has landed
-        int s = stage;
-        uint32_t ph = phase;
-        for (int i = 0; i < issued; ++i) {
-            if (s == 0) s = Shape::STAGES, ph ^= 1u;
-            --s;
-            drain(bar_full + 8 * s, ph, p.timeout_ns);
-        }
+        issued += (uint32_t)(k - k0);
+        return k == k1;
     }
 };
+
+// After a give-up: waits for the copies that are under way, by one thread of the CTA whose barriers count them.  `mine`, `peers`: stages that
+// this CTA and (in a pair) the other one have issued; they are at most a ring apart, since neither refills a stage that the other has
+// not filled.  A fill of one side alone counts that side's bytes alone: the other side's are taken off, or, where this CTA's thread has not
+// announced the fill, half of the usual number is announced.
+template <int CTAS, int TOKENS> __device__ void await_copies(uint32_t bar_full, uint32_t mine, uint32_t peers)
+{
+    using Shape = QpShape<CTAS, TOKENS>;
+    constexpr uint32_t STAGES = Shape::STAGES;
+    const uint32_t last = CTAS == 1 ? mine : max(mine, peers);
+    const unsigned long long t0 = globaltimer_ns();
+    for (uint32_t i = last > STAGES ? last - STAGES : 0; i < last; ++i) {
+        const uint32_t bar = bar_full + 8 * (i % STAGES);
+        if (CTAS == 2 && i >= peers) mbar_complete_tx(bar, Shape::STAGE_BYTES);
+        else if (CTAS == 2 && i >= mine) mbar_arrive_expect_tx(bar, Shape::STAGE_BYTES);
+        drain(bar, (i / STAGES) & 1u, t0);
+    }
+}
 
 // Persistent, one CTA per SM.
 // CTAS = 2: pairs of CTAs share every matrix instruction (cta_group::2), 256 channels x TOKENS tokens, each CTA holding
@@ -374,6 +403,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     extern __shared__ uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
     __shared__ uint32_t s_tmem;
+    __shared__ uint32_t s_gave_up, s_issued[2];      // a wait for operands or room ran out, here or in the peer; rank 0: stages that each CTA has issued
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar_full = smem_base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES;
     const uint32_t bar_tfull = bar_empty + 8 * STAGES, bar_tempty = bar_tfull + 16, bar_drain = bar_tempty + 16;
@@ -394,6 +424,11 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
         y_a = uniform(tile.row0 + (int)rank * ((tile.rows + 31) / 32 * 16));
     };
 
+    auto gave_up = [&]() {
+        s_gave_up = 1;
+        if (CTAS == 2) st_shared_cluster_u32(map_to_cta(smem_u32(&s_gave_up), rank ^ 1u), 1);
+    };
+
     if (warp == 0) {
         static_assert(STAGES <= 27, "a lane per barrier");
         if (lane < STAGES) {
@@ -405,6 +440,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
             mbar_init(i < 2 ? bar_tfull + 8 * i : i < 4 ? bar_tempty + 8 * (i - 2) : bar_drain, i < 2 || i == 4 ? 1 : 8 * CTAS);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (lane == 0) s_gave_up = 0;
         __syncwarp();
         after_previous();
         fill_schedule<TOKENS>(p, s_tile_start, s_row_start, count_of(p, lane), lane);
@@ -436,7 +472,11 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
                 ok = loader.template run<false>(p, map_b, map_a, y_b, y_a, early, ksteps);
                 early = 0;
             }
-            if (!ok && rank == 0) loader.drain_all(p);      // the peer stays until the cluster barrier at the end
+        }
+        if (lane == 0) {
+            if (rank == 0) s_issued[0] = loader.issued;
+            else st_shared_cluster_u32(map_to_cta(smem_u32(&s_issued[1]), 0), loader.issued);
+            if (!ok) gave_up();
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -475,9 +515,10 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
             }
             if (leader) {
                 if (CTAS == 1) umma_commit_one(bar_drain);      // every MMA has finished before tensor memory goes
-                else umma_commit_self(bar_drain);
+                else umma_commit_pair(bar_drain);
             }
-            drain(bar_drain, 0, p.timeout_ns);
+            drain(bar_drain, 0, globaltimer_ns());
+            if (!ok && lane == 0) gave_up();
         }
         __syncwarp();
     } else {
@@ -519,6 +560,15 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     tc_fence_before();
     __syncthreads();
     if (CTAS == 2) cluster_sync_all();          // the peer no longer signals this CTA's barriers or reads its operands
+    if (s_gave_up) {
+        // but copies may be under way, which rank 0's barriers count for both, and matrix instructions' signals to rank 1
+        if (threadIdx.x == 0) {
+            if (rank == 0) await_copies<CTAS, TOKENS>(bar_full, s_issued[0], s_issued[CTAS - 1]);
+            else drain(bar_drain, 0, globaltimer_ns());
+        }
+        __syncthreads();
+        if (CTAS == 2) cluster_sync_all();
+    }
     tc_fence_after();
     if (warp == 1) {
         if (CTAS == 1) tmem_dealloc_self(tmem, 2 * ACC_COLS);

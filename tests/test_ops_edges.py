@@ -161,3 +161,32 @@ def test_route_gradient_of_a_softmax_in_32_bits():
     want = -p[:, 0] * p[:, 1] * dgate.double()[:, 0]
     close(out[far, 0], want[far], 8e-7 * want[far].abs())
     close(out[far, 1], -want[far], 1.2e-7 * dgate.double()[far, 0])
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k,counts", [(3, 1000, 2048, None), (1, 512, 8192, None), (20, 256, 512, [10, 10]), (64, 4096, 4096, None), (700, 1024, 512, None),
+                                          (300, 512, 512, [100, 0, 200]), (5, 28672, 1024, None), (2048, 4096, 4096, None), (1200, 2048, 2048, [900, 300])])
+def test_quant_matmul_waits_that_give_up_with_copies_under_way(m, n, k, counts):
+    """Calls whose waits give up at once, because their status says so already or because of a limit of 1 us, between calls that have to be
+    right: a kernel that gave up leaves when its copies have landed, so the next one's shared and tensor memory is its own."""
+    g = gen(m + n)
+    e = 1 if counts is None else len(counts)
+    a, b = make8(g, (m, k)), make8(g, (e, n, k))
+    sa, sb = torch.rand(m, generator=g, device="cuda") * 1e-3, torch.rand((e, n), generator=g, device="cuda")
+    dc = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+    want, clear = torch.empty((m, n), dtype=BF16, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    call = lambda out, status, **kw: ops.moe_ovl_quant_matmul(a=a, a_scale=sa, b=b, b_scale=sb, out=out, expert_counts=dc, status=status, **kw)  # noqa: E731
+    call(want, clear)
+    full = torch.full((m + 2, n), 7.5, dtype=BF16, device="cuda")
+    out = torch.empty_like(want)
+    for turn in range(12):
+        aborted = torch.tensor([0, 1, 0, 0], dtype=torch.int32, device="cuda")
+        call(full[1:m + 1], aborted)
+        call(out, clear)
+        assert torch.equal(out, want)
+        late = torch.zeros(4, dtype=torch.int32, device="cuda")
+        call(full[1:m + 1], late, wait_timeout_us=1)
+        call(out, clear)
+        assert torch.equal(out, want) and int(late[0]) in (0, B.ERR_TIMEOUT)
+        assert bool((full[0] == 7.5).all()) and bool((full[m + 1] == 7.5).all())
+    assert not clear.any()
