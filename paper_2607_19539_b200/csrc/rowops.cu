@@ -577,12 +577,15 @@ __global__ void __launch_bounds__(swiglu_threads(VEC *NV)) swiglu_quant_kernel(c
     }
 }
 
+// Packs of VEC elements that a row can touch wherever it begins.
+template <int VEC> int ragged_packs(int width) { return (width + 2 * (VEC - 1)) / VEC; }
+
 // How a row of `width` elements is spread: threads per row, packs per thread, rows per block.
 struct RowShape { int threads, packs, rows_per_block; };
 
 template <int VEC> RowShape row_shape(int rows, int width, int want_values, int (*most_threads)(int), bool ragged = false)
 {
-    const int packs = (width + VEC - 1 + (ragged ? VEC - 1 : 0)) / VEC;
+    const int packs = ragged ? ragged_packs<VEC>(width) : (width + VEC - 1) / VEC;
     // few rows leave SMs idle whatever the block is: the latency of one row counts, so a thread takes few values
     const int want = rows <= 296 ? 8 : want_values;
     auto threads = [&](int n) { return ((packs + n - 1) / n + 31) / 32 * 32; };
@@ -654,10 +657,12 @@ template <int VEC, typename F> int with_packs(int packs, F f)
     return MOE_OVL_ERR_UNSUPPORTED;
 }
 
-// Calls f with the packs that the matrices allow, and whether rows are ragged in them: 16 bytes, or one element.
-template <typename T, typename F> int with_ragged(bool wide, bool ragged, F f)
+// Calls f with the packs that the matrices allow, and whether rows are ragged in them: 16 bytes, or one element.  The widest rows fill a
+// block's registers (512 threads of 64 elements) and leave no room for the one pack more that a ragged row can touch.
+template <typename T, typename F> int with_ragged(bool wide, bool ragged, int width, F f)
 {
     constexpr int VEC = 16 / (int)sizeof(T);
+    if (ragged_packs<VEC>(width) * VEC > MOE_OVL_MAX_ROW) ragged = false;
     if (wide) return f(Count<VEC>(), Count<0>());
     if (ragged) return f(Count<VEC>(), Count<1>());
     return f(Count<1>(), Count<0>());
@@ -727,7 +732,7 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
                 return launch_rows(kernel, p, s, RAGGED, a->device, static_cast<cudaStream_t>(a->stream));
             });
         };
-        return with_ragged<T>(fits(16 / es), agree(16 / es), [&](auto v, auto r) {
+        return with_ragged<T>(fits(16 / es), agree(16 / es), a->d, [&](auto v, auto r) {
             return a->weight_dtype == a->dtype ? launch(T(), v, r) : launch(0.0f, v, r);
         });
     });
@@ -797,7 +802,7 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
                 return launched();
             });
         };
-        return with_ragged<T>(fits(16 / es), agree(16 / es), [&](auto v, auto r) {
+        return with_ragged<T>(fits(16 / es), agree(16 / es), a->d, [&](auto v, auto r) {
             return a->weight_dtype == a->dtype ? launch(T(), v, r) : launch(0.0f, v, r);
         });
     });

@@ -190,3 +190,32 @@ def test_quant_matmul_waits_that_give_up_with_copies_under_way(m, n, k, counts):
         assert torch.equal(out, want) and int(late[0]) in (0, B.ERR_TIMEOUT)
         assert bool((full[0] == 7.5).all()) and bool((full[m + 1] == 7.5).all())
     assert not clear.any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("d,pad", [(32761, 0), (32762, 0), (32765, 0), (32766, 0), (32767, 0), (32768, 1), (32768, 9), (32763, 5)])
+def test_norm_and_gradient_of_the_widest_rows_that_begin_anywhere(d, pad, dtype):
+    """Aligned bases, rows that are no multiple of 16 bytes apart, up to the widest: each row can touch one pack more than it fills."""
+    g = gen(d + pad)
+    for rows in (3, 310):
+        wide = lambda t=dtype: torch.full((rows, d + pad), 7, dtype=t, device="cuda")  # noqa: E731
+        x, r, h, y, q, dy, dx = wide(), wide(), wide(), wide(), wide(torch.int8), wide(), wide()
+        cut = lambda m: m[:, :d]  # noqa: E731
+        scale, rstd, dw = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(d, device="cuda")
+        for m in (x, r, dy):
+            cut(m).copy_(normal(g, (rows, d), dtype))
+        w = normal(g, (d,), dtype) + 1
+        ops.moe_ovl_add_norm(x=cut(x), residual=cut(r), weight=w, residual_out=cut(h), y=cut(y), q=cut(q), scale=scale, rstd=rstd)
+        assert torch.equal(cut(h), (cut(x).float() + cut(r).float()).to(dtype))
+        v, rs = norm64(cut(h), w, 1e-6)
+        close(rstd, rs, 4e-6 * rs)
+        close(cut(y), v, (U[dtype] + 6e-6) * v.abs() + FLOOR[dtype])
+        close(cut(q).double() * scale.double()[:, None], v, 0.502 * v.abs().amax(1, keepdim=True) / 127)
+        ws = torch.empty(ops.moe_ovl_add_norm_workspace_bytes(rows, d), dtype=torch.uint8, device="cuda")
+        ops.moe_ovl_add_norm_backward(dy=cut(dy), h=cut(h), weight=w, rstd=rstd, d_residual=cut(r), dx=cut(dx), dweight=dw, workspace=ws)
+        want, dw_want, size, dw_size = norm_backward64(cut(dy), cut(h), w, rstd, cut(r))
+        close(cut(dx), want, U[dtype] * want.abs() + 1e-5 * size + FLOOR[dtype])
+        close(dw, dw_want, 1e-5 * dw_size + 1e-30)
+        for m in (h, y, q, dx):
+            assert pad == 0 or bool((m[:, d:] == 7).all())
