@@ -255,7 +255,7 @@ def moe_ovl_quant_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=N
     sa = _matrix(where, "a", a, a.shape, torch.int8, dev)
     if b.shape[-1] != k or b.dtype is not torch.int8 or b.get_device() != dev or b.stride(-1) != 1:
         _refuse(where, f"b has to be [..., {n}, {k}] int8 on cuda:{dev} with its columns next to each other")
-    sb = b.stride(-2)
+    sb = b.stride(0) if n == 1 and experts > 1 else b.stride(-2)        # one channel each: the experts are the rows
     if sb < k or (experts > 1 and b.stride(0) != n * sb):
         _refuse(where, "the rows of b have to lie at one distance, across experts too")
     dt = _dtype(where, "out", out)

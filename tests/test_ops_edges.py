@@ -219,3 +219,13 @@ def test_norm_and_gradient_of_the_widest_rows_that_begin_anywhere(d, pad, dtype)
         close(dw, dw_want, 1e-5 * dw_size + 1e-30)
         for m in (h, y, q, dx):
             assert pad == 0 or bool((m[:, d:] == 7).all())
+
+
+@gpu
+def test_quant_matmul_one_channel_of_every_expert():
+    """Experts of one channel each, cut out of larger ones: the distance of their rows is the experts'."""
+    g = gen(21)
+    a, whole = make8(g, (60, 64)), make8(g, (6, 10, 64))
+    sa, sb = torch.rand(60, generator=g, device="cuda"), torch.rand((6, 1), generator=g, device="cuda")
+    check_product(a, sa, whole[:, 3:4], sb, F32, [10, 0, 20, 5, 5, 20])
+    check_product(a, sa, whole[2, 3:4], sb[0], F32)
