@@ -58,6 +58,8 @@ __device__ __forceinline__ void expert_rows(int count, unsigned limit, unsigned 
     first = __shfl_up_sync(0xffffffffu, last, 1);
     if (lane == 0) first = before;
 }
+// Channels of a tile end behind the last one: without sign, where they pass 2^31 too.
+__device__ __forceinline__ bool has_channel(const QmP &p, int channel) { return (unsigned)channel < (unsigned)p.n; }
 __device__ __forceinline__ int count_of(const QmP &p, int e) { return p.counts && e < p.experts ? p.counts[e] : 0; }
 
 // The `index`-th tile of at most `height` tokens, experts in order.  One warp; every lane gets the answer.  `count`: count_of(lane).
@@ -203,9 +205,10 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     __syncwarp();
     // scales of this lane's channel and of tokens `lane`, `lane` + 32, ..: here before they are needed
     const int own = (warp - 2) * 32 + lane, ch = row_tile * QM_ROWS + own;
+    const bool in = has_channel(p, ch);
     float b_scale = 0.0f, a_scale[(BN + 31) / 32] = {};
     if (tile.rows > 0 && warp >= 2) {
-        if (ch < p.n) b_scale = p.b_scale[(long long)tile.expert * p.n + ch];
+        if (in) b_scale = p.b_scale[(long long)tile.expert * p.n + ch];
 #pragma unroll
         for (int i = 0; i < (BN + 31) / 32; ++i)
             if (i * 32 + lane < tile.rows) a_scale[i] = p.a_scale[tile.row0 + i * 32 + lane];
@@ -250,7 +253,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
 #pragma unroll
             for (int i = 1; i < (BN + 31) / 32; ++i) mine = t >= 32 * i ? a_scale[i] : mine;
             const float a0 = __shfl_sync(0xffffffffu, mine, t & 31), a1 = __shfl_sync(0xffffffffu, mine, (t + 1) & 31);
-            if (ch < p.n) {
+            if (in) {
                 Out *out = static_cast<Out *>(p.out) + (long long)(tile.row0 + t) * p.out_stride + ch;
                 store_scaled(out, (int)sum[0], a0, b_scale);
                 if (two) store_scaled(out + p.out_stride, (int)sum[1], a1, b_scale);
@@ -315,7 +318,7 @@ template <int TOKENS> __device__ __forceinline__ void fill_schedule(const QmP &p
 {
     unsigned rows_before = 0, tiles_before = 0;
     if (lane == 0) tile_start[0] = row_start[0] = 0;
-    if (!p.counts && lane == 0) tile_start[1] = (p.rows + TOKENS - 1) / TOKENS, row_start[1] = p.rows;
+    if (!p.counts && lane == 0) tile_start[1] = (p.rows - 1) / TOKENS + 1, row_start[1] = p.rows;
     const int experts = p.counts ? p.experts : 0;
 #pragma unroll 1
     for (int e0 = 0; e0 < experts; e0 += 32) {
@@ -412,7 +415,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     const uint32_t lead_full = CTAS == 1 ? bar_full : map_to_cta(bar_full, 0);
     const uint32_t lead_tempty = CTAS == 1 ? bar_tempty : map_to_cta(bar_tempty, 0);
     const int ksteps = (p.k + QM_K - 1) / QM_K, experts = p.experts > 0 ? p.experts : 1;
-    QpSchedule<CTAS, TOKENS> sched{s_tile_start, s_row_start, (p.n + CTAS * QM_ROWS - 1) / (CTAS * QM_ROWS)};
+    QpSchedule<CTAS, TOKENS> sched{s_tile_start, s_row_start, (p.n - 1) / (CTAS * QM_ROWS) + 1};
     const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
     QpLoader<CTAS, TOKENS> loader{smem_base, bar_full, bar_empty, lead_full, (int)rank};
     int early = 0;                          // stages of the first tile that are issued before the block is set up
@@ -528,7 +531,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
         for (long long t = first; t < total; t += step) {
             const auto tile = sched.at(t);
             const int ch = tile.channel0 + (int)rank * QM_ROWS + quarter * 32 + lane;
-            const bool in = ch < p.n;
+            const bool in = has_channel(p, ch);
             const float bs = in ? p.b_scale[(long long)tile.expert * p.n + ch] : 0.0f;
             // a warp leaves the loop as one: what follows needs all of its lanes
             if (!warp_wait(bar_tfull + 8 * acc, acc_phase, p, t, lane)) break;
@@ -646,7 +649,7 @@ int launch_split(const QmP &p, const QmOperands &o, int device, cudaStream_t str
     const auto kernel = quant_matmul_kernel<BN, SPLITS, Out>;
     if (!allow_smem(kernel, QmShape<BN>::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
     // most token tiles that any counts can give
-    const long long tiles = p.counts ? p.rows / BN + std::min(p.experts, p.rows) : (p.rows + BN - 1) / BN;
+    const long long tiles = p.counts ? p.rows / BN + std::min(p.experts, p.rows) : (p.rows - 1) / BN + 1;
     const long long blocks = tiles * p.row_tiles * SPLITS;
     if (blocks > 0x7fffffffll) return MOE_OVL_ERR_UNSUPPORTED;
     return launch_behind(kernel, (unsigned)blocks, dim3(QM_THREADS), QmShape<BN>::SMEM, SPLITS, stream, b, a, p);
@@ -682,9 +685,9 @@ struct QmChoice { int ctas, tokens, splits; };
 //     tokens (four waves, two) 28.9 and 26.9.
 QmChoice choose(const QmP &p)
 {
-    const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows + groups - 1) / groups;
+    const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows - 1) / groups + 1;
     auto tiles = [&](int channels, int tokens) {
-        return (long long)((p.n + channels - 1) / channels) * groups * ((per_group + tokens - 1) / tokens);
+        return (long long)((p.n - 1) / channels + 1) * groups * ((per_group - 1) / tokens + 1);
     };
     const long long ksteps = (p.k + QM_K - 1) / QM_K;
     QmChoice c = {0, per_group <= 16 ? 16 : per_group <= 64 ? 32 : 64, 1};
@@ -725,7 +728,7 @@ extern "C" int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *a)
     if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 16 != 0 || sb % 16 != 0) return MOE_OVL_ERR_UNSUPPORTED;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
-    const QmP p = {a->rows, a->n, a->k, a->num_experts, (a->n + QM_ROWS - 1) / QM_ROWS, a->expert_counts, a->a_scale, a->b_scale, a->out,
+    const QmP p = {a->rows, a->n, a->k, a->num_experts, (a->n - 1) / QM_ROWS + 1, a->expert_counts, a->a_scale, a->b_scale, a->out,
                    a->out_stride, a->status, a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : QM_TIMEOUT_NS,
                    (a->flags & MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS) != 0};
     const QmChoice c = choose(p);

@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteP p)
     after_previous();
     may_follow();
     // a warp's rows come and go together: the loop ends when its first row is beyond the last
-    for (int row0 = blockIdx.x * ROWS + (threadIdx.x / 32) * (32 / G); row0 < p.rows; row0 += gridDim.x * ROWS) {
-        const int row = row0 + lane / G;
+    for (unsigned row0 = blockIdx.x * ROWS + (threadIdx.x / 32) * (32 / G); row0 < (unsigned)p.rows; row0 += gridDim.x * ROWS) {
+        const int row = (int)row0 + lane / G;
         const bool live = row < p.rows;
         const T *logits = static_cast<const T *>(p.logits) + (long long)row * p.stride;
         T raw[NR];

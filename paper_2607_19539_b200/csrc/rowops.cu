@@ -99,8 +99,9 @@ template <int VEC> __device__ __forceinline__ void store_quant(int8_t *q, const 
 }
 __device__ __forceinline__ uint32_t keep_mask(float most) { return most <= 3.402823466e+38f ? 0xffffffffu : 0u; }
 
-// Where row `row` of a matrix begins for a thread whose first column is c.
-template <typename T> __device__ __forceinline__ T *at_row(T *base, int row, int stride, int c) { return base + ((long long)row * stride + c); }
+// Where row `row` of a matrix begins for a thread whose first column is c.  Rows are counted without sign: one step behind the last of 2^31 - 1
+// rows is still a row number.
+template <typename T> __device__ __forceinline__ T *at_row(T *base, unsigned row, int stride, int c) { return base + ((long long)row * stride + c); }
 
 // RAGGED rows: their length or their distance is no multiple of a pack, so they begin anywhere in one.  A thread then owns packs of the
 // ADDRESS space: its first column is `shift` columns further left, and shift = (row * stride) mod VEC stays the same for a block when its
@@ -152,7 +153,7 @@ template <int VEC, bool RAGGED> __device__ __forceinline__ void quant_some(int8_
     }
     store_quant<VEC>(q, v, factor, keep);
 }
-template <int VEC, bool RAGGED> __device__ __forceinline__ int shift_of(int row, int stride) { return RAGGED ? (int)((unsigned)row * (unsigned)stride % VEC) : 0; }
+template <int VEC, bool RAGGED> __device__ __forceinline__ int shift_of(unsigned row, int stride) { return RAGGED ? (int)(row * (unsigned)stride % VEC) : 0; }
 
 // Two rows in shared memory, one in use and one on its way from global memory.  Every thread copies, waits for and reads its own
 // packs only (asynchronous copies of 16 or 4 bytes), so no thread waits for another.  Partial packs are not copied.
@@ -206,7 +207,8 @@ template <typename T, int VEC, int NV, int ARRAYS, bool RAGGED> struct Feed {
 };
 
 struct NormP {
-    int rows, d;
+    unsigned rows;
+    int d;
     float per_d, eps;                           // per_d: 1 / d
     const void *x, *residual, *weight;
     void *residual_out, *y;
@@ -223,13 +225,13 @@ __device__ __forceinline__ void add_norm_rows(const NormP &p)
     __shared__ float2 buf[2][32];
     after_previous();
     may_follow();
-    const int step = gridDim.x * blockDim.y;
+    const unsigned step = gridDim.x * blockDim.y;
     const W *w = static_cast<const W *>(p.weight);
-    int row = blockIdx.x * blockDim.y + threadIdx.y;
+    unsigned row = blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= p.rows) return;                  // whole warps: rows share a block only as one warp each
     const int c0 = threadIdx.x * VEC - shift_of<VEC, RAGGED>(row, p.x_stride), across = blockDim.x * VEC;
     Pack<T, VEC> a[NV], b[NV];
-    auto load = [&](int r) {
+    auto load = [&](unsigned r) {
         const T *x = at_row(static_cast<const T *>(p.x), r, p.x_stride, c0), *res = at_row(static_cast<const T *>(p.residual), r, p.residual_stride, c0);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -314,7 +316,8 @@ template <typename T, typename W, int VEC, int NV, bool RAGGED>
 __global__ void __maxnreg__(VEC *NV <= 8 ? 40 : 128) add_norm_lean_kernel(const NormP p) { add_norm_rows<T, W, VEC, NV, RAGGED>(p); }
 
 struct NormBackP {
-    int rows, d;
+    unsigned rows;
+    int d;
     float per_d;
     const void *dy, *h, *weight, *d_residual;
     const float *rstd;
@@ -344,16 +347,16 @@ __device__ __forceinline__ void add_norm_backward_rows(const NormBackP &p)
     float acc[NV * VEC];
 #pragma unroll
     for (int i = 0; i < NV * VEC; ++i) acc[i] = 0.0f;
-    const int first = blockIdx.x * blockDim.y + threadIdx.y, step = gridDim.x * blockDim.y;
+    const unsigned first = blockIdx.x * blockDim.y + threadIdx.y, step = gridDim.x * blockDim.y;
     const W *w = static_cast<const W *>(p.weight);
     const int c0 = threadIdx.x * VEC - shift_of<VEC, RAGGED>(first, p.dy_stride), across = blockDim.x * VEC;
-    auto start = [&](int r, const T *(&at)[3]) {
+    auto start = [&](unsigned r, const T *(&at)[3]) {
         at[0] = at_row(static_cast<const T *>(p.dy), r, p.dy_stride, c0);
         at[1] = at_row(static_cast<const T *>(p.h), r, p.h_stride, c0);
         at[2] = p.d_residual ? at_row(static_cast<const T *>(p.d_residual), r, p.d_residual_stride, c0) : nullptr;
     };
     Feed<T, VEC, NV, 3, RAGGED> feed;
-    auto ask = [&](int r) {
+    auto ask = [&](unsigned r) {
         const T *at[3];
         start(r, at);
         feed.ask(at, r < p.rows, c0, p.d, across);
@@ -364,7 +367,7 @@ __device__ __forceinline__ void add_norm_backward_rows(const NormBackP &p)
     for (int i = 0; i < NV; ++i)
         if (c0 + i * across < p.d) wv[i] = load_weight<W, VEC, RAGGED>(w, c0 + i * across, p.d);
     int turn = 0;
-    for (int row = first; row < p.rows; row += step, turn ^= 1) {
+    for (unsigned row = first; row < p.rows; row += step, turn ^= 1) {
         const float rstd = p.rstd[row];
         const T *at[3];
         if constexpr (FED) {
@@ -503,7 +506,8 @@ __global__ void __launch_bounds__(1024) reduce_partials_kernel(const float *part
 }
 
 struct SwigluP {
-    int rows, f;
+    unsigned rows;
+    int f;
     const void *x;
     int8_t *q;
     float *scale;
@@ -531,12 +535,12 @@ __global__ void __launch_bounds__(swiglu_threads(VEC *NV)) swiglu_quant_kernel(c
     __shared__ float buf[2][32];
     after_previous();
     may_follow();
-    const int step = gridDim.x * blockDim.y;
-    int row = blockIdx.x * blockDim.y + threadIdx.y;
+    const unsigned step = gridDim.x * blockDim.y;
+    unsigned row = blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= p.rows) return;
     const int c0 = threadIdx.x * VEC, across = blockDim.x * VEC;
     Pack<T, VEC> a[NV], b[NV];
-    auto load = [&](int r) {
+    auto load = [&](unsigned r) {
         const T *g = at_row(static_cast<const T *>(p.x), r, p.x_stride, c0), *u = g + p.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -582,6 +586,7 @@ template <int VEC> int ragged_packs(int width) { return (width + 2 * (VEC - 1)) 
 
 // How a row of `width` elements is spread: threads per row, packs per thread, rows per block.
 struct RowShape { int threads, packs, rows_per_block; };
+int blocks_of(unsigned rows, const RowShape &s) { return (int)((rows - 1) / s.rows_per_block + 1); }
 
 template <int VEC> RowShape row_shape(int rows, int width, int want_values, int (*most_threads)(int), bool ragged = false)
 {
@@ -620,7 +625,7 @@ int whole_steps(int blocks, const RowShape &s, int rows, bool ragged) { return r
 
 template <typename K, typename P> int launch_rows(K kernel, const P &p, const RowShape &s, bool ragged, int device, cudaStream_t stream)
 {
-    const int blocks = whole_steps(resident(kernel, s.threads * s.rows_per_block, 0, (p.rows + s.rows_per_block - 1) / s.rows_per_block, device), s, p.rows, ragged);
+    const int blocks = whole_steps(resident(kernel, s.threads * s.rows_per_block, 0, blocks_of(p.rows, s), device), s, (int)p.rows, ragged);
     if (blocks < 1) return MOE_OVL_ERR_CUDA;
     return launch_behind(kernel, (unsigned)blocks, dim3(s.threads, s.rows_per_block), 0, 1, stream, p);
 }
@@ -635,9 +640,9 @@ int launch_backward(K kernel, std::atomic<int> *allowed, const NormBackP &p, con
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) return MOE_OVL_ERR_CUDA;
         if (device <= 63) allowed[device].store(1, std::memory_order_relaxed);
     }
-    blocks = resident(kernel, threads, smem, std::min((p.rows + s.rows_per_block - 1) / s.rows_per_block, NORM_PARTIALS), device);
+    blocks = resident(kernel, threads, smem, std::min(blocks_of(p.rows, s), NORM_PARTIALS), device);
     if (blocks < 1) return MOE_OVL_ERR_CUDA;
-    blocks = whole_steps(blocks, s, p.rows, ragged);
+    blocks = whole_steps(blocks, s, (int)p.rows, ragged);
     return launch_behind(kernel, (unsigned)blocks, dim3(s.threads, s.rows_per_block), smem, 1, stream, p);
 }
 
@@ -704,7 +709,7 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
         return MOE_OVL_ERR_INVALID_ARG;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
-    const NormP p = {a->rows, a->d, 1.0f / (float)a->d, a->eps, a->x, a->residual, a->weight, a->residual_out, a->y, a->q, a->scale, a->rstd,
+    const NormP p = {(unsigned)a->rows, a->d, 1.0f / (float)a->d, a->eps, a->x, a->residual, a->weight, a->residual_out, a->y, a->q, a->scale, a->rstd,
                      (int)a->x_stride, (int)a->residual_stride, (int)a->residual_out_stride, (int)a->y_stride, (int)a->q_stride};
     auto fits = [&](int vec) {
         return a->d % vec == 0 && rows_ok(a->x, a->x_stride, vec, es) && aligned(a->weight, (size_t)vec * ws) &&
@@ -723,7 +728,7 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
             using W = decltype(w);
             constexpr int VEC = decltype(v)::value;
             constexpr bool RAGGED = decltype(r)::value != 0;
-            const RowShape s = row_shape<VEC>(p.rows, p.d, VEC >= 4 ? VEC : 8, max_threads, RAGGED);
+            const RowShape s = row_shape<VEC>(a->rows, p.d, VEC >= 4 ? VEC : 8, max_threads, RAGGED);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 // An 8-bit output alone: blocks per SM count (16384 x 4096: 72 us in 40 registers, 80 us in 64).  With an output in the type of x the
@@ -770,7 +775,7 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
         if (!a->dweight) return MOE_OVL_OK;
         return cudaMemsetAsync(a->dweight, 0, (size_t)a->d * 4, stream) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
     }
-    const NormBackP p = {a->rows, a->d, 1.0f / (float)a->d, a->dy, a->h, a->weight, a->d_residual, a->rstd, a->dx,
+    const NormBackP p = {(unsigned)a->rows, a->d, 1.0f / (float)a->d, a->dy, a->h, a->weight, a->d_residual, a->rstd, a->dx,
                    a->dweight ? static_cast<float *>(a->workspace) : nullptr, (int)a->dy_stride, (int)a->h_stride,
                    (int)a->d_residual_stride, (int)a->dx_stride};
     auto fits = [&](int vec) {
@@ -788,7 +793,7 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
             using W = decltype(w);
             constexpr int VEC = decltype(v)::value;
             constexpr bool RAGGED = decltype(r)::value != 0;
-            const RowShape s = row_shape<VEC>(p.rows, p.d, 8, max_threads, RAGGED);
+            const RowShape s = row_shape<VEC>(a->rows, p.d, 8, max_threads, RAGGED);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 int blocks = 0;
@@ -820,13 +825,13 @@ extern "C" int moe_ovl_swiglu_quant(const moe_ovl_swiglu_args *a)
     if (!a->gate_up || !a->q || !a->scale || !aligned(a->gate_up, es) || !aligned(a->scale, 4)) return MOE_OVL_ERR_INVALID_ARG;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
-    const SwigluP p = {a->rows, a->f, a->gate_up, a->q, a->scale, (int)a->gate_up_stride, (int)a->q_stride};
+    const SwigluP p = {(unsigned)a->rows, a->f, a->gate_up, a->q, a->scale, (int)a->gate_up_stride, (int)a->q_stride};
     auto fits = [&](int vec) { return a->f % vec == 0 && rows_ok(a->gate_up, a->gate_up_stride, vec, es) && rows_ok(a->q, a->q_stride, vec, 1); };
     return with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto v) {
             constexpr int VEC = decltype(v)::value;
-            const RowShape s = row_shape<VEC>(p.rows, p.f, 16, swiglu_threads);
+            const RowShape s = row_shape<VEC>(a->rows, p.f, 16, swiglu_threads);
             return with_packs<VEC>(s.packs, [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 return launch_rows(swiglu_quant_kernel<T, VEC, NV>, p, s, false, a->device, static_cast<cudaStream_t>(a->stream));

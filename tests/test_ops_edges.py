@@ -229,3 +229,87 @@ def test_quant_matmul_one_channel_of_every_expert():
     sa, sb = torch.rand(60, generator=g, device="cuda"), torch.rand((6, 1), generator=g, device="cuda")
     check_product(a, sa, whole[:, 3:4], sb, F32, [10, 0, 20, 5, 5, 20])
     check_product(a, sa, whole[2, 3:4], sb[0], F32)
+
+
+def long_matrix(rows, cols, dtype, value):
+    """All one value, but for eight rows at either end."""
+    m = torch.full((rows, cols), value, dtype=dtype, device="cuda")
+    ends = torch.arange(1, 17, device="cuda").view(16, 1).expand(16, cols).to(dtype)
+    m[:8], m[-8:] = ends[:8], ends[8:]
+    return m
+
+
+def check_long(got, middle, ends):
+    """got [rows]: `middle` all over, `ends` in the eight rows at either end; in parts, for the comparison's own memory."""
+    assert torch.equal(got[:8], ends[:8]) and torch.equal(got[-8:], ends[8:])
+    for part in got[8:-8].split(1 << 28):
+        assert bool((part == middle).all())
+
+
+MOST_ROWS = 2 ** 31 - 1
+
+
+@gpu
+def test_row_operators_of_the_longest_matrices():
+    """As many rows as their count can say: one step behind the last row passes 2^31.  One column each; every row's result is that of a
+    short matrix with the same value."""
+    x = long_matrix(MOST_ROWS, 1, BF16, 3.0)
+    short = torch.cat([x[:8], x[-8:], torch.full((1, 1), 3.0, dtype=BF16, device="cuda")])
+    w = torch.full((1,), 1.5, dtype=BF16, device="cuda")
+
+    def norm(m):
+        rstd, y = torch.zeros(m.shape[0], device="cuda"), torch.zeros_like(m)
+        ops.moe_ovl_add_norm(x=m, weight=w, eps=0.5, y=y, rstd=rstd)
+        return y, rstd
+
+    y, rstd = norm(x)
+    ys, rs = norm(short)
+    check_long(rstd, rs[16], rs[:16])
+    check_long(y[:, 0], ys[16, 0], ys[:16, 0])
+    dx = torch.zeros_like(x)
+    ops.moe_ovl_add_norm_backward(dy=y, h=x, weight=w, rstd=rstd, dx=dx)
+    ds = torch.zeros_like(short)
+    ops.moe_ovl_add_norm_backward(dy=ys, h=short, weight=w, rstd=rs, dx=ds)
+    check_long(dx[:, 0], ds[16, 0], ds[:16, 0])
+    del y, dx, rstd
+    scale, q = torch.zeros(MOST_ROWS, device="cuda"), torch.zeros((MOST_ROWS, 1), dtype=torch.int8, device="cuda")
+    gate_up = x.expand(MOST_ROWS, 2).contiguous()
+    ops.moe_ovl_swiglu_quant(gate_up=gate_up, q=q, scale=scale)
+    ss, qs = torch.zeros(17, device="cuda"), torch.zeros((17, 1), dtype=torch.int8, device="cuda")
+    ops.moe_ovl_swiglu_quant(gate_up=short.expand(17, 2).contiguous(), q=qs, scale=ss)
+    check_long(scale, ss[16], ss[:16])
+    check_long(q[:, 0], qs[16, 0], qs[:16, 0])
+
+
+@gpu
+def test_router_of_the_most_rows():
+    x = long_matrix(MOST_ROWS, 1, BF16, 3.0)
+    expert, gate = torch.full((MOST_ROWS, 1), -9, dtype=torch.int32, device="cuda"), torch.zeros((MOST_ROWS, 1), device="cuda")
+    counts = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ops.moe_ovl_route(logits=x, expert=expert, gate=gate, counts=counts, score=ops.SCORE_SIGMOID, renormalise=False)
+    short = torch.cat([x[:8], x[-8:], torch.full((1, 1), 3.0, dtype=BF16, device="cuda")])
+    _, gs, _ = call_route(short, 1, score="sigmoid", renorm=False)
+    check_long(gate[:, 0], gs[16, 0], gs[:16, 0])
+    assert int(counts) == MOST_ROWS and all(not bool(part.any()) for part in expert[:, 0].split(1 << 28))
+    dx = torch.full_like(x, 7.0)
+    ops.moe_ovl_route_backward(logits=x, expert=expert, dgate=gate, dlogits=dx, score=ops.SCORE_SIGMOID, renormalise=False)
+    ds = torch.zeros_like(short)
+    ops.moe_ovl_route_backward(logits=short, expert=torch.zeros((17, 1), dtype=torch.int32, device="cuda"), dgate=gs, dlogits=ds, score=ops.SCORE_SIGMOID,
+                               renormalise=False)
+    check_long(dx[:, 0], ds[16, 0], ds[:16, 0])
+
+
+@gpu
+@pytest.mark.parametrize("long_a", [True, False])
+def test_quant_matmul_of_the_longest_matrices(long_a):
+    """As many tokens, or channels, as their count can say."""
+    big, one = long_matrix(MOST_ROWS, 16, torch.int8, 3), torch.ones((1, 16), dtype=torch.int8, device="cuda")
+    scale, unit = torch.full((MOST_ROWS,), 0.5, device="cuda"), torch.ones(1, device="cuda")
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    out = torch.zeros((MOST_ROWS, 1) if long_a else (1, MOST_ROWS), dtype=BF16, device="cuda")
+    if long_a:
+        ops.moe_ovl_quant_matmul(a=big, a_scale=scale, b=one, b_scale=unit, out=out, status=status)
+    else:
+        ops.moe_ovl_quant_matmul(a=one, a_scale=unit, b=big, b_scale=scale, out=out, status=status)
+    assert not status.any()
+    check_long(out.view(-1), 24.0, torch.arange(1, 17, device="cuda").to(BF16) * 8)
