@@ -20,6 +20,7 @@ import argparse
 import hashlib
 import json
 import os
+import re
 import socket
 import statistics
 import subprocess
@@ -37,10 +38,10 @@ METRIC = "moe_expert_return_tflops"
 UNIT = "TFLOP/s"
 FALLBACK_PEAKS = {"hbm_gbs": 6650.0, "bf16_tflops": 1590.0, "bf16_tflops_sustained": 1400.0}
 # DRAM traffic (dram__bytes_read.sum + dram__bytes_write.sum) of one GEMM-kernel launch at full size, from one
-# ncu capture; valid only for the kernel source it was taken from (sha1 of csrc/producer.cuh, first 12 digits).
+# ncu capture; valid only for the kernel source it was taken from (sha1 of csrc/producer.cuh and the headers it includes, first 12 digits).
 # A changed kernel makes the figure stale: it is then reported as null with the reason.
 NCU_PRODUCER_TRAFFIC = {
-    "mixtral": {"bytes": 2777206000 + 382403328, "kernel_sha1": "b43f127217fa",
+    "mixtral": {"bytes": 2777206000 + 382403328, "kernel_sha1": "266897c1f0cb",
                 "capture": "ncu (DRAM bytes, one pass), one launch of the GEMM kernel at full size, non-overlap mode"},
 }
 PREHEAT_S = 1.0      # untimed steps before the timed ones, so that the timed steps see the GPU's sustained state
@@ -57,9 +58,14 @@ def load_peaks():
 
 
 def kernel_sha1() -> str:
-    path = os.path.join(ROOT, "paper_2607_19539_b200", "csrc", "producer.cuh")
-    with open(path, "rb") as f:
-        return hashlib.sha1(f.read()).hexdigest()[:12]
+    """Of the GEMM kernel's source: csrc/producer.cuh and, in the order of their inclusion, the project's headers behind it."""
+    digest, files = hashlib.sha1(), ["producer.cuh"]
+    for name in files:                      # grows while it is read
+        with open(os.path.join(ROOT, "paper_2607_19539_b200", "csrc", name), "rb") as f:
+            text = f.read()
+        digest.update(text)
+        files += [h for h in re.findall(r'^#include "([^"]+)"', text.decode(), re.M) if h not in files]
+    return digest.hexdigest()[:12]
 
 
 def flops_of(shape, rows: int) -> float:

@@ -102,6 +102,16 @@ template <int BN> struct QmShape {
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
 };
 
+// Takes bytes off what the phase still waits for, as a copy of that size would.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void st_shared_cluster_u32(uint32_t addr, uint32_t v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
 // A wait that gives up, in whichever warp, leaves tile copies and matrix instructions under way: they have to land before the CTA's shared and
 // tensor memory go to somebody else.  This wait has a limit of its own, which neither a caller's short one nor an aborted status shortens.
 constexpr unsigned long long QM_LANDING_NS = 2000000000ull;
