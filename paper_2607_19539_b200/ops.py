@@ -5,11 +5,15 @@ Every tensor is the caller's, outputs and workspaces too; nothing is allocated a
 side cannot see of a tensor -- its shape, type, device and the order of its columns -- is checked here, and a tensor
 that does not fit raises MoeOvlError with ERR_INVALID_ARG before anything is launched.  Work goes to the current stream
 of the tensors' device, or to `stream`; tensors used on a stream that is not the current one are recorded on it.
+
+Nothing is recorded for autograd: outputs carry no gradient, and the two gradients are called by hand or from the backward of a
+torch.autograd.Function (whose forward runs with gradients off).  An input that requires a gradient while they are on gets a warning.
 """
 from __future__ import annotations
 
 import ctypes as C
 import struct
+import warnings
 
 import torch
 
@@ -90,6 +94,12 @@ def _vector(where, name, t, shape, dtype, device) -> None:
         _refuse(where, f"{name} has to be a contiguous {list(shape)} {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
 
 
+def _gradient_lost(where: str) -> None:
+    if torch.is_grad_enabled():
+        warnings.warn(f"{where} records nothing for autograd: an input requires a gradient that the outputs will not carry (call it under torch.no_grad() "
+                      "and take the gradient with the operator's own backward call, where it has one)", stacklevel=3)
+
+
 def _at(t) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -137,6 +147,8 @@ def moe_ovl_add_norm(*, x, weight, eps: float = 1e-6, residual=None, residual_ou
     so = _matrix(where, "residual_out", residual_out, shape, kind, dev) if residual_out is not None else 0
     sy = _matrix(where, "y", y, shape, kind, dev) if y is not None else 0
     sq = _matrix(where, "q", q, shape, torch.int8, dev) if q is not None else 0
+    if x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad):
+        _gradient_lost(where)
     if scale is not None:
         _vector(where, "scale", scale, (rows,), torch.float32, dev)
     if rstd is not None:
@@ -191,6 +203,8 @@ def moe_ovl_swiglu_quant(*, gate_up, q, scale, stream=None) -> None:
     sg = _matrix(where, "gate_up", gate_up, gate_up.shape, gate_up.dtype, dev)
     sq = _matrix(where, "q", q, (rows, f), torch.int8, dev)
     _vector(where, "scale", scale, (rows,), torch.float32, dev)
+    if gate_up.requires_grad:
+        _gradient_lost(where)
     _call(where, B.load().moe_ovl_swiglu_quant, SwigluArgs, dev, rows, f, dt, 0, gate_up.data_ptr(), q.data_ptr(), scale.data_ptr(), sg, sq,
           _stream(dev, stream, gate_up, q, scale))
 
@@ -211,6 +225,8 @@ def moe_ovl_route(*, logits, expert, gate, counts=None, bias=None, score: int = 
         _vector(where, "bias", bias, (e,), torch.float32, dev)
     if counts is not None:
         _vector(where, "counts", counts, (e,), torch.int32, dev)
+    if logits.requires_grad:
+        _gradient_lost(where)
     _call(where, B.load().moe_ovl_route, RouteArgs, dev, rows, e, k, dt, score, num_groups, top_groups, group_best, 1 if renormalise else 0, gate_scale,
           logits.data_ptr(), _at(bias), expert.data_ptr(), gate.data_ptr(), _at(counts), sl, _stream(dev, stream, logits, expert, gate, bias, counts))
 
@@ -263,6 +279,8 @@ def moe_ovl_quant_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=N
     _vector(where, "a_scale", a_scale, (rows,), torch.float32, dev)
     _vector(where, "b_scale", b_scale, b.shape[:-1], torch.float32, dev)
     _vector(where, "status", status, (4,), torch.int32, dev)
+    if a_scale.requires_grad or b_scale.requires_grad:
+        _gradient_lost(where)
     _call(where, B.load().moe_ovl_quant_matmul, QuantMatmulArgs, dev, rows, n, k, experts, dt, wait_timeout_us, flags, a.data_ptr(), a_scale.data_ptr(),
           b.data_ptr(), b_scale.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, so,
           _stream(dev, stream, a, a_scale, b, b_scale, expert_counts, out, status))

@@ -4,6 +4,7 @@ their type, the widest rows, the longest matrices, waits that give up while copi
 U, FLOOR and the comparison are those of test_ops; a tolerance that is not derived there is derived at its test.
 """
 import math
+import warnings
 
 import pytest
 
@@ -313,3 +314,30 @@ def test_quant_matmul_of_the_longest_matrices(long_a):
         ops.moe_ovl_quant_matmul(a=one, a_scale=unit, b=big, b_scale=scale, out=out, status=status)
     assert not status.any()
     check_long(out.view(-1), 24.0, torch.arange(1, 17, device="cuda").to(BF16) * 8)
+
+
+@gpu
+def test_a_gradient_is_not_lost_without_a_word():
+    """Outputs are the caller's buffers and carry no gradient: an input that requires one is warned about, unless gradients are off."""
+    g = gen(17)
+    x, w, q = normal(g, (5, 64), BF16), normal(g, (64,), BF16), torch.empty((5, 64), dtype=torch.int8, device="cuda")
+    y, s, half = torch.empty_like(x), torch.ones(5, device="cuda"), torch.empty((5, 32), dtype=torch.int8, device="cuda")
+    expert, gate, status = torch.empty((5, 2), dtype=torch.int32, device="cuda"), torch.empty((5, 2), device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    b, sb, out = make8(g, (8, 64)), torch.ones(8, device="cuda"), torch.empty((5, 8), device="cuda")
+    grad = lambda t: t.clone().requires_grad_()  # noqa: E731
+    calls = [
+        lambda f: ops.moe_ovl_add_norm(x=f(x), weight=w, y=y), lambda f: ops.moe_ovl_add_norm(x=x, weight=f(w), y=y),
+        lambda f: ops.moe_ovl_add_norm(x=x, residual=f(x), weight=w, y=y, q=q, scale=s), lambda f: ops.moe_ovl_swiglu_quant(gate_up=f(x), q=half, scale=s),
+        lambda f: ops.moe_ovl_route(logits=f(x), expert=expert, gate=gate),
+        lambda f: ops.moe_ovl_quant_matmul(a=q, a_scale=f(s), b=b, b_scale=sb, out=out, status=status),
+        lambda f: ops.moe_ovl_quant_matmul(a=q, a_scale=s, b=b, b_scale=f(sb), out=out, status=status),
+    ]
+    for call in calls:
+        with pytest.warns(UserWarning, match="autograd"):
+            call(grad)
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            call(lambda t: t)
+            with torch.no_grad():
+                call(grad)
+    torch.cuda.synchronize()
