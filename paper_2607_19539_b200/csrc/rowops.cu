@@ -9,6 +9,7 @@
 // three matrices to read and sums to keep, into shared memory (struct Feed).
 #include <algorithm>
 #include <atomic>
+#include <utility>
 
 #include "opcommon.cuh"
 
@@ -647,19 +648,25 @@ int launch_backward(K kernel, std::atomic<int> *allowed, const NormBackP &p, con
 }
 
 template <int N> struct Count { static constexpr int value = N; };
-// Calls f with the number of packs as a constant.
-template <int VEC, typename F> int with_packs(int packs, F f)
+// Calls f with the number of packs as a constant: one of those that row_shape gives for some width, a kernel for each and no others.
+template <typename F, int... N> int with_packs(int packs, std::integer_sequence<int, N...>, F f)
 {
-    if constexpr (VEC >= 4) {
-        if (packs == 1) return f(Count<1>());
-        if (packs == 4) return f(Count<4>());
-        if constexpr (VEC == 4) if (packs == 16) return f(Count<16>());
-    }
-    if (packs == 2) return f(Count<2>());
-    if (packs == 8) return f(Count<8>());
-    if constexpr (VEC <= 2) if (packs == 32) return f(Count<32>());
-    if constexpr (VEC == 1) if (packs == 64) return f(Count<64>());
-    return MOE_OVL_ERR_UNSUPPORTED;
+    int rc = MOE_OVL_ERR_UNSUPPORTED;
+    ((packs == N ? (void)(rc = f(Count<N>())) : (void)0), ...);
+    return rc;
+}
+template <int VEC> constexpr auto norm_packs()
+{
+    if constexpr (VEC == 8) return std::integer_sequence<int, 1, 4, 8>();
+    else if constexpr (VEC == 4) return std::integer_sequence<int, 1, 2, 8, 16>();
+    else return std::integer_sequence<int, 2, 8, 32, 64>();
+}
+template <int VEC> constexpr auto swiglu_packs()
+{
+    if constexpr (VEC == 8) return std::integer_sequence<int, 1, 2, 8>();
+    else if constexpr (VEC == 4) return std::integer_sequence<int, 1, 2, 4, 16>();
+    else if constexpr (VEC == 2) return std::integer_sequence<int, 2, 8, 32>();
+    else return std::integer_sequence<int, 2, 8, 32, 64>();
 }
 
 // Calls f with the packs that the matrices allow, and whether rows are ragged in them: 16 bytes, or one element.  The widest rows fill a
@@ -729,7 +736,7 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
             constexpr int VEC = decltype(v)::value;
             constexpr bool RAGGED = decltype(r)::value != 0;
             const RowShape s = row_shape<VEC>(a->rows, p.d, VEC >= 4 ? VEC : 8, max_threads, RAGGED);
-            return with_packs<VEC>(s.packs, [&](auto n) {
+            return with_packs(s.packs, norm_packs<VEC>(), [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 // An 8-bit output alone: blocks per SM count (16384 x 4096: 72 us in 40 registers, 80 us in 64).  With an output in the type of x the
                 // writes are what bounds it, and fewer blocks write better (87 us in 64, 92 us in 40).
@@ -794,7 +801,7 @@ extern "C" int moe_ovl_add_norm_backward(const moe_ovl_norm_backward_args *a)
             constexpr int VEC = decltype(v)::value;
             constexpr bool RAGGED = decltype(r)::value != 0;
             const RowShape s = row_shape<VEC>(a->rows, p.d, 8, max_threads, RAGGED);
-            return with_packs<VEC>(s.packs, [&](auto n) {
+            return with_packs(s.packs, norm_packs<VEC>(), [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 int blocks = 0;
                 static std::atomic<int> allowed[64];
@@ -832,7 +839,7 @@ extern "C" int moe_ovl_swiglu_quant(const moe_ovl_swiglu_args *a)
         auto launch = [&](auto v) {
             constexpr int VEC = decltype(v)::value;
             const RowShape s = row_shape<VEC>(a->rows, p.f, 16, swiglu_threads);
-            return with_packs<VEC>(s.packs, [&](auto n) {
+            return with_packs(s.packs, swiglu_packs<VEC>(), [&](auto n) {
                 constexpr int NV = decltype(n)::value;
                 return launch_rows(swiglu_quant_kernel<T, VEC, NV>, p, s, false, a->device, static_cast<cudaStream_t>(a->stream));
             });
