@@ -101,8 +101,8 @@ template <int VEC> __device__ __forceinline__ void store_quant(int8_t *q, const 
 __device__ __forceinline__ uint32_t keep_mask(float most) { return most <= 3.402823466e+38f ? 0xffffffffu : 0u; }
 
 // Where row `row` of a matrix begins for a thread whose first column is c.  Rows are counted without sign: one step behind the last of 2^31 - 1
-// rows is still a row number.
-template <typename T> __device__ __forceinline__ T *at_row(T *base, unsigned row, int stride, int c) { return base + ((long long)row * stride + c); }
+// rows is still a row number, but not one of a row that is read.  (The product of two signed numbers takes fewer registers.)
+template <typename T> __device__ __forceinline__ T *at_row(T *base, unsigned row, int stride, int c) { return base + ((long long)(int)row * stride + c); }
 
 // RAGGED rows: their length or their distance is no multiple of a pack, so they begin anywhere in one.  A thread then owns packs of the
 // ADDRESS space: its first column is `shift` columns further left, and shift = (row * stride) mod VEC stays the same for a block when its
