@@ -341,3 +341,19 @@ def test_a_gradient_is_not_lost_without_a_word():
             with torch.no_grad():
                 call(grad)
     torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("d", [40, 2050, 4096, 4099])
+def test_quantised_values_are_rounded_products(d, dtype):
+    """With weights of 1, a value over its row's largest is that of the inputs, and rstd is no part of it: in 8 bits it is the 32-bit product with the
+    32-bit quotient 127 / max, rounded to a whole number, ties to even.  Both roundings are defined, so the values are equal."""
+    g = gen(d + 1)
+    x = normal(g, (700, d), dtype)
+    q, scale = torch.empty((700, d), dtype=torch.int8, device="cuda"), torch.empty(700, device="cuda")
+    most = x.float().abs().amax(1, keepdim=True)
+    want = torch.round(x.float() * (torch.full_like(most, 127.0) / most)).to(torch.int8)
+    for y in (None, torch.empty_like(x)):
+        ops.moe_ovl_add_norm(x=x, weight=torch.ones(d, dtype=dtype, device="cuda"), y=y, q=q, scale=scale)
+        assert torch.equal(q, want)
