@@ -383,7 +383,7 @@ enum { MOE_OVL_BF16 = 0, MOE_OVL_F16 = 1, MOE_OVL_F32 = 2 };
 /* RMS norm of a sum:  h = x + residual, rounded to the type of x (h = x without a residual);
  *   rstd = 1 / sqrt(mean(h^2) + eps);  v = (h * rstd) * weight, in 32 bits.
  * Any of: residual_out = h;  y = v rounded to the type of x;  q, scale = v in 8 bits, scale = max|v| / 127 of the row and
- * q = v * 127 / max|v| to the nearest, ties to even, so v ~ q * scale (a row whose max|v| is below 2^-100 gives zeros);
+ * q = v * (127 / max|v|) in 32 bits, to the nearest, ties to even, so v ~ q * scale (a row whose max|v| is below 2^-100 gives zeros);
  * rstd, for the backward pass.  The norm is taken of the ROUNDED sum: it is what the next layer and the backward pass see.
  * A row that holds a NaN or an infinity gets y and scale NaN where it must and q = 0.  residual_out may be
  * residual or x itself, y may be x or residual: with the same stride. */
@@ -460,7 +460,8 @@ int moe_ovl_swiglu_quant(const moe_ovl_swiglu_args *args);
  * bias and with group_best = 1 the logits themselves are compared.
  *   gate = gate_scale * score, or with renormalise gate_scale * score / (sum of the row's chosen scores)
  *          (softmax: computed as the softmax of the chosen logits; 0 where that sum is 0).
- * A logit (or a bias) that is -inf or NaN masks its expert: score 0, never chosen.  +inf counts as the largest finite value.
+ * A logit that is -inf or NaN masks its expert: score 0, never chosen.  A bias that is -inf or NaN keeps its expert from being chosen, and
+ * no more: it has its share of the softmax.  +inf counts as the largest finite value.
  * Slots for which no expert is left hold expert -1 and gate 0. */
 enum { MOE_OVL_SCORE_SOFTMAX = 0, MOE_OVL_SCORE_SIGMOID = 1 };
 typedef struct {
@@ -511,7 +512,7 @@ int moe_ovl_route_backward(const moe_ovl_route_backward_args *args);
  * a and b: 16-byte aligned, strides multiples of 16, k a multiple of 16; otherwise MOE_OVL_ERR_UNSUPPORTED.
  * status: [4] of DEVICE memory that the caller clears once and may share between calls on one stream; status[0] becomes
  * MOE_OVL_ERR_TIMEOUT when a bounded wait inside a kernel gave up (the outputs are then unspecified, written in bounds, and
- * later calls with the same status may give up early, until the caller clears it). */
+ * later calls with the same status may give up early, until the caller clears it).  A kernel that gave up ends when what it had started has landed. */
 typedef struct {
     uint32_t struct_size;
     int32_t device;

@@ -684,7 +684,8 @@ struct QmChoice { int ctas, tokens, splits; };
 // The kernel goes by the tiles there are (with the experts' rows taken as even: the counts are on the device).  Measured, us:
 //   few tiles leave SMs idle, so they share their K: 1 token, n = k = 4096 (32 tiles) 7.3 split by 4, 8.0 unsplit; n = 1024, k = 8192 5.4 split
 //     by 8, 11.7; 128 tokens, n = 4096, k = 14336 (64 tiles) 18.1 and 20.9.  A step of K takes a CTA about 0.15 us; sharing costs about 1.2 us, and
-//     0.03 us per token of the tile, whose parts have to be added up.  With more tiles it does not pay: n = 8192, k = 2048 (64) 7.3 and 6.8;
+//     0.03 us per token of the tile, whose parts have to be added up (0.3 us less since the scales are asked for early: 6.0, 5.0 and 16.8 now).  With more
+//     tiles it does not pay: n = 8192, k = 2048 (64) 7.3 and 6.8;
 //   up to 64 tokens per expert, or where tiles of 64 fit one wave of the 148 CTAs, single CTAs: 16 experts of 64 tokens 48.4 against 49.4 in
 //     pairs (of 128: 61.1 against 55.8); 256 tokens, n = k = 4096 9.4 against 11.7.  Tiles of 32 where those fit the wave: 64 tokens, n = k = 4096
 //     8.5 against 9.2;

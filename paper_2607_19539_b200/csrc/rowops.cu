@@ -1,8 +1,9 @@
 // Row operators in front of and between the expert products: RMS norm of a sum with an optional 8-bit output, its
 // gradient, and the gated activation with an 8-bit output (entry points in include/moe_ovl.h).
 //
-// All of them read each element once, need one reduction over the row, and write once: they are bound by HBM.  A row is
-// held in registers between the two (NV packs of VEC elements per thread), so nothing is read twice.  The row's
+// All of them read each element once, need one reduction over the row, and write once: aligned rows of up to 16384 columns of 16 bits are bound by
+// HBM.  A row is held in registers between the two (NV packs of VEC elements per thread), so nothing is read twice; wider rows
+// (f32: beyond 8192 columns) are more than 512 threads' registers hold and spill (norm of 4000 x 24576, bf16: 275 us where the bytes take 105).  The row's
 // threads are one block, or one warp where the row is short (several rows per block then, and no block barrier).  Blocks
 // stay and take rows at a fixed distance, and what belongs to a column (weights, the weight gradient's sums) stays in registers.
 // The next row's loads are under way while a row is reduced and written: into registers, and in the gradient's kernel, which has
@@ -528,8 +529,8 @@ struct SwigluP {
 };
 
 // g / (1 + exp(-g)) by the approximate power of two and reciprocal: relative error about 2^-22 + |g| 2^-24 before the rounding to
-// 8 bits (a row with g < -75 throughout is zeros anyway).  The full exponential and division take 20 instructions more per element,
-// and the kernel would be bound by them, not by HBM.  exp(-g) = inf gives g * 0.
+// 8 bits, 2^-17 at g = -80.  The full exponential and division take 20 instructions more per element, and the kernel would be bound by them,
+// not by HBM.  From exp(-g) = 2^126 on (g < -87.3; infinite beyond -88.7) the reciprocal is 0, and so is the result, of less than 2^-119.
 __device__ __forceinline__ float2 silu2(float2 g)
 {
     const float2 p = mul2(g, both(-1.4426950408889634f));
@@ -750,8 +751,8 @@ extern "C" int moe_ovl_add_norm(const moe_ovl_norm_args *a)
             const RowShape s = row_shape<VEC>(a->rows, p.d, VEC >= 4 ? VEC : 8, max_threads, RAGGED);
             return with_packs(s.packs, norm_packs<VEC>(), [&](auto n) {
                 constexpr int NV = decltype(n)::value;
-                // An 8-bit output alone: blocks per SM count (16384 x 4096: 72 us in 40 registers, 80 us in 64).  With an output in the type of x the
-                // writes are what bounds it, and fewer blocks write better (87 us in 64, 92 us in 40).
+                // An 8-bit output alone: blocks per SM count (16384 x 4096, bf16: 71 us in 40 registers, 80 us in 64).  With an output in the type of x the
+                // writes are what bounds it, and fewer blocks write better (85 us in 64, 92 us in 40).  f32 rows of 4097 to 8192 columns spill in 40.
                 const auto kernel = p.q && !p.y ? add_norm_lean_kernel<T, W, VEC, NV, RAGGED> : add_norm_kernel<T, W, VEC, NV, RAGGED>;
                 return launch_rows(kernel, p, s, RAGGED, a->device, static_cast<cudaStream_t>(a->stream));
             });

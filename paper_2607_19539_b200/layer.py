@@ -42,7 +42,8 @@ def routed_rows(expert: torch.Tensor, gate: torch.Tensor, counts: torch.Tensor) 
 
 class QuantExpertLayer:
     """norm_weight [d]; router [experts, d]; w1 [experts, 2F, d] (gate rows, then up rows) and w2 [experts, d, F] in bf16, kept in 8 bits.
-    Buffers are sized for `max_tokens` and reused by every call on the current stream."""
+    Buffers are sized for `max_tokens` and reused by every call on the current stream; `status[0]` is not 0 when a bounded wait inside a product
+    gave up, and the outputs since then are not to be used (nothing waits for it here: look after a synchronize of your own)."""
 
     def __init__(self, norm_weight, router, w1, w2, *, top_k: int, max_tokens: int, eps: float = 1e-6, score: int = ops.SCORE_SOFTMAX, bias=None,
                  num_groups: int = 1, top_groups: int = 1, group_best: int = 1, renormalise: bool = True, gate_scale: float = 1.0):
