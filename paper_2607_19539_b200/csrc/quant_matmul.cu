@@ -528,6 +528,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
             }
             if (leader) {
                 if (CTAS == 1) umma_commit_one(bar_drain);      // every MMA has finished before tensor memory goes
+                else if (ok) umma_commit_self(bar_drain);       // the peer has waited for its last accumulator, and does not wait for this
                 else umma_commit_pair(bar_drain);
             }
             drain(bar_drain, 0, globaltimer_ns());
