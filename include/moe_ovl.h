@@ -533,6 +533,142 @@ typedef struct {
 } moe_ovl_quant_matmul_args;
 int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *args);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators for training experts, and for experts whose weights and activations are held in 8-bit floats.  What is said of the operators
+ * above holds for them too, `status` and its bounded waits included.  Here the operands of a product have to begin on 16 bytes, and so have their
+ * rows and matrices (MOE_OVL_ERR_UNSUPPORTED otherwise); their sizes are free. */
+
+#define MOE_OVL_MAX_GROUPS 1024    /* most experts of a product */
+#define MOE_OVL_MAX_MATMUL 16777216 /* largest n and k of a product, and longest row of the quantiser */
+#define MOE_OVL_MAX_TENSORS 65536  /* most tensors of a list of gradients */
+#define MOE_OVL_MATMUL_TEST_NO_LOADS 1u /* test hook: no tile is ever loaded, so the bounded waits run out */
+
+/* Product of 16-bit floats grouped by expert:
+ *   out[m][n] = sum_k a[m][k] * b[e][n][k]            b [num_experts, n, k]
+ *             = sum_k a[m][k] * b[e][k][n]            b [num_experts, k, n], with `transposed`
+ * summed in 32 bits and rounded once.  Rows are grouped by expert_counts as in moe_ovl_quant_matmul; without them there is one matrix b.  The gradient of
+ * a is a product again, with `transposed` the other way round: da = moe_ovl_grouped_matmul(dout, b). */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, n, k;
+    int32_t num_experts;          /* 0: one matrix b; at most MOE_OVL_MAX_GROUPS */
+    int32_t dtype;                /* of a and b: MOE_OVL_BF16 or MOE_OVL_F16 */
+    int32_t out_dtype;            /* that type, or MOE_OVL_F32 */
+    int32_t transposed;           /* 0 or 1 */
+    int32_t wait_timeout_us;      /* bound on every device-side wait; 0 = default (2 s) */
+    uint32_t flags;               /* 0, or MOE_OVL_MATMUL_TEST_NO_LOADS */
+    const void *a;                /* [rows, k] */
+    const void *b;
+    const int32_t *expert_counts; /* [num_experts], NULL without experts */
+    void *out;                    /* [rows, n] */
+    int32_t *status;              /* [4] */
+    int64_t a_stride, b_stride;   /* between rows */
+    int64_t b_expert_stride;      /* between matrices */
+    int64_t out_stride;
+    void *stream;
+} moe_ovl_grouped_matmul_args;
+int moe_ovl_grouped_matmul(const moe_ovl_grouped_matmul_args *args);
+
+/* Gradient of its weights:  dweight[e][n][k] (+)= sum over the rows m of expert e of dy[m][n] * x[m][k], in 32 bits, each value by one
+ * thread in the order of the rows (the same call gives the same bits).  An expert without rows gets zeros, or with `accumulate` keeps what it has; rows behind
+ * the last expert's are not looked at.  For b [num_experts, k, n] pass x as dy and dy as x. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, n, k;
+    int32_t num_experts;          /* 0: one matrix */
+    int32_t dtype;                /* of dy and x: MOE_OVL_BF16 or MOE_OVL_F16 */
+    int32_t out_dtype;            /* of dweight: that type, or MOE_OVL_F32 */
+    int32_t accumulate;           /* 1: added to what dweight holds, in 32 bits and rounded once */
+    int32_t wait_timeout_us;
+    uint32_t flags;               /* 0, or MOE_OVL_MATMUL_TEST_NO_LOADS */
+    const void *dy;               /* [rows, n] */
+    const void *x;                /* [rows, k] */
+    const int32_t *expert_counts; /* [num_experts], NULL without experts */
+    void *dweight;                /* [num_experts, n, k] */
+    int32_t *status;              /* [4] */
+    void *workspace;              /* DEVICE, 128-byte aligned; contents need not be kept or cleared.  Calls that may run at once need one each */
+    size_t workspace_bytes;       /* >= moe_ovl_grouped_matmul_workspace_bytes */
+    int64_t dy_stride, x_stride, dweight_stride;
+    int64_t dweight_expert_stride;
+    void *stream;
+} moe_ovl_grouped_matmul_backward_args;
+int moe_ovl_grouped_matmul_workspace_bytes(int32_t num_experts, size_t *bytes);
+int moe_ovl_grouped_matmul_backward(const moe_ovl_grouped_matmul_backward_args *args);
+
+/* Values in 8-bit floats (e4m3: four significant bits, largest 448) with a scale for each block:
+ *   v = x, or with `gated` g / (1 + exp(-g)) * u of x [rows, 2k] = g | u;
+ *   scale = max|v| / 448 of the block, q = v * 448 / max|v| divided in 32 bits, then to the nearest of e4m3, ties to even: v ~ q * scale.
+ * A block is 128 neighbours of a row (activations), or with `tiles` 128 x 128 values of a matrix (weights); the last ones may be shorter.
+ * A block whose max|v| is below 2^-100 gives zeros; one that holds a NaN or an infinity gives a NaN scale and q = 0. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t depth;                /* matrices; 1 without `tiles` */
+    int32_t rows, k;              /* of q */
+    int32_t dtype;                /* of x: MOE_OVL_BF16 ... */
+    int32_t gated, tiles;         /* 0 or 1, not both */
+    uint32_t flags;               /* 0 */
+    const void *x;                /* [depth, rows, k], gated [rows, 2k] */
+    void *q;                      /* [depth, rows, k] */
+    float *scale;                 /* [rows, ceil(k / 128)], tiles [depth, ceil(rows / 128), ceil(k / 128)]; contiguous */
+    int64_t x_stride, q_stride;   /* between rows */
+    int64_t x_far, q_far;         /* between matrices */
+    void *stream;
+} moe_ovl_block_quant_args;
+int moe_ovl_block_quant(const moe_ovl_block_quant_args *args);
+
+/* Product of 8-bit floats with a scale for each block of 128, dense or per expert as moe_ovl_quant_matmul:
+ *   out[m][n] = sum over the blocks B of K of a_scale[m][B] * b_scale[e][n / 128][B] * (sum over k in B of a[m][k] * b[e][n][k])
+ * in 32 bits, rounded once.  Operands as moe_ovl_block_quant writes them, b with `tiles`. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t rows, n, k;
+    int32_t num_experts;          /* 0: one matrix b */
+    int32_t out_dtype;
+    int32_t wait_timeout_us;
+    uint32_t flags;               /* 0, or MOE_OVL_MATMUL_TEST_NO_LOADS */
+    const void *a;                /* [rows, k] e4m3 */
+    const float *a_scale;         /* [rows, ceil(k / 128)], contiguous */
+    const void *b;                /* [num_experts, n, k] e4m3 */
+    const float *b_scale;         /* [num_experts, ceil(n / 128), ceil(k / 128)], contiguous */
+    const int32_t *expert_counts; /* [num_experts], NULL without experts */
+    void *out;                    /* [rows, n] */
+    int32_t *status;              /* [4] */
+    int64_t a_stride, b_stride;   /* between rows */
+    int64_t b_expert_stride;      /* between matrices */
+    int64_t out_stride;
+    void *stream;
+} moe_ovl_block_matmul_args;
+int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *args);
+
+/* Norm of a list of gradients, and clipping by it.  Two calls: where the gradients are spread over ranks, their norms are combined in between.
+ *   moe_ovl_grad_norm:   norm = sqrt(sum over all values of all tensors of g^2), in 64 bits beyond a thread's share, in a fixed order
+ *   moe_ovl_clip_grads:  out = g * min(1, max_norm / (norm + eps)), in 32 bits and rounded once
+ * A norm that is infinite makes the factor 0, one that is NaN makes it NaN.  The tensors of a list have any of the types each, lie densely in
+ * memory (in whatever order) and must not overlap; the lists are HOST arrays, read before the call returns.  Without `out` the gradients are clipped where
+ * they lie, and not written at all when the factor is 1. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t device;
+    int32_t num_tensors;          /* at most MOE_OVL_MAX_TENSORS */
+    uint32_t flags;               /* 0 */
+    const void *const *grads;     /* HOST array of DEVICE pointers */
+    void *const *out;             /* HOST array, or NULL (moe_ovl_clip_grads alone looks at it) */
+    const int64_t *sizes;         /* HOST array: values of each tensor */
+    const int32_t *dtypes;        /* HOST array: MOE_OVL_BF16 ... */
+    float *norm;                  /* DEVICE, one value */
+    float max_norm, eps;          /* moe_ovl_clip_grads: >= 0 */
+    void *workspace;              /* moe_ovl_grad_norm: DEVICE, 8-byte aligned; contents need not be kept or cleared.  Calls that may run at once need one each */
+    size_t workspace_bytes;       /* >= moe_ovl_grad_norm_workspace_bytes */
+    void *stream;
+} moe_ovl_grads_args;
+int moe_ovl_grad_norm_workspace_bytes(int32_t num_tensors, size_t *bytes);
+int moe_ovl_grad_norm(const moe_ovl_grads_args *args);
+int moe_ovl_clip_grads(const moe_ovl_grads_args *args);
+
 const char *moe_ovl_strerror(int code);
 /* cudaError_t of the last failing CUDA call made through this context (0 if none). */
 int moe_ovl_last_cuda_error(const moe_ovl_ctx *ctx);

@@ -38,6 +38,8 @@ EXPORTS = [
     "moe_ovl_return_slots_static", "moe_ovl_get_trace",
     "moe_ovl_add_norm", "moe_ovl_add_norm_workspace_bytes", "moe_ovl_add_norm_backward", "moe_ovl_swiglu_quant",
     "moe_ovl_route", "moe_ovl_route_backward", "moe_ovl_quant_matmul",
+    "moe_ovl_grouped_matmul", "moe_ovl_grouped_matmul_workspace_bytes", "moe_ovl_grouped_matmul_backward", "moe_ovl_block_quant",
+    "moe_ovl_block_matmul", "moe_ovl_grad_norm_workspace_bytes", "moe_ovl_grad_norm", "moe_ovl_clip_grads",
 ]
 
 
@@ -143,8 +145,11 @@ def load(rebuild_if_stale: bool = True) -> C.CDLL:
     lib.moe_ovl_last_cuda_error.argtypes = [C.c_void_p]
     lib.moe_ovl_return_slots_static.argtypes = [C.c_int32] * 5 + [C.c_void_p] * 6
     lib.moe_ovl_add_norm_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+    for name in ("moe_ovl_grouped_matmul_workspace_bytes", "moe_ovl_grad_norm_workspace_bytes"):
+        getattr(lib, name).argtypes = [C.c_int32, C.POINTER(C.c_size_t)]
     for name in ("moe_ovl_add_norm", "moe_ovl_add_norm_backward", "moe_ovl_swiglu_quant", "moe_ovl_route",
-                 "moe_ovl_route_backward", "moe_ovl_quant_matmul"):
+                 "moe_ovl_route_backward", "moe_ovl_quant_matmul", "moe_ovl_grouped_matmul", "moe_ovl_grouped_matmul_backward",
+                 "moe_ovl_block_quant", "moe_ovl_block_matmul", "moe_ovl_grad_norm", "moe_ovl_clip_grads"):
         getattr(lib, name).argtypes = [C.c_void_p]
     _lib = lib
     return lib

@@ -8,8 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe_ovl.so")
-SOURCES = ["moe_ovl.cu", "noalloc.cu", "rowops.cu", "route.cu", "quant_matmul.cu"]
-HEADERS = ["common.cuh", "plan.cuh", "producer.cuh", "mover.cuh", "ptx.cuh", "opcommon.cuh", os.path.join("..", "..", "include", "moe_ovl.h")]
+SOURCES = ["moe_ovl.cu", "noalloc.cu", "rowops.cu", "route.cu", "quant_matmul.cu", "grouped_matmul.cu", "block_matmul.cu",
+           "block_quant.cu", "gradients.cu"]
+HEADERS = ["common.cuh", "plan.cuh", "producer.cuh", "mover.cuh", "ptx.cuh", "opcommon.cuh", "matmul_tiles.cuh", os.path.join("..", "..", "include", "moe_ovl.h")]
 
 
 def _nvcc() -> str:

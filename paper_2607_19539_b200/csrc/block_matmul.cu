@@ -1,0 +1,328 @@
+// Product of 8-bit floats (e4m3) with a scale for each block of 128, dense or per expert (moe_ovl_block_matmul in include/moe_ovl.h):
+//   out[m][n] = sum over the blocks B of K of a_scale[m][B] * b_scale[e][n / 128][B] * (sum over k in B of a[m][k] * b[e][n][k]).
+//
+// A block's sum comes out of the tensor cores in 32 bits; the scales differ from block to block, so each block's sums are
+// multiplied and added up in registers: one fused operation per output and block, beside the tensor cores' 128.  A step of the pipeline is one block
+// of K, and accumulators in tensor memory go round step by step, so that the next block multiplies while this one is added.
+//
+// Many rows (BlockRows): rows of a on the matrix instruction's M side, one per lane of the accumulator.  A thread then holds one row,
+// and the columns it adds up lie in one block of channels: one factor per thread and step.
+// Few rows (BlockFew): channels on the M side and the rows on the N side, whose size goes in steps of 16; the weights are streamed, and the factors,
+// one per row, are dealt out through shared memory.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "matmul_tiles.cuh"
+
+using namespace moe_ovl;
+
+namespace {
+
+constexpr int BM_M_BYTES = TILE_CHANNELS * STAGE_ROW;
+
+struct BmP {
+    int rows, n, k, experts;
+    int row_tiles;                           // tiles of channels per expert
+    int blocks, channel_blocks;              // of 128, along K and along n
+    const int *counts;
+    const float *a_scale, *b_scale;
+    void *out;
+    long long out_stride;
+    int *status;
+    unsigned long long timeout_ns;
+    bool no_loads;                           // test hook
+    bool wide;                               // rows of the output begin on 16 bytes
+};
+
+// The wait for values asked of tensor memory; they are operands so that no use of them can move in front of it.
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                   "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ float2 pair_of(const uint32_t *v) { return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])); }
+
+// Instruction descriptor: 32-bit sums of e4m3, K along the rows of both operands.
+__device__ __forceinline__ uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t d, uint32_t stage16, uint32_t idesc)
+{
+    const uint64_t dm = umma_smem_desc(0) + stage16, dn = dm + BM_M_BYTES / 16;
+#pragma unroll
+    for (int i = 0; i < STAGE_ROW / 32; ++i) umma_f8<CTAS>(d, dm + (uint64_t)(i * 2), dn + (uint64_t)(i * 2), idesc, i > 0 ? 1u : 0u);
+}
+
+// ------------------------------------------------------------------ many rows
+
+template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
+    static constexpr int TOKENS = CTAS * TILE_CHANNELS, SHARE = CHANNELS / CTAS, COLS = CHANNELS / 2;
+    using Shape = TileShape<CTAS, BM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 512 / CHANNELS, CHANNELS, 8, true>;
+    using Schedule = TileSchedule<CHANNELS, TOKENS>;
+    using Tile = typename Schedule::Tile;
+    const BmP &p;
+    const CUtensorMap *map_a, *map_b;
+    int *tile_start, *row_start;
+    Schedule sched;
+    int rank = 0;
+
+    struct From { int a0, b0, expert; };
+    __device__ __forceinline__ void begin(int lane) { fill_schedule<TOKENS>(p, tile_start, row_start, count_of(p, lane), lane); }
+    __device__ __forceinline__ long long total() const { return sched.total(p.counts ? p.experts : 1); }
+    __device__ __forceinline__ Tile at(long long t) { return sched.at(t); }
+    __device__ __forceinline__ int steps(const Tile &) const { return p.blocks; }
+    __device__ __forceinline__ From operands(const Tile &t, bool) const
+    {
+        return {uniform((int)((unsigned)t.row0 + (unsigned)(rank * TILE_CHANNELS))), uniform(t.channel0 + rank * SHARE), uniform(t.expert)};
+    }
+    __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
+    {
+        load_2d<CTAS>(sa, map_a, bar, step * STAGE_ROW, f.a0);
+        load_3d<CTAS>(sa + BM_M_BYTES, map_b, bar, step * STAGE_ROW, f.b0, f.expert);
+    }
+    __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TOKENS, CHANNELS); }
+    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool) const { multiply_step<CTAS>(d, stage16, idesc); }
+    __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
+    {
+        const int quarter = (warp + 2) & 3, half = warp >> 2;        // a warp reads the lanes of its position among four, and half of the columns
+        const int in_tile = rank * TILE_CHANNELS + quarter * 32 + lane;
+        const bool mine = in_tile < t.rows;
+        const int ch0 = t.channel0 + half * COLS, block = ch0 / 128;
+        const float *sa = p.a_scale + (long long)(t.row0 + (mine ? in_tile : 0)) * p.blocks;
+        const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + min(block, p.channel_blocks - 1)) * p.blocks;
+        float2 acc[COLS / 2];
+#pragma unroll
+        for (int i = 0; i < COLS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+        float a_next = sa[0], b_next = sb[0];
+        for (int k = 0; k < p.blocks; ++k) {
+            const float2 s = both(a_next * b_next);
+            if (k + 1 < p.blocks) a_next = sa[k + 1], b_next = sb[k + 1];
+            if (!accs.wait(p, t.row0)) return false;
+            const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
+            uint32_t v[2][16];
+            tmem_ld16(from, v[0]);
+#pragma unroll
+            for (int c = 0; c < COLS / 16; ++c) {
+                tmem_ld_wait16(v[c & 1]);
+                if (c + 1 < COLS / 16) tmem_ld16(from + 16 * (c + 1), v[(c + 1) & 1]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[c * 8 + j] = fma2(pair_of(&v[c & 1][2 * j]), s, acc[c * 8 + j]);
+            }
+            accs.release();
+        }
+        if (mine) {
+            Out *out = static_cast<Out *>(p.out) + (long long)(t.row0 + in_tile) * p.out_stride + ch0;
+            const int left = p.n - ch0;
+            constexpr int VEC = 16 / sizeof(Out);
+            if (p.wide && left >= COLS) {
+#pragma unroll
+                for (int i = 0; i < COLS; i += VEC) {
+                    Pack<Out, VEC> pack;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) pack.v[j] = from_f32<Out>((i + j) & 1 ? acc[(i + j) / 2].y : acc[(i + j) / 2].x);
+                    store_pack(out + i, pack);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < COLS; ++i)
+                    if (i < left) out[i] = from_f32<Out>(i & 1 ? acc[i / 2].y : acc[i / 2].x);
+            }
+        }
+        return true;
+    }
+};
+
+// ------------------------------------------------------------------ few rows
+
+template <int TOKENS_, typename Out> struct BlockFew {
+    static constexpr int TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
+    using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, 200 * 1024, 256 / COLS, COLS, 4, true>;
+    using Schedule = TileSchedule<TILE_CHANNELS, TOKENS>;
+    using Tile = typename Schedule::Tile;
+    const BmP &p;
+    const CUtensorMap *map_a, *map_b;
+    int *tile_start, *row_start;
+    float *factors;                          // [4 warps][2][TOKENS]
+    Schedule sched;
+    int rank = 0;
+
+    struct From { int a0, b0, expert; };
+    __device__ __forceinline__ void begin(int lane) { fill_schedule<TOKENS>(p, tile_start, row_start, count_of(p, lane), lane); }
+    __device__ __forceinline__ long long total() const { return sched.total(p.counts ? p.experts : 1); }
+    __device__ __forceinline__ Tile at(long long t) { return sched.at(t); }
+    __device__ __forceinline__ int steps(const Tile &) const { return p.blocks; }
+    __device__ __forceinline__ From operands(const Tile &t, bool) const { return {uniform(t.row0), uniform(t.channel0), uniform(t.expert)}; }
+    __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
+    {
+        load_3d<1>(sa, map_b, bar, step * STAGE_ROW, f.b0, f.expert);
+        load_2d<1>(sa + BM_M_BYTES, map_a, bar, step * STAGE_ROW, f.a0);
+    }
+    __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TILE_CHANNELS, TOKENS); }
+    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool) const { multiply_step<1>(d, stage16, idesc); }
+    __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
+    {
+        constexpr int PER_LANE = (TOKENS + 31) / 32;
+        const int quarter = (warp + 2) & 3, ch = t.channel0 + quarter * 32 + lane;
+        float *own = factors + warp * 2 * TOKENS;
+        const float *sa = p.a_scale + (long long)t.row0 * p.blocks;
+        const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + t.channel0 / 128) * p.blocks;
+        float2 acc[TOKENS / 2];
+#pragma unroll
+        for (int i = 0; i < TOKENS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+        float a_next[PER_LANE] = {}, b_next = sb[0];
+        auto ask = [&](int k) {
+#pragma unroll
+            for (int i = 0; i < PER_LANE; ++i)
+                if (i * 32 + lane < t.rows) a_next[i] = sa[(long long)(i * 32 + lane) * p.blocks + k];
+            b_next = sb[k];
+        };
+        ask(0);
+        for (int k = 0; k < p.blocks; ++k) {
+            float *s = own + (k & 1) * TOKENS;           // two, so that a lane still reading the step before is not overtaken
+#pragma unroll
+            for (int i = 0; i < PER_LANE; ++i)
+                if (i * 32 + lane < TOKENS) s[i * 32 + lane] = a_next[i] * b_next;
+            if (k + 1 < p.blocks) ask(k + 1);
+            __syncwarp();
+            if (!accs.wait(p, t.row0)) return false;
+            const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+            for (int c = 0; c < TOKENS; c += 16) {
+                if (c < t.rows) {
+                    uint32_t v[16];
+                    tmem_ld16(from + c, v);
+                    tmem_ld_wait16(v);
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(s + c + j);
+                        acc[(c + j) / 2] = fma2(pair_of(&v[j]), make_float2(f.x, f.y), acc[(c + j) / 2]);
+                        acc[(c + j) / 2 + 1] = fma2(pair_of(&v[j + 2]), make_float2(f.z, f.w), acc[(c + j) / 2 + 1]);
+                    }
+                }
+            }
+            accs.release();
+        }
+        if ((unsigned)ch < (unsigned)p.n) {
+            Out *out = static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride + ch;
+#pragma unroll
+            for (int j = 0; j < TOKENS; ++j) {
+                if (j < t.rows) *out = from_f32<Out>(j & 1 ? acc[j / 2].y : acc[j / 2].x);
+                out += p.out_stride;
+            }
+        }
+        __syncwarp();
+        return true;
+    }
+};
+
+template <int CTAS, int CHANNELS, typename Out>
+__global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, Out>::Shape::THREADS, 1)
+block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int s_tile_start[1025], s_row_start[1025];
+    run_tiles(BlockRows<CTAS, CHANNELS, Out>{p, &map_a, &map_b, s_tile_start, s_row_start, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+}
+
+template <int TOKENS, typename Out>
+__global__ void __launch_bounds__(BlockFew<TOKENS, Out>::Shape::THREADS, 1)
+block_matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int s_tile_start[1025], s_row_start[1025];
+    __shared__ __align__(16) float s_factors[4 * 2 * TOKENS];
+    run_tiles(BlockFew<TOKENS, Out>{p, &map_a, &map_b, s_tile_start, s_row_start, s_factors, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+}
+
+struct BmOperands { const void *a, *b; long long a_stride, b_stride, b_far; };
+
+bool encode_operands(const BmP &p, const BmOperands &o, int a_rows, int b_rows, CUtensorMap *a, CUtensorMap *b)
+{
+    return encode_tiles(a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.a, p.k, p.rows, o.a_stride, 0, 0, a_rows) &&
+           encode_tiles(b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.b, p.k, p.n, o.b_stride, std::max(p.experts, 1), o.b_far, b_rows);
+}
+
+template <int CTAS, int CHANNELS, typename Out>
+int launch_rows(BmP p, const BmOperands &o, int device, cudaStream_t stream)
+{
+    using Shape = typename BlockRows<CTAS, CHANNELS, Out>::Shape;
+    CUtensorMap a, b;
+    p.row_tiles = (p.n - 1) / CHANNELS + 1;
+    if (!encode_operands(p, o, TILE_CHANNELS, CHANNELS / CTAS, &a, &b)) return MOE_OVL_ERR_CUDA;
+    static std::atomic<unsigned long long> allowed{0};
+    const auto kernel = block_matmul_kernel<CTAS, CHANNELS, Out>;
+    if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    return launch_behind(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), dim3(Shape::THREADS), Shape::SMEM, CTAS, stream, a, b, p);
+}
+
+template <int TOKENS, typename Out>
+int launch_few(BmP p, const BmOperands &o, int device, cudaStream_t stream)
+{
+    using Shape = typename BlockFew<TOKENS, Out>::Shape;
+    CUtensorMap a, b;
+    p.row_tiles = (p.n - 1) / TILE_CHANNELS + 1;
+    if (!encode_operands(p, o, TOKENS, TILE_CHANNELS, &a, &b)) return MOE_OVL_ERR_CUDA;
+    static std::atomic<unsigned long long> allowed{0};
+    const auto kernel = block_matmul_few_kernel<TOKENS, Out>;
+    if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    return launch_behind(kernel, (unsigned)sm_count(device), dim3(Shape::THREADS), Shape::SMEM, 1, stream, a, b, p);
+}
+
+// ctas 0: few rows, `tile` of them; else `tile` channels.
+struct BmChoice { int ctas, tile; };
+
+BmChoice choose(const BmP &p)
+{
+    const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows - 1) / groups + 1;
+    if (per_group <= 16) return {0, p.experts && per_group > 4 ? 32 : 16};
+    if (per_group <= 32) return {0, p.experts ? 64 : 32};
+    if (per_group <= 64) return {0, 64};
+    const long long pairs = (long long)((p.n - 1) / 256 + 1) * groups * ((per_group - 1) / 256 + 1);
+    return pairs >= 37 ? BmChoice{2, 256} : BmChoice{1, 128};
+}
+
+}  // namespace
+
+extern "C" int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *a)
+{
+    if (!a || a->struct_size != sizeof(*a) || a->device < 0 || a->rows < 0 || a->n < 1 || a->k < 1 || a->num_experts < 0 ||
+        (a->flags & ~MOE_OVL_MATMUL_TEST_NO_LOADS) != 0 || a->wait_timeout_us < 0 || !known_dtype(a->out_dtype) ||
+        (a->num_experts > 0) != (a->expert_counts != nullptr))
+        return MOE_OVL_ERR_INVALID_ARG;
+    if (a->num_experts > MOE_OVL_MAX_GROUPS || a->n > MOE_OVL_MAX_MATMUL || a->k > MOE_OVL_MAX_MATMUL) return MOE_OVL_ERR_UNSUPPORTED;
+    if (a->rows == 0) return MOE_OVL_OK;
+    const int es = dtype_bytes(a->out_dtype), experts = std::max(a->num_experts, 1);
+    if (!a->a || !a->a_scale || !a->b || !a->b_scale || !a->out || !a->status || !aligned(a->a_scale, 4) || !aligned(a->b_scale, 4) ||
+        !aligned(a->out, es) || !aligned(a->status, 4) || !aligned(a->expert_counts, 4) || (a->rows > 1 && (a->a_stride < a->k || a->out_stride < a->n)) ||
+        (a->n > 1 && a->b_stride < a->k) || (experts > 1 && a->b_expert_stride < 1))
+        return MOE_OVL_ERR_INVALID_ARG;
+    if (std::max(std::max(a->a_stride, a->b_stride), a->out_stride) > 0x7fffffff || a->b_expert_stride >= 1ll << 40) return MOE_OVL_ERR_UNSUPPORTED;
+    // strides that are never used: the tensor map wants some that hold the row and are multiples of 16 bytes
+    const long long sa = a->rows > 1 ? a->a_stride : (a->k + 15ll) / 16 * 16, sb = a->n > 1 ? a->b_stride : (a->k + 15ll) / 16 * 16;
+    const long long far = experts > 1 ? a->b_expert_stride : a->n * sb;
+    if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 16 != 0 || sb % 16 != 0 || far % 16 != 0) return MOE_OVL_ERR_UNSUPPORTED;
+    DeviceGuard guard(a->device);
+    if (!guard.ok) return MOE_OVL_ERR_CUDA;
+    BmP p = {};
+    p.rows = a->rows, p.n = a->n, p.k = a->k, p.experts = a->num_experts, p.counts = a->expert_counts;
+    p.blocks = (a->k - 1) / 128 + 1, p.channel_blocks = (a->n - 1) / 128 + 1;
+    p.a_scale = a->a_scale, p.b_scale = a->b_scale, p.out = a->out, p.out_stride = a->out_stride, p.status = a->status;
+    p.timeout_ns = a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : TILE_TIMEOUT_NS;
+    p.no_loads = (a->flags & MOE_OVL_MATMUL_TEST_NO_LOADS) != 0;
+    p.wide = aligned(a->out, 16) && (a->rows == 1 || a->out_stride * es % 16 == 0);
+    const BmOperands o = {a->a, a->b, sa, sb, far};
+    const BmChoice c = choose(p);
+    const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+    return with_dtype(a->out_dtype, [&](auto t) {
+        using Out = decltype(t);
+        if (c.ctas == 2) return launch_rows<2, 256, Out>(p, o, a->device, stream);
+        if (c.ctas == 1) return launch_rows<1, 128, Out>(p, o, a->device, stream);
+        switch (c.tile) {
+        case 16: return launch_few<16, Out>(p, o, a->device, stream);
+        case 32: return launch_few<32, Out>(p, o, a->device, stream);
+        default: return launch_few<64, Out>(p, o, a->device, stream);
+        }
+    });
+}

@@ -1,0 +1,272 @@
+// Norm of a list of gradients and clipping by it (moe_ovl_grad_norm, moe_ovl_clip_grads in include/moe_ovl.h).
+//
+// A list goes to the kernel as a parameter, up to LIST_LONG tensors per launch, so no table has to be copied or kept on the device.  The
+// elements of all its tensors are dealt out in chunks, a contiguous run of them to each block, which finds its first tensor by bisection
+// and walks on from there.  Squares are summed in 32 bits over a thread's share of a chunk (32 values at most) and in 64 bits beyond; a share whose 32-bit
+// sum overflows, or is so small that squares may have vanished, is summed again in 64.  Every block's sum has its place in the workspace and one
+// block adds them up in order: the same call gives the same bits.
+#include <algorithm>
+
+#include "opcommon.cuh"
+
+using namespace moe_ovl;
+
+namespace {
+
+constexpr int GN_THREADS = 256, GN_PER_THREAD = 32, GN_CHUNK = GN_THREADS * GN_PER_THREAD;
+constexpr int GN_BLOCKS = 148 * 4;           // most blocks of a launch
+constexpr int LIST_SHORT = 32, LIST_LONG = 960;      // 32 KB of parameters are allowed
+
+struct Tensor {
+    const void *from;
+    void *to;
+    long long size;
+    unsigned chunk;                          // chunks in front of it
+    int dtype;
+};
+template <int N> struct TensorList {
+    int count;
+    unsigned chunks;
+    Tensor t[N];
+};
+
+template <int N> __device__ __forceinline__ int tensor_at(const TensorList<N> &list, unsigned chunk)
+{
+    int lo = 0, hi = list.count - 1;         // the last one whose first chunk is not behind
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (list.t[mid].chunk <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// The values of a chunk that are this thread's: f(index of a pack's first value, values in it (VEC or 1)).  Packs of 16 bytes where the memory allows, single
+// values in front of the first and behind the last.
+template <int VEC, typename F> __device__ __forceinline__ void for_packs(long long begin, long long end, int head, F f)
+{
+    const long long first = min(begin + head, end), packs = (end - first) / VEC;
+    if (begin + (int)threadIdx.x < first) f(begin + (int)threadIdx.x, false);
+#pragma unroll 4
+    for (long long i = threadIdx.x; i < packs; i += GN_THREADS) f(first + i * VEC, true);
+    const long long last = first + packs * VEC + (int)threadIdx.x;
+    if (last < end) f(last, false);
+}
+template <typename T> __device__ __forceinline__ int head_of(const T *p) { return (int)((16u - ((unsigned)(unsigned long long)p & 15u)) & 15u) / (int)sizeof(T); }
+
+template <typename T> __device__ __forceinline__ double chunk_sum(const T *x, long long begin, long long end)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    const int head = head_of(x + begin);
+    float2 sum = make_float2(0.0f, 0.0f);
+    unsigned bits = 0;                       // of anything but zeros
+    for_packs<VEC>(begin, end, head, [&](long long i, bool whole) {
+        if (whole) {
+            const Pack<T, VEC> a = load_pack<T, VEC>(x + i);
+            const uint4 raw = *reinterpret_cast<const uint4 *>(&a);
+            bits |= raw.x | raw.y | raw.z | raw.w;
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+                const float2 v = to_f32x2(&a.v[e]);
+                sum = fma2(v, v, sum);
+            }
+        } else {
+            const float v = to_f32(x[i]);
+            sum.x = fmaf(v, v, sum.x);
+            bits |= __float_as_uint(v);
+        }
+    });
+    const float both_sums = sum.x + sum.y;
+    if (both_sums >= 1e-30f && both_sums <= 1e38f) return (double)both_sums;
+    if (bits == 0) return 0.0;
+    double wide = 0.0;
+    for_packs<1>(begin, end, 0, [&](long long i, bool) { wide += (double)to_f32(x[i]) * (double)to_f32(x[i]); });
+    return wide;
+}
+
+__device__ __forceinline__ double block_sum(double v, double *s)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (threadIdx.x % 32 == 0) s[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = 0.0;
+    for (unsigned i = 0; i < blockDim.x / 32; ++i) v += s[i];
+    return v;
+}
+
+template <int N>
+__global__ void __launch_bounds__(GN_THREADS)
+grad_norm_kernel(const __grid_constant__ TensorList<N> list, double *partial)
+{
+    __shared__ double s_sums[GN_THREADS / 32];
+    after_previous();
+    may_follow();
+    const unsigned first = (unsigned)((unsigned long long)list.chunks * blockIdx.x / gridDim.x);
+    const unsigned last = (unsigned)((unsigned long long)list.chunks * (blockIdx.x + 1) / gridDim.x);
+    double sum = 0.0;
+    int at = first < last ? tensor_at(list, first) : 0;
+    for (unsigned c = first; c < last; ++c) {
+        while (at + 1 < list.count && list.t[at + 1].chunk <= c) ++at;
+        const Tensor &t = list.t[at];
+        const long long begin = (long long)(c - t.chunk) * GN_CHUNK, end = min(begin + GN_CHUNK, t.size);
+        if (t.dtype == MOE_OVL_BF16) sum += chunk_sum(static_cast<const __nv_bfloat16 *>(t.from), begin, end);
+        else if (t.dtype == MOE_OVL_F16) sum += chunk_sum(static_cast<const __half *>(t.from), begin, end);
+        else sum += chunk_sum(static_cast<const float *>(t.from), begin, end);
+    }
+    sum = block_sum(sum, s_sums);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+constexpr int GN_FINISH = 512;
+__global__ void __launch_bounds__(GN_FINISH)
+grad_norm_finish_kernel(const double *partial, int count, float *norm)
+{
+    __shared__ double s_sums[GN_FINISH / 32];
+    after_previous();
+    may_follow();
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < count; i += GN_FINISH) sum += partial[i];
+    sum = block_sum(sum, s_sums);
+    if (threadIdx.x == 0) *norm = (float)sqrt(sum);
+}
+
+template <typename T> __device__ __forceinline__ void scale_chunk(const T *x, T *y, long long begin, long long end, float factor)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    auto one = [&](long long i) { y[i] = from_f32<T>(to_f32(x[i]) * factor); };
+    const int head = head_of(x + begin);
+    if (head != head_of(y + begin)) {
+        for_packs<1>(begin, end, 0, [&](long long i, bool) { one(i); });
+        return;
+    }
+    for_packs<VEC>(begin, end, head, [&](long long i, bool whole) {
+        if (!whole) return one(i);
+        Pack<T, VEC> a = load_pack<T, VEC>(x + i);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) a.v[e] = from_f32<T>(to_f32(a.v[e]) * factor);
+        store_pack(y + i, a);
+    });
+}
+
+// Chunks from the last to the first: what the norm has read last is still in L2.
+template <int N>
+__global__ void __launch_bounds__(GN_THREADS)
+clip_grads_kernel(const __grid_constant__ TensorList<N> list, const float *norm, float max_norm, float eps, bool in_place)
+{
+    after_previous();
+    may_follow();
+    const float ratio = __fdiv_rn(max_norm, *norm + eps);
+    const float factor = ratio >= 1.0f ? 1.0f : ratio;           // NaN stays
+    if (in_place && factor == 1.0f) return;
+    const unsigned first = (unsigned)((unsigned long long)list.chunks * blockIdx.x / gridDim.x);
+    const unsigned last = (unsigned)((unsigned long long)list.chunks * (blockIdx.x + 1) / gridDim.x);
+    int at = first < last ? tensor_at(list, last - 1) : 0;
+    for (unsigned c = last; c-- > first;) {
+        while (list.t[at].chunk > c) --at;
+        const Tensor &t = list.t[at];
+        const long long begin = (long long)(c - t.chunk) * GN_CHUNK, end = min(begin + GN_CHUNK, t.size);
+        if (t.dtype == MOE_OVL_BF16) scale_chunk(static_cast<const __nv_bfloat16 *>(t.from), static_cast<__nv_bfloat16 *>(t.to), begin, end, factor);
+        else if (t.dtype == MOE_OVL_F16) scale_chunk(static_cast<const __half *>(t.from), static_cast<__half *>(t.to), begin, end, factor);
+        else scale_chunk(static_cast<const float *>(t.from), static_cast<float *>(t.to), begin, end, factor);
+    }
+}
+
+bool valid(const moe_ovl_grads_args *a)
+{
+    if (!a || a->struct_size != sizeof(*a) || a->device < 0 || a->num_tensors < 0 || a->flags != 0 || !a->norm || !aligned(a->norm, 4)) return false;
+    if (a->num_tensors > 0 && (!a->grads || !a->sizes || !a->dtypes)) return false;
+    for (int i = 0; i < a->num_tensors; ++i)
+        if (!known_dtype(a->dtypes[i]) || a->sizes[i] < 0 || (a->sizes[i] > 0 && (!a->grads[i] || !aligned(a->grads[i], dtype_bytes(a->dtypes[i]))))) return false;
+    return true;
+}
+bool supported(const moe_ovl_grads_args *a)
+{
+    // chunks are counted in 32 bits
+    long long chunks = 0;
+    for (int i = 0; i < a->num_tensors; ++i) {
+        if (a->sizes[i] > 1ll << 42) return false;
+        chunks += (a->sizes[i] + GN_CHUNK - 1) / GN_CHUNK;
+        if (chunks > 0x7fffffff) return false;
+    }
+    return a->num_tensors <= MOE_OVL_MAX_TENSORS;
+}
+
+// Takes the next tensors that are not empty into a list; `next` moves on.
+template <int N> bool fill(TensorList<N> &list, const moe_ovl_grads_args *a, int &next)
+{
+    list.count = 0, list.chunks = 0;
+    for (; next < a->num_tensors && list.count < N; ++next) {
+        if (a->sizes[next] == 0) continue;
+        list.t[list.count++] = {a->grads[next], a->out ? a->out[next] : const_cast<void *>(a->grads[next]), a->sizes[next], list.chunks, a->dtypes[next]};
+        list.chunks += (unsigned)((a->sizes[next] + GN_CHUNK - 1) / GN_CHUNK);
+    }
+    return list.count > 0;
+}
+// Calls f with one list after the other; a short call's list is short, as its parameters are copied for every launch.
+template <typename F> int for_lists(const moe_ovl_grads_args *a, F f)
+{
+    int next = 0, rc = MOE_OVL_OK;
+    auto all = [&](auto &list) {
+        while (rc == MOE_OVL_OK && fill(list, a, next)) rc = f(list);
+    };
+    if (a->num_tensors <= LIST_SHORT) {
+        TensorList<LIST_SHORT> list;
+        all(list);
+    } else {
+        TensorList<LIST_LONG> list;
+        all(list);
+    }
+    return rc;
+}
+int launches_of(int num_tensors) { return (num_tensors + LIST_LONG - 1) / LIST_LONG; }
+
+}  // namespace
+
+extern "C" int moe_ovl_grad_norm_workspace_bytes(int32_t num_tensors, size_t *bytes)
+{
+    if (!bytes || num_tensors < 0) return MOE_OVL_ERR_INVALID_ARG;
+    if (num_tensors > MOE_OVL_MAX_TENSORS) return MOE_OVL_ERR_UNSUPPORTED;
+    *bytes = sizeof(double) * GN_BLOCKS * (size_t)std::max(launches_of(num_tensors), 1);
+    return MOE_OVL_OK;
+}
+
+extern "C" int moe_ovl_grad_norm(const moe_ovl_grads_args *a)
+{
+    if (!valid(a)) return MOE_OVL_ERR_INVALID_ARG;
+    if (!supported(a)) return MOE_OVL_ERR_UNSUPPORTED;
+    size_t need = 0;
+    moe_ovl_grad_norm_workspace_bytes(a->num_tensors, &need);
+    if (!a->workspace || a->workspace_bytes < need || !aligned(a->workspace, 8)) return MOE_OVL_ERR_WORKSPACE;
+    DeviceGuard guard(a->device);
+    if (!guard.ok) return MOE_OVL_ERR_CUDA;
+    const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+    double *partial = static_cast<double *>(a->workspace);
+    int count = 0;
+    const int rc = for_lists(a, [&](auto &list) {
+        constexpr int N = (int)(sizeof(list.t) / sizeof(list.t[0]));
+        const unsigned blocks = std::min<unsigned>(list.chunks, GN_BLOCKS);
+        double *to = partial + count;
+        count += (int)blocks;
+        return launch_behind(grad_norm_kernel<N>, blocks, dim3(GN_THREADS), 0, 1, stream, list, to);
+    });
+    if (rc != MOE_OVL_OK) return rc;
+    return launch_behind(grad_norm_finish_kernel, 1, dim3(GN_FINISH), 0, 1, stream, static_cast<const double *>(partial), count, a->norm);
+}
+
+extern "C" int moe_ovl_clip_grads(const moe_ovl_grads_args *a)
+{
+    if (!valid(a) || !(a->max_norm >= 0.0f) || !(a->eps >= 0.0f)) return MOE_OVL_ERR_INVALID_ARG;
+    for (int i = 0; a->out && i < a->num_tensors; ++i)
+        if (a->sizes[i] > 0 && (!a->out[i] || !aligned(a->out[i], dtype_bytes(a->dtypes[i])))) return MOE_OVL_ERR_INVALID_ARG;
+    if (!supported(a)) return MOE_OVL_ERR_UNSUPPORTED;
+    DeviceGuard guard(a->device);
+    if (!guard.ok) return MOE_OVL_ERR_CUDA;
+    const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+    return for_lists(a, [&](auto &list) {
+        constexpr int N = (int)(sizeof(list.t) / sizeof(list.t[0]));
+        const unsigned blocks = std::min<unsigned>(list.chunks, GN_BLOCKS);
+        return launch_behind(clip_grads_kernel<N>, blocks, dim3(GN_THREADS), 0, 1, stream, list, static_cast<const float *>(a->norm), a->max_norm, a->eps,
+                             a->out == nullptr);
+    });
+}

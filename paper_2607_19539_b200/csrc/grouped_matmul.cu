@@ -1,0 +1,348 @@
+// Products of 16-bit floats grouped by expert, and their gradients (moe_ovl_grouped_matmul, moe_ovl_grouped_matmul_backward in include/moe_ovl.h):
+//   out[m][n]   = sum_k a[m][k] * b[e][n][k], or a[m][k] * b[e][k][n]      (m a row of expert e)
+//   dweight[e][n][k] = sum over the rows m of expert e of dy[m][n] * x[m][k]
+//
+// One kernel for the three.  The matrix instruction's M side is what lies next to each other in the output (n of out, k of dweight), 128 of them per CTA, one
+// per lane of the accumulator, so that a warp's 32 lanes store 32 neighbours; its N side is the output's rows, of which there may be few
+// (a decode batch's tokens) and whose number goes in steps of 16.  Operands are taken from where they lie: with K (what is summed over) along their rows, or
+// down their columns, which the instruction's descriptors tell apart, so no matrix is transposed in memory.
+// The gradient of the weights sums over an expert's rows, which end anywhere inside a step of 64 rows.  What follows them belongs to the next expert
+// and has to count as 0 on both sides (0 * NaN is NaN), so each expert's operands are read through tensor maps of its own, cut off at its last
+// row; a small kernel in front writes them into the workspace.
+#include <algorithm>
+
+#include "matmul_tiles.cuh"
+
+using namespace moe_ovl;
+
+namespace {
+
+constexpr int GM_K = STAGE_ROW / 2;          // K per pipeline stage
+constexpr int GM_BOX = STAGE_ROW * GM_K;     // bytes of 64 columns x 64 rows, K down the columns
+constexpr int GM_M_BYTES = TILE_CHANNELS * STAGE_ROW;
+
+// What K runs along: rows of both operands; columns of the M side's; columns of both
+enum { FORM_ROWS = 0, FORM_MIXED = 1, FORM_COLUMNS = 2 };
+
+struct GmP {
+    int rows, n, k, experts;                 // n: the M side; k: sum, or (FORM_COLUMNS) the N side
+    int row_tiles;                           // tiles of the M side
+    const int *counts;
+    void *out;
+    long long out_stride, out_far;           // between rows, between experts (FORM_COLUMNS)
+    int *status;
+    unsigned long long timeout_ns;
+    uint32_t types;                          // of the instruction descriptor
+    bool no_loads;                           // test hook
+    bool accumulate;
+    const CUtensorMap *expert_maps;          // FORM_COLUMNS: [experts][2]
+};
+
+// Operands with K down the columns: 64 columns x 8 rows of K are one swizzle atom of 1024 bytes; atoms follow each other along K, then (GM_BOX bytes
+// on) along the columns.
+__device__ __forceinline__ uint64_t columns_desc(uint32_t saddr)
+{
+    return (umma_smem_desc(saddr) & ~((uint64_t)0x3fff << 16)) | ((uint64_t)(GM_BOX >> 4) << 16);
+}
+
+template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
+    static constexpr int SHARE = TOKENS / CTAS;                              // of the N side, per CTA
+    static constexpr int COLS = TOKENS < 32 ? 32 : TOKENS;                   // of tensor memory
+    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 2, COLS, 8, false>;
+    using Schedule = TileSchedule<CTAS * TILE_CHANNELS, TOKENS>;
+    using Tile = typename Schedule::Tile;                                    // FORM_COLUMNS: row0, rows are those of the output
+    const GmP &p;
+    const CUtensorMap *map_m, *map_n;
+    int *tile_start, *row_start;
+    Schedule sched;
+    int rank = 0;
+
+    struct From { const CUtensorMap *m, *n; int m0, n0, k0, expert; };
+
+    __device__ __forceinline__ void begin(int lane) { fill_schedule<TOKENS>(p, tile_start, row_start, count_of(p, lane), lane); }
+    __device__ __forceinline__ int groups() const { return p.counts ? p.experts : 1; }
+    __device__ __forceinline__ long long total() const
+    {
+        if constexpr (FORM == FORM_COLUMNS) return (long long)groups() * p.row_tiles * ((p.k - 1) / TOKENS + 1);
+        else return sched.total(groups());
+    }
+    __device__ __forceinline__ Tile at(long long t)
+    {
+        if constexpr (FORM == FORM_COLUMNS) {
+            const int wide = (p.k - 1) / TOKENS + 1, per = p.row_tiles * wide;
+            const int e = (int)(t / per), i = (int)(t - (long long)e * per), row0 = i % wide * TOKENS;
+            return {e, i / wide * (CTAS * TILE_CHANNELS), row0, min(TOKENS, p.k - row0)};
+        } else {
+            return sched.at(t);
+        }
+    }
+    __device__ __forceinline__ int steps(const Tile &t) const
+    {
+        return (int)(((unsigned)(FORM == FORM_COLUMNS ? row_start[t.expert + 1] - row_start[t.expert] : p.k) + GM_K - 1) / GM_K);
+    }
+    // Fewer rows than a full tile: a narrower instruction, whose halves the CTAs of a pair hold.
+    __device__ __forceinline__ int width(const Tile &t) const { return (t.rows + 16 * CTAS - 1) / (16 * CTAS) * (16 * CTAS); }
+    __device__ __forceinline__ From operands(const Tile &t, bool leader) const
+    {
+        From f = {map_m, map_n, uniform(t.channel0 + rank * TILE_CHANNELS), uniform((int)((unsigned)t.row0 + (unsigned)(rank * (width(t) / CTAS)))), 0, uniform(t.expert)};
+        if constexpr (FORM == FORM_COLUMNS) {
+            f.m = p.expert_maps + 2 * f.expert, f.n = f.m + 1;
+            f.k0 = uniform(row_start[t.expert]);
+            if (leader) {
+                acquire_map(f.m);
+                acquire_map(f.n);
+            }
+        }
+        return f;
+    }
+    __device__ __forceinline__ static void acquire_map(const CUtensorMap *map)
+    {
+        asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(map) : "memory");
+    }
+    __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
+    {
+        const int k = f.k0 + step * GM_K;
+        if constexpr (FORM == FORM_ROWS) {
+            load_3d<CTAS>(sa, f.m, bar, k, f.m0, f.expert);
+        } else if constexpr (FORM == FORM_MIXED) {
+#pragma unroll
+            for (int i = 0; i < TILE_CHANNELS / 64; ++i) load_3d<CTAS>(sa + i * GM_BOX, f.m, bar, f.m0 + 64 * i, k, f.expert);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TILE_CHANNELS / 64; ++i) load_2d<CTAS>(sa + i * GM_BOX, f.m, bar, f.m0 + 64 * i, k);
+        }
+        if constexpr (FORM == FORM_COLUMNS) {
+#pragma unroll
+            for (int i = 0; i < SHARE / 64; ++i) load_2d<CTAS>(sa + GM_M_BYTES + i * GM_BOX, f.n, bar, f.n0 + 64 * i, k);
+        } else {
+            load_2d<CTAS>(sa + GM_M_BYTES, f.n, bar, k, f.n0);
+        }
+    }
+    __device__ __forceinline__ uint32_t instruction(const Tile &t) const
+    {
+        return p.types | (1u << 4) | (FORM != FORM_ROWS ? 1u << 15 : 0u) | (FORM == FORM_COLUMNS ? 1u << 16 : 0u) | ((uint32_t)(width(t) >> 3) << 17) |
+               ((uint32_t)(CTAS * TILE_CHANNELS >> 4) << 24);
+    }
+    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool first) const
+    {
+        const uint64_t dm = (FORM == FORM_ROWS ? umma_smem_desc(0) : columns_desc(0)) + stage16;
+        const uint64_t dn = (FORM == FORM_COLUMNS ? columns_desc(0) : umma_smem_desc(0)) + stage16 + GM_M_BYTES / 16;
+        constexpr int STEP_M = FORM == FORM_ROWS ? 2 : 16 * STAGE_ROW / 16, STEP_N = FORM == FORM_COLUMNS ? 16 * STAGE_ROW / 16 : 2;
+#pragma unroll
+        for (int i = 0; i < GM_K / 16; ++i)
+            umma_f16<CTAS>(d, dm + (uint64_t)(i * STEP_M), dn + (uint64_t)(i * STEP_N), idesc, first && i == 0 ? 0u : 1u);
+    }
+    __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const GmP &, int warp, int lane) const
+    {
+        const int quarter = (warp + 2) & 3, half = warp >> 2;        // a warp reads the lanes of its position among four; every other 32 columns
+        const int ch = t.channel0 + rank * TILE_CHANNELS + quarter * 32 + lane;
+        const bool in = (unsigned)ch < (unsigned)p.n, none = steps(t) == 0;
+        if (none && p.accumulate) return true;
+        if (!none && !accs.wait(p, t.row0)) return false;
+        for (int c = half * 32; c < t.rows; c += 64) {
+            uint32_t v[32] = {};
+            if (!none) {
+                tmem_ld32(accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
+                tmem_ld_wait();
+            }
+            Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)(t.row0 + c) * p.out_stride + ch;
+            const int left = t.rows - c;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                if (in && j < left) {
+                    float sum = __uint_as_float(v[j]);
+                    if (FORM == FORM_COLUMNS && p.accumulate) sum += to_f32(*out);
+                    *out = from_f32<Out>(sum);
+                }
+                out += p.out_stride;
+            }
+        }
+        if (!none) accs.release();
+        return true;
+    }
+};
+
+template <int CTAS, int TOKENS, int FORM, typename Out>
+__global__ void __launch_bounds__(GmWork<CTAS, TOKENS, FORM, Out>::Shape::THREADS, 1)
+grouped_matmul_kernel(const __grid_constant__ CUtensorMap map_m, const __grid_constant__ CUtensorMap map_n, const __grid_constant__ GmP p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int s_tile_start[1025], s_row_start[1025];
+    using Work = GmWork<CTAS, TOKENS, FORM, Out>;
+    run_tiles(Work{p, &map_m, &map_n, s_tile_start, s_row_start, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+}
+
+// The tensor maps of one expert's rows: those of all rows, ending at its last one.  A warp per expert.
+constexpr int MAPS_WARPS = 4;
+__global__ void __launch_bounds__(32 * MAPS_WARPS)
+expert_maps_kernel(const __grid_constant__ CUtensorMap map_m, const __grid_constant__ CUtensorMap map_n, const GmP p, CUtensorMap *maps)
+{
+    __shared__ __align__(128) CUtensorMap s_map[MAPS_WARPS][2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = blockIdx.x * MAPS_WARPS + warp;
+    for (int i = lane; i < 64; i += 32)
+        reinterpret_cast<uint32_t *>(s_map[warp])[i] = i < 32 ? reinterpret_cast<const uint32_t *>(&map_m)[i] : reinterpret_cast<const uint32_t *>(&map_n)[i - 32];
+    after_previous();
+    may_follow();
+    const int experts = p.counts ? p.experts : 1;
+    if (e >= experts) return;
+    unsigned end = (unsigned)p.rows;
+    if (p.counts) {
+        // saturating at `rows`: sums of parts that are each at most that need 64 bits
+        unsigned long long sum = 0;
+        for (int i = lane; i <= e; i += 32) sum += (unsigned)min(max(p.counts[i], 0), p.rows);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        end = (unsigned)min(sum, (unsigned long long)p.rows);
+    }
+    __syncwarp();
+    if (lane < 2) {
+        // an expert in front of which there are no rows has none itself, and is never read; a map needs at least one
+        const unsigned rows = max(end, 1u);
+        asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"l"((unsigned long long)smem_u32(&s_map[warp][lane])), "r"(rows) : "memory");
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;"
+                     ::"l"(maps + 2 * e + i), "r"(smem_u32(&s_map[warp][i])) : "memory");
+}
+
+struct GmMaps { CUtensorMap m, n; };
+
+template <int CTAS, int TOKENS, int FORM, typename Out>
+int launch(const GmP &p, const GmMaps &maps, int device, cudaStream_t stream)
+{
+    using Shape = typename GmWork<CTAS, TOKENS, FORM, Out>::Shape;
+    static std::atomic<unsigned long long> allowed{0};
+    const auto kernel = grouped_matmul_kernel<CTAS, TOKENS, FORM, Out>;
+    if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    return launch_behind(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), dim3(Shape::THREADS), Shape::SMEM, CTAS, stream, maps.m, maps.n, p);
+}
+
+struct GmChoice { int ctas, tokens; };
+
+GmChoice choose(const GmP &p)
+{
+    const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows - 1) / groups + 1;
+    auto tiles = [&](int channels, int tokens) {
+        return (long long)((p.n - 1) / channels + 1) * groups * ((per_group - 1) / tokens + 1);
+    };
+    if (p.experts && per_group > 4 && per_group <= 64) return {1, per_group <= 16 ? 32 : 64};
+    if (per_group <= 16) return {1, 16};
+    if (per_group <= 32 || tiles(TILE_CHANNELS, 32) <= 148) return {1, 32};
+    if (per_group <= 64 || tiles(TILE_CHANNELS, 64) <= 148) return {1, 64};
+    const long long w128 = (tiles(2 * TILE_CHANNELS, 128) + 73) / 74, w256 = (tiles(2 * TILE_CHANNELS, 256) + 73) / 74;
+    return {2, per_group <= 128 || 8 * w128 <= 13 * w256 ? 128 : 256};
+}
+
+uint32_t instruction_types(int dtype) { return dtype == MOE_OVL_BF16 ? (1u << 7) | (1u << 10) : 0u; }
+CUtensorMapDataType map_type(int dtype) { return dtype == MOE_OVL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16; }
+bool float16(int dtype) { return dtype == MOE_OVL_BF16 || dtype == MOE_OVL_F16; }
+constexpr long long FAR = 1ll << 39;         // elements: the tensor map's limit on strides is 2^40 bytes
+
+}  // namespace
+
+extern "C" int moe_ovl_grouped_matmul(const moe_ovl_grouped_matmul_args *a)
+{
+    if (!a || a->struct_size != sizeof(*a) || a->device < 0 || a->rows < 0 || a->n < 1 || a->k < 1 || a->num_experts < 0 ||
+        (a->transposed & ~1) != 0 || (a->flags & ~MOE_OVL_MATMUL_TEST_NO_LOADS) != 0 || a->wait_timeout_us < 0 || !float16(a->dtype) ||
+        (a->out_dtype != a->dtype && a->out_dtype != MOE_OVL_F32) || (a->num_experts > 0) != (a->expert_counts != nullptr))
+        return MOE_OVL_ERR_INVALID_ARG;
+    if (a->num_experts > MOE_OVL_MAX_GROUPS || a->n > MOE_OVL_MAX_MATMUL || a->k > MOE_OVL_MAX_MATMUL) return MOE_OVL_ERR_UNSUPPORTED;
+    if (a->rows == 0) return MOE_OVL_OK;
+    const int experts = std::max(a->num_experts, 1), b_rows = a->transposed ? a->k : a->n, b_cols = a->transposed ? a->n : a->k;
+    if (!a->a || !a->b || !a->out || !a->status || !aligned(a->out, dtype_bytes(a->out_dtype)) || !aligned(a->status, 4) || !aligned(a->expert_counts, 4) ||
+        !aligned(a->a, 2) || !aligned(a->b, 2) || (a->rows > 1 && (a->a_stride < a->k || a->out_stride < a->n)) || (b_rows > 1 && a->b_stride < b_cols) ||
+        (experts > 1 && a->b_expert_stride < 1))
+        return MOE_OVL_ERR_INVALID_ARG;
+    if (std::max(std::max(a->a_stride, a->b_stride), a->out_stride) > 0x7fffffff || a->b_expert_stride >= FAR) return MOE_OVL_ERR_UNSUPPORTED;
+    // strides that are never used: the tensor map wants some that hold the row and are multiples of 16 bytes
+    const long long sa = a->rows > 1 ? a->a_stride : (a->k + 7ll) / 8 * 8, sb = b_rows > 1 ? a->b_stride : (b_cols + 7ll) / 8 * 8;
+    const long long far = experts > 1 ? a->b_expert_stride : b_rows * sb;
+    if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 8 != 0 || sb % 8 != 0 || far % 8 != 0) return MOE_OVL_ERR_UNSUPPORTED;
+    DeviceGuard guard(a->device);
+    if (!guard.ok) return MOE_OVL_ERR_CUDA;
+    GmP p = {};
+    p.rows = a->rows, p.n = a->n, p.k = a->k, p.experts = a->num_experts, p.counts = a->expert_counts;
+    p.out = a->out, p.out_stride = a->out_stride, p.status = a->status;
+    p.timeout_ns = a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : TILE_TIMEOUT_NS;
+    p.types = instruction_types(a->dtype), p.no_loads = (a->flags & MOE_OVL_MATMUL_TEST_NO_LOADS) != 0;
+    const GmChoice c = choose(p);
+    p.row_tiles = (p.n - 1) / (c.ctas * TILE_CHANNELS) + 1;
+    GmMaps maps;
+    const CUtensorMapDataType type = map_type(a->dtype);
+    if (!encode_tiles(&maps.m, type, 2, a->b, b_cols, b_rows, 2 * sb, experts, 2 * far, a->transposed ? GM_K : TILE_CHANNELS) ||
+        !encode_tiles(&maps.n, type, 2, a->a, a->k, a->rows, 2 * sa, 0, 0, c.tokens / c.ctas))
+        return MOE_OVL_ERR_CUDA;
+    const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+    return with_dtype(a->out_dtype, [&](auto t) {
+        using Out = decltype(t);
+        auto form = [&](auto f) {
+            constexpr int F = decltype(f)::value;
+            if (c.ctas == 1) {
+                switch (c.tokens) {
+                case 16: return launch<1, 16, F, Out>(p, maps, a->device, stream);
+                case 32: return launch<1, 32, F, Out>(p, maps, a->device, stream);
+                default: return launch<1, 64, F, Out>(p, maps, a->device, stream);
+                }
+            }
+            return c.tokens == 128 ? launch<2, 128, F, Out>(p, maps, a->device, stream) : launch<2, 256, F, Out>(p, maps, a->device, stream);
+        };
+        return a->transposed ? form(std::integral_constant<int, FORM_MIXED>()) : form(std::integral_constant<int, FORM_ROWS>());
+    });
+}
+
+extern "C" int moe_ovl_grouped_matmul_workspace_bytes(int32_t num_experts, size_t *bytes)
+{
+    if (!bytes || num_experts < 0) return MOE_OVL_ERR_INVALID_ARG;
+    if (num_experts > MOE_OVL_MAX_GROUPS) return MOE_OVL_ERR_UNSUPPORTED;
+    *bytes = sizeof(CUtensorMap) * 2 * (size_t)std::max(num_experts, 1);
+    return MOE_OVL_OK;
+}
+
+extern "C" int moe_ovl_grouped_matmul_backward(const moe_ovl_grouped_matmul_backward_args *a)
+{
+    if (!a || a->struct_size != sizeof(*a) || a->device < 0 || a->rows < 0 || a->n < 1 || a->k < 1 || a->num_experts < 0 ||
+        (a->accumulate & ~1) != 0 || (a->flags & ~MOE_OVL_MATMUL_TEST_NO_LOADS) != 0 || a->wait_timeout_us < 0 || !float16(a->dtype) ||
+        (a->out_dtype != a->dtype && a->out_dtype != MOE_OVL_F32) || (a->num_experts > 0) != (a->expert_counts != nullptr))
+        return MOE_OVL_ERR_INVALID_ARG;
+    if (a->num_experts > MOE_OVL_MAX_GROUPS || a->n > MOE_OVL_MAX_MATMUL || a->k > MOE_OVL_MAX_MATMUL) return MOE_OVL_ERR_UNSUPPORTED;
+    const int experts = std::max(a->num_experts, 1);
+    size_t need = 0;
+    moe_ovl_grouped_matmul_workspace_bytes(a->num_experts, &need);
+    if (!a->dweight || !a->status || !aligned(a->dweight, dtype_bytes(a->out_dtype)) || !aligned(a->status, 4) || !aligned(a->expert_counts, 4) ||
+        (a->rows > 0 && (!a->dy || !a->x || !aligned(a->dy, 2) || !aligned(a->x, 2))) || (a->rows > 1 && (a->dy_stride < a->n || a->x_stride < a->k)) ||
+        (a->n > 1 && a->dweight_stride < a->k) || (experts > 1 && a->dweight_expert_stride < 1))
+        return MOE_OVL_ERR_INVALID_ARG;
+    if (!a->workspace || a->workspace_bytes < need || !aligned(a->workspace, 128)) return MOE_OVL_ERR_WORKSPACE;
+    if (std::max(std::max(a->dy_stride, a->x_stride), a->dweight_stride) > 0x7fffffff || a->dweight_expert_stride >= FAR) return MOE_OVL_ERR_UNSUPPORTED;
+    const long long sy = a->rows > 1 ? a->dy_stride : (a->n + 7ll) / 8 * 8, sx = a->rows > 1 ? a->x_stride : (a->k + 7ll) / 8 * 8;
+    if (a->rows > 0 && (!aligned(a->dy, 16) || !aligned(a->x, 16) || sy % 8 != 0 || sx % 8 != 0)) return MOE_OVL_ERR_UNSUPPORTED;
+    DeviceGuard guard(a->device);
+    if (!guard.ok) return MOE_OVL_ERR_CUDA;
+    // without rows the weights' gradient is still written: nothing is read, through maps of the workspace's own bytes
+    const bool none = a->rows == 0;
+    GmP p = {};
+    p.rows = a->rows, p.n = a->k, p.k = a->n, p.experts = a->num_experts, p.counts = a->expert_counts;
+    p.out = a->dweight, p.out_stride = a->dweight_stride, p.out_far = a->dweight_expert_stride, p.status = a->status;
+    p.timeout_ns = a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : TILE_TIMEOUT_NS;
+    p.types = instruction_types(a->dtype), p.no_loads = (a->flags & MOE_OVL_MATMUL_TEST_NO_LOADS) != 0, p.accumulate = a->accumulate != 0;
+    p.expert_maps = static_cast<const CUtensorMap *>(a->workspace);
+    GmMaps maps;
+    const CUtensorMapDataType type = map_type(a->dtype);
+    if (!encode_tiles(&maps.m, type, 2, none ? a->workspace : a->x, a->k, std::max(a->rows, 1), 2 * sx, 0, 0, GM_K) ||
+        !encode_tiles(&maps.n, type, 2, none ? a->workspace : a->dy, a->n, std::max(a->rows, 1), 2 * sy, 0, 0, GM_K))
+        return MOE_OVL_ERR_CUDA;
+    const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+    const int rc = launch_behind(expert_maps_kernel, (unsigned)((experts + MAPS_WARPS - 1) / MAPS_WARPS), dim3(32 * MAPS_WARPS), 0, 1, stream, maps.m, maps.n, p,
+                                 static_cast<CUtensorMap *>(a->workspace));
+    if (rc != MOE_OVL_OK) return rc;
+    // few tiles: smaller ones, by one CTA each
+    const long long pairs = (long long)experts * ((p.n - 1) / 256 + 1) * ((p.k - 1) / 256 + 1);
+    const bool pair = pairs > 37;
+    p.row_tiles = (p.n - 1) / (pair ? 256 : 128) + 1;
+    return with_dtype(a->out_dtype, [&](auto t) {
+        using Out = decltype(t);
+        return pair ? launch<2, 256, FORM_COLUMNS, Out>(p, maps, a->device, stream) : launch<1, 128, FORM_COLUMNS, Out>(p, maps, a->device, stream);
+    });
+}

@@ -1,0 +1,417 @@
+// Shared by the products whose rows may be grouped by expert: where experts' rows and tiles begin, the waits and what follows one that
+// gives up, tensor maps, and the body of a persistent kernel that loads, multiplies and finishes tiles in three roles.
+#pragma once
+
+#include <atomic>
+
+#include "opcommon.cuh"
+#include "ptx.cuh"
+
+namespace moe_ovl {
+
+enum : long long { SITE_TILE_EMPTY = 32, SITE_TILE_FULL, SITE_TILE_DONE };
+
+constexpr int TILE_CHANNELS = 128;           // matrix instruction rows per CTA
+constexpr int STAGE_ROW = 128;               // bytes of K per pipeline stage and row: one row of the 128-byte swizzle
+constexpr int TILE_GROUP = 16;               // token tiles that are worked on side by side, see TileSchedule
+constexpr unsigned long long TILE_TIMEOUT_NS = 2000000000ull;
+
+// Inclusive sums over the lanes, none above `limit` (< 2^31; nor is v).  A loop, not unrolled: this runs once, before anything else
+// can, and every line of its code is fetched from memory then.
+__device__ __forceinline__ unsigned scan_up_to(unsigned v, unsigned limit, int lane)
+{
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned w = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v = min(v + w, limit);
+    }
+    return v;
+}
+
+// Rows of 32 experts from e0 on, one per lane: where each one's rows begin and end, given the rows before.  Counts are cut
+// so that no expert reaches beyond the rows there are.
+__device__ __forceinline__ void expert_rows(int count, unsigned limit, unsigned before, int lane, unsigned &first, unsigned &last)
+{
+    last = min(before + scan_up_to(min((unsigned)max(count, 0), limit), limit, lane), limit);
+    first = __shfl_up_sync(0xffffffffu, last, 1);
+    if (lane == 0) first = before;
+}
+template <typename P> __device__ __forceinline__ int count_of(const P &p, int e) { return p.counts && e < p.experts ? p.counts[e] : 0; }
+
+// Takes bytes off what the phase still waits for, as a copy of that size would.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void st_shared_cluster_u32(uint32_t addr, uint32_t v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// A wait that gives up, in whichever warp, leaves tile copies and matrix instructions under way: they have to land before the CTA's shared and
+// tensor memory go to somebody else.  This wait has a limit of its own, which neither a caller's short one nor an aborted status shortens.
+constexpr unsigned long long LANDING_NS = 2000000000ull;
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long since)
+{
+    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - since < LANDING_NS) {}
+}
+
+// A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
+template <typename P> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const P &p, long long index, int lane)
+{
+    bool ok = true;
+    if (lane == 0) ok = mbar_wait(bar, parity, p, SITE_TILE_DONE, index);
+    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    if (ok) mbar_try_wait(bar, parity);      // done already: this lane's own look, for the order of what it reads next
+    return ok;
+}
+
+// Order of the tiles: experts one after the other; inside an expert up to TILE_GROUP token tiles form a group, and for each tile
+// of channels all token tiles of the group come next to each other.  The CTAs that run side by side then share one
+// tile of weights in L2, and the weights are read from HBM once per group (4096 tokens of the largest tiles).  Every worker (a
+// CTA or a pair) takes every workers-th tile, so a role only ever moves forward through the experts.
+template <int CHANNELS, int TOKENS> struct TileSchedule {
+    const int *tile_start, *row_start;       // [experts + 1] token tiles and rows before each expert, in shared memory
+    int row_tiles, expert = 0;
+    struct Tile { int expert, channel0, row0, rows; };
+    __device__ long long total(int experts) const { return (long long)tile_start[experts] * row_tiles; }
+    __device__ Tile at(long long index)
+    {
+        while (index >= (long long)tile_start[expert + 1] * row_tiles) ++expert;
+        const int tiles = tile_start[expert + 1] - tile_start[expert];
+        const int i = (int)(index - (long long)tile_start[expert] * row_tiles);
+        const int group = i / (TILE_GROUP * row_tiles), first = group * TILE_GROUP, wide = min(TILE_GROUP, tiles - first);
+        const int j = i - group * TILE_GROUP * row_tiles;
+        const int row0 = row_start[expert] + (first + j % wide) * TOKENS;
+        return {expert, j / wide * CHANNELS, row0, min(TOKENS, row_start[expert + 1] - row0)};
+    }
+};
+
+// One warp fills the schedule's tables.  `count`: count_of(lane), asked for early.
+template <int TOKENS, typename P> __device__ __forceinline__ void fill_schedule(const P &p, int *tile_start, int *row_start, int count, int lane)
+{
+    unsigned rows_before = 0, tiles_before = 0;
+    if (lane == 0) tile_start[0] = row_start[0] = 0;
+    if (!p.counts && lane == 0) tile_start[1] = (p.rows - 1) / TOKENS + 1, row_start[1] = p.rows;
+    const int experts = p.counts ? p.experts : 0;
+#pragma unroll 1
+    for (int e0 = 0; e0 < experts; e0 += 32) {
+        const int e = e0 + lane;
+        unsigned first, last;
+        expert_rows(e0 == 0 ? count : count_of(p, e), (unsigned)p.rows, rows_before, lane, first, last);
+        const unsigned tiles = tiles_before + scan_up_to((last - first + TOKENS - 1) / TOKENS, 0x7fffffffu, lane);
+        if (e < experts) {
+            tile_start[e + 1] = (int)tiles;
+            row_start[e + 1] = (int)last;
+        }
+        tiles_before = __shfl_sync(0xffffffffu, tiles, 31);
+        rows_before = __shfl_sync(0xffffffffu, last, 31);
+    }
+    __syncwarp();
+}
+
+// ------------------------------------------------------------------ persistent tiles in three roles
+
+// CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
+// ACC_COLS columns of tensor memory go round; with PER_STEP every step of K has one of its own (and the finishing warps add them up), otherwise every tile.
+template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, bool PER_STEP_> struct TileShape {
+    static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_;
+    static constexpr bool PER_STEP = PER_STEP_;
+    static constexpr int STAGES = SMEM_BYTES_ / STAGE_BYTES_;
+    static constexpr int THREADS = 64 + 32 * FINISHERS;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
+    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32, "tensor memory");
+};
+
+// The finishing warps' way through the accumulators.
+template <typename Shape> struct Accumulators {
+    uint32_t bar_full, lead_empty, tmem;
+    bool remote;                             // the barrier that counts releases is the other CTA's
+    int lane, acc = 0;
+    uint32_t phase = 0;
+    template <typename P> __device__ __forceinline__ bool wait(const P &p, long long index)
+    {
+        const bool ok = warp_wait(bar_full + 8 * acc, phase, p, index, lane);
+        tc_fence_after();
+        return ok;
+    }
+    __device__ __forceinline__ uint32_t columns() const { return tmem + (uint32_t)(acc * Shape::ACC_COLS); }
+    __device__ __forceinline__ void release()
+    {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (remote) mbar_arrive_cluster(lead_empty + 8 * acc);
+            else mbar_arrive(lead_empty + 8 * acc);
+        }
+        if (++acc == Shape::ACCS) acc = 0, phase ^= 1u;
+    }
+};
+
+// After a give-up: waits for the copies that are under way, by one thread of the CTA whose barriers count them.  `mine`, `peers`: stages that
+// this CTA and (in a pair) the other one have issued; they are at most a ring apart, since neither refills a stage that the other has
+// not filled.  A fill of one side alone counts that side's bytes alone: the other side's are taken off, or, where this CTA's thread has not
+// announced the fill, half of the usual number is announced.
+template <typename Shape> __device__ void await_copies(uint32_t bar_full, uint32_t mine, uint32_t peers)
+{
+    constexpr uint32_t STAGES = Shape::STAGES;
+    const uint32_t last = Shape::CTAS == 1 ? mine : max(mine, peers);
+    const unsigned long long t0 = globaltimer_ns();
+    for (uint32_t i = last > STAGES ? last - STAGES : 0; i < last; ++i) {
+        const uint32_t bar = bar_full + 8 * (i % STAGES);
+        if (Shape::CTAS == 2 && i >= peers) mbar_complete_tx(bar, Shape::STAGE_BYTES);
+        else if (Shape::CTAS == 2 && i >= mine) mbar_arrive_expect_tx(bar, Shape::STAGE_BYTES);
+        drain(bar, (i / STAGES) & 1u, t0);
+    }
+}
+
+// Body of a persistent kernel: one load warp, one warp that issues the matrix instructions, FINISHERS warps that read the
+// accumulators.  Each role walks the same tiles.  The whole of a load or matrix warp runs its loop, with everything the same in all lanes, and one
+// elected lane issues: copies and matrix instructions take their operands from uniform registers.
+// `Work` says what a tile is: begin(lane) fills the tables, by one warp; total(); at(t); steps(tile) of K, 0 for a tile that nothing is loaded for;
+// load(tile's operands, shared address, barrier, step); instruction(tile); multiply(accumulator, stage's address / 16, instruction, first);
+// finish(tile, accumulators, warp, lane), false when a wait gave up.
+template <typename Work, typename P> __device__ __forceinline__ void run_tiles(Work work, const P &p, uint8_t *smem_raw)
+{
+    using Shape = typename Work::Shape;
+    constexpr int CTAS = Shape::CTAS, STAGES = Shape::STAGES, ACCS = Shape::ACCS;
+    __shared__ __align__(8) uint64_t s_bars[2 * STAGES + 2 * ACCS + 1];
+    __shared__ uint32_t s_tmem;
+    __shared__ uint32_t s_gave_up, s_issued[2];      // a wait for operands or room ran out, here or in the peer; rank 0: stages that each CTA has issued
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * STAGES;
+    const uint32_t bar_tfull = bar_empty + 8 * STAGES, bar_tempty = bar_tfull + 8 * ACCS, bar_drain = bar_tempty + 8 * ACCS;
+    const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
+    const uint32_t rank = CTAS == 1 ? 0 : cluster_ctarank();
+    const uint32_t lead_full = CTAS == 1 ? bar_full : map_to_cta(bar_full, 0);
+    const uint32_t lead_tempty = CTAS == 1 ? bar_tempty : map_to_cta(bar_tempty, 0);
+    const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    work.rank = (int)rank;
+    bool ok = true;
+    auto gave_up = [&]() {
+        s_gave_up = 1;
+        if (CTAS == 2) st_shared_cluster_u32(map_to_cta(smem_u32(&s_gave_up), rank ^ 1u), 1);
+    };
+
+    if (warp == 0) {
+        for (int i = lane; i < 2 * STAGES + 2 * ACCS + 1; i += 32)
+            // full: the first CTA's load thread arrives, expecting all CTAs' bytes; accumulators empty: one arrival per finishing warp
+            mbar_init(bar_full + 8 * i, i >= 2 * STAGES + ACCS && i < 2 * STAGES + 2 * ACCS ? Shape::FINISHERS * CTAS : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (lane == 0) s_gave_up = 0;
+        __syncwarp();
+        after_previous();
+        work.begin(lane);
+    } else if (warp == 1) {
+        if (CTAS == 1) tmem_alloc_self(smem_u32(&s_tmem), ACCS * Shape::ACC_COLS);
+        else tmem_alloc(smem_u32(&s_tmem), ACCS * Shape::ACC_COLS);
+    }
+    tc_fence_before();
+    after_previous();
+    __syncthreads();
+    if (CTAS == 2) cluster_sync_all();
+    may_follow();
+    tc_fence_after();
+    const uint32_t tmem = uniform(s_tmem);
+    const long long total = work.total();
+
+    if (warp == 0) {
+        int stage = 0;
+        uint32_t phase = 0, issued = 0;
+        if (!p.no_loads) {
+            const bool leader = elect_one();
+            for (long long t = first; ok && t < total; t += step) {
+                const auto tile = work.at(t);
+                const auto from = work.operands(tile, leader);
+                const int steps = uniform(work.steps(tile));
+                int k = 0;
+                for (; k < steps; ++k) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, t));
+                    if (!ok) break;
+                    if (leader) {
+                        if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, CTAS * Shape::STAGE_BYTES);
+                        work.load(from, smem_base + stage * Shape::STAGE_BYTES, lead_full + 8 * stage, k);
+                    }
+                    if (++stage == STAGES) stage = 0, phase ^= 1u;
+                }
+                issued += (uint32_t)k;
+            }
+        }
+        __syncwarp();
+        if (lane == 0) {
+            if (rank == 0) s_issued[0] = issued;
+            else st_shared_cluster_u32(map_to_cta(smem_u32(&s_issued[1]), 0), issued);
+            if (!ok) gave_up();
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            const bool leader = elect_one();
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            for (long long t = first; ok && t < total; t += step) {
+                const auto tile = work.at(t);
+                const uint32_t idesc = uniform(work.instruction(tile));
+                const int steps = uniform(work.steps(tile));
+                for (int k = 0; k < steps; ++k) {
+                    const bool begins = Shape::PER_STEP || k == 0, ends = Shape::PER_STEP || k == steps - 1;
+                    if (begins) {
+                        ok = __all_sync(0xffffffffu, mbar_wait<CTAS == 2>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
+                        if (!ok) break;
+                    }
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (leader) {
+                        work.multiply(tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins);
+                        if (CTAS == 1) umma_commit_one(bar_empty + 8 * stage);
+                        else umma_commit_pair(bar_empty + 8 * stage);
+                        if (ends) {
+                            if (CTAS == 1) umma_commit_one(bar_tfull + 8 * acc);
+                            else umma_commit_pair(bar_tfull + 8 * acc);
+                        }
+                    }
+                    if (++stage == STAGES) stage = 0, phase ^= 1u;
+                    if (ends && ++acc == ACCS) acc = 0, acc_phase ^= 1u;
+                }
+            }
+            if (leader) {
+                if (CTAS == 1) umma_commit_one(bar_drain);      // every MMA has finished before tensor memory goes
+                else if (ok) umma_commit_self(bar_drain);       // the peer has waited for its last accumulator, and does not wait for this
+                else umma_commit_pair(bar_drain);
+            }
+            drain(bar_drain, 0, globaltimer_ns());
+            if (!ok && lane == 0) gave_up();
+        }
+        __syncwarp();
+    } else {
+        Accumulators<Shape> accs{bar_tfull, lead_tempty, tmem, rank != 0, lane};
+        for (long long t = first; t < total; t += step)
+            if (!work.finish(work.at(t), accs, p, warp - 2, lane)) break;         // a warp leaves the loop as one
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CTAS == 2) cluster_sync_all();          // the peer no longer signals this CTA's barriers or reads its operands
+    if (s_gave_up) {
+        // but copies may be under way, which rank 0's barriers count for both, and matrix instructions' signals to rank 1
+        if (threadIdx.x == 0) {
+            if (rank == 0) await_copies<Shape>(bar_full, s_issued[0], s_issued[CTAS - 1]);
+            else drain(bar_drain, 0, globaltimer_ns());
+        }
+        __syncthreads();
+        if (CTAS == 2) cluster_sync_all();
+    }
+    tc_fence_after();
+    if (warp == 1) {
+        if (CTAS == 1) tmem_dealloc_self(tmem, ACCS * Shape::ACC_COLS);
+        else tmem_dealloc(tmem, ACCS * Shape::ACC_COLS);
+    }
+}
+
+// Tile loads of two and three dimensions, into this CTA's shared memory, counted on its barrier or (CTAS == 2) on one that may be the peer's.
+template <int CTAS> __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)
+{
+    if constexpr (CTAS == 1) tma_load_2d_self(dst, map, bar, x, y);
+    else tma_load_2d(dst, map, bar, x, y);
+}
+template <int CTAS> __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    if constexpr (CTAS == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
+}
+
+// D[tmem] (+)= A[smem] * B[smem] with 32-bit sums, by this CTA or by the CTA pair: 16-bit floats, K = 16, or 8-bit floats, K = 32.
+template <int CTAS> __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        umma_bf16(d_tmem, a_desc, b_desc, idesc, accumulate);
+}
+template <int CTAS> __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+
+// ------------------------------------------------------------------ host
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+inline EncodeTiledFn encode_fn()
+{
+    static std::atomic<EncodeTiledFn> known{nullptr};
+    EncodeTiledFn f = known.load(std::memory_order_acquire);
+    if (f) return f;
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult res;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess)
+        return nullptr;
+    f = reinterpret_cast<EncodeTiledFn>(fn);
+    known.store(f, std::memory_order_release);
+    return f;
+}
+
+// `depth` matrices (0: one, in a map of two dimensions) of `rows` rows of `cols` elements; rows lie `stride` bytes apart, matrices `far` bytes.
+// Boxes of 128 bytes x box_rows rows with the 128-byte swizzle; what lies beyond a matrix is read as 0.
+inline bool encode_tiles(CUtensorMap *map, CUtensorMapDataType type, int element, const void *base, long long cols, long long rows, long long stride,
+                         int depth, long long far, int box_rows)
+{
+    const EncodeTiledFn f = encode_fn();
+    if (!f) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
+    const cuuint64_t strides[2] = {(cuuint64_t)stride, (cuuint64_t)far};
+    const cuuint32_t box[3] = {(cuuint32_t)(STAGE_ROW / element), (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    return f(map, type, depth ? 3 : 2, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Allows a kernel its dynamic shared memory, once per device.
+template <typename K> bool allow_smem(K kernel, int bytes, int device, std::atomic<unsigned long long> &done)
+{
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
+inline int sm_count(int device)
+{
+    static std::atomic<int> known[64];
+    if (device >= 64) return 148;
+    int n = known[device].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 2) return 2;
+        known[device].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+}  // namespace moe_ovl

@@ -7,22 +7,17 @@
 // register, and a warp's 32 lanes store 32 neighbouring channels of a token.  Sums are exact 32-bit integers, so splitting
 // K over the CTAs of a cluster and adding their parts changes nothing.
 #include <algorithm>
-#include <atomic>
 
-#include "opcommon.cuh"
-#include "ptx.cuh"
+#include "matmul_tiles.cuh"
 
 using namespace moe_ovl;
 
 namespace {
 
-constexpr int QM_ROWS = 128;                 // channels per CTA
-constexpr int QM_K = 128;                    // K per pipeline stage: one 128-byte swizzle row
+constexpr int QM_ROWS = TILE_CHANNELS;       // channels per CTA
+constexpr int QM_K = STAGE_ROW;              // K per pipeline stage: one 128-byte swizzle row
 constexpr int QM_A_BYTES = QM_ROWS * QM_K;
 constexpr int QM_THREADS = 192;              // load warp, MMA warp, 4 epilogue warps
-constexpr unsigned long long QM_TIMEOUT_NS = 2000000000ull;
-
-enum : long long { SITE_QM_EMPTY = 32, SITE_QM_FULL, SITE_QM_DONE };
 
 struct QmP {
     int rows, n, k, experts;                 // experts 0: one matrix
@@ -38,30 +33,8 @@ struct QmP {
 
 struct QmTile { int expert, row0, rows; };   // rows 0: beyond the last tile
 
-// Inclusive sums over the lanes, none above `limit` (< 2^31; nor is v).  A loop, not unrolled: this runs once, before anything else
-// can, and every line of its code is fetched from memory then.
-__device__ __forceinline__ unsigned scan_up_to(unsigned v, unsigned limit, int lane)
-{
-#pragma unroll 1
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned w = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v = min(v + w, limit);
-    }
-    return v;
-}
-
-// Rows of 32 experts from e0 on, one per lane: where each one's rows begin and end, given the rows before.  Counts are cut
-// so that no expert reaches beyond the rows there are.
-__device__ __forceinline__ void expert_rows(int count, unsigned limit, unsigned before, int lane, unsigned &first, unsigned &last)
-{
-    last = min(before + scan_up_to(min((unsigned)max(count, 0), limit), limit, lane), limit);
-    first = __shfl_up_sync(0xffffffffu, last, 1);
-    if (lane == 0) first = before;
-}
 // Channels of a tile end behind the last one: without sign, where they pass 2^31 too.
 __device__ __forceinline__ bool has_channel(const QmP &p, int channel) { return (unsigned)channel < (unsigned)p.n; }
-__device__ __forceinline__ int count_of(const QmP &p, int e) { return p.counts && e < p.experts ? p.counts[e] : 0; }
-
 // The `index`-th tile of at most `height` tokens, experts in order.  One warp; every lane gets the answer.  `count`: count_of(lane).
 __device__ QmTile find_tile(const QmP &p, int index, int height, int count, int lane)
 {
@@ -101,34 +74,6 @@ template <int BN> struct QmShape {
     static constexpr int STAGES = 104 * 1024 / STAGE_BYTES;
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
 };
-
-// Takes bytes off what the phase still waits for, as a copy of that size would.
-__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void st_shared_cluster_u32(uint32_t addr, uint32_t v)
-{
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-
-// A wait that gives up, in whichever warp, leaves tile copies and matrix instructions under way: they have to land before the CTA's shared and
-// tensor memory go to somebody else.  This wait has a limit of its own, which neither a caller's short one nor an aborted status shortens.
-constexpr unsigned long long QM_LANDING_NS = 2000000000ull;
-__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long since)
-{
-    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - since < QM_LANDING_NS) {}
-}
-
-// A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const QmP &p, long long index, int lane)
-{
-    bool ok = true;
-    if (lane == 0) ok = mbar_wait(bar, parity, p, SITE_QM_DONE, index);
-    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-    if (ok) mbar_try_wait(bar, parity);      // done already: this lane's own look, for the order of what it reads next
-    return ok;
-}
 
 // Few tiles: one tile (128 channels x BN tokens) per cluster, whose SPLITS CTAs share its K.  Each leaves its part in its shared
 // memory, and the tokens are dealt out for the sum and the scaling.
@@ -179,7 +124,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
             int stage = 0;
             uint32_t phase = 0;
             for (int k = k0; k < k1; ++k, ++issued) {
-                if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, k))) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, k))) break;
                 const uint32_t sa = smem_base + stage * STAGE_BYTES;
                 if (leader) {
                     mbar_arrive_expect_tx(bar_full + 8 * stage, STAGE_BYTES);
@@ -194,7 +139,7 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
             int stage = 0;
             uint32_t phase = 0;
             for (int k = k0; k < k1; ++k) {
-                if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k))) {
+                if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k))) {
                     s_gave_up = 1;
                     break;
                 }
@@ -291,60 +236,16 @@ quant_matmul_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
 // ------------------------------------------------------------------ enough tiles for every SM: persistent CTAs, alone or in pairs
 
 constexpr int QP_THREADS = 320;              // load warp, MMA warp, 8 epilogue warps
-constexpr int QP_GROUP = 16;                 // token tiles that are worked on side by side, see QpSchedule
 
 // CTAS CTAs work on a tile of 128 * CTAS channels x TOKENS tokens: each holds 128 channels and its share of the tokens.  What
 // is not needed for tokens deepens the pipeline: with few tokens the kernel streams weights, and the bytes in flight carry it.
-template <int CTAS, int TOKENS> struct QpShape {
+template <int CTAS_, int TOKENS> struct QpShape {
+    static constexpr int CTAS = CTAS_;
     static constexpr int STAGE_BYTES = QM_A_BYTES + TOKENS / CTAS * QM_K;
     static constexpr int STAGES = 200 * 1024 / STAGE_BYTES;
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 512;
     static constexpr int ACC_COLS = TOKENS < 32 ? 32 : TOKENS;      // of tensor memory, per accumulator
 };
-
-// Order of the tiles: experts one after the other; inside an expert up to QP_GROUP token tiles form a group, and for each tile
-// of channels all token tiles of the group come next to each other.  The CTAs that run side by side then share one
-// tile of weights in L2, and the weights are read from HBM once per group (4096 tokens of the largest tiles).  Every worker (a
-// CTA or a pair) takes every workers-th tile, so a role only ever moves forward through the experts.
-template <int CTAS, int TOKENS> struct QpSchedule {
-    const int *tile_start, *row_start;       // [experts + 1] token tiles and rows before each expert, in shared memory
-    int row_tiles, expert = 0;
-    struct Tile { int expert, channel0, row0, rows; };
-    __device__ long long total(int experts) const { return (long long)tile_start[experts] * row_tiles; }
-    __device__ Tile at(long long index)
-    {
-        while (index >= (long long)tile_start[expert + 1] * row_tiles) ++expert;
-        const int tiles = tile_start[expert + 1] - tile_start[expert];
-        const int i = (int)(index - (long long)tile_start[expert] * row_tiles);
-        const int group = i / (QP_GROUP * row_tiles), first = group * QP_GROUP, wide = min(QP_GROUP, tiles - first);
-        const int j = i - group * QP_GROUP * row_tiles;
-        const int row0 = row_start[expert] + (first + j % wide) * TOKENS;
-        return {expert, j / wide * (CTAS * QM_ROWS), row0, min(TOKENS, row_start[expert + 1] - row0)};
-    }
-};
-
-// One warp fills the schedule's tables.  `count`: count_of(lane), asked for early.
-template <int TOKENS> __device__ __forceinline__ void fill_schedule(const QmP &p, int *tile_start, int *row_start, int count, int lane)
-{
-    unsigned rows_before = 0, tiles_before = 0;
-    if (lane == 0) tile_start[0] = row_start[0] = 0;
-    if (!p.counts && lane == 0) tile_start[1] = (p.rows - 1) / TOKENS + 1, row_start[1] = p.rows;
-    const int experts = p.counts ? p.experts : 0;
-#pragma unroll 1
-    for (int e0 = 0; e0 < experts; e0 += 32) {
-        const int e = e0 + lane;
-        unsigned first, last;
-        expert_rows(e0 == 0 ? count : count_of(p, e), (unsigned)p.rows, rows_before, lane, first, last);
-        const unsigned tiles = tiles_before + scan_up_to((last - first + TOKENS - 1) / TOKENS, 0x7fffffffu, lane);
-        if (e < experts) {
-            tile_start[e + 1] = (int)tiles;
-            row_start[e + 1] = (int)last;
-        }
-        tiles_before = __shfl_sync(0xffffffffu, tiles, 31);
-        rows_before = __shfl_sync(0xffffffffu, last, 31);
-    }
-    __syncwarp();
-}
 
 // The load warp's place in its sequence of stages.  The whole warp runs the loop, with everything in it the same in all lanes, and
 // one elected lane issues: tile copies take their operands from uniform registers, and where the compiler cannot tell that a
@@ -362,7 +263,7 @@ template <int CTAS, int TOKENS> struct QpLoader {
     {
         int k = k0;
         for (; k < k1; ++k) {
-            if (!FRESH && !__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_QM_EMPTY, y_b))) break;
+            if (!FRESH && !__all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, y_b))) break;
             const uint32_t sa = smem_base + stage * Shape::STAGE_BYTES;
             if (leader) {
                 if (CTAS == 1) {
@@ -381,24 +282,6 @@ template <int CTAS, int TOKENS> struct QpLoader {
         return k == k1;
     }
 };
-
-// After a give-up: waits for the copies that are under way, by one thread of the CTA whose barriers count them.  `mine`, `peers`: stages that
-// this CTA and (in a pair) the other one have issued; they are at most a ring apart, since neither refills a stage that the other has
-// not filled.  A fill of one side alone counts that side's bytes alone: the other side's are taken off, or, where this CTA's thread has not
-// announced the fill, half of the usual number is announced.
-template <int CTAS, int TOKENS> __device__ void await_copies(uint32_t bar_full, uint32_t mine, uint32_t peers)
-{
-    using Shape = QpShape<CTAS, TOKENS>;
-    constexpr uint32_t STAGES = Shape::STAGES;
-    const uint32_t last = CTAS == 1 ? mine : max(mine, peers);
-    const unsigned long long t0 = globaltimer_ns();
-    for (uint32_t i = last > STAGES ? last - STAGES : 0; i < last; ++i) {
-        const uint32_t bar = bar_full + 8 * (i % STAGES);
-        if (CTAS == 2 && i >= peers) mbar_complete_tx(bar, Shape::STAGE_BYTES);
-        else if (CTAS == 2 && i >= mine) mbar_arrive_expect_tx(bar, Shape::STAGE_BYTES);
-        drain(bar, (i / STAGES) & 1u, t0);
-    }
-}
 
 // Persistent, one CTA per SM.
 // CTAS = 2: pairs of CTAs share every matrix instruction (cta_group::2), 256 channels x TOKENS tokens, each CTA holding
@@ -425,7 +308,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     const uint32_t lead_full = CTAS == 1 ? bar_full : map_to_cta(bar_full, 0);
     const uint32_t lead_tempty = CTAS == 1 ? bar_tempty : map_to_cta(bar_tempty, 0);
     const int ksteps = (p.k + QM_K - 1) / QM_K, experts = p.experts > 0 ? p.experts : 1;
-    QpSchedule<CTAS, TOKENS> sched{s_tile_start, s_row_start, (p.n - 1) / (CTAS * QM_ROWS) + 1};
+    TileSchedule<CTAS * QM_ROWS, TOKENS> sched{s_tile_start, s_row_start, (p.n - 1) / (CTAS * QM_ROWS) + 1};
     const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
     QpLoader<CTAS, TOKENS> loader{smem_base, bar_full, bar_empty, lead_full, (int)rank};
     int early = 0;                          // stages of the first tile that are issued before the block is set up
@@ -501,12 +384,12 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
             for (long long t = first; ok && t < total; t += step) {
                 // fewer tokens than a full tile: a narrower instruction
                 const uint32_t idesc = uniform(umma_idesc_i8(CTAS * QM_ROWS, (sched.at(t).rows + 16 * CTAS - 1) / (16 * CTAS) * (16 * CTAS)));
-                ok = __all_sync(0xffffffffu, mbar_wait<CTAS == 2>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_QM_DONE, t));
+                ok = __all_sync(0xffffffffu, mbar_wait<CTAS == 2>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(acc * ACC_COLS);
                 for (int k = 0; k < ksteps; ++k) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_QM_FULL, k));
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k));
                     if (!ok) break;
                     tc_fence_after();
                     if (leader) {
@@ -577,7 +460,7 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     if (s_gave_up) {
         // but copies may be under way, which rank 0's barriers count for both, and matrix instructions' signals to rank 1
         if (threadIdx.x == 0) {
-            if (rank == 0) await_copies<CTAS, TOKENS>(bar_full, s_issued[0], s_issued[CTAS - 1]);
+            if (rank == 0) await_copies<Shape>(bar_full, s_issued[0], s_issued[CTAS - 1]);
             else drain(bar_drain, 0, globaltimer_ns());
         }
         __syncthreads();
@@ -590,65 +473,13 @@ quant_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_b, const __gri
     }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static std::atomic<EncodeTiledFn> known{nullptr};
-    EncodeTiledFn f = known.load(std::memory_order_acquire);
-    if (f) return f;
-    void *fn = nullptr;
-    cudaDriverEntryPointQueryResult res;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess)
-        return nullptr;
-    f = reinterpret_cast<EncodeTiledFn>(fn);
-    known.store(f, std::memory_order_release);
-    return f;
-}
-
-// Rows of k bytes, `stride` bytes apart, in boxes of 128 bytes x box_rows rows with the 128-byte swizzle; what lies beyond the
-// matrix is read as 0.
-bool encode_bytes(CUtensorMap *map, const void *base, long long rows, int k, long long stride, int box_rows)
-{
-    const EncodeTiledFn f = encode_fn();
-    if (!f) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)stride};
-    const cuuint32_t box[2] = {QM_K, (cuuint32_t)box_rows}, step[2] = {1, 1};
-    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Allows a kernel its dynamic shared memory, once per device.
-template <typename K> bool allow_smem(K kernel, int bytes, int device, std::atomic<unsigned long long> &done)
-{
-    const unsigned long long bit = device < 64 ? 1ull << device : 0;
-    if (bit && (done.load(std::memory_order_relaxed) & bit)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    done.fetch_or(bit, std::memory_order_relaxed);
-    return true;
-}
-
-int sm_count(int device)
-{
-    static std::atomic<int> known[64];
-    if (device >= 64) return 148;
-    int n = known[device].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 2) return 2;
-        known[device].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 // The operands as the tensor maps need them.  A map's box and the kernel's tile come from the same constant, in the two functions below.
 struct QmOperands { const void *a, *b; long long b_rows, a_stride, b_stride; };
 
 bool encode_operands(const QmP &p, const QmOperands &o, int token_rows, CUtensorMap *a, CUtensorMap *b)
 {
-    return encode_bytes(b, o.b, o.b_rows, p.k, o.b_stride, QM_ROWS) && encode_bytes(a, o.a, p.rows, p.k, o.a_stride, token_rows);
+    return encode_tiles(b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.b, p.k, o.b_rows, o.b_stride, 0, 0, QM_ROWS) &&
+           encode_tiles(a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.a, p.k, p.rows, o.a_stride, 0, 0, token_rows);
 }
 
 template <int BN, int SPLITS, typename Out>
@@ -741,7 +572,7 @@ extern "C" int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *a)
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;
     const QmP p = {a->rows, a->n, a->k, a->num_experts, (a->n - 1) / QM_ROWS + 1, a->expert_counts, a->a_scale, a->b_scale, a->out,
-                   a->out_stride, a->status, a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : QM_TIMEOUT_NS,
+                   a->out_stride, a->status, a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : TILE_TIMEOUT_NS,
                    (a->flags & MOE_OVL_QUANT_MATMUL_TEST_NO_LOADS) != 0};
     const QmChoice c = choose(p);
     const QmOperands o = {a->a, a->b, b_rows, sa, sb};

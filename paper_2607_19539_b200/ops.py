@@ -1,12 +1,13 @@
 """Operators around the expert layer (declared in include/moe_ovl.h): the norm in front of it, the router, the gated
-activation and the 8-bit integer product, by the names that the C interface gives them.
+activation and the 8-bit integer product; experts in 8-bit floats with a scale per block; the experts' products with their
+gradients, the gradients' norm and clipping.  They go by the names that the C interface gives them.
 
 Every tensor is the caller's, outputs and workspaces too; nothing is allocated and nothing is waited for.  What the C
 side cannot see of a tensor -- its shape, type, device and the order of its columns -- is checked here, and a tensor
 that does not fit raises MoeOvlError with ERR_INVALID_ARG before anything is launched.  Work goes to the current stream
 of the tensors' device, or to `stream`; tensors used on a stream that is not the current one are recorded on it.
 
-Nothing is recorded for autograd: outputs carry no gradient, and the two gradients are called by hand or from the backward of a
+Nothing is recorded for autograd: outputs carry no gradient, and the gradients are called by hand or from the backward of a
 torch.autograd.Function (whose forward runs with gradients off).  An input that requires a gradient while they are on gets a warning.
 """
 from __future__ import annotations
@@ -14,6 +15,7 @@ from __future__ import annotations
 import ctypes as C
 import struct
 import warnings
+from array import array
 
 import torch
 
@@ -24,7 +26,11 @@ DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 SCORES = {"softmax": SCORE_SOFTMAX, "sigmoid": SCORE_SIGMOID}
 FLAG_QUANT_MATMUL_TEST_NO_LOADS = 1
+FLAG_MATMUL_TEST_NO_LOADS = 1
 MAX_ROW, MAX_ROUTED, MAX_TOP_K, MAX_QUANT_K = 32768, 1024, 32, 131056
+MAX_GROUPS, MAX_MATMUL, MAX_TENSORS = 1024, 16777216, 65536
+BLOCK = 128             # values of K that share a scale of moe_ovl_block_matmul
+FLOAT8 = torch.float8_e4m3fn
 
 _u32, _i32, _i64, _f32, _ptr = C.c_uint32, C.c_int32, C.c_int64, C.c_float, C.c_void_p
 
@@ -54,6 +60,16 @@ RouteBackwardArgs = _struct("RouteBackwardArgs", "u struct_size;i device,rows,nu
                             "p logits,expert,dgate,dlogits;l logits_stride,dlogits_stride;p stream")
 QuantMatmulArgs = _struct("QuantMatmulArgs", "u struct_size;i device,rows,n,k,num_experts,out_dtype,wait_timeout_us;u flags;"
                           "p a,a_scale,b,b_scale,expert_counts,out,status;l a_stride,b_stride,out_stride;p stream")
+
+GroupedMatmulArgs = _struct("GroupedMatmulArgs", "u struct_size;i device,rows,n,k,num_experts,dtype,out_dtype,transposed,wait_timeout_us;u flags;"
+                            "p a,b,expert_counts,out,status;l a_stride,b_stride,b_expert_stride,out_stride;p stream")
+GroupedMatmulBackwardArgs = _struct("GroupedMatmulBackwardArgs", "u struct_size;i device,rows,n,k,num_experts,dtype,out_dtype,accumulate,wait_timeout_us;u flags;"
+                                    "p dy,x,expert_counts,dweight,status,workspace;z workspace_bytes;l dy_stride,x_stride,dweight_stride,dweight_expert_stride;"
+                                    "p stream")
+BlockQuantArgs = _struct("BlockQuantArgs", "u struct_size;i device,depth,rows,k,dtype,gated,tiles;u flags;p x,q,scale;l x_stride,q_stride,x_far,q_far;p stream")
+BlockMatmulArgs = _struct("BlockMatmulArgs", "u struct_size;i device,rows,n,k,num_experts,out_dtype,wait_timeout_us;u flags;"
+                          "p a,a_scale,b,b_scale,expert_counts,out,status;l a_stride,b_stride,b_expert_stride,out_stride;p stream")
+GradsArgs = _struct("GradsArgs", "u struct_size;i device,num_tensors;u flags;p grads,out,sizes,dtypes,norm;f max_norm,eps;p workspace;z workspace_bytes;p stream")
 
 
 def _refuse(where: str, what: str):
@@ -284,3 +300,221 @@ def moe_ovl_quant_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=N
     _call(where, B.load().moe_ovl_quant_matmul, QuantMatmulArgs, dev, rows, n, k, experts, dt, wait_timeout_us, flags, a.data_ptr(), a_scale.data_ptr(),
           b.data_ptr(), b_scale.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, so,
           _stream(dev, stream, a, a_scale, b, b_scale, expert_counts, out, status))
+
+
+def _matrices(where, name, t, shape, dtype, device):
+    """Strides between rows and between matrices of a tensor of three dimensions (or of two: one matrix) whose columns lie next to each other."""
+    if tuple(t.shape) not in (shape, shape[1:] if shape[0] == 1 else shape) or t.dtype is not dtype or t.get_device() != device:
+        _refuse(where, f"{name} has to be {list(shape)} {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
+    depth, rows, cols = shape
+    s0, s1 = t.stride()[-2:]
+    far = t.stride(0) if t.dim() == 3 else 0
+    if (s1 != 1 and cols > 1) or s0 < 0:
+        _refuse(where, f"{name}: the columns of a row have to lie next to each other (strides {t.stride()})")
+    if rows > 1 and s0 < cols:
+        _refuse(where, f"{name}: rows must not overlap (strides {t.stride()})")
+    return s0, far
+
+
+def _apart(where, name, shape, row_stride, far) -> None:
+    """Refuses matrices that are written and would overlap: either matrices lie behind each other or their rows interleave."""
+    depth, rows, cols = shape
+    if depth < 2 or rows * cols == 0:
+        return
+    if far >= (rows - 1) * row_stride + cols or (far >= cols and (rows == 1 or row_stride >= (depth - 1) * far + cols)):
+        return
+    _refuse(where, f"{name}: the matrices of the experts must not overlap")
+
+
+def _experts(where, name, t, expert_counts, device) -> int:
+    if expert_counts is None:
+        if t.dim() == 3 and t.shape[0] != 1:
+            _refuse(where, "several experts need expert_counts")
+        return 0
+    if t.dim() != 3 or t.shape[0] < 1:
+        _refuse(where, f"with expert_counts {name} has to have three dimensions, the experts first")
+    _vector(where, "expert_counts", expert_counts, (t.shape[0],), torch.int32, device)
+    return t.shape[0]
+
+
+def _workspace(where, workspace, device) -> int:
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        _refuse(where, f"workspace has to be contiguous on cuda:{device}")
+    return workspace.numel() * workspace.element_size()
+
+
+def _needs_gradient(*tensors) -> bool:
+    return any(t.requires_grad for t in tensors)
+
+
+def moe_ovl_grouped_matmul(*, a, b, out, status, expert_counts=None, transposed: bool = False, wait_timeout_us: int = 0, flags: int = 0, stream=None) -> None:
+    """out = a @ b^T in 16-bit floats, rows of a grouped by expert: b [experts, n, k], or with `transposed` a @ b, b [experts, k, n].  Without expert_counts
+    b is one matrix.  The gradient of a is moe_ovl_grouped_matmul(a=dout, b=b, transposed=not transposed)."""
+    where = "moe_ovl_grouped_matmul"
+    dev = _device(where, a)
+    if a.dim() != 2 or b.dim() not in (2, 3) or out.dim() != 2:
+        _refuse(where, "a has to be [rows, k], b [n, k] or [experts, n, k], out [rows, n]")
+    if a.dtype not in (torch.bfloat16, torch.float16):
+        _refuse(where, f"a has to be bfloat16 or float16, not {a.dtype}")
+    if out.dtype is not a.dtype and out.dtype is not torch.float32:
+        _refuse(where, f"out has to be {a.dtype} or float32, not {out.dtype}")
+    rows, k = a.shape
+    experts = _experts(where, "b", b, expert_counts, dev)
+    n = b.shape[-1] if transposed else b.shape[-2]
+    sa = _matrix(where, "a", a, a.shape, a.dtype, dev)
+    sb, far = _matrices(where, "b", b, (max(experts, 1), k, n) if transposed else (max(experts, 1), n, k), a.dtype, dev)
+    so = _matrix(where, "out", out, (rows, n), out.dtype, dev)
+    _vector(where, "status", status, (4,), torch.int32, dev)
+    if _needs_gradient(a, b):
+        _gradient_lost(where)
+    _call(where, B.load().moe_ovl_grouped_matmul, GroupedMatmulArgs, dev, rows, n, k, experts, DTYPES[a.dtype], DTYPES[out.dtype], 1 if transposed else 0,
+          wait_timeout_us, flags, a.data_ptr(), b.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, far, so,
+          _stream(dev, stream, a, b, expert_counts, out, status))
+
+
+def moe_ovl_grouped_matmul_workspace_bytes(num_experts: int) -> int:
+    n = C.c_size_t(0)
+    _done(B.load().moe_ovl_grouped_matmul_workspace_bytes(int(num_experts), C.byref(n)), "moe_ovl_grouped_matmul_workspace_bytes")
+    return int(n.value)
+
+
+def moe_ovl_grouped_matmul_backward(*, dy, x, dweight, status, workspace, expert_counts=None, accumulate: bool = False, wait_timeout_us: int = 0,
+                                    flags: int = 0, stream=None) -> None:
+    """dweight[e] = dy_e^T @ x_e over the rows of each expert, or added to what dweight holds.  The workspace has
+    moe_ovl_grouped_matmul_workspace_bytes bytes."""
+    where = "moe_ovl_grouped_matmul_backward"
+    dev = _device(where, dy)
+    if dy.dim() != 2 or x.dim() != 2 or dweight.dim() not in (2, 3):
+        _refuse(where, "dy has to be [rows, n], x [rows, k], dweight [n, k] or [experts, n, k]")
+    if dy.dtype not in (torch.bfloat16, torch.float16):
+        _refuse(where, f"dy has to be bfloat16 or float16, not {dy.dtype}")
+    if dweight.dtype is not dy.dtype and dweight.dtype is not torch.float32:
+        _refuse(where, f"dweight has to be {dy.dtype} or float32, not {dweight.dtype}")
+    rows, n = dy.shape
+    k = x.shape[1]
+    experts = _experts(where, "dweight", dweight, expert_counts, dev)
+    shape = (max(experts, 1), n, k)
+    sy = _matrix(where, "dy", dy, dy.shape, dy.dtype, dev)
+    sx = _matrix(where, "x", x, (rows, k), dy.dtype, dev)
+    sw, far = _matrices(where, "dweight", dweight, shape, dweight.dtype, dev)
+    _apart(where, "dweight", shape, sw, far)
+    _vector(where, "status", status, (4,), torch.int32, dev)
+    nbytes = _workspace(where, workspace, dev)
+    _call(where, B.load().moe_ovl_grouped_matmul_backward, GroupedMatmulBackwardArgs, dev, rows, n, k, experts, DTYPES[dy.dtype], DTYPES[dweight.dtype],
+          1 if accumulate else 0, wait_timeout_us, flags, dy.data_ptr(), x.data_ptr(), _at(expert_counts), dweight.data_ptr(), status.data_ptr(),
+          workspace.data_ptr(), nbytes, sy, sx, sw, far, _stream(dev, stream, dy, x, expert_counts, dweight, status, workspace))
+
+
+def moe_ovl_block_quant(*, x, q, scale, gated: bool = False, tiles: bool = False, stream=None) -> None:
+    """x in 8-bit floats with a scale for each 128 values of a row (or with `tiles` for each 128 x 128 of a matrix, x [n, k] or [experts, n, k]).  With `gated`
+    x is [rows, 2k] and silu(gate) * up is what becomes 8 bits, gate in the first k columns."""
+    where = "moe_ovl_block_quant"
+    dev, dt = _device(where, x), _dtype(where, "x", x)
+    if x.dim() != 2 and not (tiles and x.dim() == 3):
+        _refuse(where, "x has to be [rows, k], or with tiles [n, k] or [experts, n, k]")
+    if gated and (tiles or x.shape[1] % 2):
+        _refuse(where, "with gated x has to be [rows, 2k], and tiles cannot be asked for")
+    depth, rows, k = x.shape[0] if x.dim() == 3 else 1, x.shape[-2], x.shape[-1] // 2 if gated else x.shape[-1]
+    if k < 1 or depth < 1:
+        _refuse(where, f"x has no values: {list(x.shape)}")
+    sx, x_far = _matrices(where, "x", x, (depth, rows, x.shape[-1]), x.dtype, dev)
+    if q.dim() != x.dim():
+        _refuse(where, f"q has to have {x.dim()} dimensions as x")
+    sq, q_far = _matrices(where, "q", q, (depth, rows, k), FLOAT8, dev)
+    _apart(where, "q", (depth, rows, k), sq, q_far)
+    blocks = -(-k // BLOCK)
+    _vector(where, "scale", scale, (*x.shape[:-2], -(-rows // BLOCK), blocks) if tiles else (rows, blocks), torch.float32, dev)
+    if x.requires_grad:
+        _gradient_lost(where)
+    _call(where, B.load().moe_ovl_block_quant, BlockQuantArgs, dev, depth, rows, k, dt, 1 if gated else 0, 1 if tiles else 0, 0, x.data_ptr(), q.data_ptr(),
+          scale.data_ptr(), sx, sq, x_far, q_far, _stream(dev, stream, x, q, scale))
+
+
+def moe_ovl_block_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=None, wait_timeout_us: int = 0, flags: int = 0, stream=None) -> None:
+    """out = a @ b^T in 8-bit floats, a with a scale per row and 128 values, b with one per 128 x 128 (as moe_ovl_block_quant gives them).  b is [n, k], or
+    with expert_counts [experts, n, k] and the rows of a are grouped by expert."""
+    where = "moe_ovl_block_matmul"
+    dev = _device(where, a)
+    if a.dim() != 2 or b.dim() not in (2, 3) or out.dim() != 2:
+        _refuse(where, "a has to be [rows, k], b [n, k] or [experts, n, k], out [rows, n]")
+    rows, k = a.shape
+    experts = _experts(where, "b", b, expert_counts, dev)
+    n, blocks = b.shape[-2], -(-k // BLOCK)
+    sa = _matrix(where, "a", a, a.shape, FLOAT8, dev)
+    sb, far = _matrices(where, "b", b, (max(experts, 1), n, k), FLOAT8, dev)
+    dt = _dtype(where, "out", out)
+    so = _matrix(where, "out", out, (rows, n), out.dtype, dev)
+    _vector(where, "a_scale", a_scale, (rows, blocks), torch.float32, dev)
+    _vector(where, "b_scale", b_scale, (*b.shape[:-2], -(-n // BLOCK), blocks), torch.float32, dev)
+    _vector(where, "status", status, (4,), torch.int32, dev)
+    if _needs_gradient(a_scale, b_scale):
+        _gradient_lost(where)
+    _call(where, B.load().moe_ovl_block_matmul, BlockMatmulArgs, dev, rows, n, k, experts, dt, wait_timeout_us, flags, a.data_ptr(), a_scale.data_ptr(),
+          b.data_ptr(), b_scale.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, far, so,
+          _stream(dev, stream, a, a_scale, b, b_scale, expert_counts, out, status))
+
+
+def _dense(t) -> bool:
+    """Whether a tensor's values fill a stretch of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    size = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != size:
+            return False
+        size *= n
+    return True
+
+
+def _tensor_list(where, name, tensors, device):
+    """Addresses, sizes and types of a list of tensors as arrays."""
+    for t in tensors:
+        if t.get_device() != device:
+            _refuse(where, f"every tensor of {name} has to be on cuda:{device}, not {t.device}")
+        if not _dense(t):
+            _refuse(where, f"the tensors of {name} have to fill the memory that they span (strides {t.stride()} of {list(t.shape)})")
+    at = [t.data_ptr() for t in tensors if t.numel()]
+    if len(set(at)) != len(at):
+        _refuse(where, f"a tensor is twice in {name}")
+    return (array("Q", [t.data_ptr() for t in tensors]), array("q", [t.numel() for t in tensors]), array("i", [_dtype(where, f"every tensor of {name}", t) for t in tensors]))
+
+
+def moe_ovl_grad_norm_workspace_bytes(num_tensors: int) -> int:
+    n = C.c_size_t(0)
+    _done(B.load().moe_ovl_grad_norm_workspace_bytes(int(num_tensors), C.byref(n)), "moe_ovl_grad_norm_workspace_bytes")
+    return int(n.value)
+
+
+def moe_ovl_grad_norm(*, grads, norm, workspace, stream=None) -> None:
+    """norm[0] = the square root of the sum of the squares of all values of a list of tensors.  The workspace has moe_ovl_grad_norm_workspace_bytes
+    bytes.  Ranks that hold different gradients combine their norms (the root of the sum of squares) before moe_ovl_clip_grads."""
+    where = "moe_ovl_grad_norm"
+    dev, grads = _device(where, norm), list(grads)
+    at, sizes, dtypes = _tensor_list(where, "grads", grads, dev)
+    _vector(where, "norm", norm, (1,), torch.float32, dev)
+    nbytes = _workspace(where, workspace, dev)
+    _call(where, B.load().moe_ovl_grad_norm, GradsArgs, dev, len(grads), 0, _host(at), 0, _host(sizes), _host(dtypes), norm.data_ptr(), 0.0, 0.0,
+          workspace.data_ptr(), nbytes, _stream(dev, stream, *grads, norm, workspace))
+
+
+def moe_ovl_clip_grads(*, grads, norm, max_norm: float, eps: float = 1e-6, out=None, stream=None) -> None:
+    """Every value of a list of tensors times min(1, max_norm / (norm[0] + eps)), where it lies or into the tensors of `out`."""
+    where = "moe_ovl_clip_grads"
+    dev, grads = _device(where, norm), list(grads)
+    at, sizes, dtypes = _tensor_list(where, "grads", grads, dev)
+    to = None
+    if out is not None:
+        out = list(out)
+        if len(out) != len(grads):
+            _refuse(where, f"out has {len(out)} tensors, grads {len(grads)}")
+        for g, o in zip(grads, out):
+            if o.shape != g.shape or o.dtype is not g.dtype or any(s != z for s, z, n in zip(o.stride(), g.stride(), g.shape) if n != 1):
+                _refuse(where, f"a tensor of out has to be {list(g.shape)} {g.dtype} with strides {g.stride()}, not {list(o.shape)} {o.dtype} with {o.stride()}")
+        to = _tensor_list(where, "out", out, dev)[0]
+    _vector(where, "norm", norm, (1,), torch.float32, dev)
+    _call(where, B.load().moe_ovl_clip_grads, GradsArgs, dev, len(grads), 0, _host(at), 0 if to is None else _host(to), _host(sizes), _host(dtypes), norm.data_ptr(),
+          max_norm, eps, 0, 0, _stream(dev, stream, *grads, norm, *(out or ())))
+
+
+def _host(a) -> int:
+    return a.buffer_info()[0]
