@@ -56,11 +56,20 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned lo
     while (!mbar_try_wait(bar, parity) && globaltimer_ns() - since < LANDING_NS) {}
 }
 
+// mbar_wait, with its clock left alone at first: most waits of a pipeline are short, and reading the clock takes longer than they do.
+template <typename P> __device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity, const P &p, long long site, long long index)
+{
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait(bar, parity, p, site, index);
+}
+
 // A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
 template <typename P> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const P &p, long long index, int lane)
 {
     bool ok = true;
-    if (lane == 0) ok = mbar_wait(bar, parity, p, SITE_TILE_DONE, index);
+    if (lane == 0) ok = short_wait(bar, parity, p, SITE_TILE_DONE, index);
     ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
     if (ok) mbar_try_wait(bar, parity);      // done already: this lane's own look, for the order of what it reads next
     return ok;
@@ -123,15 +132,23 @@ template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_
     static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32, "tensor memory");
 };
 
-// The finishing warps' way through the accumulators.
+// Arrival of a reader of tensor memory, on a barrier that may be the peer CTA's.  What it gives back has been read (tcgen05.wait, and the fence
+// in front of it) and nothing was written, so it needs no release of memory at cluster scope, which would wait for the warp's loads and stores.
+__device__ __forceinline__ void arrive_read(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+// The finishing warps' way through the accumulators.  With PER_STEP a stage's "empty" is an accumulator's "full" too: one signal per step of the matrix
+// instructions instead of two (each costs as much as a step's instructions, see block_matmul.cu).
 template <typename Shape> struct Accumulators {
+    static constexpr int SIGNALS = Shape::PER_STEP ? Shape::STAGES : Shape::ACCS;
     uint32_t bar_full, lead_empty, tmem;
-    bool remote;                             // the barrier that counts releases is the other CTA's
-    int lane, acc = 0;
+    int lane, acc = 0, signal = 0;
     uint32_t phase = 0;
     template <typename P> __device__ __forceinline__ bool wait(const P &p, long long index)
     {
-        const bool ok = warp_wait(bar_full + 8 * acc, phase, p, index, lane);
+        const bool ok = warp_wait(bar_full + 8 * signal, phase, p, index, lane);
         tc_fence_after();
         return ok;
     }
@@ -140,11 +157,9 @@ template <typename Shape> struct Accumulators {
     {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-            if (remote) mbar_arrive_cluster(lead_empty + 8 * acc);
-            else mbar_arrive(lead_empty + 8 * acc);
-        }
-        if (++acc == Shape::ACCS) acc = 0, phase ^= 1u;
+        if (lane == 0) arrive_read(lead_empty + 8 * acc);
+        if (++acc == Shape::ACCS) acc = 0;
+        if (++signal == SIGNALS) signal = 0, phase ^= 1u;
     }
 };
 
@@ -226,7 +241,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 const int steps = uniform(work.steps(tile));
                 int k = 0;
                 for (; k < steps; ++k) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, t));
+                    ok = __all_sync(0xffffffffu, short_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, t));
                     if (!ok) break;
                     if (leader) {
                         if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, CTAS * Shape::STAGE_BYTES);
@@ -256,17 +271,17 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 for (int k = 0; k < steps; ++k) {
                     const bool begins = Shape::PER_STEP || k == 0, ends = Shape::PER_STEP || k == steps - 1;
                     if (begins) {
-                        ok = __all_sync(0xffffffffu, mbar_wait<CTAS == 2>(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
+                        ok = __all_sync(0xffffffffu, short_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
                         if (!ok) break;
                     }
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k));
+                    ok = __all_sync(0xffffffffu, short_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k));
                     if (!ok) break;
                     tc_fence_after();
                     if (leader) {
                         work.multiply(tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins);
                         if (CTAS == 1) umma_commit_one(bar_empty + 8 * stage);
                         else umma_commit_pair(bar_empty + 8 * stage);
-                        if (ends) {
+                        if (!Shape::PER_STEP && ends) {
                             if (CTAS == 1) umma_commit_one(bar_tfull + 8 * acc);
                             else umma_commit_pair(bar_tfull + 8 * acc);
                         }
@@ -285,7 +300,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
         }
         __syncwarp();
     } else {
-        Accumulators<Shape> accs{bar_tfull, lead_tempty, tmem, rank != 0, lane};
+        Accumulators<Shape> accs{Shape::PER_STEP ? bar_empty : bar_tfull, lead_tempty, tmem, lane};
         for (long long t = first; t < total; t += step)
             if (!work.finish(work.at(t), accs, p, warp - 2, lane)) break;         // a warp leaves the loop as one
         __syncwarp();
