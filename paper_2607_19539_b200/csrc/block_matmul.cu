@@ -48,9 +48,10 @@ __device__ __forceinline__ float2 pair_of(const uint32_t *v) { return make_float
 
 // Instruction descriptor: 32-bit sums of e4m3, K along the rows of both operands.
 __device__ __forceinline__ uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
-template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t d, uint32_t stage16, uint32_t idesc)
+// One step: 128 values of K.  `n16`: where the N side's operand begins in its stage, / 16.
+template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t d, uint32_t stage16, uint32_t n16, uint32_t idesc)
 {
-    const uint64_t dm = umma_smem_desc(0) + stage16, dn = dm + BM_M_BYTES / 16;
+    const uint64_t dm = umma_smem_desc(0) + stage16, dn = dm + n16;
 #pragma unroll
     for (int i = 0; i < STAGE_ROW / 32; ++i) umma_f8<CTAS>(d, dm + (uint64_t)(i * 2), dn + (uint64_t)(i * 2), idesc, i > 0 ? 1u : 0u);
 }
@@ -58,8 +59,8 @@ template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t d, ui
 // ------------------------------------------------------------------ many rows
 
 template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
-    static constexpr int TOKENS = CTAS * TILE_CHANNELS, SHARE = CHANNELS / CTAS, COLS = CHANNELS / 2;
-    using Shape = TileShape<CTAS, BM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 512 / CHANNELS, CHANNELS, 8, true>;
+    static constexpr int TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
+    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 200 * 1024, 4, 128, 8, PARTS>;
     using Schedule = TileSchedule<CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
     const BmP &p;
@@ -80,16 +81,20 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
     __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
     {
         load_2d<CTAS>(sa, map_a, bar, step * STAGE_ROW, f.a0);
-        load_3d<CTAS>(sa + BM_M_BYTES, map_b, bar, step * STAGE_ROW, f.b0, f.expert);
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) load_3d<CTAS>(sa + BM_M_BYTES + i * SHARE * STAGE_ROW, map_b, bar, step * STAGE_ROW, f.b0 + i * 128, f.expert);
     }
-    __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TOKENS, CHANNELS); }
-    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool) const { multiply_step<CTAS>(d, stage16, idesc); }
+    __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TOKENS, 128); }
+    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool, int part) const
+    {
+        multiply_step<CTAS>(d, stage16, (BM_M_BYTES + part * SHARE * STAGE_ROW) / 16, idesc);
+    }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
     {
-        const int quarter = (warp + 2) & 3, half = warp >> 2;        // a warp reads the lanes of its position among four, and half of the columns
+        const int quarter = (warp + Shape::CONTROL) & 3, half = PARTS == 1 ? warp >> 2 : 0;  // a warp reads the lanes of its position among four, and its part's columns or half of them
         const int in_tile = rank * TILE_CHANNELS + quarter * 32 + lane;
         const bool mine = in_tile < t.rows;
-        const int ch0 = t.channel0 + half * COLS, block = ch0 / 128;
+        const int block = t.channel0 / 128 + accs.part, ch0 = block * 128 + half * COLS;
         const float *sa = p.a_scale + (long long)(t.row0 + (mine ? in_tile : 0)) * p.blocks;
         const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + min(block, p.channel_blocks - 1)) * p.blocks;
         float2 acc[COLS / 2];
@@ -107,10 +112,10 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
             for (int c = 0; c < COLS / 16; ++c) {
                 tmem_ld_wait16(v[c & 1]);
                 if (c + 1 < COLS / 16) tmem_ld16(from + 16 * (c + 1), v[(c + 1) & 1]);
+                else accs.release();                     // all of them are in registers
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[c * 8 + j] = fma2(pair_of(&v[c & 1][2 * j]), s, acc[c * 8 + j]);
             }
-            accs.release();
         }
         if (mine) {
             Out *out = static_cast<Out *>(p.out) + (long long)(t.row0 + in_tile) * p.out_stride + ch0;
@@ -138,7 +143,7 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
 
 template <int TOKENS_, typename Out> struct BlockFew {
     static constexpr int TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
-    using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, 200 * 1024, 256 / COLS, COLS, 4, true>;
+    using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, 200 * 1024, 256 / COLS, COLS, 4, 1>;
     using Schedule = TileSchedule<TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
     const BmP &p;
@@ -160,11 +165,11 @@ template <int TOKENS_, typename Out> struct BlockFew {
         load_2d<1>(sa + BM_M_BYTES, map_a, bar, step * STAGE_ROW, f.a0);
     }
     __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TILE_CHANNELS, TOKENS); }
-    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool) const { multiply_step<1>(d, stage16, idesc); }
+    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool, int) const { multiply_step<1>(d, stage16, BM_M_BYTES / 16, idesc); }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
     {
         constexpr int PER_LANE = (TOKENS + 31) / 32;
-        const int quarter = (warp + 2) & 3, ch = t.channel0 + quarter * 32 + lane;
+        const int quarter = (warp + Shape::CONTROL) & 3, ch = t.channel0 + quarter * 32 + lane;
         float *own = factors + warp * 2 * TOKENS;
         const float *sa = p.a_scale + (long long)t.row0 * p.blocks;
         const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + t.channel0 / 128) * p.blocks;
@@ -250,7 +255,7 @@ int launch_rows(BmP p, const BmOperands &o, int device, cudaStream_t stream)
     using Shape = typename BlockRows<CTAS, CHANNELS, Out>::Shape;
     CUtensorMap a, b;
     p.row_tiles = (p.n - 1) / CHANNELS + 1;
-    if (!encode_operands(p, o, TILE_CHANNELS, CHANNELS / CTAS, &a, &b)) return MOE_OVL_ERR_CUDA;
+    if (!encode_operands(p, o, TILE_CHANNELS, 128 / CTAS, &a, &b)) return MOE_OVL_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
     const auto kernel = block_matmul_kernel<CTAS, CHANNELS, Out>;
     if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;

@@ -48,7 +48,7 @@ __device__ __forceinline__ uint64_t columns_desc(uint32_t saddr)
 template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
     static constexpr int SHARE = TOKENS / CTAS;                              // of the N side, per CTA
     static constexpr int COLS = TOKENS < 32 ? 32 : TOKENS;                   // of tensor memory
-    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 2, COLS, 8, false>;
+    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 2, COLS, 8, 0>;
     using Schedule = TileSchedule<CTAS * TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;                                    // FORM_COLUMNS: row0, rows are those of the output
     const GmP &p;
@@ -123,7 +123,7 @@ template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
         return p.types | (1u << 4) | (FORM != FORM_ROWS ? 1u << 15 : 0u) | (FORM == FORM_COLUMNS ? 1u << 16 : 0u) | ((uint32_t)(width(t) >> 3) << 17) |
                ((uint32_t)(CTAS * TILE_CHANNELS >> 4) << 24);
     }
-    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool first) const
+    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool first, int) const
     {
         const uint64_t dm = (FORM == FORM_ROWS ? umma_smem_desc(0) : columns_desc(0)) + stage16;
         const uint64_t dn = (FORM == FORM_COLUMNS ? columns_desc(0) : umma_smem_desc(0)) + stage16 + GM_M_BYTES / 16;

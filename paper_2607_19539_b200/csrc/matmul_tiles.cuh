@@ -122,14 +122,16 @@ template <int TOKENS, typename P> __device__ __forceinline__ void fill_schedule(
 // ------------------------------------------------------------------ persistent tiles in three roles
 
 // CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
-// ACC_COLS columns of tensor memory go round; with PER_STEP every step of K has one of its own (and the finishing warps add them up), otherwise every tile.
-template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, bool PER_STEP_> struct TileShape {
+// ACC_COLS columns of tensor memory go round.  PARTS 0: a tile has one accumulator, for all of its steps.  Otherwise every step has PARTS of them, side by side in the
+// tile, which a share of the finishing warps each adds up.
+template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, int PARTS_> struct TileShape {
     static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_;
-    static constexpr bool PER_STEP = PER_STEP_;
+    static constexpr bool PER_STEP = PARTS_ > 0;
+    static constexpr int PARTS = PARTS_ > 0 ? PARTS_ : 1;
     static constexpr int STAGES = SMEM_BYTES_ / STAGE_BYTES_;
-    static constexpr int THREADS = 64 + 32 * FINISHERS;
+    static constexpr int CONTROL = 2, THREADS = 32 * (CONTROL + FINISHERS);      // the load and the matrix warp
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
-    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32, "tensor memory");
+    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32 && ACCS % PARTS == 0 && FINISHERS % PARTS == 0, "tensor memory");
 };
 
 // Arrival of a reader of tensor memory, on a barrier that may be the peer CTA's.  What it gives back has been read (tcgen05.wait, and the fence
@@ -139,16 +141,14 @@ __device__ __forceinline__ void arrive_read(uint32_t cluster_bar)
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-// The finishing warps' way through the accumulators.  With PER_STEP a stage's "empty" is an accumulator's "full" too: one signal per step of the matrix
-// instructions instead of two (each costs as much as a step's instructions, see block_matmul.cu).
+// A finishing warp's way through the accumulators (of its part).
 template <typename Shape> struct Accumulators {
-    static constexpr int SIGNALS = Shape::PER_STEP ? Shape::STAGES : Shape::ACCS;
     uint32_t bar_full, lead_empty, tmem;
-    int lane, acc = 0, signal = 0;
+    int lane, part = 0, acc = 0;
     uint32_t phase = 0;
     template <typename P> __device__ __forceinline__ bool wait(const P &p, long long index)
     {
-        const bool ok = warp_wait(bar_full + 8 * signal, phase, p, index, lane);
+        const bool ok = warp_wait(bar_full + 8 * acc, phase, p, index, lane);
         tc_fence_after();
         return ok;
     }
@@ -158,8 +158,7 @@ template <typename Shape> struct Accumulators {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) arrive_read(lead_empty + 8 * acc);
-        if (++acc == Shape::ACCS) acc = 0;
-        if (++signal == SIGNALS) signal = 0, phase ^= 1u;
+        if ((acc += Shape::PARTS) >= Shape::ACCS) acc = part, phase ^= 1u;
     }
 };
 
@@ -184,7 +183,7 @@ template <typename Shape> __device__ void await_copies(uint32_t bar_full, uint32
 // accumulators.  Each role walks the same tiles.  The whole of a load or matrix warp runs its loop, with everything the same in all lanes, and one
 // elected lane issues: copies and matrix instructions take their operands from uniform registers.
 // `Work` says what a tile is: begin(lane) fills the tables, by one warp; total(); at(t); steps(tile) of K, 0 for a tile that nothing is loaded for;
-// load(tile's operands, shared address, barrier, step); instruction(tile); multiply(accumulator, stage's address / 16, instruction, first);
+// load(tile's operands, shared address, barrier, step); instruction(tile); multiply(accumulator, stage's address / 16, instruction, first, part);
 // finish(tile, accumulators, warp, lane), false when a wait gave up.
 template <typename Work, typename P> __device__ __forceinline__ void run_tiles(Work work, const P &p, uint8_t *smem_raw)
 {
@@ -211,7 +210,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     if (warp == 0) {
         for (int i = lane; i < 2 * STAGES + 2 * ACCS + 1; i += 32)
             // full: the first CTA's load thread arrives, expecting all CTAs' bytes; accumulators empty: one arrival per finishing warp
-            mbar_init(bar_full + 8 * i, i >= 2 * STAGES + ACCS && i < 2 * STAGES + 2 * ACCS ? Shape::FINISHERS * CTAS : 1);
+            mbar_init(bar_full + 8 * i, i >= 2 * STAGES + ACCS && i < 2 * STAGES + 2 * ACCS ? Shape::FINISHERS / Shape::PARTS * CTAS : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (lane == 0) s_gave_up = 0;
         __syncwarp();
@@ -229,8 +228,13 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     tc_fence_after();
     const uint32_t tmem = uniform(s_tmem);
     const long long total = work.total();
-
-    if (warp == 0) {
+    if (warp >= Shape::CONTROL) {
+        const int part = (warp - Shape::CONTROL) / (Shape::FINISHERS / Shape::PARTS);
+        Accumulators<Shape> accs{bar_tfull, lead_tempty, tmem, lane, part, part};
+        for (long long t = first; t < total; t += step)
+            if (!work.finish(work.at(t), accs, p, warp - Shape::CONTROL, lane)) break;         // a warp leaves the loop as one
+        __syncwarp();
+    } else if (warp == 0) {
         int stage = 0;
         uint32_t phase = 0, issued = 0;
         if (!p.no_loads) {
@@ -270,24 +274,28 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 const int steps = uniform(work.steps(tile));
                 for (int k = 0; k < steps; ++k) {
                     const bool begins = Shape::PER_STEP || k == 0, ends = Shape::PER_STEP || k == steps - 1;
-                    if (begins) {
-                        ok = __all_sync(0xffffffffu, short_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
-                        if (!ok) break;
-                    }
                     ok = __all_sync(0xffffffffu, short_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k));
                     if (!ok) break;
-                    tc_fence_after();
+#pragma unroll
+                    for (int part = 0; part < Shape::PARTS; ++part) {
+                        if (begins) ok = ok && __all_sync(0xffffffffu, short_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (leader) {
+                            work.multiply(tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins, part);
+                            if (ends) {
+                                if (CTAS == 1) umma_commit_one(bar_tfull + 8 * acc);
+                                else umma_commit_pair(bar_tfull + 8 * acc);
+                            }
+                        }
+                        if (ends && ++acc == ACCS) acc = 0, acc_phase ^= 1u;
+                    }
+                    if (!ok) break;
                     if (leader) {
-                        work.multiply(tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins);
                         if (CTAS == 1) umma_commit_one(bar_empty + 8 * stage);
                         else umma_commit_pair(bar_empty + 8 * stage);
-                        if (!Shape::PER_STEP && ends) {
-                            if (CTAS == 1) umma_commit_one(bar_tfull + 8 * acc);
-                            else umma_commit_pair(bar_tfull + 8 * acc);
-                        }
                     }
                     if (++stage == STAGES) stage = 0, phase ^= 1u;
-                    if (ends && ++acc == ACCS) acc = 0, acc_phase ^= 1u;
                 }
             }
             if (leader) {
@@ -298,11 +306,6 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
             drain(bar_drain, 0, globaltimer_ns());
             if (!ok && lane == 0) gave_up();
         }
-        __syncwarp();
-    } else {
-        Accumulators<Shape> accs{Shape::PER_STEP ? bar_empty : bar_tfull, lead_tempty, tmem, lane};
-        for (long long t = first; t < total; t += step)
-            if (!work.finish(work.at(t), accs, p, warp - 2, lane)) break;         // a warp leaves the loop as one
         __syncwarp();
     }
     tc_fence_before();
