@@ -102,12 +102,12 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
         for (int i = 0; i < COLS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
         float a_next = sa[0], b_next = sb[0];
         for (int k = 0; k < p.blocks; ++k) {
-            const float2 s = both(a_next * b_next);
-            if (k + 1 < p.blocks) a_next = sa[k + 1], b_next = sb[k + 1];
             if (!accs.wait(p, t.row0)) return false;
             const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
             uint32_t v[2][16];
             tmem_ld16(from, v[0]);
+            const float2 s = both(a_next * b_next);
+            if (k + 1 < p.blocks) a_next = sa[k + 1], b_next = sb[k + 1];
 #pragma unroll
             for (int c = 0; c < COLS / 16; ++c) {
                 tmem_ld_wait16(v[c & 1]);

@@ -56,8 +56,9 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned lo
     while (!mbar_try_wait(bar, parity) && globaltimer_ns() - since < LANDING_NS) {}
 }
 
-// mbar_wait, with its clock left alone at first: most waits of a pipeline are short, and reading the clock takes longer than they do.
-template <typename P> __device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity, const P &p, long long site, long long index)
+// mbar_wait in two parts: most of a pipeline's waits are over when they begin, and what else there is to a wait (its clock above all, which takes longer to
+// read than they last) stays out of the loops.
+template <typename P> __device__ __noinline__ bool long_wait(uint32_t bar, uint32_t parity, const P &p, long long site, long long index)
 {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
@@ -65,14 +66,12 @@ template <typename P> __device__ __forceinline__ bool short_wait(uint32_t bar, u
     return mbar_wait(bar, parity, p, site, index);
 }
 
-// A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
-template <typename P> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const P &p, long long index, int lane)
+// A whole warp's wait, by all of its lanes alike: a branch for one of them and passing on what it has seen takes longer than the wait mostly does
+// (the block product of 7919 x 28672 x 4096, a wait per 128 columns and 128 of K: 901 us with one lane's polls, 861 with all).
+template <typename P> __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const P &p, long long site, long long index)
 {
-    bool ok = true;
-    if (lane == 0) ok = short_wait(bar, parity, p, SITE_TILE_DONE, index);
-    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-    if (ok) mbar_try_wait(bar, parity);      // done already: this lane's own look, for the order of what it reads next
-    return ok;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, long_wait(bar, parity, p, site, index));
 }
 
 // Order of the tiles: experts one after the other; inside an expert up to TILE_GROUP token tiles form a group, and for each tile
@@ -148,7 +147,7 @@ template <typename Shape> struct Accumulators {
     uint32_t phase = 0;
     template <typename P> __device__ __forceinline__ bool wait(const P &p, long long index)
     {
-        const bool ok = warp_wait(bar_full + 8 * acc, phase, p, index, lane);
+        const bool ok = warp_wait(bar_full + 8 * acc, phase, p, SITE_TILE_DONE, index);
         tc_fence_after();
         return ok;
     }
@@ -245,7 +244,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 const int steps = uniform(work.steps(tile));
                 int k = 0;
                 for (; k < steps; ++k) {
-                    ok = __all_sync(0xffffffffu, short_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, t));
+                    ok = warp_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, t);
                     if (!ok) break;
                     if (leader) {
                         if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, CTAS * Shape::STAGE_BYTES);
@@ -274,11 +273,11 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 const int steps = uniform(work.steps(tile));
                 for (int k = 0; k < steps; ++k) {
                     const bool begins = Shape::PER_STEP || k == 0, ends = Shape::PER_STEP || k == steps - 1;
-                    ok = __all_sync(0xffffffffu, short_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k));
+                    ok = warp_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k);
                     if (!ok) break;
 #pragma unroll
                     for (int part = 0; part < Shape::PARTS; ++part) {
-                        if (begins) ok = ok && __all_sync(0xffffffffu, short_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t));
+                        if (begins) ok = ok && warp_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t);
                         if (!ok) break;
                         tc_fence_after();
                         if (leader) {

@@ -75,6 +75,16 @@ template <int BN> struct QmShape {
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
 };
 
+// A whole warp's wait, polled by one lane: the others' polls would only compete with the load and MMA threads' own.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const QmP &p, long long index, int lane)
+{
+    bool ok = true;
+    if (lane == 0) ok = mbar_wait(bar, parity, p, SITE_TILE_DONE, index);
+    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    if (ok) mbar_try_wait(bar, parity);      // done already: this lane's own look, for the order of what it reads next
+    return ok;
+}
+
 // Few tiles: one tile (128 channels x BN tokens) per cluster, whose SPLITS CTAs share its K.  Each leaves its part in its shared
 // memory, and the tokens are dealt out for the sum and the scaling.
 template <int BN, int SPLITS, typename Out>
