@@ -49,11 +49,11 @@ __device__ __forceinline__ float2 pair_of(const uint32_t *v) { return make_float
 // Instruction descriptor: 32-bit sums of e4m3, K along the rows of both operands.
 __device__ __forceinline__ uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
 // One step: 128 values of K.  `n16`: where the N side's operand begins in its stage, / 16.
-template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t d, uint32_t stage16, uint32_t n16, uint32_t idesc)
+template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t on, uint32_t d, uint32_t stage16, uint32_t n16, uint32_t idesc)
 {
     const uint64_t dm = umma_smem_desc(0) + stage16, dn = dm + n16;
 #pragma unroll
-    for (int i = 0; i < STAGE_ROW / 32; ++i) umma_f8<CTAS>(d, dm + (uint64_t)(i * 2), dn + (uint64_t)(i * 2), idesc, i > 0 ? 1u : 0u);
+    for (int i = 0; i < STAGE_ROW / 32; ++i) umma_f8<CTAS>(on, d, dm + (uint64_t)(i * 2), dn + (uint64_t)(i * 2), idesc, i > 0 ? 1u : 0u);
 }
 
 // ------------------------------------------------------------------ many rows
@@ -78,16 +78,16 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
     {
         return {uniform((int)((unsigned)t.row0 + (unsigned)(rank * TILE_CHANNELS))), uniform(t.channel0 + rank * SHARE), uniform(t.expert)};
     }
-    __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
+    __device__ __forceinline__ void load(uint32_t on, const From &f, uint32_t sa, uint32_t bar, int step) const
     {
-        load_2d<CTAS>(sa, map_a, bar, step * STAGE_ROW, f.a0);
+        load_2d<CTAS>(on, sa, map_a, bar, step * STAGE_ROW, f.a0);
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) load_3d<CTAS>(sa + BM_M_BYTES + i * SHARE * STAGE_ROW, map_b, bar, step * STAGE_ROW, f.b0 + i * 128, f.expert);
+        for (int i = 0; i < PARTS; ++i) load_3d<CTAS>(on, sa + BM_M_BYTES + i * SHARE * STAGE_ROW, map_b, bar, step * STAGE_ROW, f.b0 + i * 128, f.expert);
     }
     __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TOKENS, 128); }
-    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool, int part) const
+    __device__ __forceinline__ void multiply(uint32_t on, uint32_t d, uint32_t stage16, uint32_t idesc, bool, int part) const
     {
-        multiply_step<CTAS>(d, stage16, (BM_M_BYTES + part * SHARE * STAGE_ROW) / 16, idesc);
+        multiply_step<CTAS>(on, d, stage16, (BM_M_BYTES + part * SHARE * STAGE_ROW) / 16, idesc);
     }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
     {
@@ -104,17 +104,16 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
         for (int k = 0; k < p.blocks; ++k) {
             if (!accs.wait(p, t.row0)) return false;
             const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
-            uint32_t v[2][16];
-            tmem_ld16(from, v[0]);
             const float2 s = both(a_next * b_next);
             if (k + 1 < p.blocks) a_next = sa[k + 1], b_next = sb[k + 1];
 #pragma unroll
             for (int c = 0; c < COLS / 16; ++c) {
-                tmem_ld_wait16(v[c & 1]);
-                if (c + 1 < COLS / 16) tmem_ld16(from + 16 * (c + 1), v[(c + 1) & 1]);
-                else accs.release();                     // all of them are in registers
+                uint32_t v[16];
+                tmem_ld16(from + 16 * c, v);
+                tmem_ld_wait16(v);
+                if (c + 1 == COLS / 16) accs.release();          // all of them are in registers
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[c * 8 + j] = fma2(pair_of(&v[c & 1][2 * j]), s, acc[c * 8 + j]);
+                for (int j = 0; j < 8; ++j) acc[c * 8 + j] = fma2(pair_of(&v[2 * j]), s, acc[c * 8 + j]);
             }
         }
         if (mine) {
@@ -159,13 +158,13 @@ template <int TOKENS_, typename Out> struct BlockFew {
     __device__ __forceinline__ Tile at(long long t) { return sched.at(t); }
     __device__ __forceinline__ int steps(const Tile &) const { return p.blocks; }
     __device__ __forceinline__ From operands(const Tile &t, bool) const { return {uniform(t.row0), uniform(t.channel0), uniform(t.expert)}; }
-    __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
+    __device__ __forceinline__ void load(uint32_t on, const From &f, uint32_t sa, uint32_t bar, int step) const
     {
-        load_3d<1>(sa, map_b, bar, step * STAGE_ROW, f.b0, f.expert);
-        load_2d<1>(sa + BM_M_BYTES, map_a, bar, step * STAGE_ROW, f.a0);
+        load_3d<1>(on, sa, map_b, bar, step * STAGE_ROW, f.b0, f.expert);
+        load_2d<1>(on, sa + BM_M_BYTES, map_a, bar, step * STAGE_ROW, f.a0);
     }
     __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TILE_CHANNELS, TOKENS); }
-    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool, int) const { multiply_step<1>(d, stage16, BM_M_BYTES / 16, idesc); }
+    __device__ __forceinline__ void multiply(uint32_t on, uint32_t d, uint32_t stage16, uint32_t idesc, bool, int) const { multiply_step<1>(on, d, stage16, BM_M_BYTES / 16, idesc); }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
     {
         constexpr int PER_LANE = (TOKENS + 31) / 32;

@@ -99,23 +99,23 @@ template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
     {
         asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(map) : "memory");
     }
-    __device__ __forceinline__ void load(const From &f, uint32_t sa, uint32_t bar, int step) const
+    __device__ __forceinline__ void load(uint32_t on, const From &f, uint32_t sa, uint32_t bar, int step) const
     {
         const int k = f.k0 + step * GM_K;
         if constexpr (FORM == FORM_ROWS) {
-            load_3d<CTAS>(sa, f.m, bar, k, f.m0, f.expert);
+            load_3d<CTAS>(on, sa, f.m, bar, k, f.m0, f.expert);
         } else if constexpr (FORM == FORM_MIXED) {
 #pragma unroll
-            for (int i = 0; i < TILE_CHANNELS / 64; ++i) load_3d<CTAS>(sa + i * GM_BOX, f.m, bar, f.m0 + 64 * i, k, f.expert);
+            for (int i = 0; i < TILE_CHANNELS / 64; ++i) load_3d<CTAS>(on, sa + i * GM_BOX, f.m, bar, f.m0 + 64 * i, k, f.expert);
         } else {
 #pragma unroll
-            for (int i = 0; i < TILE_CHANNELS / 64; ++i) load_2d<CTAS>(sa + i * GM_BOX, f.m, bar, f.m0 + 64 * i, k);
+            for (int i = 0; i < TILE_CHANNELS / 64; ++i) load_2d<CTAS>(on, sa + i * GM_BOX, f.m, bar, f.m0 + 64 * i, k);
         }
         if constexpr (FORM == FORM_COLUMNS) {
 #pragma unroll
-            for (int i = 0; i < SHARE / 64; ++i) load_2d<CTAS>(sa + GM_M_BYTES + i * GM_BOX, f.n, bar, f.n0 + 64 * i, k);
+            for (int i = 0; i < SHARE / 64; ++i) load_2d<CTAS>(on, sa + GM_M_BYTES + i * GM_BOX, f.n, bar, f.n0 + 64 * i, k);
         } else {
-            load_2d<CTAS>(sa + GM_M_BYTES, f.n, bar, k, f.n0);
+            load_2d<CTAS>(on, sa + GM_M_BYTES, f.n, bar, k, f.n0);
         }
     }
     __device__ __forceinline__ uint32_t instruction(const Tile &t) const
@@ -123,14 +123,14 @@ template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
         return p.types | (1u << 4) | (FORM != FORM_ROWS ? 1u << 15 : 0u) | (FORM == FORM_COLUMNS ? 1u << 16 : 0u) | ((uint32_t)(width(t) >> 3) << 17) |
                ((uint32_t)(CTAS * TILE_CHANNELS >> 4) << 24);
     }
-    __device__ __forceinline__ void multiply(uint32_t d, uint32_t stage16, uint32_t idesc, bool first, int) const
+    __device__ __forceinline__ void multiply(uint32_t on, uint32_t d, uint32_t stage16, uint32_t idesc, bool first, int) const
     {
         const uint64_t dm = (FORM == FORM_ROWS ? umma_smem_desc(0) : columns_desc(0)) + stage16;
         const uint64_t dn = (FORM == FORM_COLUMNS ? columns_desc(0) : umma_smem_desc(0)) + stage16 + GM_M_BYTES / 16;
         constexpr int STEP_M = FORM == FORM_ROWS ? 2 : 16 * STAGE_ROW / 16, STEP_N = FORM == FORM_COLUMNS ? 16 * STAGE_ROW / 16 : 2;
 #pragma unroll
         for (int i = 0; i < GM_K / 16; ++i)
-            umma_f16<CTAS>(d, dm + (uint64_t)(i * STEP_M), dn + (uint64_t)(i * STEP_N), idesc, first && i == 0 ? 0u : 1u);
+            umma_f16<CTAS>(on, d, dm + (uint64_t)(i * STEP_M), dn + (uint64_t)(i * STEP_N), idesc, first && i == 0 ? 0u : 1u);
     }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const GmP &, int warp, int lane) const
     {

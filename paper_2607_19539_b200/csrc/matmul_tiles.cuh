@@ -118,6 +118,86 @@ template <int TOKENS, typename P> __device__ __forceinline__ void fill_schedule(
     __syncwarp();
 }
 
+// What one elected lane does of a warp that runs the same code in all of them: the instruction is predicated (`on`: in the elected lane), and its operands are made by
+// all lanes alike, in uniform registers.  Behind a branch for one lane they would have to be gathered from that lane, which takes longer than the rest of a step.
+
+// Tile loads of two and three dimensions, into this CTA's shared memory, counted on its barrier or (CTAS == 2) on one that may be the peer's.
+template <int CTAS> __device__ __forceinline__ void load_2d(uint32_t on, uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)
+{
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(on)
+            : "memory");
+}
+template <int CTAS> __device__ __forceinline__ void load_3d(uint32_t on, uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+            "@q cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+            "@q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(on)
+            : "memory");
+}
+__device__ __forceinline__ void expect_bytes(uint32_t on, uint32_t bar, uint32_t bytes)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}"
+        ::"r"(bar), "r"(bytes), "r"(on)
+        : "memory");
+}
+
+// D[tmem] (+)= A[smem] * B[smem] with 32-bit sums, by this CTA or by the CTA pair: 16-bit floats, K = 16, or 8-bit floats, K = 32.
+#define MOE_OVL_UMMA(GROUP, KIND)                                                                                                   \
+    asm volatile(                                                                                                                   \
+        "{\n\t.reg .pred p, q;\n\t"                                                                                                 \
+        "setp.ne.b32 p, %4, 0;\n\t"                                                                                                 \
+        "setp.ne.b32 q, %5, 0;\n\t"                                                                                                 \
+        "@q tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, p;\n\t}"                                              \
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)                                               \
+        : "memory")
+template <int CTAS> __device__ __forceinline__ void umma_f16(uint32_t on, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (CTAS == 1) MOE_OVL_UMMA("1", "f16");
+    else MOE_OVL_UMMA("2", "f16");
+}
+template <int CTAS> __device__ __forceinline__ void umma_f8(uint32_t on, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (CTAS == 1) MOE_OVL_UMMA("1", "f8f6f4");
+    else MOE_OVL_UMMA("2", "f8f6f4");
+}
+#undef MOE_OVL_UMMA
+// One arrival, in both CTAs of a pair, when every matrix instruction issued so far by this thread has finished.
+template <int CTAS> __device__ __forceinline__ void commit(uint32_t on, uint32_t bar)
+{
+    if constexpr (CTAS == 1)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+            ::"r"(bar), "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+            "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+            ::"r"(bar), "h"((uint16_t)3), "r"(on)
+            : "memory");
+}
+
 // ------------------------------------------------------------------ persistent tiles in three roles
 
 // CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
@@ -182,7 +262,7 @@ template <typename Shape> __device__ void await_copies(uint32_t bar_full, uint32
 // accumulators.  Each role walks the same tiles.  The whole of a load or matrix warp runs its loop, with everything the same in all lanes, and one
 // elected lane issues: copies and matrix instructions take their operands from uniform registers.
 // `Work` says what a tile is: begin(lane) fills the tables, by one warp; total(); at(t); steps(tile) of K, 0 for a tile that nothing is loaded for;
-// load(tile's operands, shared address, barrier, step); instruction(tile); multiply(accumulator, stage's address / 16, instruction, first, part);
+// load(on, tile's operands, shared address, barrier, step); instruction(tile); multiply(on, accumulator, stage's address / 16, instruction, first, part);
 // finish(tile, accumulators, warp, lane), false when a wait gave up.
 template <typename Work, typename P> __device__ __forceinline__ void run_tiles(Work work, const P &p, uint8_t *smem_raw)
 {
@@ -237,7 +317,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
         int stage = 0;
         uint32_t phase = 0, issued = 0;
         if (!p.no_loads) {
-            const bool leader = elect_one();
+            const uint32_t leader = elect_one(), announces = leader && rank == 0;
             for (long long t = first; ok && t < total; t += step) {
                 const auto tile = work.at(t);
                 const auto from = work.operands(tile, leader);
@@ -246,10 +326,8 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 for (; k < steps; ++k) {
                     ok = warp_wait(bar_empty + 8 * stage, phase ^ 1u, p, SITE_TILE_EMPTY, t);
                     if (!ok) break;
-                    if (leader) {
-                        if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, CTAS * Shape::STAGE_BYTES);
-                        work.load(from, smem_base + stage * Shape::STAGE_BYTES, lead_full + 8 * stage, k);
-                    }
+                    expect_bytes(announces, bar_full + 8 * stage, CTAS * Shape::STAGE_BYTES);
+                    work.load(leader, from, smem_base + stage * Shape::STAGE_BYTES, lead_full + 8 * stage, k);
                     if (++stage == STAGES) stage = 0, phase ^= 1u;
                 }
                 issued += (uint32_t)k;
@@ -264,7 +342,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
-            const bool leader = elect_one();
+            const uint32_t leader = elect_one();
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             for (long long t = first; ok && t < total; t += step) {
@@ -280,20 +358,12 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                         if (begins) ok = ok && warp_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t);
                         if (!ok) break;
                         tc_fence_after();
-                        if (leader) {
-                            work.multiply(tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins, part);
-                            if (ends) {
-                                if (CTAS == 1) umma_commit_one(bar_tfull + 8 * acc);
-                                else umma_commit_pair(bar_tfull + 8 * acc);
-                            }
-                        }
+                        work.multiply(leader, tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins, part);
+                        if (ends) commit<CTAS>(leader, bar_tfull + 8 * acc);
                         if (ends && ++acc == ACCS) acc = 0, acc_phase ^= 1u;
                     }
                     if (!ok) break;
-                    if (leader) {
-                        if (CTAS == 1) umma_commit_one(bar_empty + 8 * stage);
-                        else umma_commit_pair(bar_empty + 8 * stage);
-                    }
+                    commit<CTAS>(leader, bar_empty + 8 * stage);
                     if (++stage == STAGES) stage = 0, phase ^= 1u;
                 }
             }
@@ -324,55 +394,6 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
         if (CTAS == 1) tmem_dealloc_self(tmem, ACCS * Shape::ACC_COLS);
         else tmem_dealloc(tmem, ACCS * Shape::ACC_COLS);
     }
-}
-
-// Tile loads of two and three dimensions, into this CTA's shared memory, counted on its barrier or (CTAS == 2) on one that may be the peer's.
-template <int CTAS> __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)
-{
-    if constexpr (CTAS == 1) tma_load_2d_self(dst, map, bar, x, y);
-    else tma_load_2d(dst, map, bar, x, y);
-}
-template <int CTAS> __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
-{
-    if constexpr (CTAS == 1)
-        asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
-                     : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
-                     : "memory");
-}
-
-// D[tmem] (+)= A[smem] * B[smem] with 32-bit sums, by this CTA or by the CTA pair: 16-bit floats, K = 16, or 8-bit floats, K = 32.
-template <int CTAS> __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
-{
-    if constexpr (CTAS == 1)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-            : "memory");
-    else
-        umma_bf16(d_tmem, a_desc, b_desc, idesc, accumulate);
-}
-template <int CTAS> __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
-{
-    if constexpr (CTAS == 1)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "setp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-            : "memory");
 }
 
 // ------------------------------------------------------------------ host
