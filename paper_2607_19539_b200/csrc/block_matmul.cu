@@ -35,8 +35,22 @@ struct BmP {
     bool wide;                               // rows of the output begin on 16 bytes
 };
 
-// The wait for values asked of tensor memory; they are operands so that no use of them can move in front of it.
-__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&v)[16])
+// 32 lanes x 8 columns, and the wait for values asked of tensor memory; they are operands of the wait so that no use of them can move in front of it.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[16])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
@@ -60,12 +74,14 @@ template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t on, u
 
 template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
     static constexpr int TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
-    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 200 * 1024, 4, 128, 8, PARTS>;
+    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 168 * 1024, 4, 128, 8, PARTS>;
+    static constexpr int STAGE_OUT = 32 * 128;
     using Schedule = TileSchedule<CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
     const BmP &p;
     const CUtensorMap *map_a, *map_b;
     int *tile_start, *row_start;
+    uint8_t *stage;                          // [finishing warps][STAGE_OUT]
     Schedule sched;
     int rank = 0;
 
@@ -106,35 +122,59 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
             const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
             const float2 s = both(a_next * b_next);
             if (k + 1 < p.blocks) a_next = sa[k + 1], b_next = sb[k + 1];
+            // eight columns at a time: the sums take 128 of the 168 registers, and two chunks or wider ones push other values out of them
 #pragma unroll
-            for (int c = 0; c < COLS / 16; ++c) {
-                uint32_t v[16];
-                tmem_ld16(from + 16 * c, v);
-                tmem_ld_wait16(v);
-                if (c + 1 == COLS / 16) accs.release();          // all of them are in registers
+            for (int c = 0; c < COLS; c += 8) {
+                uint32_t v[8];
+                tmem_ld8(from + c, v);
+                tmem_ld_wait(v);
+                if (c + 8 == COLS) accs.release();               // all of them are in registers
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[c * 8 + j] = fma2(pair_of(&v[2 * j]), s, acc[c * 8 + j]);
+                for (int j = 0; j < 4; ++j) acc[c / 2 + j] = fma2(pair_of(&v[2 * j]), s, acc[c / 2 + j]);
             }
         }
-        if (mine) {
-            Out *out = static_cast<Out *>(p.out) + (long long)(t.row0 + in_tile) * p.out_stride + ch0;
-            const int left = p.n - ch0;
-            constexpr int VEC = 16 / sizeof(Out);
-            if (p.wide && left >= COLS) {
+        store(t, acc, rank * TILE_CHANNELS + quarter * 32, ch0, stage + warp * STAGE_OUT, lane);
+        return true;
+    }
+    // A warp's 32 rows of COLS sums: 128 bytes of each row go through shared memory, 16 bytes of them in turn, so that a store's lanes lie next to each other.  A thread's own
+    // row straight from its registers is 32 lines of memory per store, which took as long as nine steps of K.
+    __device__ __forceinline__ void store(const Tile &t, const float2 (&acc)[COLS / 2], int row0, int ch0, uint8_t *own, int lane) const
+    {
+        constexpr int VEC = 16 / (int)sizeof(Out), WIDE = 128 / (int)sizeof(Out);
+        const int rows = min(t.rows - row0, 32);
+        Out *out = static_cast<Out *>(p.out) + (long long)(t.row0 + row0) * p.out_stride + ch0;
 #pragma unroll
-                for (int i = 0; i < COLS; i += VEC) {
-                    Pack<Out, VEC> pack;
+        for (int c0 = 0; c0 < COLS; c0 += WIDE) {
+            const int left = p.n - ch0 - c0;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) pack.v[j] = from_f32<Out>((i + j) & 1 ? acc[(i + j) / 2].y : acc[(i + j) / 2].x);
-                    store_pack(out + i, pack);
+            for (int i = 0; i < 8; ++i) {
+                Pack<Out, VEC> pack;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int c = c0 + i * VEC + j;
+                    pack.v[j] = from_f32<Out>(c & 1 ? acc[c / 2].y : acc[c / 2].x);
+                }
+                *reinterpret_cast<uint4 *>(own + lane * 128 + (i ^ (lane & 7)) * 16) = *reinterpret_cast<const uint4 *>(&pack);
+            }
+            __syncwarp();
+            if (p.wide && left >= WIDE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int row = i * 4 + lane / 8;
+                    const uint4 piece = *reinterpret_cast<const uint4 *>(own + row * 128 + ((lane ^ row) & 7) * 16);
+                    if (row < rows) *reinterpret_cast<uint4 *>(out + (long long)row * p.out_stride + c0 + lane % 8 * VEC) = piece;
                 }
             } else {
+                for (int row = 0; row < rows; ++row)
 #pragma unroll
-                for (int i = 0; i < COLS; ++i)
-                    if (i < left) out[i] = from_f32<Out>(i & 1 ? acc[i / 2].y : acc[i / 2].x);
+                    for (int c = 0; c < WIDE; c += 32) {
+                        const int col = c + lane;
+                        const Out v = *reinterpret_cast<const Out *>(own + row * 128 + ((col / VEC ^ row) & 7) * 16 + col % VEC * (int)sizeof(Out));
+                        if (col < left) out[(long long)row * p.out_stride + c0 + col] = v;
+                    }
             }
+            __syncwarp();
         }
-        return true;
     }
 };
 
@@ -197,7 +237,7 @@ template <int TOKENS_, typename Out> struct BlockFew {
                 if (c < t.rows) {
                     uint32_t v[16];
                     tmem_ld16(from + c, v);
-                    tmem_ld_wait16(v);
+                    tmem_ld_wait(v);
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
                         const float4 f = *reinterpret_cast<const float4 *>(s + c + j);
@@ -227,7 +267,9 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
-    run_tiles(BlockRows<CTAS, CHANNELS, Out>{p, &map_a, &map_b, s_tile_start, s_row_start, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+    using Work = BlockRows<CTAS, CHANNELS, Out>;
+    __shared__ __align__(16) uint8_t s_out[Work::Shape::FINISHERS * Work::STAGE_OUT];
+    run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_out, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
 template <int TOKENS, typename Out>
