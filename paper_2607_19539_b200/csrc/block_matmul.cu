@@ -35,29 +35,6 @@ struct BmP {
     bool wide;                               // rows of the output begin on 16 bytes
 };
 
-// 32 lanes x 8 columns, and the wait for values asked of tensor memory; they are operands of the wait so that no use of them can move in front of it.
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-                 : "r"(taddr)
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[8])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7])
-                 :
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
-                   "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
-                 :
-                 : "memory");
-}
 __device__ __forceinline__ float2 pair_of(const uint32_t *v) { return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])); }
 
 // Instruction descriptor: 32-bit sums of e4m3, K along the rows of both operands.
@@ -74,7 +51,7 @@ template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t on, u
 
 template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
     static constexpr int TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
-    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 168 * 1024, 4, 128, 8, PARTS>;
+    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 168 * 1024, 4, 128, 8, 1, PARTS>;
     static constexpr int STAGE_OUT = 32 * 128;
     using Schedule = TileSchedule<CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;

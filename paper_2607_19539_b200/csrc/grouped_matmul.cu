@@ -21,6 +21,10 @@ constexpr int GM_K = STAGE_ROW / 2;          // K per pipeline stage
 constexpr int GM_BOX = STAGE_ROW * GM_K;     // bytes of 64 columns x 64 rows, K down the columns
 constexpr int GM_M_BYTES = TILE_CHANNELS * STAGE_ROW;
 
+// The tensor cores cut a sum off where they add to it, instead of rounding: its error grows with the number of steps, 8.4e-6 of a gradient over 6000 rows where 32-bit
+// sums are off by 9e-7.  16-bit outputs do not see that; for 32-bit ones a sum ends after 512 of K, and the finishing warps add the pieces up in registers.
+constexpr int GM_SEGMENT = 512 / GM_K;
+
 // What K runs along: rows of both operands; columns of the M side's; columns of both
 enum { FORM_ROWS = 0, FORM_MIXED = 1, FORM_COLUMNS = 2 };
 
@@ -48,7 +52,8 @@ __device__ __forceinline__ uint64_t columns_desc(uint32_t saddr)
 template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
     static constexpr int SHARE = TOKENS / CTAS;                              // of the N side, per CTA
     static constexpr int COLS = TOKENS < 32 ? 32 : TOKENS;                   // of tensor memory
-    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 2, COLS, 8, 0>;
+    static constexpr bool WIDE = sizeof(Out) == 4;
+    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, 200 * 1024, 2, COLS, 8, WIDE ? GM_SEGMENT : 0>;
     using Schedule = TileSchedule<CTAS * TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;                                    // FORM_COLUMNS: row0, rows are those of the output
     const GmP &p;
@@ -132,6 +137,17 @@ template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
         for (int i = 0; i < GM_K / 16; ++i)
             umma_f16<CTAS>(on, d, dm + (uint64_t)(i * STEP_M), dn + (uint64_t)(i * STEP_N), idesc, first && i == 0 ? 0u : 1u);
     }
+    // 32 rows of the output from row c of the tile on, one column per lane.
+    __device__ __forceinline__ void store(const Tile &t, const float *sum, int c, int ch, bool in) const
+    {
+        Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)(t.row0 + c) * p.out_stride + ch;
+        const int left = t.rows - c;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (in && j < left) *out = from_f32<Out>(FORM == FORM_COLUMNS && p.accumulate ? sum[j] + to_f32(*out) : sum[j]);
+            out += p.out_stride;
+        }
+    }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const GmP &, int warp, int lane) const
     {
         const int quarter = (warp + 2) & 3, half = warp >> 2;        // a warp reads the lanes of its position among four; every other 32 columns
@@ -139,23 +155,43 @@ template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
         const bool in = (unsigned)ch < (unsigned)p.n, none = steps(t) == 0;
         if (none && p.accumulate) return true;
         if (!none && !accs.wait(p, t.row0)) return false;
+        if constexpr (WIDE) {
+            constexpr int MINE = TOKENS <= 32 ? 32 : TOKENS / 2;
+            float acc[MINE] = {};
+            if (half * 32 < COLS) {
+                for (int k = 0; k < steps(t); k += GM_SEGMENT) {
+                    if (k > 0 && !accs.wait(p, t.row0)) return false;
+                    const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 32);
+#pragma unroll
+                    for (int c = 0; c < MINE; c += 8) {
+                        uint32_t v[8];
+                        tmem_ld8(from + c % 32 + c / 32 * 64, v);
+                        tmem_ld_wait(v);
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2) {
+                            const float2 sum = add2(make_float2(acc[c + j], acc[c + j + 1]), make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])));
+                            acc[c + j] = sum.x, acc[c + j + 1] = sum.y;
+                        }
+                    }
+                    accs.release();
+                }
+#pragma unroll
+                for (int c = 0; c < MINE; c += 32) store(t, &acc[c], half * 32 + c * 2, ch, in);
+            } else {
+                for (int k = 0; k < steps(t); k += GM_SEGMENT) {
+                    if (k > 0 && !accs.wait(p, t.row0)) return false;
+                    accs.release();
+                }
+            }
+            return true;
+        }
         for (int c = half * 32; c < t.rows; c += 64) {
             uint32_t v[32] = {};
             if (!none) {
                 tmem_ld32(accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
                 tmem_ld_wait();
             }
-            Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)(t.row0 + c) * p.out_stride + ch;
-            const int left = t.rows - c;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                if (in && j < left) {
-                    float sum = __uint_as_float(v[j]);
-                    if (FORM == FORM_COLUMNS && p.accumulate) sum += to_f32(*out);
-                    *out = from_f32<Out>(sum);
-                }
-                out += p.out_stride;
-            }
+            store(t, reinterpret_cast<const float *>(v), c, ch, in);
         }
         if (!none) accs.release();
         return true;

@@ -198,15 +198,37 @@ template <int CTAS> __device__ __forceinline__ void commit(uint32_t on, uint32_t
             : "memory");
 }
 
+// 32 lanes x 8 columns, and the wait for values asked of tensor memory; they are operands of the wait so that no use of them can move in front of it.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                   "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+
 // ------------------------------------------------------------------ persistent tiles in three roles
 
 // CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
-// ACC_COLS columns of tensor memory go round.  PARTS 0: a tile has one accumulator, for all of its steps.  Otherwise every step has PARTS of them, side by side in the
-// tile, which a share of the finishing warps each adds up.
-template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, int PARTS_> struct TileShape {
-    static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_;
-    static constexpr bool PER_STEP = PARTS_ > 0;
-    static constexpr int PARTS = PARTS_ > 0 ? PARTS_ : 1;
+// ACC_COLS columns of tensor memory go round.  SEGMENT 0: a tile has one accumulator, for all of its steps.  Otherwise every SEGMENT steps have PARTS of them, side by side
+// in the tile, which a share of the finishing warps each adds up.
+template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, int SEGMENT_, int PARTS_ = 1> struct TileShape {
+    static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_, SEGMENT = SEGMENT_, PARTS = PARTS_;
     static constexpr int STAGES = SMEM_BYTES_ / STAGE_BYTES_;
     static constexpr int CONTROL = 2, THREADS = 32 * (CONTROL + FINISHERS);      // the load and the matrix warp
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
@@ -350,7 +372,8 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 const uint32_t idesc = uniform(work.instruction(tile));
                 const int steps = uniform(work.steps(tile));
                 for (int k = 0; k < steps; ++k) {
-                    const bool begins = Shape::PER_STEP || k == 0, ends = Shape::PER_STEP || k == steps - 1;
+                    const bool begins = Shape::SEGMENT ? k % max(Shape::SEGMENT, 1) == 0 : k == 0;
+                    const bool ends = k == steps - 1 || (Shape::SEGMENT && k % max(Shape::SEGMENT, 1) == Shape::SEGMENT - 1);
                     ok = warp_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k);
                     if (!ok) break;
 #pragma unroll
