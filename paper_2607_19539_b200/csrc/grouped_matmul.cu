@@ -141,11 +141,18 @@ template <int CTAS, int TOKENS, int FORM, typename Out> struct GmWork {
     __device__ __forceinline__ void store(const Tile &t, const float *sum, int c, int ch, bool in) const
     {
         Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)(t.row0 + c) * p.out_stride + ch;
-        const int left = t.rows - c;
+        const int left = in ? t.rows - c : 0;
+        if (FORM == FORM_COLUMNS && p.accumulate) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            if (in && j < left) *out = from_f32<Out>(FORM == FORM_COLUMNS && p.accumulate ? sum[j] + to_f32(*out) : sum[j]);
-            out += p.out_stride;
+            for (int j = 0; j < 32; ++j)
+                if (j < left) out[j * p.out_stride] = from_f32<Out>(sum[j] + to_f32(out[j * p.out_stride]));
+        } else if (left >= 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, out += p.out_stride) *out = from_f32<Out>(sum[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, out += p.out_stride)
+                if (j < left) *out = from_f32<Out>(sum[j]);
         }
     }
     __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const GmP &, int warp, int lane) const
