@@ -842,7 +842,7 @@ def test_refusals_of_the_c_calls():
             dict(dy=p + 1), dict(dweight=p + 2), dict(dy_stride=63), dict(x_stride=63), dict(dweight_stride=63), dict(dweight_expert_stride=0)])
     refused("moe_ovl_grouped_matmul_backward", ops.GroupedMatmulBackwardArgs, good, [dict(num_experts=1025), dict(n=1 << 25), dict(dy=p + 8), dict(x=p + 2), dict(dy_stride=68),
             dict(x_stride=1 << 31), dict(dweight_expert_stride=1 << 39)], B.ERR_UNSUPPORTED)
-    refused("moe_ovl_grouped_matmul_backward", ops.GroupedMatmulBackwardArgs, good, [dict(workspace=0), dict(workspace=p + 64), dict(workspace_bytes=511)], B.ERR_WORKSPACE)
+    refused("moe_ovl_grouped_matmul_backward", ops.GroupedMatmulBackwardArgs, good, [dict(workspace=0), dict(workspace=p + 64), dict(workspace_bytes=519)], B.ERR_WORKSPACE)
     good = dict(rows=9, depth=1, k=64, x=p, q=p, scale=p, x_stride=64, q_stride=64)
     refused("moe_ovl_block_quant", ops.BlockQuantArgs, good, [dict(struct_size=8), dict(device=-1), dict(depth=0), dict(depth=2), dict(rows=-1), dict(k=0), dict(dtype=3), dict(gated=2),
             dict(tiles=2), dict(gated=1, tiles=1, x_stride=128), dict(flags=1), dict(x=0), dict(q=0), dict(scale=0), dict(scale=p + 1), dict(x=p + 1), dict(x_stride=63), dict(q_stride=63),
@@ -870,8 +870,8 @@ def test_refusals_of_the_c_calls():
 
 
 def test_workspaces_and_limits():
-    assert ops.moe_ovl_grouped_matmul_workspace_bytes(0) == ops.moe_ovl_grouped_matmul_workspace_bytes(1) == 256
-    assert ops.moe_ovl_grouped_matmul_workspace_bytes(ops.MAX_GROUPS) == 256 * ops.MAX_GROUPS
+    assert ops.moe_ovl_grouped_matmul_workspace_bytes(0) == ops.moe_ovl_grouped_matmul_workspace_bytes(1) == 260
+    assert ops.moe_ovl_grouped_matmul_workspace_bytes(ops.MAX_GROUPS) == 260 * ops.MAX_GROUPS
     assert ops.moe_ovl_grad_norm_workspace_bytes(0) == ops.moe_ovl_grad_norm_workspace_bytes(960) < ops.moe_ovl_grad_norm_workspace_bytes(961)
     for call, n, code in ((ops.moe_ovl_grouped_matmul_workspace_bytes, -1, B.ERR_INVALID_ARG), (ops.moe_ovl_grouped_matmul_workspace_bytes, 1025, B.ERR_UNSUPPORTED),
                           (ops.moe_ovl_grad_norm_workspace_bytes, -1, B.ERR_INVALID_ARG), (ops.moe_ovl_grad_norm_workspace_bytes, 65537, B.ERR_UNSUPPORTED)):
