@@ -50,7 +50,7 @@ template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t on, u
 // ------------------------------------------------------------------ many rows
 
 template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
-    static constexpr int TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
+    static constexpr int SPLITS = 1, TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
     using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 168 * 1024, 4, 128, 8, 1, PARTS>;
     static constexpr int STAGE_OUT = 32 * 128;
     using Schedule = TileSchedule<CHANNELS, TOKENS>;
@@ -158,7 +158,7 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
 // ------------------------------------------------------------------ few rows
 
 template <int TOKENS_, typename Out> struct BlockFew {
-    static constexpr int TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
+    static constexpr int SPLITS = 1, TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
     using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, 200 * 1024, 256 / COLS, COLS, 4, 1>;
     using Schedule = TileSchedule<TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
@@ -242,7 +242,7 @@ template <int CTAS, int CHANNELS, typename Out>
 __global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, Out>::Shape::THREADS, 1)
 block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
 {
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
     using Work = BlockRows<CTAS, CHANNELS, Out>;
     __shared__ __align__(16) uint8_t s_out[Work::Shape::FINISHERS * Work::STAGE_OUT];
@@ -253,7 +253,7 @@ template <int TOKENS, typename Out>
 __global__ void __launch_bounds__(BlockFew<TOKENS, Out>::Shape::THREADS, 1)
 block_matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
 {
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
     __shared__ __align__(16) float s_factors[4 * 2 * TOKENS];
     run_tiles(BlockFew<TOKENS, Out>{p, &map_a, &map_b, s_tile_start, s_row_start, s_factors, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);

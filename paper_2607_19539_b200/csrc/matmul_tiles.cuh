@@ -222,6 +222,13 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[16])
                  : "memory");
 }
 
+__device__ __forceinline__ float4 ld_shared_cluster_f32x4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
 // ------------------------------------------------------------------ persistent tiles in three roles
 
 // CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
@@ -285,7 +292,8 @@ template <typename Shape> __device__ void await_copies(uint32_t bar_full, uint32
 // elected lane issues: copies and matrix instructions take their operands from uniform registers.
 // `Work` says what a tile is: begin(lane) fills the tables, by one warp; total(); at(t); steps(tile) of K, 0 for a tile that nothing is loaded for;
 // load(on, tile's operands, shared address, barrier, step); instruction(tile); multiply(on, accumulator, stage's address / 16, instruction, first, part);
-// finish(tile, accumulators, warp, lane), false when a wait gave up.
+// finish(tile, accumulators, warp, lane), false when a wait gave up.  With SPLITS > 1 a cluster of that many CTAs works on one tile, each on its `split` of the steps; finish()
+// leaves the part in shared memory and join(tile), called by all threads when the parts of all are there, adds them up.
 template <typename Work, typename P> __device__ __forceinline__ void run_tiles(Work work, const P &p, uint8_t *smem_raw)
 {
     using Shape = typename Work::Shape;
@@ -294,14 +302,18 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     __shared__ uint32_t s_tmem;
     __shared__ uint32_t s_gave_up, s_issued[2];      // a wait for operands or room ran out, here or in the peer; rank 0: stages that each CTA has issued
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t operands16 = (smem_base & 0x3ffffu) / 16;         // in a cluster the address has the CTA's place above these bits
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * STAGES;
     const uint32_t bar_tfull = bar_empty + 8 * STAGES, bar_tempty = bar_tfull + 8 * ACCS, bar_drain = bar_tempty + 8 * ACCS;
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
-    const uint32_t rank = CTAS == 1 ? 0 : cluster_ctarank();
+    // alone, one of a pair, or one of Work::SPLITS that share a tile's steps
+    static_assert(CTAS == 1 || Work::SPLITS == 1, "pairs do not share steps");
+    const uint32_t place = CTAS * Work::SPLITS == 1 ? 0 : cluster_ctarank(), rank = CTAS == 1 ? 0 : place;
     const uint32_t lead_full = CTAS == 1 ? bar_full : map_to_cta(bar_full, 0);
     const uint32_t lead_tempty = CTAS == 1 ? bar_tempty : map_to_cta(bar_tempty, 0);
-    const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    const long long first = blockIdx.x / (CTAS * Work::SPLITS), step = gridDim.x / (CTAS * Work::SPLITS);
     work.rank = (int)rank;
+    if constexpr (Work::SPLITS > 1) work.split = (int)place;
     bool ok = true;
     auto gave_up = [&]() {
         s_gave_up = 1;
@@ -381,7 +393,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                         if (begins) ok = ok && warp_wait(bar_tempty + 8 * acc, acc_phase ^ 1u, p, SITE_TILE_DONE, t);
                         if (!ok) break;
                         tc_fence_after();
-                        work.multiply(leader, tmem + (uint32_t)(acc * Shape::ACC_COLS), (smem_base + (uint32_t)stage * Shape::STAGE_BYTES) / 16, idesc, begins, part);
+                        work.multiply(leader, tmem + (uint32_t)(acc * Shape::ACC_COLS), operands16 + (uint32_t)stage * (Shape::STAGE_BYTES / 16), idesc, begins, part);
                         if (ends) commit<CTAS>(leader, bar_tfull + 8 * acc);
                         if (ends && ++acc == ACCS) acc = 0, acc_phase ^= 1u;
                     }
@@ -403,6 +415,12 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     tc_fence_before();
     __syncthreads();
     if (CTAS == 2) cluster_sync_all();          // the peer no longer signals this CTA's barriers or reads its operands
+    if constexpr (Work::SPLITS > 1) {
+        cluster_sync_all();                     // the parts are in everybody's shared memory
+        if (first < total) work.join(work.at(first));
+        __syncwarp();
+        cluster_sync_all();                     // and stay until everybody has read them
+    }
     if (s_gave_up) {
         // but copies may be under way, which rank 0's barriers count for both, and matrix instructions' signals to rank 1
         if (threadIdx.x == 0) {
