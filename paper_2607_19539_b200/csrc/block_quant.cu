@@ -3,7 +3,7 @@
 //
 // 16-bit values lie half-way between two of e4m3's steps often (max|v| = 1.75 puts one in sixteen there), so the quotient is rounded as
 // division rounds it: a product with a rounded 448 / max|v| would send ties either way.  The division is one by Newton's step on the remainder (P. Markstein, Computation
-// of elementary functions on the IBM RISC System/6000 processor, 1990): with r the rounded reciprocal of d, q0 = n r and q = q0 + r (n - d q0), the
+// of elementary functions on the IBM RISC System/6000 processor, 1990): with r the reciprocal of d, q0 = n r and q = q0 + r (n - d q0), the
 // remainder formed exactly by a fused operation.  n and d are scaled by a power of two, d into [2, 4), so that nothing overflows.
 #include <cuda_fp8.h>
 
@@ -29,14 +29,19 @@ __device__ __forceinline__ Divisor divisor_of(float most)
 {
     Divisor d;
     d.none = !(most >= BQ_TINY && most <= 3.402823466e38f);
-    d.scale = most < BQ_TINY ? 0.0f : most > 3.402823466e38f ? __int_as_float(0x7fffffff) : __fdiv_rn(most, BQ_LARGEST);
+    const bool low = most < BQ_TINY;
     if (d.none) most = 1.0f;
+    // by the same step: the reciprocal of 448 is a constant
+    const float s0 = most * (1.0f / BQ_LARGEST), scale = fmaf(fmaf(-s0, BQ_LARGEST, most), 1.0f / BQ_LARGEST, s0);
+    d.scale = low ? 0.0f : d.none ? __int_as_float(0x7fffffff) : scale;
     // 2^(1 - exponent of most): the exponent field is 27 .. 254, so that of the power 228 .. 1
     const float power = __uint_as_float((255u - (__float_as_uint(most) >> 23)) << 23);
     const float whole = most * power;
     d.factor = both(BQ_LARGEST * power);
     d.minus_d = both(-whole);
-    d.inverse = both(__frcp_rn(whole));
+    float inverse;       // within a unit in the last place: what that leaves of the quotient's error is 2^-22 of a unit
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(whole));
+    d.inverse = both(inverse);
     return d;
 }
 template <typename T> __device__ __forceinline__ float2 divided(float2 v, const Divisor &d)
@@ -49,9 +54,17 @@ template <typename T> __device__ __forceinline__ float2 divided(float2 v, const 
 }
 __device__ __forceinline__ uint16_t rounded(float2 v) { return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3); }
 
+// g / (1 + exp(-g)) * u; exp(-g) = 2^(-g / ln 2).
 __device__ __forceinline__ float2 gate(float2 g, float2 u)
 {
-    return make_float2(g.x / (1.0f + __expf(-g.x)) * u.x, g.y / (1.0f + __expf(-g.y)) * u.y);
+    const float2 power = mul2(g, both(-1.4426950408889634f));
+    float2 e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(power.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(power.y));
+    e = add2(e, both(1.0f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(e.y));
+    return mul2(mul2(g, s), u);
 }
 
 struct BqP {
@@ -73,31 +86,32 @@ template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_some
     for (int i = 0; i < VEC; ++i) r.v[i] = i < left ? p[i] : from_f32<T>(0.0f);
     return r;
 }
-template <int VEC> __device__ __forceinline__ void store_some(uint8_t *q, const uint8_t (&v)[VEC], int left)
+// A pack's values in 8 bits, of which `left` exist.
+template <typename T, int VEC> __device__ __forceinline__ void store_rounded(uint8_t *q, const float2 (&v)[(VEC + 1) / 2], const Divisor &d, int left)
 {
-    if (left >= VEC && VEC > 1) {
-        Pack<uint8_t, VEC> p;
+    uint32_t w[(VEC + 3) / 4] = {};
+    if (!d.none) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) p.v[i] = v[i];
-        store_pack(q, p);
+        for (int i = 0; i < VEC; i += 4) {
+            w[i / 4] = rounded(divided<T>(v[i / 2], d));
+            if (VEC > 2) w[i / 4] |= (uint32_t)rounded(divided<T>(v[(i / 2 + 1) % ((VEC + 1) / 2)], d)) << 16;
+        }
+    }
+    if (VEC == 8 && left >= VEC) {
+        *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[VEC / 8]);
+    } else if (VEC == 4 && left >= VEC) {
+        *reinterpret_cast<uint32_t *>(q) = w[0];
     } else {
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-            if (i < left) q[i] = v[i];
+            if (i < left) q[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
     }
 }
-// A pack's values in 8 bits.
-template <typename T, int VEC> __device__ __forceinline__ void quantise(const float (&v)[VEC], const Divisor &d, uint8_t (&q)[VEC])
+// A pack as floats (an odd one out has a 0 beside it).
+template <typename T, int VEC> __device__ __forceinline__ void floats(const Pack<T, VEC> &a, float2 (&v)[(VEC + 1) / 2])
 {
-    if constexpr (VEC == 1) {
-        q[0] = (uint8_t)(d.none ? 0 : rounded(divided<T>(make_float2(v[0], 0.0f), d)));
-    } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 2) {
-            const uint16_t two = d.none ? (uint16_t)0 : rounded(divided<T>(make_float2(v[i], v[i + 1]), d));
-            q[i] = (uint8_t)two, q[i + 1] = (uint8_t)(two >> 8);
-        }
-    }
+    for (int e = 0; e < VEC; e += 2) v[e / 2] = VEC == 1 ? make_float2(to_f32(a.v[0]), 0.0f) : to_f32x2(&a.v[e]);
 }
 
 constexpr int BQ_THREADS = 256;
@@ -113,47 +127,53 @@ block_quant_kernel(const BqP p)
     after_previous();
     may_follow();
     const T *x = static_cast<const T *>(p.x);
-    // whole warps stay: the shuffles below need all of their lanes
-    for (unsigned long long u0 = group; u0 - threadIdx.x % 32 / LANES < p.units; u0 += (unsigned long long)groups * AHEAD) {
+    // A group's blocks are AHEAD neighbours.  Whole warps stay: the shuffles below need all of their lanes.
+    const unsigned first_of_warp = (group - threadIdx.x % 32 / LANES) * AHEAD;
+    for (unsigned done = 0; first_of_warp + done < p.units; done += groups * AHEAD) {
+        const unsigned u0 = group * AHEAD + done;
         Pack<T, VEC> a[AHEAD][PER], b[AHEAD][PER];
-        unsigned row[AHEAD], block[AHEAD];
+        unsigned row = p.blocks == 1 ? u0 : (unsigned)__umul64hi(p.magic, u0), block = u0 - row * (unsigned)p.blocks;
+        const unsigned row0 = row, block0 = block;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const unsigned long long u = u0 + (unsigned long long)groups * i;
-            row[i] = (unsigned)__umul64hi(p.magic, u), block[i] = (unsigned)u - row[i] * (unsigned)p.blocks;
-            if (p.blocks == 1) row[i] = (unsigned)u, block[i] = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                const int col = (int)block[i] * BQ_BLOCK + (j * LANES + lane) * VEC, left = u < p.units ? p.k - col : 0;
-                const T *at = x + (long long)row[i] * p.x_stride + col;
+                const int col = (int)block * BQ_BLOCK + (j * LANES + lane) * VEC, left = u0 + i < p.units ? p.k - col : 0;
+                const T *at = x + (long long)row * p.x_stride + col;
                 a[i][j] = load_some<T, VEC>(at, left);
                 if (GATED) b[i][j] = load_some<T, VEC>(at + p.k, left);
             }
+            if (++block == (unsigned)p.blocks) block = 0, ++row;
         }
+        row = row0, block = block0;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            float v[PER][VEC], most = 0.0f;
-#pragma unroll
-            for (int j = 0; j < PER; ++j)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[j][e] = to_f32(a[i][j].v[e]);
-                    if (GATED) v[j][e] = gate(make_float2(v[j][e], 0.0f), make_float2(to_f32(b[i][j].v[e]), 0.0f)).x;
-                    most = max_abs(most, v[j][e]);
-                }
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) most = max_abs(most, __shfl_xor_sync(0xffffffffu, most, o));
-            const unsigned long long u = u0 + (unsigned long long)groups * i;
-            if (u >= p.units) continue;
-            const Divisor d = divisor_of(most);
-            if (lane == 0) p.scale[(long long)row[i] * p.blocks + block[i]] = d.scale;
+            float2 v[PER][(VEC + 1) / 2];
+            float most = 0.0f;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                const int col = (int)block[i] * BQ_BLOCK + (j * LANES + lane) * VEC;
-                uint8_t q[VEC];
-                quantise<T, VEC>(v[j], d, q);
-                store_some<VEC>(p.q + (long long)row[i] * p.q_stride + col, q, p.k - col);
+                floats(a[i][j], v[j]);
+                if (GATED) {
+                    float2 up[(VEC + 1) / 2];
+                    floats(b[i][j], up);
+#pragma unroll
+                    for (int e = 0; e < (VEC + 1) / 2; ++e) v[j][e] = gate(v[j][e], up[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < (VEC + 1) / 2; ++e) most = max_abs(most, v[j][e]);
             }
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) most = max_abs(most, __shfl_xor_sync(0xffffffffu, most, o));
+            if (u0 + i < p.units) {
+                const Divisor d = divisor_of(most);
+                if (lane == 0) p.scale[u0 + i] = d.scale;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int col = (int)block * BQ_BLOCK + (j * LANES + lane) * VEC;
+                    store_rounded<T, VEC>(p.q + (long long)row * p.q_stride + col, v[j], d, p.k - col);
+                }
+            }
+            if (++block == (unsigned)p.blocks) block = 0, ++row;
         }
     }
 }
@@ -180,7 +200,11 @@ block_quant_tiles_kernel(const BqP p)
 #pragma unroll
     for (int i = 0; i < PACKS; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) most = max_abs(most, to_f32(a[i].v[e]));
+        for (int e = 0; e < (VEC + 1) / 2; ++e) {
+            float2 v[(VEC + 1) / 2];
+            floats(a[i], v);
+            most = max_abs(most, v[e]);
+        }
     most = warp_max(most);
     if (threadIdx.x % 32 == 0) s_most[threadIdx.x / 32] = most;
     __syncthreads();
@@ -191,12 +215,9 @@ block_quant_tiles_kernel(const BqP p)
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
         const long long row = row0 + i * ROWS;
-        float v[VEC];
-        uint8_t out[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = to_f32(a[i].v[e]);
-        quantise<T, VEC>(v, d, out);
-        if (row < p.rows) store_some<VEC>(q + row * p.q_stride, out, p.k - col);
+        float2 v[(VEC + 1) / 2];
+        floats(a[i], v);
+        if (row < p.rows) store_rounded<T, VEC>(q + row * p.q_stride, v, d, p.k - col);
     }
 }
 
@@ -214,7 +235,7 @@ template <typename T, int VEC, bool GATED> int launch_rows(BqP p, cudaStream_t s
         part.x = static_cast<const T *>(p.x) + done * p.x_stride;
         part.q = p.q + done * p.q_stride;
         part.scale = p.scale + done * p.blocks;
-        const unsigned blocks = std::min<unsigned>((part.units + PER_BLOCK - 1) / PER_BLOCK, 148 * 8);
+        const unsigned blocks = std::min<unsigned>((part.units + PER_BLOCK - 1) / PER_BLOCK, 148 * 8);        // of AHEAD units per group where there are that many
         const int rc = launch_behind(block_quant_kernel<T, VEC, GATED>, blocks, dim3(BQ_THREADS), 0, 1, stream, part);
         if (rc != MOE_OVL_OK) return rc;
     }

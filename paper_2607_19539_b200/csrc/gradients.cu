@@ -13,8 +13,8 @@ using namespace moe_ovl;
 
 namespace {
 
-constexpr int GN_THREADS = 256, GN_PER_THREAD = 32, GN_CHUNK = GN_THREADS * GN_PER_THREAD;
-constexpr int GN_BLOCKS = 148 * 4;           // most blocks of a launch
+constexpr int GN_THREADS = 256, GN_PER_THREAD = 64, GN_CHUNK = GN_THREADS * GN_PER_THREAD;
+constexpr int GN_BLOCKS = 148 * 8;           // most blocks of a launch
 constexpr int LIST_SHORT = 32, LIST_LONG = 960;      // 32 KB of parameters are allowed
 
 struct Tensor {
@@ -41,16 +41,36 @@ template <int N> __device__ __forceinline__ int tensor_at(const TensorList<N> &l
     return lo;
 }
 
-// The values of a chunk that are this thread's: f(index of a pack's first value, values in it (VEC or 1)).  Packs of 16 bytes where the memory allows, single
-// values in front of the first and behind the last.
-template <int VEC, typename F> __device__ __forceinline__ void for_packs(long long begin, long long end, int head, F f)
+// The values of a chunk that are this thread's: packs(indices of up to AT_ONCE packs' first values, how many), whose loads come before anything is done with them, and one(index) for
+// values in front of the first pack of 16 bytes and behind the last.
+constexpr int AT_ONCE = 4;
+template <int VEC, typename Packs, typename One>
+__device__ __forceinline__ void for_values(long long begin, long long end, int head, Packs packs, One one)
 {
-    const long long first = min(begin + head, end), packs = (end - first) / VEC;
-    if (begin + (int)threadIdx.x < first) f(begin + (int)threadIdx.x, false);
-#pragma unroll 4
-    for (long long i = threadIdx.x; i < packs; i += GN_THREADS) f(first + i * VEC, true);
-    const long long last = first + packs * VEC + (int)threadIdx.x;
-    if (last < end) f(last, false);
+    const long long first = min(begin + head, end), count = (end - first) / VEC;
+    if (begin + (int)threadIdx.x < first) one(begin + (int)threadIdx.x);
+    for (long long i = threadIdx.x; i < count; i += AT_ONCE * GN_THREADS) {
+        const int n = (int)min((count - i + GN_THREADS - 1) / GN_THREADS, (long long)AT_ONCE);
+        packs(first + i * VEC, n);
+    }
+    const long long last = first + count * VEC + (int)threadIdx.x;
+    if (last < end) one(last);
+}
+template <typename F> __device__ __forceinline__ void for_each(long long begin, long long end, F f)
+{
+    for (long long i = begin + (int)threadIdx.x; i < end; i += GN_THREADS) f(i);
+}
+template <typename T> struct Four { Pack<T, 16 / sizeof(T)> pack[AT_ONCE]; };
+template <typename T> __device__ __forceinline__ Four<T> load_four(const T *p, int n)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    Four<T> r;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+        if (k < n) r.pack[k] = load_pack<T, VEC>(p + k * GN_THREADS * VEC);
+        else *reinterpret_cast<uint4 *>(&r.pack[k]) = make_uint4(0, 0, 0, 0);
+    }
+    return r;
 }
 template <typename T> __device__ __forceinline__ int head_of(const T *p) { return (int)((16u - ((unsigned)(unsigned long long)p & 15u)) & 15u) / (int)sizeof(T); }
 
@@ -60,27 +80,28 @@ template <typename T> __device__ __forceinline__ double chunk_sum(const T *x, lo
     const int head = head_of(x + begin);
     float2 sum = make_float2(0.0f, 0.0f);
     unsigned bits = 0;                       // of anything but zeros
-    for_packs<VEC>(begin, end, head, [&](long long i, bool whole) {
-        if (whole) {
-            const Pack<T, VEC> a = load_pack<T, VEC>(x + i);
-            const uint4 raw = *reinterpret_cast<const uint4 *>(&a);
+    for_values<VEC>(begin, end, head, [&](long long i, int n) {
+        const Four<T> a = load_four(x + i, n);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const uint4 raw = *reinterpret_cast<const uint4 *>(&a.pack[k]);
             bits |= raw.x | raw.y | raw.z | raw.w;
 #pragma unroll
             for (int e = 0; e < VEC; e += 2) {
-                const float2 v = to_f32x2(&a.v[e]);
+                const float2 v = to_f32x2(&a.pack[k].v[e]);
                 sum = fma2(v, v, sum);
             }
-        } else {
-            const float v = to_f32(x[i]);
-            sum.x = fmaf(v, v, sum.x);
-            bits |= __float_as_uint(v);
         }
+    }, [&](long long i) {
+        const float v = to_f32(x[i]);
+        sum.x = fmaf(v, v, sum.x);
+        bits |= __float_as_uint(v);
     });
     const float both_sums = sum.x + sum.y;
     if (both_sums >= 1e-30f && both_sums <= 1e38f) return (double)both_sums;
     if (bits == 0) return 0.0;
     double wide = 0.0;
-    for_packs<1>(begin, end, 0, [&](long long i, bool) { wide += (double)to_f32(x[i]) * (double)to_f32(x[i]); });
+    for_each(begin, end, [&](long long i) { wide += (double)to_f32(x[i]) * (double)to_f32(x[i]); });
     return wide;
 }
 
@@ -136,17 +157,16 @@ template <typename T> __device__ __forceinline__ void scale_chunk(const T *x, T 
     constexpr int VEC = 16 / sizeof(T);
     auto one = [&](long long i) { y[i] = from_f32<T>(to_f32(x[i]) * factor); };
     const int head = head_of(x + begin);
-    if (head != head_of(y + begin)) {
-        for_packs<1>(begin, end, 0, [&](long long i, bool) { one(i); });
-        return;
-    }
-    for_packs<VEC>(begin, end, head, [&](long long i, bool whole) {
-        if (!whole) return one(i);
-        Pack<T, VEC> a = load_pack<T, VEC>(x + i);
+    if (head != head_of(y + begin)) return for_each(begin, end, one);
+    for_values<VEC>(begin, end, head, [&](long long i, int n) {
+        Four<T> a = load_four(x + i, n);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) a.v[e] = from_f32<T>(to_f32(a.v[e]) * factor);
-        store_pack(y + i, a);
-    });
+        for (int k = 0; k < AT_ONCE; ++k) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) a.pack[k].v[e] = from_f32<T>(to_f32(a.pack[k].v[e]) * factor);
+            if (k < n) store_pack(y + i + k * GN_THREADS * VEC, a.pack[k]);
+        }
+    }, one);
 }
 
 // Chunks from the last to the first: what the norm has read last is still in L2.
