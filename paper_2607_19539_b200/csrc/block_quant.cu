@@ -77,17 +77,23 @@ struct BqP {
     unsigned long long magic;                // floor(2^64 / blocks) + 1: 32-bit quotients by blocks
 };
 
-// A pack of VEC values of which `left` exist.
-template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_some(const T *p, int left)
+// A pack of VEC values of which `left` exist.  EVEN: all of them or none, which takes no branch.
+template <typename T, int VEC, bool EVEN> __device__ __forceinline__ Pack<T, VEC> load_some(const T *p, int left)
 {
-    if (left >= VEC) return load_pack<T, VEC>(p);
-    Pack<T, VEC> r;
+    Pack<T, VEC> r = {};
+    if (EVEN) {
+        if (left > 0) r = load_pack<T, VEC>(p);
+    } else if (left >= VEC) {
+        r = load_pack<T, VEC>(p);
+    } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) r.v[i] = i < left ? p[i] : from_f32<T>(0.0f);
+        for (int i = 0; i < VEC; ++i)
+            if (i < left) r.v[i] = p[i];
+    }
     return r;
 }
 // A pack's values in 8 bits, of which `left` exist.
-template <typename T, int VEC> __device__ __forceinline__ void store_rounded(uint8_t *q, const float2 (&v)[(VEC + 1) / 2], const Divisor &d, int left)
+template <typename T, int VEC, bool EVEN> __device__ __forceinline__ void store_rounded(uint8_t *q, const float2 (&v)[(VEC + 1) / 2], const Divisor &d, int left)
 {
     uint32_t w[(VEC + 3) / 4] = {};
     if (!d.none) {
@@ -97,10 +103,11 @@ template <typename T, int VEC> __device__ __forceinline__ void store_rounded(uin
             if (VEC > 2) w[i / 4] |= (uint32_t)rounded(divided<T>(v[(i / 2 + 1) % ((VEC + 1) / 2)], d)) << 16;
         }
     }
-    if (VEC == 8 && left >= VEC) {
-        *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[VEC / 8]);
-    } else if (VEC == 4 && left >= VEC) {
-        *reinterpret_cast<uint32_t *>(q) = w[0];
+    if (VEC > 1 && (EVEN || left >= VEC)) {
+        if (left > 0) {
+            if (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[VEC / 8]);
+            else *reinterpret_cast<uint32_t *>(q) = w[0];
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
@@ -114,64 +121,65 @@ template <typename T, int VEC> __device__ __forceinline__ void floats(const Pack
     for (int e = 0; e < VEC; e += 2) v[e / 2] = VEC == 1 ? make_float2(to_f32(a.v[0]), 0.0f) : to_f32x2(&a.v[e]);
 }
 
-constexpr int BQ_THREADS = 256;
+constexpr int BQ_THREADS = 256, BQ_RESIDENT = 8;     // blocks per SM
 
-// Blocks of 1 x 128.  LANES lanes work on a block, PER packs of VEC values each; a thread has AHEAD blocks' loads under way.
-template <typename T, int VEC, bool GATED>
+// Blocks of 1 x 128.  LANES lanes work on a block, PER packs of VEC values each; a group of lanes has the loads of AHEAD neighbouring blocks under way.
+template <typename T, int VEC, bool GATED> struct BqShape {
+    static constexpr int LANES = VEC == 1 ? 32 : BQ_BLOCK / VEC / 2, PER = BQ_BLOCK / VEC / LANES, AHEAD = VEC == 1 ? 1 : 2;
+};
+template <typename T, int VEC, bool GATED, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
 block_quant_kernel(const BqP p)
 {
-    constexpr int LANES = BQ_BLOCK / VEC < 32 ? BQ_BLOCK / VEC : 32, PER = BQ_BLOCK / VEC / LANES, AHEAD = VEC > 1 ? (GATED ? 2 : 4) : 1;
+    using Shape = BqShape<T, VEC, GATED>;
+    constexpr int LANES = Shape::LANES, PER = Shape::PER, AHEAD = Shape::AHEAD, HALF = (VEC + 1) / 2;
     const int lane = threadIdx.x % LANES;
-    const unsigned group = blockIdx.x * (BQ_THREADS / LANES) + threadIdx.x / LANES, groups = gridDim.x * (BQ_THREADS / LANES);
+    const unsigned group = blockIdx.x * (BQ_THREADS / LANES) + threadIdx.x / LANES, step = gridDim.x * (BQ_THREADS / LANES) * AHEAD;
     after_previous();
     may_follow();
-    const T *x = static_cast<const T *>(p.x);
-    // A group's blocks are AHEAD neighbours.  Whole warps stay: the shuffles below need all of their lanes.
-    const unsigned first_of_warp = (group - threadIdx.x % 32 / LANES) * AHEAD;
-    for (unsigned done = 0; first_of_warp + done < p.units; done += groups * AHEAD) {
-        const unsigned u0 = group * AHEAD + done;
-        Pack<T, VEC> a[AHEAD][PER], b[AHEAD][PER];
-        unsigned row = p.blocks == 1 ? u0 : (unsigned)__umul64hi(p.magic, u0), block = u0 - row * (unsigned)p.blocks;
-        const unsigned row0 = row, block0 = block;
+    // whole warps stay: the shuffles need all of their lanes
+    const unsigned own = group * AHEAD, first = own - threadIdx.x % 32 / LANES * AHEAD;
+    for (unsigned done = 0; first + done < p.units; done += step) {
+        const unsigned u = own + done, row0 = p.blocks == 1 ? u : (unsigned)__umul64hi(p.magic, u), block0 = u - row0 * (unsigned)p.blocks;
+        Pack<T, VEC> a[AHEAD][PER], b[GATED ? AHEAD : 1][PER];
+        unsigned row = row0, block = block0;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
+            const int col = (int)block * BQ_BLOCK + lane * VEC, left = u + i < p.units ? p.k - col : 0;
+            const T *at = static_cast<const T *>(p.x) + (long long)row * p.x_stride + col;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                const int col = (int)block * BQ_BLOCK + (j * LANES + lane) * VEC, left = u0 + i < p.units ? p.k - col : 0;
-                const T *at = x + (long long)row * p.x_stride + col;
-                a[i][j] = load_some<T, VEC>(at, left);
-                if (GATED) b[i][j] = load_some<T, VEC>(at + p.k, left);
+                a[i][j] = load_some<T, VEC, EVEN>(at + j * LANES * VEC, left - j * LANES * VEC);
+                if (GATED) b[i][j] = load_some<T, VEC, EVEN>(at + j * LANES * VEC + p.k, left - j * LANES * VEC);
             }
             if (++block == (unsigned)p.blocks) block = 0, ++row;
         }
         row = row0, block = block0;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            float2 v[PER][(VEC + 1) / 2];
+            float2 v[PER][HALF];
             float most = 0.0f;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
                 floats(a[i][j], v[j]);
                 if (GATED) {
-                    float2 up[(VEC + 1) / 2];
+                    float2 up[HALF];
                     floats(b[i][j], up);
 #pragma unroll
-                    for (int e = 0; e < (VEC + 1) / 2; ++e) v[j][e] = gate(v[j][e], up[e]);
+                    for (int e = 0; e < HALF; ++e) v[j][e] = gate(v[j][e], up[e]);
                 }
 #pragma unroll
-                for (int e = 0; e < (VEC + 1) / 2; ++e) most = max_abs(most, v[j][e]);
+                for (int e = 0; e < HALF; ++e) most = max_abs(most, v[j][e]);
             }
 #pragma unroll
             for (int o = LANES / 2; o > 0; o >>= 1) most = max_abs(most, __shfl_xor_sync(0xffffffffu, most, o));
-            if (u0 + i < p.units) {
+            if (u + i < p.units) {
                 const Divisor d = divisor_of(most);
-                if (lane == 0) p.scale[u0 + i] = d.scale;
+                if (lane == 0) p.scale[u + i] = d.scale;
+                const int col = (int)block * BQ_BLOCK + lane * VEC;
+                uint8_t *q = p.q + (long long)row * p.q_stride + col;
 #pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const int col = (int)block * BQ_BLOCK + (j * LANES + lane) * VEC;
-                    store_rounded<T, VEC>(p.q + (long long)row * p.q_stride + col, v[j], d, p.k - col);
-                }
+                for (int j = 0; j < PER; ++j) store_rounded<T, VEC, EVEN>(q + j * LANES * VEC, v[j], d, p.k - col - j * LANES * VEC);
             }
             if (++block == (unsigned)p.blocks) block = 0, ++row;
         }
@@ -179,7 +187,7 @@ block_quant_kernel(const BqP p)
 }
 
 // Blocks of 128 x 128, one thread block each: the values stay in registers between the maximum and the division.
-template <typename T, int VEC>
+template <typename T, int VEC, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
 block_quant_tiles_kernel(const BqP p)
 {
@@ -195,7 +203,7 @@ block_quant_tiles_kernel(const BqP p)
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
         const long long row = row0 + i * ROWS;
-        a[i] = load_some<T, VEC>(x + row * p.x_stride, row < p.rows ? p.k - col : 0);
+        a[i] = load_some<T, VEC, EVEN>(x + row * p.x_stride, row < p.rows ? p.k - col : 0);
     }
 #pragma unroll
     for (int i = 0; i < PACKS; ++i)
@@ -217,13 +225,13 @@ block_quant_tiles_kernel(const BqP p)
         const long long row = row0 + i * ROWS;
         float2 v[(VEC + 1) / 2];
         floats(a[i], v);
-        if (row < p.rows) store_rounded<T, VEC>(q + row * p.q_stride, v, d, p.k - col);
+        if (row < p.rows) store_rounded<T, VEC, EVEN>(q + row * p.q_stride, v, d, p.k - col);
     }
 }
 
-template <typename T, int VEC, bool GATED> int launch_rows(BqP p, cudaStream_t stream)
+template <typename T, int VEC, bool GATED, bool EVEN> int launch_rows(BqP p, cudaStream_t stream)
 {
-    constexpr int PER_BLOCK = BQ_THREADS / (BQ_BLOCK / VEC < 32 ? BQ_BLOCK / VEC : 32);
+    constexpr int PER_BLOCK = BQ_THREADS / BqShape<T, VEC, GATED>::LANES * BqShape<T, VEC, GATED>::AHEAD;
     // units are counted in 32 bits: very many rows go in several launches
     const int at_once = (int)std::min<long long>(p.rows, (1ll << 30) / p.blocks);
     const int rows = p.rows;
@@ -235,14 +243,14 @@ template <typename T, int VEC, bool GATED> int launch_rows(BqP p, cudaStream_t s
         part.x = static_cast<const T *>(p.x) + done * p.x_stride;
         part.q = p.q + done * p.q_stride;
         part.scale = p.scale + done * p.blocks;
-        const unsigned blocks = std::min<unsigned>((part.units + PER_BLOCK - 1) / PER_BLOCK, 148 * 8);        // of AHEAD units per group where there are that many
-        const int rc = launch_behind(block_quant_kernel<T, VEC, GATED>, blocks, dim3(BQ_THREADS), 0, 1, stream, part);
+        const unsigned blocks = std::min<unsigned>((part.units + PER_BLOCK - 1) / PER_BLOCK, 148 * BQ_RESIDENT);
+        const int rc = launch_behind(block_quant_kernel<T, VEC, GATED, EVEN>, blocks, dim3(BQ_THREADS), 0, 1, stream, part);
         if (rc != MOE_OVL_OK) return rc;
     }
     return MOE_OVL_OK;
 }
 
-template <typename T, int VEC> int launch_tiles(const BqP &p, int depth, cudaStream_t stream)
+template <typename T, int VEC, bool EVEN> int launch_tiles(const BqP &p, int depth, cudaStream_t stream)
 {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -253,7 +261,7 @@ template <typename T, int VEC> int launch_tiles(const BqP &p, int depth, cudaStr
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, block_quant_tiles_kernel<T, VEC>, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, block_quant_tiles_kernel<T, VEC, EVEN>, p) == cudaSuccess ? MOE_OVL_OK : MOE_OVL_ERR_CUDA;
 }
 
 }  // namespace
@@ -284,8 +292,9 @@ extern "C" int moe_ovl_block_quant(const moe_ovl_block_quant_args *a)
         // packs of 16 bytes in, VEC bytes out, wherever a row, a matrix or the gate's other half begins
         const bool rows_fit = a->rows == 1 || (a->x_stride % VEC == 0 && a->q_stride % VEC == 0);
         const bool packs = aligned(a->x, 16) && aligned(a->q, VEC) && rows_fit && p.x_far % VEC == 0 && p.q_far % VEC == 0 && (!a->gated || a->k % VEC == 0);
-        if (a->tiles) return packs ? launch_tiles<T, VEC>(p, a->depth, stream) : launch_tiles<T, 1>(p, a->depth, stream);
-        if (a->gated) return packs ? launch_rows<T, VEC, true>(p, stream) : launch_rows<T, 1, true>(p, stream);
-        return packs ? launch_rows<T, VEC, false>(p, stream) : launch_rows<T, 1, false>(p, stream);
+        const bool even = a->k % VEC == 0;
+        if (a->tiles) return !packs ? launch_tiles<T, 1, true>(p, a->depth, stream) : even ? launch_tiles<T, VEC, true>(p, a->depth, stream) : launch_tiles<T, VEC, false>(p, a->depth, stream);
+        if (a->gated) return packs ? launch_rows<T, VEC, true, true>(p, stream) : launch_rows<T, 1, true, true>(p, stream);
+        return !packs ? launch_rows<T, 1, false, true>(p, stream) : even ? launch_rows<T, VEC, false, true>(p, stream) : launch_rows<T, VEC, false, false>(p, stream);
     });
 }
