@@ -87,7 +87,7 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
         const int quarter = (warp + Shape::CONTROL) & 3, half = PARTS == 1 ? warp >> 2 : 0;  // a warp reads the lanes of its position among four, and its part's columns or half of them
         const int in_tile = rank * TILE_CHANNELS + quarter * 32 + lane;
         const bool mine = in_tile < t.rows;
-        const int block = t.channel0 / 128 + accs.part, ch0 = block * 128 + half * COLS;
+        const int block = t.channel0 / 128 + accs.group, ch0 = block * 128 + half * COLS;
         const float *sa = p.a_scale + (long long)(t.row0 + (mine ? in_tile : 0)) * p.blocks;
         const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + min(block, p.channel_blocks - 1)) * p.blocks;
         float2 acc[COLS / 2];
@@ -157,63 +157,83 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
 
 // ------------------------------------------------------------------ few rows
 
-template <int TOKENS_, typename Out> struct BlockFew {
-    static constexpr int SPLITS = 1, TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
-    using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, 200 * 1024, 256 / COLS, COLS, 4, 1>;
+template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
+    static constexpr int SPLITS = SPLITS_, TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
+    // Two groups of four warps take the steps in turn: what a warp does for one (a wait, its factors, 16 to 64 columns) takes longer than the weights of a step take to come.
+    static constexpr int RING_BYTES = (SPLITS == 1 ? 176 : 64) * 1024, PER_SM = SPLITS == 1 ? 1 : 2;
+    using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, RING_BYTES, 256 / COLS, COLS, 8, 1, 1, 2>;
     using Schedule = TileSchedule<TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
     const BmP &p;
     const CUtensorMap *map_a, *map_b;
     int *tile_start, *row_start;
-    float *factors;                          // [4 warps][2][TOKENS]
+    float *factors;                          // [8 warps][2][TOKENS]
+    float *part;                             // [TOKENS][TILE_CHANNELS]: the second group's sums, and with SPLITS > 1 this CTA's
     Schedule sched;
-    int rank = 0;
+    int rank = 0, split = 0, turn = 0;       // turn: the group whose step is next
+    bool lost = false;                       // a wait gave up
 
-    struct From { int a0, b0, expert; };
+    struct From { int a0, b0, expert, k0; };
     __device__ __forceinline__ void begin(int lane) { fill_schedule<TOKENS>(p, tile_start, row_start, count_of(p, lane), lane); }
     __device__ __forceinline__ long long total() const { return sched.total(p.counts ? p.experts : 1); }
     __device__ __forceinline__ Tile at(long long t) { return sched.at(t); }
-    __device__ __forceinline__ int steps(const Tile &) const { return p.blocks; }
-    __device__ __forceinline__ From operands(const Tile &t, bool) const { return {uniform(t.row0), uniform(t.channel0), uniform(t.expert)}; }
+    __device__ __forceinline__ int step_of(int i) const { return p.blocks * i / SPLITS; }
+    __device__ __forceinline__ int steps(const Tile &) const { return SPLITS == 1 ? p.blocks : step_of(split + 1) - step_of(split); }
+    __device__ __forceinline__ From operands(const Tile &t, bool) const { return {uniform(t.row0), uniform(t.channel0), uniform(t.expert), SPLITS == 1 ? 0 : uniform(step_of(split))}; }
     __device__ __forceinline__ void load(uint32_t on, const From &f, uint32_t sa, uint32_t bar, int step) const
     {
-        load_3d<1>(on, sa, map_b, bar, step * STAGE_ROW, f.b0, f.expert);
-        load_2d<1>(on, sa + BM_M_BYTES, map_a, bar, step * STAGE_ROW, f.a0);
+        load_3d<1>(on, sa, map_b, bar, (f.k0 + step) * STAGE_ROW, f.b0, f.expert);
+        load_2d<1>(on, sa + BM_M_BYTES, map_a, bar, (f.k0 + step) * STAGE_ROW, f.a0);
     }
     __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TILE_CHANNELS, TOKENS); }
     __device__ __forceinline__ void multiply(uint32_t on, uint32_t d, uint32_t stage16, uint32_t idesc, bool, int) const { multiply_step<1>(on, d, stage16, BM_M_BYTES / 16, idesc); }
-    __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane) const
+
+    // The groups meet at barriers that have no time limit: a warp whose wait gave up goes on without waiting for sums.
+    static constexpr int THERE = 1, TAKEN = 2;       // named barriers
+    __device__ __forceinline__ static void meet(int barrier, bool waits)
+    {
+        if (waits) asm volatile("bar.sync %0, 256;" ::"r"(barrier) : "memory");
+        else asm volatile("bar.arrive %0, 256;" ::"r"(barrier) : "memory");
+    }
+    __device__ __forceinline__ bool finish(const Tile &t, Accumulators<Shape> &accs, const BmP &, int warp, int lane)
     {
         constexpr int PER_LANE = (TOKENS + 31) / 32;
         const int quarter = (warp + Shape::CONTROL) & 3, ch = t.channel0 + quarter * 32 + lane;
+        const int from = SPLITS == 1 ? 0 : step_of(split), all = steps(t);
         float *own = factors + warp * 2 * TOKENS;
-        const float *sa = p.a_scale + (long long)t.row0 * p.blocks;
-        const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + t.channel0 / 128) * p.blocks;
+        const float *sa = p.a_scale + (long long)t.row0 * p.blocks + from;
+        const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + t.channel0 / 128) * p.blocks + from;
         float2 acc[TOKENS / 2];
 #pragma unroll
         for (int i = 0; i < TOKENS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
-        float a_next[PER_LANE] = {}, b_next = sb[0];
+        float a_next[PER_LANE] = {}, b_next = 0.0f;
         auto ask = [&](int k) {
+            if (k >= all) return;
 #pragma unroll
             for (int i = 0; i < PER_LANE; ++i)
                 if (i * 32 + lane < t.rows) a_next[i] = sa[(long long)(i * 32 + lane) * p.blocks + k];
             b_next = sb[k];
         };
-        ask(0);
-        for (int k = 0; k < p.blocks; ++k) {
-            float *s = own + (k & 1) * TOKENS;           // two, so that a lane still reading the step before is not overtaken
+        const int k0 = (accs.group + turn) & 1;          // its first step of this tile
+        turn = (turn + all) & 1;
+        ask(k0);
+        for (int k = k0; k < all; k += 2) {
+            float *s = own + (k & 2) / 2 * TOKENS;       // two, so that a lane still reading the step before is not overtaken
 #pragma unroll
             for (int i = 0; i < PER_LANE; ++i)
                 if (i * 32 + lane < TOKENS) s[i * 32 + lane] = a_next[i] * b_next;
-            if (k + 1 < p.blocks) ask(k + 1);
+            ask(k + 2);
             __syncwarp();
-            if (!accs.wait(p, t.row0)) return false;
-            const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16);
+            if (lost || !accs.wait(p, t.row0)) {
+                lost = true;
+                continue;
+            }
+            const uint32_t columns = accs.columns() + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll
             for (int c = 0; c < TOKENS; c += 16) {
                 if (c < t.rows) {
                     uint32_t v[16];
-                    tmem_ld16(from + c, v);
+                    tmem_ld16(columns + c, v);
                     tmem_ld_wait(v);
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
@@ -225,16 +245,40 @@ template <int TOKENS_, typename Out> struct BlockFew {
             }
             accs.release();
         }
-        if ((unsigned)ch < (unsigned)p.n) {
-            Out *out = static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride + ch;
+        float *mine = part + quarter * 32 + lane;
+        if (accs.group == 1) {
 #pragma unroll
-            for (int j = 0; j < TOKENS; ++j) {
-                if (j < t.rows) *out = from_f32<Out>(j & 1 ? acc[j / 2].y : acc[j / 2].x);
-                out += p.out_stride;
+            for (int j = 0; j < TOKENS; ++j)
+                if (j < t.rows) mine[j * TILE_CHANNELS] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+            meet(THERE, false);
+            if (SPLITS == 1) meet(TAKEN, true);
+            return true;
+        }
+        meet(THERE, true);
+#pragma unroll
+        for (int j = 0; j < TOKENS; ++j) {
+            if (j < t.rows) {
+                float &sum = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+                sum += mine[j * TILE_CHANNELS];
+                if (SPLITS > 1) mine[j * TILE_CHANNELS] = sum;
             }
         }
-        __syncwarp();
+        if constexpr (SPLITS == 1) {
+            meet(TAKEN, false);
+            if ((unsigned)ch < (unsigned)p.n) {
+                Out *out = static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride + ch;
+#pragma unroll
+                for (int j = 0; j < TOKENS; ++j) {
+                    if (j < t.rows) *out = from_f32<Out>(j & 1 ? acc[j / 2].y : acc[j / 2].x);
+                    out += p.out_stride;
+                }
+            }
+        }
         return true;
+    }
+    __device__ __forceinline__ void join(const Tile &t) const
+    {
+        join_parts<SPLITS>(part, static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride, p.out_stride, t.channel0, p.n, t.rows, split, false);
     }
 };
 
@@ -249,14 +293,15 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_out, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
-template <int TOKENS, typename Out>
-__global__ void __launch_bounds__(BlockFew<TOKENS, Out>::Shape::THREADS, 1)
+template <int TOKENS, int SPLITS, typename Out>
+__global__ void __launch_bounds__(BlockFew<TOKENS, SPLITS, Out>::Shape::THREADS, BlockFew<TOKENS, SPLITS, Out>::PER_SM)
 block_matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
 {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
-    __shared__ __align__(16) float s_factors[4 * 2 * TOKENS];
-    run_tiles(BlockFew<TOKENS, Out>{p, &map_a, &map_b, s_tile_start, s_row_start, s_factors, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+    using Work = BlockFew<TOKENS, SPLITS, Out>;
+    __shared__ __align__(16) float s_factors[Work::Shape::FINISHERS * 2 * TOKENS];
+    run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_factors, reinterpret_cast<float *>(smem_raw + Work::Shape::SMEM), {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
 struct BmOperands { const void *a, *b; long long a_stride, b_stride, b_far; };
@@ -280,30 +325,46 @@ int launch_rows(BmP p, const BmOperands &o, int device, cudaStream_t stream)
     return launch_behind(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), dim3(Shape::THREADS), Shape::SMEM, CTAS, stream, a, b, p);
 }
 
-template <int TOKENS, typename Out>
-int launch_few(BmP p, const BmOperands &o, int device, cudaStream_t stream)
+template <int TOKENS, int SPLITS, typename Out>
+int launch_few(BmP p, const BmOperands &o, long long tiles, int device, cudaStream_t stream)
 {
-    using Shape = typename BlockFew<TOKENS, Out>::Shape;
+    using Work = BlockFew<TOKENS, SPLITS, Out>;
+    constexpr int SMEM = Work::Shape::SMEM + TOKENS * TILE_CHANNELS * 4;
     CUtensorMap a, b;
     p.row_tiles = (p.n - 1) / TILE_CHANNELS + 1;
     if (!encode_operands(p, o, TOKENS, TILE_CHANNELS, &a, &b)) return MOE_OVL_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
-    const auto kernel = block_matmul_few_kernel<TOKENS, Out>;
-    if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
-    return launch_behind(kernel, (unsigned)sm_count(device), dim3(Shape::THREADS), Shape::SMEM, 1, stream, a, b, p);
+    const auto kernel = block_matmul_few_kernel<TOKENS, SPLITS, Out>;
+    if (!allow_smem(kernel, SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    const unsigned blocks = SPLITS > 1 ? (unsigned)(tiles * SPLITS) : (unsigned)sm_count(device);
+    return launch_behind(kernel, blocks, dim3(Work::Shape::THREADS), SMEM, SPLITS, stream, a, b, p);
+}
+template <int TOKENS, typename Out>
+int launch_few(int splits, const BmP &p, const BmOperands &o, long long tiles, int device, cudaStream_t stream)
+{
+    switch (splits) {
+    case 1: return launch_few<TOKENS, 1, Out>(p, o, tiles, device, stream);
+    case 2: return launch_few<TOKENS, 2, Out>(p, o, tiles, device, stream);
+    case 4: return launch_few<TOKENS, 4, Out>(p, o, tiles, device, stream);
+    default: return launch_few<TOKENS, 8, Out>(p, o, tiles, device, stream);
+    }
 }
 
-// ctas 0: few rows, `tile` of them; else `tile` channels.
-struct BmChoice { int ctas, tile; };
+// ctas 0: few rows, `tile` of them, by `splits` CTAs each; else `tile` channels.  tiles: the most that any counts can give.
+struct BmChoice { int ctas, tile, splits; long long tiles; };
 
 BmChoice choose(const BmP &p)
 {
     const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows - 1) / groups + 1;
-    if (per_group <= 16) return {0, p.experts && per_group > 4 ? 32 : 16};
-    if (per_group <= 32) return {0, p.experts ? 64 : 32};
-    if (per_group <= 64) return {0, 64};
+    if (per_group <= 64) {
+        const int few = per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64;
+        const long long most = (long long)p.channel_blocks * (p.counts ? p.rows / few + groups : (p.rows - 1) / few + 1);
+        const int splits = splits_of(most, 2, p.blocks, std::min(few, per_group));
+        if (splits > 1) return {0, few, splits, most};
+        return {0, p.experts && per_group > 4 ? std::min(64, 2 * few) : few, 1, 0};
+    }
     const long long pairs = (long long)((p.n - 1) / 256 + 1) * groups * ((per_group - 1) / 256 + 1);
-    return pairs >= 37 ? BmChoice{2, 256} : BmChoice{1, 128};
+    return pairs >= 37 ? BmChoice{2, 256, 1, 0} : BmChoice{1, 128, 1, 0};
 }
 
 }  // namespace
@@ -343,9 +404,9 @@ extern "C" int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *a)
         if (c.ctas == 2) return launch_rows<2, 256, Out>(p, o, a->device, stream);
         if (c.ctas == 1) return launch_rows<1, 128, Out>(p, o, a->device, stream);
         switch (c.tile) {
-        case 16: return launch_few<16, Out>(p, o, a->device, stream);
-        case 32: return launch_few<32, Out>(p, o, a->device, stream);
-        default: return launch_few<64, Out>(p, o, a->device, stream);
+        case 16: return launch_few<16, Out>(c.splits, p, o, c.tiles, a->device, stream);
+        case 32: return launch_few<32, Out>(c.splits, p, o, c.tiles, a->device, stream);
+        default: return launch_few<64, Out>(c.splits, p, o, c.tiles, a->device, stream);
         }
     });
 }

@@ -41,10 +41,9 @@ template <int N> __device__ __forceinline__ int tensor_at(const TensorList<N> &l
     return lo;
 }
 
-// The values of a chunk that are this thread's: packs(indices of up to AT_ONCE packs' first values, how many), whose loads come before anything is done with them, and one(index) for
+// The values of a chunk that are this thread's: packs(index of the first value of up to AT_ONCE packs, GN_THREADS packs apart, how many), whose loads come before anything is done with them, and one(index) for
 // values in front of the first pack of 16 bytes and behind the last.
-constexpr int AT_ONCE = 4;
-template <int VEC, typename Packs, typename One>
+template <int VEC, int AT_ONCE, typename Packs, typename One>
 __device__ __forceinline__ void for_values(long long begin, long long end, int head, Packs packs, One one)
 {
     const long long first = min(begin + head, end), count = (end - first) / VEC;
@@ -60,11 +59,11 @@ template <typename F> __device__ __forceinline__ void for_each(long long begin, 
 {
     for (long long i = begin + (int)threadIdx.x; i < end; i += GN_THREADS) f(i);
 }
-template <typename T> struct Four { Pack<T, 16 / sizeof(T)> pack[AT_ONCE]; };
-template <typename T> __device__ __forceinline__ Four<T> load_four(const T *p, int n)
+template <typename T, int AT_ONCE> struct Packs { Pack<T, 16 / sizeof(T)> pack[AT_ONCE]; };
+template <int AT_ONCE, typename T> __device__ __forceinline__ Packs<T, AT_ONCE> load_packs(const T *p, int n)
 {
     constexpr int VEC = 16 / sizeof(T);
-    Four<T> r;
+    Packs<T, AT_ONCE> r;
 #pragma unroll
     for (int k = 0; k < AT_ONCE; ++k) {
         if (k < n) r.pack[k] = load_pack<T, VEC>(p + k * GN_THREADS * VEC);
@@ -80,8 +79,9 @@ template <typename T> __device__ __forceinline__ double chunk_sum(const T *x, lo
     const int head = head_of(x + begin);
     float2 sum = make_float2(0.0f, 0.0f);
     unsigned bits = 0;                       // of anything but zeros
-    for_values<VEC>(begin, end, head, [&](long long i, int n) {
-        const Four<T> a = load_four(x + i, n);
+    constexpr int AT_ONCE = 4;               // 8: 146 us instead of 121 for 0.84 GB
+    for_values<VEC, AT_ONCE>(begin, end, head, [&](long long i, int n) {
+        const Packs<T, AT_ONCE> a = load_packs<AT_ONCE>(x + i, n);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const uint4 raw = *reinterpret_cast<const uint4 *>(&a.pack[k]);
@@ -158,8 +158,9 @@ template <typename T> __device__ __forceinline__ void scale_chunk(const T *x, T 
     auto one = [&](long long i) { y[i] = from_f32<T>(to_f32(x[i]) * factor); };
     const int head = head_of(x + begin);
     if (head != head_of(y + begin)) return for_each(begin, end, one);
-    for_values<VEC>(begin, end, head, [&](long long i, int n) {
-        Four<T> a = load_four(x + i, n);
+    constexpr int AT_ONCE = 8;               // 4: 289 us instead of 273 for 0.84 GB
+    for_values<VEC, AT_ONCE>(begin, end, head, [&](long long i, int n) {
+        Packs<T, AT_ONCE> a = load_packs<AT_ONCE>(x + i, n);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
 #pragma unroll

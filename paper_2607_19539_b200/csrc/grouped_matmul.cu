@@ -168,23 +168,10 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
         for (int i = 0; i < GM_K / 16; ++i)
             umma_f16<CTAS>(on, d, dm + (uint64_t)(i * STEP_M), dn + (uint64_t)(i * STEP_N), idesc, first && i == 0 ? 0u : 1u);
     }
-    // The tile's output: a warp adds up a row, four columns per lane, SPLITS loads in flight.  The CTAs and their warps take the rows in turn.
     __device__ __forceinline__ void join(const Tile &t) const
     {
-        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, ch = t.channel0 + 4 * lane;
-        Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)t.row0 * p.out_stride + ch;
-        for (int j = split + SPLITS * warp; j < t.rows; j += SPLITS * (Shape::THREADS / 32)) {
-            float4 v[SPLITS];
-#pragma unroll
-            for (int s = 0; s < SPLITS; ++s) v[s] = ld_shared_cluster_f32x4(map_to_cta(smem_u32(part + j * TILE_CHANNELS + 4 * lane), (uint32_t)s));
-            float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
-#pragma unroll
-            for (int s = 1; s < SPLITS; ++s) sum[0] += v[s].x, sum[1] += v[s].y, sum[2] += v[s].z, sum[3] += v[s].w;
-            Out *at = out + (long long)j * p.out_stride;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if ((unsigned)(ch + i) < (unsigned)p.n) at[i] = from_f32<Out>(FORM == FORM_COLUMNS && p.accumulate ? sum[i] + to_f32(at[i]) : sum[i]);
-        }
+        Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)t.row0 * p.out_stride;
+        join_parts<SPLITS>(part, out, p.out_stride, t.channel0, p.n, t.rows, split, FORM == FORM_COLUMNS && p.accumulate);
     }
     // 32 rows of the output from row c of the tile on, one column per lane.
     __device__ __forceinline__ void store(const Tile &t, const float *sum, int c, int ch, bool in) const
@@ -335,17 +322,6 @@ int launch_split(int splits, const GmP &p, const GmMaps &maps, long long tiles, 
     case 4: return launch<1, TOKENS, FORM, 4, Out>(p, maps, tiles, device, stream);
     default: return launch<1, TOKENS, FORM, 8, Out>(p, maps, tiles, device, stream);
     }
-}
-
-// How many CTAs share a tile's steps of K: as many as there are clusters of on the device at once (a second wave costs more than sharing gains), four steps for each at least.  A step
-// takes a CTA about 0.15 us; sharing costs about 1.2 us, and 0.03 us per row of the tile, whose parts have to be added up.  Measured, us: 1 row, n = 512, k = 4096 12.1 unshared, 5.2 with
-// eight; 64 rows 11.9 and 6.4; n = k = 4096, 1 row 12.4 and 6.6 with four; 64 rows, n = 512, k = 1024 4.9 and 5.6.
-int splits_of(long long tiles, int per_sm, long long steps, int rows)
-{
-    const int clusters[3] = {74 * per_sm, per_sm == 2 ? 71 : 33, per_sm == 2 ? 33 : 15};     // of 2, 4, 8 CTAs
-    int s = 1;
-    for (int i = 0; i < 3 && tiles <= clusters[i] && steps >= 8 * s; ++i) s *= 2;
-    return steps * (s - 1) * 15 > s * (120 + 3 * rows) ? s : 1;
 }
 
 // splits > 1: a cluster of that many CTAs per tile; tiles: the most that any counts can give.

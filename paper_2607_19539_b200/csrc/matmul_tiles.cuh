@@ -233,13 +233,13 @@ __device__ __forceinline__ float4 ld_shared_cluster_f32x4(uint32_t addr)
 
 // CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
 // ACC_COLS columns of tensor memory go round.  SEGMENT 0: a tile has one accumulator, for all of its steps.  Otherwise every SEGMENT steps have PARTS of them, side by side
-// in the tile, which a share of the finishing warps each adds up.
-template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, int SEGMENT_, int PARTS_ = 1> struct TileShape {
-    static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_, SEGMENT = SEGMENT_, PARTS = PARTS_;
+// in the tile, which a share of the finishing warps each adds up.  TURNS > 1: that many groups of them take the accumulators in turn.
+template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, int SEGMENT_, int PARTS_ = 1, int TURNS_ = 1> struct TileShape {
+    static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_, SEGMENT = SEGMENT_, PARTS = PARTS_, GROUPS = PARTS_ * TURNS_;
     static constexpr int STAGES = SMEM_BYTES_ / STAGE_BYTES_;
     static constexpr int CONTROL = 2, THREADS = 32 * (CONTROL + FINISHERS);      // the load and the matrix warp
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
-    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32 && ACCS % PARTS == 0 && FINISHERS % PARTS == 0, "tensor memory");
+    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32 && ACCS % GROUPS == 0 && FINISHERS % GROUPS == 0, "tensor memory");
 };
 
 // Arrival of a reader of tensor memory, on a barrier that may be the peer CTA's.  What it gives back has been read (tcgen05.wait, and the fence
@@ -249,10 +249,10 @@ __device__ __forceinline__ void arrive_read(uint32_t cluster_bar)
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-// A finishing warp's way through the accumulators (of its part).
+// A finishing warp's way through the accumulators of its group.
 template <typename Shape> struct Accumulators {
     uint32_t bar_full, lead_empty, tmem;
-    int lane, part = 0, acc = 0;
+    int lane, group = 0, acc = 0;
     uint32_t phase = 0;
     template <typename P> __device__ __forceinline__ bool wait(const P &p, long long index)
     {
@@ -266,7 +266,7 @@ template <typename Shape> struct Accumulators {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) arrive_read(lead_empty + 8 * acc);
-        if ((acc += Shape::PARTS) >= Shape::ACCS) acc = part, phase ^= 1u;
+        if ((acc += Shape::GROUPS) >= Shape::ACCS) acc = group, phase ^= 1u;
     }
 };
 
@@ -323,7 +323,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     if (warp == 0) {
         for (int i = lane; i < 2 * STAGES + 2 * ACCS + 1; i += 32)
             // full: the first CTA's load thread arrives, expecting all CTAs' bytes; accumulators empty: one arrival per finishing warp
-            mbar_init(bar_full + 8 * i, i >= 2 * STAGES + ACCS && i < 2 * STAGES + 2 * ACCS ? Shape::FINISHERS / Shape::PARTS * CTAS : 1);
+            mbar_init(bar_full + 8 * i, i >= 2 * STAGES + ACCS && i < 2 * STAGES + 2 * ACCS ? Shape::FINISHERS / Shape::GROUPS * CTAS : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (lane == 0) s_gave_up = 0;
         __syncwarp();
@@ -342,8 +342,8 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     const uint32_t tmem = uniform(s_tmem);
     const long long total = work.total();
     if (warp >= Shape::CONTROL) {
-        const int part = (warp - Shape::CONTROL) / (Shape::FINISHERS / Shape::PARTS);
-        Accumulators<Shape> accs{bar_tfull, lead_tempty, tmem, lane, part, part};
+        const int group = (warp - Shape::CONTROL) / (Shape::FINISHERS / Shape::GROUPS);
+        Accumulators<Shape> accs{bar_tfull, lead_tempty, tmem, lane, group, group};
         for (long long t = first; t < total; t += step)
             if (!work.finish(work.at(t), accs, p, warp - Shape::CONTROL, lane)) break;         // a warp leaves the loop as one
         __syncwarp();
@@ -437,6 +437,26 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
     }
 }
 
+// The output of a tile whose steps a cluster has shared: a warp adds up the parts of a row, four columns per lane, SPLITS loads in flight.  The CTAs and their warps take the
+// rows in turn.  part: [rows][TILE_CHANNELS] in shared memory, at the same place in every CTA; out: the tile's first row.
+template <int SPLITS, typename Out>
+__device__ __forceinline__ void join_parts(const float *part, Out *out, long long stride, int channel0, int n, int rows, int split, bool accumulate)
+{
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, ch = channel0 + 4 * lane;
+    for (int j = split + SPLITS * warp; j < rows; j += SPLITS * (blockDim.x / 32)) {
+        float4 v[SPLITS];
+#pragma unroll
+        for (int s = 0; s < SPLITS; ++s) v[s] = ld_shared_cluster_f32x4(map_to_cta(smem_u32(part + j * TILE_CHANNELS + 4 * lane), (uint32_t)s));
+        float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+        for (int s = 1; s < SPLITS; ++s) sum[0] += v[s].x, sum[1] += v[s].y, sum[2] += v[s].z, sum[3] += v[s].w;
+        Out *at = out + (long long)j * stride + ch;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((unsigned)(ch + i) < (unsigned)n) at[i] = from_f32<Out>(accumulate ? sum[i] + to_f32(at[i]) : sum[i]);
+    }
+}
+
 // ------------------------------------------------------------------ host
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -491,6 +511,17 @@ inline int sm_count(int device)
         known[device].store(n, std::memory_order_relaxed);
     }
     return n;
+}
+
+// How many CTAs share a tile's steps of K: as many as there are clusters of on the device at once (a second wave costs more than sharing gains), four steps for each at least.  A step
+// takes a CTA about 0.15 us; sharing costs about 1.2 us, and 0.03 us per row of the tile, whose parts have to be added up.  Measured, us: 1 row, n = 512, k = 4096 12.1 unshared, 5.2 with
+// eight; 64 rows 11.9 and 6.4; n = k = 4096, 1 row 12.4 and 6.6 with four; 64 rows, n = 512, k = 1024 4.9 and 5.6.
+inline int splits_of(long long tiles, int per_sm, long long steps, int rows)
+{
+    const int clusters[3] = {74 * per_sm, per_sm == 2 ? 71 : 33, per_sm == 2 ? 33 : 15};     // of 2, 4, 8 CTAs
+    int s = 1;
+    for (int i = 0; i < 3 && tiles <= clusters[i] && steps >= 8 * s; ++i) s *= 2;
+    return steps * (s - 1) * 15 > s * (120 + 3 * rows) ? s : 1;
 }
 
 }  // namespace moe_ovl
