@@ -49,8 +49,8 @@ template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t on, u
 
 // ------------------------------------------------------------------ many rows
 
-template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
-    static constexpr int SPLITS = 1, TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
+template <int CTAS, int CHANNELS, int SPLITS_, typename Out> struct BlockRows {
+    static constexpr int SPLITS = SPLITS_, PITCH = TILE_CHANNELS + 4, TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
     using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 168 * 1024, 4, 128, 8, 1, PARTS>;
     static constexpr int STAGE_OUT = 32 * 128;
     using Schedule = TileSchedule<CHANNELS, TOKENS>;
@@ -59,23 +59,26 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
     const CUtensorMap *map_a, *map_b;
     int *tile_start, *row_start;
     uint8_t *stage;                          // [finishing warps][STAGE_OUT]
+    float *part;                             // SPLITS > 1: [TOKENS][PITCH], where the operands were: a part is written when the last of them has been read
     Schedule sched;
-    int rank = 0;
+    int rank = 0, split = 0;
 
-    struct From { int a0, b0, expert; };
+    struct From { int a0, b0, expert, k0; };
     __device__ __forceinline__ void begin(int lane) { fill_schedule<TOKENS>(p, tile_start, row_start, count_of(p, lane), lane); }
     __device__ __forceinline__ long long total() const { return sched.total(p.counts ? p.experts : 1); }
     __device__ __forceinline__ Tile at(long long t) { return sched.at(t); }
-    __device__ __forceinline__ int steps(const Tile &) const { return p.blocks; }
+    __device__ __forceinline__ int step_of(int i) const { return p.blocks * i / SPLITS; }
+    __device__ __forceinline__ int steps(const Tile &) const { return SPLITS == 1 ? p.blocks : step_of(split + 1) - step_of(split); }
     __device__ __forceinline__ From operands(const Tile &t, bool) const
     {
-        return {uniform((int)((unsigned)t.row0 + (unsigned)(rank * TILE_CHANNELS))), uniform(t.channel0 + rank * SHARE), uniform(t.expert)};
+        return {uniform((int)((unsigned)t.row0 + (unsigned)(rank * TILE_CHANNELS))), uniform(t.channel0 + rank * SHARE), uniform(t.expert), SPLITS == 1 ? 0 : uniform(step_of(split))};
     }
     __device__ __forceinline__ void load(uint32_t on, const From &f, uint32_t sa, uint32_t bar, int step) const
     {
-        load_2d<CTAS>(on, sa, map_a, bar, step * STAGE_ROW, f.a0);
+        const int k = (f.k0 + step) * STAGE_ROW;
+        load_2d<CTAS>(on, sa, map_a, bar, k, f.a0);
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) load_3d<CTAS>(on, sa + BM_M_BYTES + i * SHARE * STAGE_ROW, map_b, bar, step * STAGE_ROW, f.b0 + i * 128, f.expert);
+        for (int i = 0; i < PARTS; ++i) load_3d<CTAS>(on, sa + BM_M_BYTES + i * SHARE * STAGE_ROW, map_b, bar, k, f.b0 + i * 128, f.expert);
     }
     __device__ __forceinline__ uint32_t instruction(const Tile &) const { return idesc_e4m3(TOKENS, 128); }
     __device__ __forceinline__ void multiply(uint32_t on, uint32_t d, uint32_t stage16, uint32_t idesc, bool, int part) const
@@ -88,17 +91,18 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
         const int in_tile = rank * TILE_CHANNELS + quarter * 32 + lane;
         const bool mine = in_tile < t.rows;
         const int block = t.channel0 / 128 + accs.group, ch0 = block * 128 + half * COLS;
-        const float *sa = p.a_scale + (long long)(t.row0 + (mine ? in_tile : 0)) * p.blocks;
-        const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + min(block, p.channel_blocks - 1)) * p.blocks;
+        const int k0 = SPLITS == 1 ? 0 : step_of(split), all = steps(t);
+        const float *sa = p.a_scale + (long long)(t.row0 + (mine ? in_tile : 0)) * p.blocks + k0;
+        const float *sb = p.b_scale + ((long long)t.expert * p.channel_blocks + min(block, p.channel_blocks - 1)) * p.blocks + k0;
         float2 acc[COLS / 2];
 #pragma unroll
         for (int i = 0; i < COLS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
         float a_next = sa[0], b_next = sb[0];
-        for (int k = 0; k < p.blocks; ++k) {
+        for (int k = 0; k < all; ++k) {
             if (!accs.wait(p, t.row0)) return false;
             const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
             const float2 s = both(a_next * b_next);
-            if (k + 1 < p.blocks) a_next = sa[k + 1], b_next = sb[k + 1];
+            if (k + 1 < all) a_next = sa[k + 1], b_next = sb[k + 1];
             // eight columns at a time: the sums take 128 of the 168 registers, and two chunks or wider ones push other values out of them
 #pragma unroll
             for (int c = 0; c < COLS; c += 8) {
@@ -110,8 +114,18 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
                 for (int j = 0; j < 4; ++j) acc[c / 2 + j] = fma2(pair_of(&v[2 * j]), s, acc[c / 2 + j]);
             }
         }
+        if constexpr (SPLITS > 1) {
+            float *own = part + in_tile * PITCH + half * COLS;
+#pragma unroll
+            for (int i = 0; i < COLS; i += 4) *reinterpret_cast<float4 *>(own + i) = make_float4(acc[i / 2].x, acc[i / 2].y, acc[i / 2 + 1].x, acc[i / 2 + 1].y);
+            return true;
+        }
         store(t, acc, rank * TILE_CHANNELS + quarter * 32, ch0, stage + warp * STAGE_OUT, lane);
         return true;
+    }
+    __device__ __forceinline__ void join(const Tile &t) const
+    {
+        join_parts<SPLITS, PITCH>(part, static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride, p.out_stride, t.channel0, p.n, t.rows, split, false);
     }
     // A warp's 32 rows of COLS sums: 128 bytes of each row go through shared memory, 16 bytes of them in turn, so that a store's lanes lie next to each other.  A thread's own
     // row straight from its registers is 32 lines of memory per store, which took as long as nine steps of K.
@@ -160,7 +174,9 @@ template <int CTAS, int CHANNELS, typename Out> struct BlockRows {
 template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
     static constexpr int SPLITS = SPLITS_, TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
     // Two groups of four warps take the steps in turn: what a warp does for one (a wait, its factors, 16 to 64 columns) takes longer than the weights of a step take to come.
-    static constexpr int RING_BYTES = (SPLITS == 1 ? 176 : 64) * 1024, PER_SM = SPLITS == 1 ? 1 : 2;
+    static constexpr int RING_BYTES = (SPLITS > 1 ? 64 : TOKENS == 64 ? 56 : 80) * 1024;
+    // Blocks: where the tiles are no multiple of the SMs, those that have two work on both at once (1 row, 28672 x 4096 22.7 -> 20.6 us; 40 rows of 32 experts, 2048 x 1408 12.4 -> 10.7).
+    static constexpr int PER_SM = 2;
     using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, RING_BYTES, 256 / COLS, COLS, 8, 1, 1, 2>;
     using Schedule = TileSchedule<TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
@@ -282,15 +298,17 @@ template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
     }
 };
 
-template <int CTAS, int CHANNELS, typename Out>
-__global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, Out>::Shape::THREADS, 1)
+template <int CTAS, int CHANNELS, int SPLITS, typename Out>
+__global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, SPLITS, Out>::Shape::THREADS, 1)
 block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
 {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
-    using Work = BlockRows<CTAS, CHANNELS, Out>;
+    using Work = BlockRows<CTAS, CHANNELS, SPLITS, Out>;
+    static_assert(SPLITS == 1 || (CTAS == 1 && CHANNELS == TILE_CHANNELS && Work::TOKENS * Work::PITCH * 4 <= Work::Shape::STAGES * Work::Shape::STAGE_BYTES), "room for the parts");
+    float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ __align__(16) uint8_t s_out[Work::Shape::FINISHERS * Work::STAGE_OUT];
-    run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_out, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+    run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_out, part, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
 template <int TOKENS, int SPLITS, typename Out>
@@ -312,17 +330,18 @@ bool encode_operands(const BmP &p, const BmOperands &o, int a_rows, int b_rows, 
            encode_tiles(b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.b, p.k, p.n, o.b_stride, std::max(p.experts, 1), o.b_far, b_rows);
 }
 
-template <int CTAS, int CHANNELS, typename Out>
-int launch_rows(BmP p, const BmOperands &o, int device, cudaStream_t stream)
+template <int CTAS, int CHANNELS, int SPLITS, typename Out>
+int launch_rows(BmP p, const BmOperands &o, long long tiles, int device, cudaStream_t stream)
 {
-    using Shape = typename BlockRows<CTAS, CHANNELS, Out>::Shape;
+    using Shape = typename BlockRows<CTAS, CHANNELS, SPLITS, Out>::Shape;
     CUtensorMap a, b;
     p.row_tiles = (p.n - 1) / CHANNELS + 1;
     if (!encode_operands(p, o, TILE_CHANNELS, 128 / CTAS, &a, &b)) return MOE_OVL_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
-    const auto kernel = block_matmul_kernel<CTAS, CHANNELS, Out>;
+    const auto kernel = block_matmul_kernel<CTAS, CHANNELS, SPLITS, Out>;
     if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
-    return launch_behind(kernel, (unsigned)(sm_count(device) / CTAS * CTAS), dim3(Shape::THREADS), Shape::SMEM, CTAS, stream, a, b, p);
+    const unsigned blocks = SPLITS > 1 ? (unsigned)(tiles * SPLITS) : (unsigned)(sm_count(device) / CTAS * CTAS);
+    return launch_behind(kernel, blocks, dim3(Shape::THREADS), Shape::SMEM, CTAS * SPLITS, stream, a, b, p);
 }
 
 template <int TOKENS, int SPLITS, typename Out>
@@ -336,7 +355,7 @@ int launch_few(BmP p, const BmOperands &o, long long tiles, int device, cudaStre
     static std::atomic<unsigned long long> allowed{0};
     const auto kernel = block_matmul_few_kernel<TOKENS, SPLITS, Out>;
     if (!allow_smem(kernel, SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
-    const unsigned blocks = SPLITS > 1 ? (unsigned)(tiles * SPLITS) : (unsigned)sm_count(device);
+    const unsigned blocks = SPLITS > 1 ? (unsigned)(tiles * SPLITS) : (unsigned)sm_count(device) * Work::PER_SM;
     return launch_behind(kernel, blocks, dim3(Work::Shape::THREADS), SMEM, SPLITS, stream, a, b, p);
 }
 template <int TOKENS, typename Out>
@@ -350,7 +369,7 @@ int launch_few(int splits, const BmP &p, const BmOperands &o, long long tiles, i
     }
 }
 
-// ctas 0: few rows, `tile` of them, by `splits` CTAs each; else `tile` channels.  tiles: the most that any counts can give.
+// ctas 0: few rows, `tile` of them; else `tile` channels.  splits > 1: a cluster of that many CTAs per tile.  tiles: the most that any counts can give.
 struct BmChoice { int ctas, tile, splits; long long tiles; };
 
 BmChoice choose(const BmP &p)
@@ -359,12 +378,14 @@ BmChoice choose(const BmP &p)
     if (per_group <= 64) {
         const int few = per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64;
         const long long most = (long long)p.channel_blocks * (p.counts ? p.rows / few + groups : (p.rows - 1) / few + 1);
-        const int splits = splits_of(most, 2, p.blocks, std::min(few, per_group));
+        const int splits = splits_of(most, 2, p.blocks, std::min(few, per_group), 280);
         if (splits > 1) return {0, few, splits, most};
         return {0, p.experts && per_group > 4 ? std::min(64, 2 * few) : few, 1, 0};
     }
     const long long pairs = (long long)((p.n - 1) / 256 + 1) * groups * ((per_group - 1) / 256 + 1);
-    return pairs >= 37 ? BmChoice{2, 256, 1, 0} : BmChoice{1, 128, 1, 0};
+    if (pairs >= 37) return {2, 256, 1, 0};
+    const long long most = (long long)p.channel_blocks * (p.counts ? p.rows / TILE_CHANNELS + groups : (p.rows - 1) / TILE_CHANNELS + 1);
+    return {1, 128, splits_of(most, 1, p.blocks, TILE_CHANNELS, 350), most};
 }
 
 }  // namespace
@@ -401,8 +422,15 @@ extern "C" int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *a)
     const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
     return with_dtype(a->out_dtype, [&](auto t) {
         using Out = decltype(t);
-        if (c.ctas == 2) return launch_rows<2, 256, Out>(p, o, a->device, stream);
-        if (c.ctas == 1) return launch_rows<1, 128, Out>(p, o, a->device, stream);
+        if (c.ctas == 2) return launch_rows<2, 256, 1, Out>(p, o, 0, a->device, stream);
+        if (c.ctas == 1) {
+            switch (c.splits) {
+            case 1: return launch_rows<1, 128, 1, Out>(p, o, 0, a->device, stream);
+            case 2: return launch_rows<1, 128, 2, Out>(p, o, c.tiles, a->device, stream);
+            case 4: return launch_rows<1, 128, 4, Out>(p, o, c.tiles, a->device, stream);
+            default: return launch_rows<1, 128, 8, Out>(p, o, c.tiles, a->device, stream);
+            }
+        }
         switch (c.tile) {
         case 16: return launch_few<16, Out>(c.splits, p, o, c.tiles, a->device, stream);
         case 32: return launch_few<32, Out>(c.splits, p, o, c.tiles, a->device, stream);

@@ -336,7 +336,7 @@ GmChoice choose(const GmP &p)
     const int few = per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64;
     // what any counts can give
     const long long most = (long long)((p.n - 1) / TILE_CHANNELS + 1) * (p.counts ? p.rows / few + groups : (p.rows - 1) / few + 1);
-    const int splits = splits_of(most, 2, (p.k - 1) / GM_K + 1, std::min(few, per_group));
+    const int splits = splits_of(most, 2, (p.k - 1) / GM_K + 1, std::min(few, per_group), 150);
     if (splits > 1) return {1, few, splits, most};
     if (p.experts && per_group > 4 && per_group <= 64) return {1, per_group <= 16 ? 32 : 64, 1, 0};
     if (per_group <= 16) return {1, 16, 1, 0};
@@ -462,7 +462,7 @@ extern "C" int moe_ovl_grouped_matmul_backward(const moe_ovl_grouped_matmul_back
     const bool pair = pairs > 37;
     p.row_tiles = (p.n - 1) / (pair ? 256 : 128) + 1;
     const long long tiles = (long long)experts * p.row_tiles * ((p.k - 1) / 128 + 1), narrow = (long long)experts * p.row_tiles * ((p.k - 1) / 64 + 1);
-    const int steps = a->rows / experts / GM_K, splits = splits_of(tiles, 1, steps, 128), narrow_splits = splits_of(narrow, 2, steps, 64);
+    const int steps = a->rows / experts / GM_K, splits = splits_of(tiles, 1, steps, 128, 150), narrow_splits = splits_of(narrow, 2, steps, 64, 150);
     const bool wide = (splits > 1 ? 31 : 22) * narrow_splits <= 43 * splits;
     return with_dtype(a->out_dtype, [&](auto t) {
         using Out = decltype(t);

@@ -438,15 +438,15 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
 }
 
 // The output of a tile whose steps a cluster has shared: a warp adds up the parts of a row, four columns per lane, SPLITS loads in flight.  The CTAs and their warps take the
-// rows in turn.  part: [rows][TILE_CHANNELS] in shared memory, at the same place in every CTA; out: the tile's first row.
-template <int SPLITS, typename Out>
+// rows in turn.  part: [rows][PITCH] in shared memory, at the same place in every CTA; out: the tile's first row.
+template <int SPLITS, int PITCH = TILE_CHANNELS, typename Out>
 __device__ __forceinline__ void join_parts(const float *part, Out *out, long long stride, int channel0, int n, int rows, int split, bool accumulate)
 {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, ch = channel0 + 4 * lane;
     for (int j = split + SPLITS * warp; j < rows; j += SPLITS * (blockDim.x / 32)) {
         float4 v[SPLITS];
 #pragma unroll
-        for (int s = 0; s < SPLITS; ++s) v[s] = ld_shared_cluster_f32x4(map_to_cta(smem_u32(part + j * TILE_CHANNELS + 4 * lane), (uint32_t)s));
+        for (int s = 0; s < SPLITS; ++s) v[s] = ld_shared_cluster_f32x4(map_to_cta(smem_u32(part + j * PITCH + 4 * lane), (uint32_t)s));
         float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
 #pragma unroll
         for (int s = 1; s < SPLITS; ++s) sum[0] += v[s].x, sum[1] += v[s].y, sum[2] += v[s].z, sum[3] += v[s].w;
@@ -514,14 +514,14 @@ inline int sm_count(int device)
 }
 
 // How many CTAs share a tile's steps of K: as many as there are clusters of on the device at once (a second wave costs more than sharing gains), four steps for each at least.  A step
-// takes a CTA about 0.15 us; sharing costs about 1.2 us, and 0.03 us per row of the tile, whose parts have to be added up.  Measured, us: 1 row, n = 512, k = 4096 12.1 unshared, 5.2 with
+// takes a CTA `step_ns` ns; sharing costs about 1.2 us, and 0.03 us per row of the tile, whose parts have to be added up.  Measured, us: 1 row, n = 512, k = 4096 12.1 unshared, 5.2 with
 // eight; 64 rows 11.9 and 6.4; n = k = 4096, 1 row 12.4 and 6.6 with four; 64 rows, n = 512, k = 1024 4.9 and 5.6.
-inline int splits_of(long long tiles, int per_sm, long long steps, int rows)
+inline int splits_of(long long tiles, int per_sm, long long steps, int rows, int step_ns)
 {
     const int clusters[3] = {74 * per_sm, per_sm == 2 ? 71 : 33, per_sm == 2 ? 33 : 15};     // of 2, 4, 8 CTAs
     int s = 1;
     for (int i = 0; i < 3 && tiles <= clusters[i] && steps >= 8 * s; ++i) s *= 2;
-    return steps * (s - 1) * 15 > s * (120 + 3 * rows) ? s : 1;
+    return steps * (s - 1) * step_ns > s * (1200ll + 30 * rows) ? s : 1;
 }
 
 }  // namespace moe_ovl
