@@ -39,8 +39,9 @@ __device__ __forceinline__ Divisor divisor_of(float most)
     const float whole = most * power;
     d.factor = both(BQ_LARGEST * power);
     d.minus_d = both(-whole);
-    float inverse;       // within a unit in the last place: what that leaves of the quotient's error is 2^-22 of a unit
+    float inverse;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(whole));
+    inverse = fmaf(inverse, fmaf(-whole, inverse, 1.0f), inverse);
     d.inverse = both(inverse);
     return d;
 }
