@@ -103,15 +103,18 @@ template <int CTAS, int CHANNELS, int SPLITS_, typename Out> struct BlockRows {
             const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
             const float2 s = both(a_next * b_next);
             if (k + 1 < all) a_next = sa[k + 1], b_next = sb[k + 1];
-            // eight columns at a time: the sums take 128 of the 168 registers, and two chunks or wider ones push other values out of them
+            // 16 columns at a time: the sums take 128 of the 168 registers, and two chunks or wider ones push other values out of them
 #pragma unroll
-            for (int c = 0; c < COLS; c += 8) {
-                uint32_t v[8];
-                tmem_ld8(from + c, v);
+            for (int c = 0; c < COLS; c += 16) {
+                uint32_t v[16];
+                tmem_ld16(from + c, v);
                 tmem_ld_wait(v);
-                if (c + 8 == COLS) accs.release();               // all of them are in registers
+                if (c + 16 == COLS) {
+                    accs.release();               // all of them are in registers
+                    accs.look();
+                }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[c / 2 + j] = fma2(pair_of(&v[2 * j]), s, acc[c / 2 + j]);
+                for (int j = 0; j < 8; ++j) acc[c / 2 + j] = fma2(pair_of(&v[2 * j]), s, acc[c / 2 + j]);
             }
         }
         if constexpr (SPLITS > 1) {

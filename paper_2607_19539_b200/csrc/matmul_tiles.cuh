@@ -244,9 +244,13 @@ template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_
 
 // Arrival of a reader of tensor memory, on a barrier that may be the peer CTA's.  What it gives back has been read (tcgen05.wait, and the fence
 // in front of it) and nothing was written, so it needs no release of memory at cluster scope, which would wait for the warp's loads and stores.
-__device__ __forceinline__ void arrive_read(uint32_t cluster_bar)
+__device__ __forceinline__ void arrive_read(uint32_t on, uint32_t cluster_bar)
 {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+        "@q mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}"
+        ::"r"(cluster_bar), "r"(on)
+        : "memory");
 }
 
 // A finishing warp's way through the accumulators of its group.
@@ -254,18 +258,22 @@ template <typename Shape> struct Accumulators {
     uint32_t bar_full, lead_empty, tmem;
     int lane, group = 0, acc = 0;
     uint32_t phase = 0;
+    bool there = false;                      // this lane has seen what wait() would wait for
     template <typename P> __device__ __forceinline__ bool wait(const P &p, long long index)
     {
-        const bool ok = warp_wait(bar_full + 8 * acc, phase, p, SITE_TILE_DONE, index);
+        const bool ok = __all_sync(0xffffffffu, there) || warp_wait(bar_full + 8 * acc, phase, p, SITE_TILE_DONE, index);
+        there = false;
         tc_fence_after();
         return ok;
     }
+    // A look at the next one ahead of its wait, for whoever has something else to do meanwhile; behind release().
+    __device__ __forceinline__ void look() { there = mbar_test_wait(bar_full + 8 * acc, phase); }
     __device__ __forceinline__ uint32_t columns() const { return tmem + (uint32_t)(acc * Shape::ACC_COLS); }
     __device__ __forceinline__ void release()
     {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_read(lead_empty + 8 * acc);
+        arrive_read(lane == 0, lead_empty + 8 * acc);
         if ((acc += Shape::GROUPS) >= Shape::ACCS) acc = group, phase ^= 1u;
     }
 };
