@@ -409,7 +409,7 @@ extern "C" int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *a)
     if (std::max(std::max(a->a_stride, a->b_stride), a->out_stride) > 0x7fffffff || a->b_expert_stride >= 1ll << 40) return MOE_OVL_ERR_UNSUPPORTED;
     // strides that are never used: the tensor map wants some that hold the row and are multiples of 16 bytes
     const long long sa = a->rows > 1 ? a->a_stride : (a->k + 15ll) / 16 * 16, sb = a->n > 1 ? a->b_stride : (a->k + 15ll) / 16 * 16;
-    const long long far = experts > 1 ? a->b_expert_stride : a->n * sb;
+    const long long far = experts > 1 ? a->b_expert_stride : sb;
     if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 16 != 0 || sb % 16 != 0 || far % 16 != 0) return MOE_OVL_ERR_UNSUPPORTED;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;

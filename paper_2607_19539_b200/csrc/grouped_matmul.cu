@@ -23,7 +23,8 @@ constexpr int GM_BOX = STAGE_ROW * GM_K;     // bytes of 64 columns x 64 rows, K
 constexpr int GM_M_BYTES = TILE_CHANNELS * STAGE_ROW;
 
 // The tensor cores cut a sum off where they add to it, instead of rounding: its error grows with the number of steps, 8.4e-6 of a gradient over 6000 rows where 32-bit
-// sums are off by 9e-7.  16-bit outputs do not see that; for 32-bit ones a sum ends after 512 of K, and the finishing warps add the pieces up in registers.
+// sums are off by 9e-7.  For 32-bit outputs, and for gradients, whose sums have no end, a sum ends after 512 of K, and the finishing warps add the pieces up in registers; other
+// 16-bit outputs do not see the difference.
 constexpr int GM_SEGMENT = 512 / GM_K;
 
 // What K runs along: rows of both operands; columns of the M side's; columns of both
@@ -55,7 +56,7 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
     static constexpr int SPLITS = SPLITS_;
     static constexpr int SHARE = TOKENS / CTAS;                              // of the N side, per CTA
     static constexpr int COLS = TOKENS < 32 ? 32 : TOKENS;                   // of tensor memory
-    static constexpr bool WIDE = sizeof(Out) == 4;
+    static constexpr bool WIDE = sizeof(Out) == 4 || FORM == FORM_COLUMNS;   // in segments of K
     static constexpr int RING_BYTES = (SPLITS == 1 ? 200 : TOKENS > 64 ? 128 : 72) * 1024;
     static constexpr int PER_SM = SPLITS > 1 && TOKENS <= 64 ? 2 : 1;        // blocks: a cluster finds its place where there is room for another one
     using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, RING_BYTES, 2, COLS, 8, WIDE ? GM_SEGMENT : 0>;
@@ -369,7 +370,7 @@ extern "C" int moe_ovl_grouped_matmul(const moe_ovl_grouped_matmul_args *a)
     if (std::max(std::max(a->a_stride, a->b_stride), a->out_stride) > 0x7fffffff || a->b_expert_stride >= FAR) return MOE_OVL_ERR_UNSUPPORTED;
     // strides that are never used: the tensor map wants some that hold the row and are multiples of 16 bytes
     const long long sa = a->rows > 1 ? a->a_stride : (a->k + 7ll) / 8 * 8, sb = b_rows > 1 ? a->b_stride : (b_cols + 7ll) / 8 * 8;
-    const long long far = experts > 1 ? a->b_expert_stride : b_rows * sb;
+    const long long far = experts > 1 ? a->b_expert_stride : sb;
     if (!aligned(a->a, 16) || !aligned(a->b, 16) || sa % 8 != 0 || sb % 8 != 0 || far % 8 != 0) return MOE_OVL_ERR_UNSUPPORTED;
     DeviceGuard guard(a->device);
     if (!guard.ok) return MOE_OVL_ERR_CUDA;

@@ -1,12 +1,13 @@
 """A whole expert layer around the library's operators, with all experts on this GPU: norm of the residual sum, router, experts
-in 8-bit integers, gate-weighted sum.  What lies between the operators (the router's projection, sorting rows by expert,
-the weighted sum) is plain torch.
+in 8-bit integers or in 8-bit floats with a scale per block, gate-weighted sum.  What lies between the operators (the router's projection, sorting
+rows by expert, the weighted sum) is plain torch.  `expert_ffn` is the experts' part for training: its products and their gradients are operators
+under torch's autograd, and `clip_gradients` clips what a backward pass has left.
 
 The same routing also feeds the bf16 experts of moe_ovl_expert_return (`routed_rows` gives its arguments), and
 
     python -m paper_2607_19539_b200.layer
 
-runs both on random weights and prints how far they are apart.
+runs all of them on random weights, prints how far they are apart, and takes a training step.
 """
 from __future__ import annotations
 
@@ -51,8 +52,7 @@ class QuantExpertLayer:
         self.experts, self.d, self.f = w2.shape
         if w1.shape != (self.experts, 2 * self.f, self.d) or router.shape != (self.experts, self.d):
             raise B.MoeOvlError(B.ERR_INVALID_ARG, "QuantExpertLayer: w1 has to be [experts, 2F, d], w2 [experts, d, F], router [experts, d]")
-        self.w1, self.s1 = quantise_channels(w1)
-        self.w2, self.s2 = quantise_channels(w2)
+        self.hold(w1, w2)
         self.choice = dict(score=score, bias=bias, num_groups=num_groups, top_groups=top_groups, group_best=group_best, renormalise=renormalise,
                            gate_scale=gate_scale)
         dev, t, rows = w1.device, max_tokens, max_tokens * top_k
@@ -62,6 +62,11 @@ class QuantExpertLayer:
         self.gate_up, self.hidden, self.hidden_scale = new(rows, 2 * self.f, dtype=w1.dtype), new(rows, self.f, dtype=torch.int8), new(rows)
         self.rows_out = new(rows, self.d, dtype=w1.dtype)
         self.status = torch.zeros(4, dtype=torch.int32, device=dev)
+
+    def hold(self, w1, w2) -> None:
+        """Keeps the experts' weights in 8 bits."""
+        self.w1, self.s1 = quantise_channels(w1)
+        self.w2, self.s2 = quantise_channels(w2)
 
     def route(self, x, residual=None, residual_out=None) -> RoutedRows:
         """Norm (bf16 for the router, 8 bits for the experts) and choice; self.y, self.q and self.scale hold the normed rows."""
@@ -94,6 +99,86 @@ class QuantExpertLayer:
         return torch.where(self.expert[:t].unsqueeze(-1) >= 0, rows * gate, 0.0).sum(1).to(x.dtype)      # an empty slot's row was never written
 
 
+def quantise_blocks(w: torch.Tensor):
+    """Weights [..., channels, k] in 8-bit floats with a scale per 128 x 128: (float8_e4m3fn, float32 [..., ceil(channels / 128), ceil(k / 128)])."""
+    w = w.detach().contiguous()
+    q = torch.empty(w.shape, dtype=ops.FLOAT8, device=w.device)
+    scale = torch.empty((*w.shape[:-2], -(-w.shape[-2] // ops.BLOCK), -(-w.shape[-1] // ops.BLOCK)), device=w.device)
+    ops.moe_ovl_block_quant(x=w, q=q, scale=scale, tiles=True)
+    return q, scale
+
+
+class BlockExpertLayer(QuantExpertLayer):
+    """The same layer with its experts in 8-bit floats: a scale per 128 values of a row and per 128 x 128 weights.  d and F have to be multiples of 16."""
+
+    def hold(self, w1, w2) -> None:
+        if self.d % 16 or self.f % 16:
+            raise B.MoeOvlError(B.ERR_UNSUPPORTED, "BlockExpertLayer: d and F have to be multiples of 16")
+        self.w1, self.s1 = quantise_blocks(w1)
+        self.w2, self.s2 = quantise_blocks(w2)
+
+    def experts_of(self, r: RoutedRows):
+        n, token, dev = r.token.shape[0], r.token, r.token.device
+        t = n // self.k
+        q = torch.empty((t, self.d), dtype=ops.FLOAT8, device=dev)
+        scale = torch.empty((t, self.s1.shape[-1]), device=dev)
+        ops.moe_ovl_block_quant(x=self.y[:t], q=q, scale=scale)
+        hidden = torch.empty((n, self.f), dtype=ops.FLOAT8, device=dev)
+        hidden_scale = torch.empty((n, self.s2.shape[-1]), device=dev)
+        rows = q.view(torch.uint8)[token].view(ops.FLOAT8)          # torch gathers bytes
+        ops.moe_ovl_block_matmul(a=rows, a_scale=scale[token], b=self.w1, b_scale=self.s1, out=self.gate_up[:n], expert_counts=r.counts, status=self.status)
+        ops.moe_ovl_block_quant(x=self.gate_up[:n], q=hidden, scale=hidden_scale, gated=True)
+        ops.moe_ovl_block_matmul(a=hidden, a_scale=hidden_scale, b=self.w2, b_scale=self.s2, out=self.rows_out[:n], expert_counts=r.counts, status=self.status)
+        return self.rows_out[:n]
+
+
+class ExpertProduct(torch.autograd.Function):
+    """rows @ weight[e]^T for the rows of every expert, with both gradients by the operators.  Rows behind the last expert's give zeros, and get them.  The counts are looked at
+    again on the way back: they have to be what they were."""
+
+    @staticmethod
+    def forward(ctx, rows, weight, counts, status):
+        ctx.save_for_backward(rows, weight, counts, status)
+        out = torch.zeros((rows.shape[0], weight.shape[1]), dtype=rows.dtype, device=rows.device)
+        ops.moe_ovl_grouped_matmul(a=rows, b=weight, out=out, expert_counts=counts, status=status)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        rows, weight, counts, status = ctx.saved_tensors
+        dout = dout.contiguous()
+        drows = dweight = None
+        if ctx.needs_input_grad[0]:
+            drows = torch.zeros_like(rows)
+            ops.moe_ovl_grouped_matmul(a=dout, b=weight, out=drows, expert_counts=counts, transposed=True, status=status)
+        if ctx.needs_input_grad[1]:
+            dweight = torch.empty_like(weight)
+            workspace = torch.empty(ops.moe_ovl_grouped_matmul_workspace_bytes(weight.shape[0]), dtype=torch.uint8, device=rows.device)
+            ops.moe_ovl_grouped_matmul_backward(dy=dout, x=rows, dweight=dweight, expert_counts=counts, status=status, workspace=workspace)
+        return drows, dweight, None, None
+
+
+def expert_ffn(rows, w1, w2, counts, status):
+    """Rows grouped by expert ([n, d], counts [experts] int32) through their experts, for training: w1 [experts, 2F, d] (gate rows, then up rows), w2 [experts, d, F].
+    `status`: 4 int32 that the caller clears once; look at it after a synchronize of your own."""
+    counts = counts.clone()             # the router's buffer may hold the next batch's by the time of the backward pass
+    gate, up = ExpertProduct.apply(rows, w1, counts, status).float().chunk(2, dim=1)
+    hidden = (torch.nn.functional.silu(gate) * up).to(rows.dtype)
+    return ExpertProduct.apply(hidden, w2, counts, status)
+
+
+def clip_gradients(parameters, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
+    """Scales the gradients of the parameters that have one, so that their norm is max_norm at most; returns the norm before, on the device."""
+    grads = [p.grad for p in parameters if p.grad is not None]
+    if not grads:
+        return torch.zeros(1)
+    norm = torch.empty(1, device=grads[0].device)
+    workspace = torch.empty(ops.moe_ovl_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device=norm.device)
+    ops.moe_ovl_grad_norm(grads=grads, norm=norm, workspace=workspace)
+    ops.moe_ovl_clip_grads(grads=grads, norm=norm, max_norm=max_norm, eps=eps)
+    return norm
+
+
 def bf16_experts(layer: QuantExpertLayer, r: RoutedRows, tokens: int, w1, w2, mode: int = B.MODE_AUTO):
     """The same routing through moe_ovl_expert_return: one source rank, every expert local, bf16 weights.  Every slot has to be taken."""
     dev, n = w1.device, r.token.shape[0]
@@ -109,12 +194,12 @@ def bf16_experts(layer: QuantExpertLayer, r: RoutedRows, tokens: int, w1, w2, mo
     return out
 
 
-def random_layer(tokens: int, d: int, f: int, experts: int, top_k: int, seed: int = 0, device="cuda:0", **choice):
+def random_layer(tokens: int, d: int, f: int, experts: int, top_k: int, seed: int = 0, device="cuda:0", kind=QuantExpertLayer, **choice):
     """Random weights of that size: (layer, x, residual, w1, w2)."""
     g = torch.Generator(device=device).manual_seed(seed)
     normal = lambda *shape, scale=1.0: (torch.randn(shape, generator=g, device=device) * scale).to(torch.bfloat16)  # noqa: E731
     w1, w2 = normal(experts, 2 * f, d, scale=d ** -0.5), normal(experts, d, f, scale=f ** -0.5)
-    layer = QuantExpertLayer(1 + normal(d, scale=0.1), normal(experts, d, scale=d ** -0.5), w1, w2, top_k=top_k, max_tokens=tokens, **choice)
+    layer = kind(1 + normal(d, scale=0.1), normal(experts, d, scale=d ** -0.5), w1, w2, top_k=top_k, max_tokens=tokens, **choice)
     return layer, normal(tokens, d), normal(tokens, d), w1, w2
 
 
@@ -124,18 +209,36 @@ def main() -> None:
     residual_out = torch.empty_like(x)
     out = layer(x, residual, residual_out)
     ref = bf16_experts(layer, routed_rows(layer.expert, layer.gate, layer.counts), tokens, w1, w2)
-    far = (out.double() - ref.double()).norm(dim=1) / ref.double().norm(dim=1)
-    print(f"{tokens} tokens, 64 experts, top 6: 8-bit experts against bf16 experts, relative distance per token "
-          f"median {float(far.median()):.4f}, largest {float(far.max()):.4f}; rows per expert {int(layer.counts.min())} .. {int(layer.counts.max())}")
+    block = random_layer(tokens, d=2048, f=1408, experts=64, top_k=6, kind=BlockExpertLayer)[0]
+
+    def distance(out):
+        far = (out.double() - ref.double()).norm(dim=1) / ref.double().norm(dim=1)
+        return f"relative distance per token median {float(far.median()):.4f}, largest {float(far.max()):.4f}"
+
+    print(f"{tokens} tokens, 64 experts, top 6, rows per expert {int(layer.counts.min())} .. {int(layer.counts.max())}: 8-bit experts against bf16 experts, {distance(out)}; "
+          f"in 8-bit floats {distance(block(x, residual, residual_out))}")
     begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-    for _ in range(3):
-        layer(x, residual, residual_out)
-    begin.record()
-    for _ in range(10):
-        layer(x, residual, residual_out)
-    end.record()
+    for name, each in (("8-bit integers", layer), ("8-bit floats", block)):
+        for _ in range(3):
+            each(x, residual, residual_out)
+        begin.record()
+        for _ in range(10):
+            each(x, residual, residual_out)
+        end.record()
+        torch.cuda.synchronize()
+        print(f"layer in {name} {begin.elapsed_time(end) / 10:.3f} ms per call, the torch steps between the operators included")
+
+    r = routed_rows(layer.expert, layer.gate, layer.counts)
+    rows, w1, w2 = layer.y[r.token], w1.requires_grad_(), w2.requires_grad_()
+    for step in range(4):
+        begin.record()
+        w1.grad = w2.grad = None
+        expert_ffn(rows, w1, w2, r.counts, layer.status).backward(torch.full_like(rows, 1e-3))
+        norm = clip_gradients([w1, w2], 1.0)
+        end.record()
     torch.cuda.synchronize()
-    print(f"8-bit layer {begin.elapsed_time(end) / 10:.3f} ms per call, the torch steps between the operators included")
+    print(f"experts' training step (forward, backward, clipping; {rows.shape[0]} rows in bf16) {begin.elapsed_time(end):.3f} ms, gradient norm {float(norm):.3f} before clipping, "
+          f"status {layer.status.tolist()}")
 
 
 if __name__ == "__main__":

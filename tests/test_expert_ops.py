@@ -711,6 +711,134 @@ def test_streams_and_graph_capture():
 
 
 @gpu
+def test_two_streams_at_once():
+    """Two training passes side by side, each with workspaces and a status of its own, give the bits of each alone."""
+    a, b = Training(seed=1), Training(rows=700, counts=(0, 300, 100, 299), seed=2)
+    want = [a.run(a.x)[:5], b.run(b.x)[:5]]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for t, s in zip((a, b), streams):
+            t.run(t.x, stream=s)
+    torch.cuda.synchronize()
+    for t, w in zip((a, b), want):
+        for got, ref in zip([t.y, t.dx, t.dw1, t.dw2, t.norm], w):
+            assert torch.equal(got, ref)
+        assert not t.st.any()
+
+
+@gpu
+def test_values_at_the_ends_of_the_types():
+    """Subnormal operands, exact in products and sums: 16-bit floats and e4m3 (2^-9), and the largest values."""
+    st = status()
+    for dtype, small, large in ((F16, 2.0 ** -24, 2.0 ** 10), (BF16, 2.0 ** -133, 2.0 ** 100), (F16, 65504.0, 2.0 ** -8), (BF16, 2.0 ** 127, 2.0 ** -120)):
+        a = torch.zeros((3, 64), dtype=dtype, device="cuda")
+        a[0], a[1, ::2], a[2, 7] = small, -small, small
+        b = torch.full((8, 64), large, dtype=dtype, device="cuda")
+        for transposed, w in ((False, b), (True, b.t().contiguous())):
+            out = torch.empty((3, 8), device="cuda")
+            ops.moe_ovl_grouped_matmul(a=a, b=w, out=out, transposed=transposed, status=st)
+            assert torch.equal(out, product64(a, w, None, transposed).float())
+    for m in (3, 200):
+        a, b = torch.zeros((m, 256), dtype=F8, device="cuda"), torch.full((130, 256), 448.0, device="cuda").to(F8)
+        a.view(torch.uint8)[0], a.view(torch.uint8)[1, ::3], a.view(torch.uint8)[2] = 1, 0x87, 0x7e          # 2^-9, -7 * 2^-9, 448
+        sa, sb = torch.full((m, 2), 2.0 ** 40, device="cuda"), torch.full((2, 2), 2.0 ** -60, device="cuda")
+        check_block(a, sa, b, sb, None, F32)
+
+
+@gpu
+def test_experts_that_interleave():
+    """Matrices whose rows lie between each other's (k or n first in memory): read from there, and written there."""
+    g = gen(21)
+    counts, n, k = [20, 0, 33], 72, 136
+    a = whole(g, (53, k), BF16)
+    b = whole(g, (n, 3, k), BF16).transpose(0, 1)                                 # [3, n, k]
+    check_grouped(a, b, counts, False, F32)
+    check_grouped(a, whole(g, (k, 3, n), BF16).transpose(0, 1), counts, True, F32)
+    dy = whole(g, (53, n), BF16)
+    full, st = torch.full((n, 3, k), 7.5, device="cuda"), status()
+    ops.moe_ovl_grouped_matmul_backward(dy=dy, x=a, dweight=full.transpose(0, 1), expert_counts=device_counts(counts), status=st, workspace=workspace(3))
+    assert torch.equal(full.transpose(0, 1), gradient64(dy, a, counts).float())
+    a8, sa, b8, sb = block_operands(g, 53, n, 144, 3)
+    check_block(a8, sa, b8.transpose(0, 1).contiguous().transpose(0, 1), sb, counts, F32)
+    x = normal(g, (200, 3, 256), F32).transpose(0, 1)
+    q, scale = torch.empty((200, 3, 256), dtype=F8, device="cuda").transpose(0, 1), torch.empty((3, 2, 2), device="cuda")
+    ops.moe_ovl_block_quant(x=x, q=q, scale=scale, tiles=True)
+    flat = torch.empty((3, 200, 256), dtype=F8, device="cuda")
+    again = torch.empty_like(scale)
+    ops.moe_ovl_block_quant(x=x.contiguous(), q=flat, scale=again, tiles=True)
+    assert torch.equal(q.contiguous().view(torch.uint8), flat.view(torch.uint8)) and torch.equal(scale, again)
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    """Rows and matrices that lie so far apart that element and byte offsets pass 32 bits."""
+    g = gen(22)
+    far, k, n = 1_500_000_016, 64, 72
+
+    def spread(shape, dtype, strides):
+        full = torch.empty(sum((d - 1) * s for d, s in zip(shape, strides)) + 1, dtype=dtype, device="cuda")
+        return full.as_strided(shape, strides)
+
+    a, out = spread((3, k), BF16, (far, 1)), spread((3, n), BF16, (far, 1))
+    a.copy_(whole(g, (3, k), BF16))
+    b = spread((3, n, k), BF16, (2 * far, k, 1))
+    b.copy_(whole(g, (3, n, k), BF16))
+    counts, st = device_counts([1, 0, 2]), status()
+    ops.moe_ovl_grouped_matmul(a=a, b=b, out=out, expert_counts=counts, status=st)
+    assert torch.equal(out, product64(a, b, [1, 0, 2]).to(BF16))
+    dy = whole(g, (3, n), BF16)
+    ops.moe_ovl_grouped_matmul_backward(dy=dy, x=a, dweight=b, expert_counts=counts, status=st, workspace=workspace(3))      # written where the weights were
+    assert torch.equal(b, gradient64(dy, a, [1, 0, 2]).to(BF16)) and not st.any()
+    del b
+    x = spread((3, 2 * 144), BF16, (far, 1))
+    x.copy_(normal(g, (3, 2 * 144), BF16))
+    q, scale = spread((3, 144), F8, (far, 1)), torch.empty((3, 2), device="cuda")
+    ops.moe_ovl_block_quant(x=x, q=q, scale=scale, gated=True)
+    near, again = torch.empty((3, 144), dtype=F8, device="cuda"), torch.empty_like(scale)
+    ops.moe_ovl_block_quant(x=x.contiguous(), q=near, scale=again, gated=True)
+    assert torch.equal(q.contiguous().view(torch.uint8), near.view(torch.uint8)) and torch.equal(scale, again)
+    w, sw = whole(g, (n, 144), F8), torch.ones((1, 2), device="cuda")
+    ops.moe_ovl_block_matmul(a=q, a_scale=scale, b=w, b_scale=sw, out=out, status=st)
+    dense = torch.empty((3, n), dtype=BF16, device="cuda")
+    ops.moe_ovl_block_matmul(a=near, a_scale=scale, b=w, b_scale=sw, out=dense, status=st)
+    assert torch.equal(out, dense)
+    del a, out, x, q
+    big = torch.zeros(2 ** 31 + 77, dtype=BF16, device="cuda")
+    big[-5:], big[2 ** 31 - 3] = 3.0, 4.0
+    assert abs(float(norm_of([big])) - math.sqrt(5 * 9 + 16)) < 1e-5
+    ops.moe_ovl_clip_grads(grads=[big], norm=torch.ones(1, device="cuda"), max_norm=0.5, eps=0.0)
+    assert big[-5:].tolist() == [1.5] * 5 and big[2 ** 31 - 3] == 2.0 and float(big.sum(dtype=torch.float64)) == 9.5
+
+
+@gpu
+def test_most_rows():
+    """2^31 - 1 rows: the last ones are found, multiplied, and end where the experts' counts say."""
+    rows, e = 2 ** 31 - 1, 2
+    counts = device_counts([rows - 70, 60])
+    x = torch.zeros((rows, 8), dtype=F16, device="cuda")
+    x[-70:-10, 0] = torch.arange(60, device="cuda").half()
+    x[-10:] = NAN
+    x[5, 1] = 2.0
+    w, st = torch.zeros((e, 1, 8), dtype=F16, device="cuda"), status()
+    w[0], w[1] = 1.0, 3.0
+    out = torch.zeros((rows, 1), dtype=F16, device="cuda")
+    ops.moe_ovl_grouped_matmul(a=x, b=w, out=out, expert_counts=counts, status=st)
+    assert torch.equal(out[-70:-10, 0], 3 * torch.arange(60, device="cuda").half()) and not out[-10:].any() and out[5] == 2.0
+    dw = torch.empty((e, 8, 8), device="cuda")
+    ops.moe_ovl_grouped_matmul_backward(dy=x, x=x, dweight=dw, expert_counts=counts, status=st, workspace=workspace(e))
+    assert not st.any()
+    want = torch.zeros((e, 8, 8), device="cuda")
+    want[0, 1, 1], want[1, 0, 0] = 4.0, float((torch.arange(60) ** 2).sum())
+    assert torch.equal(dw, want)
+    del out
+    q, scale = torch.empty((rows, 8), dtype=F8, device="cuda"), torch.empty((rows, 1), device="cuda")
+    ops.moe_ovl_block_quant(x=x, q=q, scale=scale)
+    assert scale[5, 0] == torch.tensor(2.0) / 448 and scale[-11, 0] == torch.tensor(59.0) / 448 and bool(scale[-10:].isnan().all()) and not scale[6:1000].any()
+    assert q[-11].float().tolist() == [448.0] + [0.0] * 7
+
+
+@gpu
 def test_same_bits_every_time():
     t = Training(rows=5000, d=512, f=256, counts=(1700, 0, 3000, 300))
     first = t.run(t.x)
