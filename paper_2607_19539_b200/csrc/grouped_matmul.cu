@@ -23,9 +23,9 @@ constexpr int GM_BOX = STAGE_ROW * GM_K;     // bytes of 64 columns x 64 rows, K
 constexpr int GM_M_BYTES = TILE_CHANNELS * STAGE_ROW;
 
 // The tensor cores cut a sum off where they add to it, instead of rounding: its error grows with the number of steps, 8.4e-6 of a gradient over 6000 rows where 32-bit
-// sums are off by 9e-7.  For 32-bit outputs, and for gradients, whose sums have no end, a sum ends after 512 of K, and the finishing warps add the pieces up in registers; other
-// 16-bit outputs do not see the difference.
-constexpr int GM_SEGMENT = 512 / GM_K;
+// sums are off by 9e-7.  For 32-bit outputs a sum ends after 512 of K, and the finishing warps add the pieces up in registers.  16-bit outputs do not see the difference; gradients
+// in 16 bits, whose sums have no end, are cut after 4096, so that no wait for one is long.
+constexpr int segment_of(bool wide, bool gradient) { return (wide ? 512 : gradient ? 4096 : 0) / GM_K; }
 
 // What K runs along: rows of both operands; columns of the M side's; columns of both
 enum { FORM_ROWS = 0, FORM_MIXED = 1, FORM_COLUMNS = 2 };
@@ -56,10 +56,10 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
     static constexpr int SPLITS = SPLITS_;
     static constexpr int SHARE = TOKENS / CTAS;                              // of the N side, per CTA
     static constexpr int COLS = TOKENS < 32 ? 32 : TOKENS;                   // of tensor memory
-    static constexpr bool WIDE = sizeof(Out) == 4 || FORM == FORM_COLUMNS;   // in segments of K
+    static constexpr int SEGMENT = segment_of(sizeof(Out) == 4, FORM == FORM_COLUMNS);
     static constexpr int RING_BYTES = (SPLITS == 1 ? 200 : TOKENS > 64 ? 128 : 72) * 1024;
     static constexpr int PER_SM = SPLITS > 1 && TOKENS <= 64 ? 2 : 1;        // blocks: a cluster finds its place where there is room for another one
-    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, RING_BYTES, 2, COLS, 8, WIDE ? GM_SEGMENT : 0>;
+    using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, RING_BYTES, 2, COLS, 8, SEGMENT>;
     using Schedule = TileSchedule<CTAS * TILE_CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;                                    // FORM_COLUMNS: row0, rows are those of the output
     const GmP &p;
@@ -206,11 +206,11 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
         const bool in = (unsigned)ch < (unsigned)p.n, none = steps(t) == 0;
         if (none && p.accumulate && SPLITS == 1) return true;
         if (!none && !accs.wait(p, t.row0)) return false;
-        if constexpr (WIDE) {
+        if constexpr (SEGMENT > 0) {
             constexpr int MINE = TOKENS <= 32 ? 32 : TOKENS / 2;
             float acc[MINE] = {};
             if (half * 32 < COLS) {
-                for (int k = 0; k < steps(t); k += GM_SEGMENT) {
+                for (int k = 0; k < steps(t); k += SEGMENT) {
                     if (k > 0 && !accs.wait(p, t.row0)) return false;
                     const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 32);
 #pragma unroll
@@ -229,7 +229,7 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
 #pragma unroll
                 for (int c = 0; c < MINE; c += 32) store(t, &acc[c], half * 32 + c * 2, ch, in);
             } else {
-                for (int k = 0; k < steps(t); k += GM_SEGMENT) {
+                for (int k = 0; k < steps(t); k += SEGMENT) {
                     if (k > 0 && !accs.wait(p, t.row0)) return false;
                     accs.release();
                 }
