@@ -9,8 +9,6 @@
 // and the columns it adds up lie in one block of channels: one factor per thread and step.
 // Few rows (BlockFew): channels on the M side and the rows on the N side, whose size goes in steps of 16; the weights are streamed, and the factors,
 // one per row, are dealt out through shared memory.
-#include <cuda_fp8.h>
-
 #include <algorithm>
 
 #include "matmul_tiles.cuh"
@@ -176,8 +174,8 @@ template <int CTAS, int CHANNELS, int SPLITS_, typename Out> struct BlockRows {
 
 template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
     static constexpr int SPLITS = SPLITS_, TOKENS = TOKENS_, COLS = TOKENS < 32 ? 32 : TOKENS;
-    // Two groups of four warps take the steps in turn: what a warp does for one (a wait, its factors, 16 to 64 columns) takes longer than the weights of a step take to come.
-    static constexpr int RING_BYTES = (SPLITS > 1 ? 64 : TOKENS == 64 ? 56 : 80) * 1024;
+    // Two groups of four warps take the steps in turn: what a warp does for one (a wait, its factors, 16 or 32 columns) takes longer than the weights of a step take to come.
+    static constexpr int RING_BYTES = (SPLITS > 1 ? 64 : 80) * 1024;
     // Blocks: where the tiles are no multiple of the SMs, those that have two work on both at once (1 row, 28672 x 4096 22.7 -> 20.6 us; 40 rows of 32 experts, 2048 x 1408 12.4 -> 10.7).
     static constexpr int PER_SM = 2;
     using Shape = TileShape<1, BM_M_BYTES + TOKENS * STAGE_ROW, RING_BYTES, 256 / COLS, COLS, 8, 1, 1, 2>;
@@ -372,23 +370,27 @@ int launch_few(int splits, const BmP &p, const BmOperands &o, long long tiles, i
     }
 }
 
-// ctas 0: few rows, `tile` of them; else `tile` channels.  splits > 1: a cluster of that many CTAs per tile.  tiles: the most that any counts can give.
+// ctas 0: few rows, `tile` of them; else `tile` channels.  splits > 1: a cluster of that many CTAs per tile; tiles: the most that any counts can give.
 struct BmChoice { int ctas, tile, splits; long long tiles; };
 
+// The kernel goes by the tiles there are (with the experts' rows taken as even: the counts are on the device).  Measured, us:
+//   up to 32 rows on the N side: 32 rows, n = k = 4096 15.7, and 17.7 with the rows on the M side; 64 rows 16.8 and 14.3.  Experts' rows are never even, so from a mean of 5 on their tiles are
+//     taken twice as high: 256 rows of 16 experts, n = 8192, k = 2048 47.4 and 46.9;
+//   single CTAs or pairs: a pair's step of 256 x 256 takes about 0.54 us, a single one's of 128 x 128 0.35.  1024 rows, n = k = 4096 (two waves of the 148, one of the 74) 23.0 and 17.7; 512 rows 13.6 and 17.0;
+//     2048 rows of 16 experts, n = 8192, k = 2048 68 and 77, 4096 rows 113 and 97;
+//   few tiles share their steps (splits_of): 32 rows, n = k = 4096 15.7 alone, 7.6 shared, 128 rows 14.8 and 9.3.
 BmChoice choose(const BmP &p)
 {
     const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows - 1) / groups + 1;
-    if (per_group <= 64) {
-        const int few = per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64;
-        const long long most = (long long)p.channel_blocks * (p.counts ? p.rows / few + groups : (p.rows - 1) / few + 1);
-        const int splits = splits_of(most, 2, p.blocks, std::min(few, per_group), 280);
-        if (splits > 1) return {0, few, splits, most};
-        return {0, p.experts && per_group > 4 ? std::min(64, 2 * few) : few, 1, 0};
+    auto most = [&](int height) { return (long long)p.channel_blocks * (p.counts ? p.rows / height + groups : (p.rows - 1) / height + 1); };
+    if (per_group <= 32) {
+        const int few = per_group <= 16 ? 16 : 32, splits = splits_of(most(few), 2, p.blocks, std::min(few, per_group), 280);
+        if (splits > 1) return {0, few, splits, most(few)};
+        return {0, p.experts && per_group > 4 ? 32 : few, 1, 0};
     }
-    const long long pairs = (long long)((p.n - 1) / 256 + 1) * groups * ((per_group - 1) / 256 + 1);
-    if (pairs >= 37) return {2, 256, 1, 0};
-    const long long most = (long long)p.channel_blocks * (p.counts ? p.rows / TILE_CHANNELS + groups : (p.rows - 1) / TILE_CHANNELS + 1);
-    return {1, 128, splits_of(most, 1, p.blocks, TILE_CHANNELS, 350), most};
+    const long long singles = (long long)p.channel_blocks * groups * ((per_group - 1) / 128 + 1), pairs = (long long)((p.n - 1) / 256 + 1) * groups * ((per_group - 1) / 256 + 1);
+    if ((singles + 147) / 148 * 35 > (pairs + 73) / 74 * 54) return {2, 256, 1, 0};
+    return {1, 128, splits_of(most(TILE_CHANNELS), 1, p.blocks, std::min(TILE_CHANNELS, per_group), 350), most(TILE_CHANNELS)};
 }
 
 }  // namespace
@@ -434,10 +436,6 @@ extern "C" int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *a)
             default: return launch_rows<1, 128, 8, Out>(p, o, c.tiles, a->device, stream);
             }
         }
-        switch (c.tile) {
-        case 16: return launch_few<16, Out>(c.splits, p, o, c.tiles, a->device, stream);
-        case 32: return launch_few<32, Out>(c.splits, p, o, c.tiles, a->device, stream);
-        default: return launch_few<64, Out>(c.splits, p, o, c.tiles, a->device, stream);
-        }
+        return c.tile == 16 ? launch_few<16, Out>(c.splits, p, o, c.tiles, a->device, stream) : launch_few<32, Out>(c.splits, p, o, c.tiles, a->device, stream);
     });
 }

@@ -8,8 +8,7 @@
 // down their columns, which the instruction's descriptors tell apart, so no matrix is transposed in memory.
 // The gradient of the weights sums over an expert's rows, which end anywhere inside a step of 64 rows.  What follows them belongs to the next expert
 // and has to count as 0 on both sides (0 * NaN is NaN), so each expert's operands are read through tensor maps of its own, cut off at its last
-// row; a small kernel in front writes them into the
-// workspace.
+// row; a small kernel in front writes them into the workspace.
 #include <algorithm>
 
 #include "matmul_tiles.cuh"
@@ -328,23 +327,29 @@ int launch_split(int splits, const GmP &p, const GmMaps &maps, long long tiles, 
 // splits > 1: a cluster of that many CTAs per tile; tiles: the most that any counts can give.
 struct GmChoice { int ctas, tokens, splits; long long tiles; };
 
+// The kernel goes by the tiles there are (with the experts' rows taken as even: the counts are on the device).  Measured, us:
+//   few tiles of up to 128 rows share their steps (splits_of); of 256 rows, n = k = 4096, that would be 15.6 against 14.0 in pairs;
+//   up to 16 rows single CTAs, whose start is shorter: 1 row, n = 28672, k = 4096 39.7 against 43.3 in pairs of 128 rows, n = k = 128 2.8 and 3.3; and for more rows where
+//     their tiles fit half of the SMs: 100 rows, n = k = 512 4.0 and 4.9.  Experts' rows are never even, so from a mean of 5 on they go in pairs: 80 rows of 16 experts, n = 8192, k = 2048
+//     83.5 and 80.4, 96 of 64, n = 1408 45.1 and 43.3;
+//   pairs take 128 or 256 rows, whose tiles cost about 8 : 13: 512 rows, n = k = 4096 (one wave of the 74 pairs each) 15.0 and 23.8, 2048 rows (four waves, two) 48.4 and 45.7; 4096 rows of 16
+//     experts, n = 8192, k = 2048 149 and 129.
 GmChoice choose(const GmP &p)
 {
     const int groups = p.experts ? std::min(p.experts, p.rows) : 1, per_group = (p.rows - 1) / groups + 1;
     auto tiles = [&](int channels, int tokens) {
         return (long long)((p.n - 1) / channels + 1) * groups * ((per_group - 1) / tokens + 1);
     };
-    const int few = per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64;
-    // what any counts can give
-    const long long most = (long long)((p.n - 1) / TILE_CHANNELS + 1) * (p.counts ? p.rows / few + groups : (p.rows - 1) / few + 1);
-    const int splits = splits_of(most, 2, (p.k - 1) / GM_K + 1, std::min(few, per_group), 150);
-    if (splits > 1) return {1, few, splits, most};
-    if (p.experts && per_group > 4 && per_group <= 64) return {1, per_group <= 16 ? 32 : 64, 1, 0};
-    if (per_group <= 16) return {1, 16, 1, 0};
-    if (per_group <= 32 || tiles(TILE_CHANNELS, 32) <= 148) return {1, 32, 1, 0};
-    if (per_group <= 64 || tiles(TILE_CHANNELS, 64) <= 148) return {1, 64, 1, 0};
+    if (per_group <= 128) {
+        const int few = per_group <= 16 ? 16 : per_group <= 32 ? 32 : 64;
+        const long long most = (long long)((p.n - 1) / TILE_CHANNELS + 1) * (p.counts ? p.rows / few + groups : (p.rows - 1) / few + 1);
+        const int splits = splits_of(most, 2, (p.k - 1) / GM_K + 1, std::min(few, per_group), 150);
+        if (splits > 1) return {1, few, splits, most};
+        if ((per_group <= 16 && !(p.experts && per_group > 4)) || tiles(TILE_CHANNELS, 16) <= 74) return {1, 16, 1, 0};
+        return {2, 128, 1, 0};
+    }
     const long long w128 = (tiles(2 * TILE_CHANNELS, 128) + 73) / 74, w256 = (tiles(2 * TILE_CHANNELS, 256) + 73) / 74;
-    return {2, per_group <= 128 || 8 * w128 <= 13 * w256 ? 128 : 256, 1, 0};
+    return {2, 8 * w128 <= 13 * w256 ? 128 : 256, 1, 0};
 }
 
 uint32_t instruction_types(int dtype) { return dtype == MOE_OVL_BF16 ? (1u << 7) | (1u << 10) : 0u; }
@@ -398,13 +403,7 @@ extern "C" int moe_ovl_grouped_matmul(const moe_ovl_grouped_matmul_args *a)
                 default: return launch_split<64, F, Out>(c.splits, p, maps, c.tiles, a->device, stream);
                 }
             }
-            if (c.ctas == 1) {
-                switch (c.tokens) {
-                case 16: return launch<1, 16, F, 1, Out>(p, maps, 0, a->device, stream);
-                case 32: return launch<1, 32, F, 1, Out>(p, maps, 0, a->device, stream);
-                default: return launch<1, 64, F, 1, Out>(p, maps, 0, a->device, stream);
-                }
-            }
+            if (c.ctas == 1) return launch<1, 16, F, 1, Out>(p, maps, 0, a->device, stream);
             return c.tokens == 128 ? launch<2, 128, F, 1, Out>(p, maps, 0, a->device, stream) : launch<2, 256, F, 1, Out>(p, maps, 0, a->device, stream);
         };
         return a->transposed ? form(std::integral_constant<int, FORM_MIXED>()) : form(std::integral_constant<int, FORM_ROWS>());
