@@ -128,8 +128,21 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
                 acquire_map(f.m);
                 acquire_map(f.n);
             }
+            if (SPLITS == 1 && p.accumulate) ask_for_output(t);
         }
         return f;
+    }
+    // What a tile is added to comes into L2 when its operands begin to come.
+    __device__ __forceinline__ void ask_for_output(const Tile &t) const
+    {
+        constexpr int LINE = 128 / (int)sizeof(Out), LINES = TILE_CHANNELS / LINE;
+        const int ch0 = t.channel0 + rank * TILE_CHANNELS;
+        const Out *out = static_cast<const Out *>(p.out) + t.expert * p.out_far + (long long)t.row0 * p.out_stride;
+        for (int i = threadIdx.x & 31; i < t.rows * LINES; i += 32) {
+            const int ch = ch0 + i % LINES * LINE;
+            if (ch < p.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(out + (long long)(i / LINES) * p.out_stride + ch));
+        }
+        __syncwarp();
     }
     __device__ __forceinline__ static void acquire_map(const CUtensorMap *map)
     {
@@ -185,11 +198,7 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
         }
         Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)(t.row0 + c) * p.out_stride + ch;
         const int left = in ? t.rows - c : 0;
-        if (FORM == FORM_COLUMNS && p.accumulate) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < left) out[j * p.out_stride] = from_f32<Out>(sum[j] + to_f32(out[j * p.out_stride]));
-        } else if (left >= 32) {
+        if (left >= 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j, out += p.out_stride) *out = from_f32<Out>(sum[j]);
         } else {
@@ -204,13 +213,18 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
         const int ch = t.channel0 + rank * TILE_CHANNELS + quarter * 32 + lane;
         const bool in = (unsigned)ch < (unsigned)p.n, none = steps(t) == 0;
         if (none && p.accumulate && SPLITS == 1) return true;
-        if (!none && !accs.wait(p, t.row0)) return false;
         if constexpr (SEGMENT > 0) {
             constexpr int MINE = TOKENS <= 32 ? 32 : TOKENS / 2;
             float acc[MINE] = {};
             if (half * 32 < COLS) {
+                if (FORM == FORM_COLUMNS && SPLITS == 1 && p.accumulate) {
+                    // what is added to comes while the first segment is multiplied.  Lanes and rows outside the output read its last ones, so that no load waits behind a branch
+                    const Out *old = static_cast<const Out *>(p.out) + t.expert * p.out_far + (long long)t.row0 * p.out_stride + min(ch, p.n - 1);
+#pragma unroll
+                    for (int c = 0; c < MINE; ++c) acc[c] = to_f32(old[(long long)min(half * 32 + c % 32 + c / 32 * 64, t.rows - 1) * p.out_stride]);
+                }
                 for (int k = 0; k < steps(t); k += SEGMENT) {
-                    if (k > 0 && !accs.wait(p, t.row0)) return false;
+                    if (!accs.wait(p, t.row0)) return false;
                     const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 32);
 #pragma unroll
                     for (int c = 0; c < MINE; c += 8) {
@@ -229,22 +243,24 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
                 for (int c = 0; c < MINE; c += 32) store(t, &acc[c], half * 32 + c * 2, ch, in);
             } else {
                 for (int k = 0; k < steps(t); k += SEGMENT) {
-                    if (k > 0 && !accs.wait(p, t.row0)) return false;
+                    if (!accs.wait(p, t.row0)) return false;
                     accs.release();
                 }
             }
             return true;
-        }
-        for (int c = half * 32; c < t.rows; c += 64) {
-            uint32_t v[32] = {};
-            if (!none) {
-                tmem_ld32(accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
-                tmem_ld_wait();
+        } else {
+            if (!none && !accs.wait(p, t.row0)) return false;
+            for (int c = half * 32; c < t.rows; c += 64) {
+                uint32_t v[32] = {};
+                if (!none) {
+                    tmem_ld32(accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
+                    tmem_ld_wait();
+                }
+                store(t, reinterpret_cast<const float *>(v), c, ch, in);
             }
-            store(t, reinterpret_cast<const float *>(v), c, ch, in);
+            if (!none) accs.release();
+            return true;
         }
-        if (!none) accs.release();
-        return true;
     }
 };
 

@@ -471,12 +471,16 @@ def _tensor_list(where, name, tensors, device):
     for t in tensors:
         if t.get_device() != device:
             _refuse(where, f"every tensor of {name} has to be on cuda:{device}, not {t.device}")
-        if not _dense(t):
+        if not t.is_contiguous() and not _dense(t):
             _refuse(where, f"the tensors of {name} have to fill the memory that they span (strides {t.stride()} of {list(t.shape)})")
-    at = [t.data_ptr() for t in tensors if t.numel()]
-    if len(set(at)) != len(at):
+    kinds = [DTYPES.get(t.dtype, -1) for t in tensors]
+    if -1 in kinds:
+        _refuse(where, f"every tensor of {name} has to be bfloat16, float16 or float32, not {tensors[kinds.index(-1)].dtype}")
+    at, sizes = [t.data_ptr() for t in tensors], [t.numel() for t in tensors]
+    real = at if 0 not in sizes else [a for a, n in zip(at, sizes) if n]
+    if len(set(real)) != len(real):
         _refuse(where, f"a tensor is twice in {name}")
-    return (array("Q", [t.data_ptr() for t in tensors]), array("q", [t.numel() for t in tensors]), array("i", [_dtype(where, f"every tensor of {name}", t) for t in tensors]))
+    return array("Q", at), array("q", sizes), array("i", kinds)
 
 
 def moe_ovl_grad_norm_workspace_bytes(num_tensors: int) -> int:
@@ -508,7 +512,8 @@ def moe_ovl_clip_grads(*, grads, norm, max_norm: float, eps: float = 1e-6, out=N
         if len(out) != len(grads):
             _refuse(where, f"out has {len(out)} tensors, grads {len(grads)}")
         for g, o in zip(grads, out):
-            if o.shape != g.shape or o.dtype is not g.dtype or any(s != z for s, z, n in zip(o.stride(), g.stride(), g.shape) if n != 1):
+            if o.dtype is not g.dtype or o.shape != g.shape or (not (g.is_contiguous() and o.is_contiguous()) and
+                                                               any(s != z for s, z, n in zip(o.stride(), g.stride(), g.shape) if n != 1)):
                 _refuse(where, f"a tensor of out has to be {list(g.shape)} {g.dtype} with strides {g.stride()}, not {list(o.shape)} {o.dtype} with {o.stride()}")
         to = _tensor_list(where, "out", out, dev)[0]
     _vector(where, "norm", norm, (1,), torch.float32, dev)
