@@ -536,7 +536,7 @@ int moe_ovl_quant_matmul(const moe_ovl_quant_matmul_args *args);
 /* ---------------------------------------------------------------------------------------------------------------
  * Operators for training experts, and for experts whose weights and activations are held in 8-bit floats.  What is said of the operators
  * above holds for them too, `status` and its bounded waits included.  Here the operands of a product have to begin on 16 bytes, and so have their
- * rows and matrices (MOE_OVL_ERR_UNSUPPORTED otherwise); their sizes are free. */
+ * rows and matrices (MOE_OVL_ERR_UNSUPPORTED otherwise); their sizes are free.  Outputs must not overlap inputs, unless it is said that they may be the same. */
 
 #define MOE_OVL_MAX_GROUPS 1024    /* most experts of a product */
 #define MOE_OVL_MAX_MATMUL 16777216 /* largest n and k of a product, and longest row of the quantiser */
@@ -647,9 +647,9 @@ int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *args);
 /* Norm of a list of gradients, and clipping by it.  Two calls: where the gradients are spread over ranks, their norms are combined in between.
  *   moe_ovl_grad_norm:   norm = sqrt(sum over all values of all tensors of g^2), in 64 bits beyond a thread's share, in a fixed order
  *   moe_ovl_clip_grads:  out = g * min(1, max_norm / (norm + eps)), in 32 bits and rounded once
- * A norm that is infinite makes the factor 0, one that is NaN makes it NaN.  The tensors of a list have any of the types each, lie densely in
- * memory (in whatever order) and must not overlap; the lists are HOST arrays, read before the call returns.  Without `out` the gradients are clipped where
- * they lie, and not written at all when the factor is 1. */
+ * A norm that is infinite makes the factor 0, one that is NaN makes it NaN; where norm + eps is 0 it is 1.  The tensors of a list have any of the types each, lie densely in
+ * memory (in whatever order) and must not overlap each other; the lists are HOST arrays, read before the call returns.  Without `out` (or where it names the same
+ * tensors) the gradients are clipped where they lie; without it they are not written at all when the factor is 1. */
 typedef struct {
     uint32_t struct_size;
     int32_t device;

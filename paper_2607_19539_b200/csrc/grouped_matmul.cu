@@ -264,6 +264,9 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
     }
 };
 
+// Bound by the tensor cores where there are many rows (49152 of 8 experts, 2816 x 2048: 347-377 us, 1.50-1.63 PFLOP/s, the tensor pipe at work for 96 % of the time; the gradient of those weights
+// 382-414 us, 92 %), by the weights' way from HBM where there are few (96 rows of 16 experts, 8192 x 2048: 81 us, 6.7 TB/s).  Pairs of CTAs and tiles of 256 x 256 halve what a CTA needs out of L2
+// for an operation; accumulators are double buffered, so that a tile is stored while the next one is multiplied.
 template <int CTAS, int TOKENS, int FORM, int SPLITS, typename Out>
 __global__ void __launch_bounds__(GmWork<CTAS, TOKENS, FORM, SPLITS, Out>::Shape::THREADS, GmWork<CTAS, TOKENS, FORM, SPLITS, Out>::PER_SM)
 grouped_matmul_kernel(const __grid_constant__ CUtensorMap map_m, const __grid_constant__ CUtensorMap map_n, const __grid_constant__ GmP p)
