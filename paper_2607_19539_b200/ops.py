@@ -16,6 +16,7 @@ import ctypes as C
 import struct
 import warnings
 from array import array
+from operator import attrgetter
 
 import torch
 
@@ -304,15 +305,15 @@ def moe_ovl_quant_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=N
 
 def _matrices(where, name, t, shape, dtype, device):
     """Strides between rows and between matrices of a tensor of three dimensions (or of two: one matrix) whose columns lie next to each other."""
-    if tuple(t.shape) not in (shape, shape[1:] if shape[0] == 1 else shape) or t.dtype is not dtype or t.get_device() != device:
-        _refuse(where, f"{name} has to be {list(shape)} {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
     depth, rows, cols = shape
-    s0, s1 = t.stride()[-2:]
-    far = t.stride(0) if t.dim() == 3 else 0
+    if (t.shape != shape and (depth != 1 or t.shape != shape[1:])) or t.dtype is not dtype or t.get_device() != device:
+        _refuse(where, f"{name} has to be {list(shape)} {dtype} on cuda:{device}, not {list(t.shape)} {t.dtype} on {t.device}")
+    strides = t.stride()
+    far, s0, s1 = strides if len(strides) == 3 else (0, *strides)
     if (s1 != 1 and cols > 1) or s0 < 0:
-        _refuse(where, f"{name}: the columns of a row have to lie next to each other (strides {t.stride()})")
+        _refuse(where, f"{name}: the columns of a row have to lie next to each other (strides {strides})")
     if rows > 1 and s0 < cols:
-        _refuse(where, f"{name}: rows must not overlap (strides {t.stride()})")
+        _refuse(where, f"{name}: rows must not overlap (strides {strides})")
     return s0, far
 
 
@@ -343,10 +344,6 @@ def _workspace(where, workspace, device) -> int:
     return workspace.numel() * workspace.element_size()
 
 
-def _needs_gradient(*tensors) -> bool:
-    return any(t.requires_grad for t in tensors)
-
-
 def moe_ovl_grouped_matmul(*, a, b, out, status, expert_counts=None, transposed: bool = False, wait_timeout_us: int = 0, flags: int = 0, stream=None) -> None:
     """out = a @ b^T in 16-bit floats, rows of a grouped by expert: b [experts, n, k], or with `transposed` a @ b, b [experts, k, n].  Without expert_counts
     b is one matrix.  The gradient of a is moe_ovl_grouped_matmul(a=dout, b=b, transposed=not transposed)."""
@@ -365,7 +362,7 @@ def moe_ovl_grouped_matmul(*, a, b, out, status, expert_counts=None, transposed:
     sb, far = _matrices(where, "b", b, (max(experts, 1), k, n) if transposed else (max(experts, 1), n, k), a.dtype, dev)
     so = _matrix(where, "out", out, (rows, n), out.dtype, dev)
     _vector(where, "status", status, (4,), torch.int32, dev)
-    if _needs_gradient(a, b):
+    if a.requires_grad or b.requires_grad:
         _gradient_lost(where)
     _call(where, B.load().moe_ovl_grouped_matmul, GroupedMatmulArgs, dev, rows, n, k, experts, DTYPES[a.dtype], DTYPES[out.dtype], 1 if transposed else 0,
           wait_timeout_us, flags, a.data_ptr(), b.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, far, so,
@@ -447,7 +444,7 @@ def moe_ovl_block_matmul(*, a, a_scale, b, b_scale, out, status, expert_counts=N
     _vector(where, "a_scale", a_scale, (rows, blocks), torch.float32, dev)
     _vector(where, "b_scale", b_scale, (*b.shape[:-2], -(-n // BLOCK), blocks), torch.float32, dev)
     _vector(where, "status", status, (4,), torch.int32, dev)
-    if _needs_gradient(a_scale, b_scale):
+    if a_scale.requires_grad or b_scale.requires_grad:
         _gradient_lost(where)
     _call(where, B.load().moe_ovl_block_matmul, BlockMatmulArgs, dev, rows, n, k, experts, dt, wait_timeout_us, flags, a.data_ptr(), a_scale.data_ptr(),
           b.data_ptr(), b_scale.data_ptr(), _at(expert_counts), out.data_ptr(), status.data_ptr(), sa, sb, far, so,
@@ -466,21 +463,28 @@ def _dense(t) -> bool:
     return True
 
 
+_dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
+
+
 def _tensor_list(where, name, tensors, device):
-    """Addresses, sizes and types of a list of tensors as arrays."""
-    for t in tensors:
-        if t.get_device() != device:
-            _refuse(where, f"every tensor of {name} has to be on cuda:{device}, not {t.device}")
-        if not t.is_contiguous() and not _dense(t):
-            _refuse(where, f"the tensors of {name} have to fill the memory that they span (strides {t.stride()} of {list(t.shape)})")
-    kinds = [DTYPES.get(t.dtype, -1) for t in tensors]
+    """Addresses, sizes and types of a list of tensors as arrays, and whether all are contiguous."""
+    if not all(isinstance(t, torch.Tensor) for t in tensors):
+        _refuse(where, f"{name} has to be a list of tensors")
+    if any(d != device for d in map(torch.Tensor.get_device, tensors)):
+        _refuse(where, f"every tensor of {name} has to be on cuda:{device}, not {[str(t.device) for t in tensors if t.get_device() != device][0]}")
+    contiguous = all(map(torch.Tensor.is_contiguous, tensors))
+    if not contiguous:
+        for t in tensors:
+            if not _dense(t):
+                _refuse(where, f"the tensors of {name} have to fill the memory that they span (strides {t.stride()} of {list(t.shape)})")
+    kinds = [DTYPES.get(t, -1) for t in map(_dtype_of, tensors)]
     if -1 in kinds:
         _refuse(where, f"every tensor of {name} has to be bfloat16, float16 or float32, not {tensors[kinds.index(-1)].dtype}")
-    at, sizes = [t.data_ptr() for t in tensors], [t.numel() for t in tensors]
+    at, sizes = list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors))
     real = at if 0 not in sizes else [a for a, n in zip(at, sizes) if n]
     if len(set(real)) != len(real):
         _refuse(where, f"a tensor is twice in {name}")
-    return array("Q", at), array("q", sizes), array("i", kinds)
+    return array("Q", at), array("q", sizes), array("i", kinds), contiguous
 
 
 def moe_ovl_grad_norm_workspace_bytes(num_tensors: int) -> int:
@@ -494,7 +498,7 @@ def moe_ovl_grad_norm(*, grads, norm, workspace, stream=None) -> None:
     bytes.  Ranks that hold different gradients combine their norms (the root of the sum of squares) before moe_ovl_clip_grads."""
     where = "moe_ovl_grad_norm"
     dev, grads = _device(where, norm), list(grads)
-    at, sizes, dtypes = _tensor_list(where, "grads", grads, dev)
+    at, sizes, dtypes, _ = _tensor_list(where, "grads", grads, dev)
     _vector(where, "norm", norm, (1,), torch.float32, dev)
     nbytes = _workspace(where, workspace, dev)
     _call(where, B.load().moe_ovl_grad_norm, GradsArgs, dev, len(grads), 0, _host(at), 0, _host(sizes), _host(dtypes), norm.data_ptr(), 0.0, 0.0,
@@ -505,17 +509,17 @@ def moe_ovl_clip_grads(*, grads, norm, max_norm: float, eps: float = 1e-6, out=N
     """Every value of a list of tensors times min(1, max_norm / (norm[0] + eps)), where it lies or into the tensors of `out`."""
     where = "moe_ovl_clip_grads"
     dev, grads = _device(where, norm), list(grads)
-    at, sizes, dtypes = _tensor_list(where, "grads", grads, dev)
+    at, sizes, dtypes, plain = _tensor_list(where, "grads", grads, dev)
     to = None
     if out is not None:
         out = list(out)
         if len(out) != len(grads):
             _refuse(where, f"out has {len(out)} tensors, grads {len(grads)}")
-        for g, o in zip(grads, out):
-            if o.dtype is not g.dtype or o.shape != g.shape or (not (g.is_contiguous() and o.is_contiguous()) and
-                                                               any(s != z for s, z, n in zip(o.stride(), g.stride(), g.shape) if n != 1)):
-                _refuse(where, f"a tensor of out has to be {list(g.shape)} {g.dtype} with strides {g.stride()}, not {list(o.shape)} {o.dtype} with {o.stride()}")
-        to = _tensor_list(where, "out", out, dev)[0]
+        to, _, kinds, as_plain = _tensor_list(where, "out", out, dev)
+        if not plain or not as_plain or kinds != dtypes or list(map(_shape_of, out)) != list(map(_shape_of, grads)):
+            for g, o in zip(grads, out):
+                if o.shape != g.shape or o.dtype is not g.dtype or any(s != z for s, z, n in zip(o.stride(), g.stride(), g.shape) if n != 1):
+                    _refuse(where, f"a tensor of out has to be {list(g.shape)} {g.dtype} with strides {g.stride()}, not {list(o.shape)} {o.dtype} with {o.stride()}")
     _vector(where, "norm", norm, (1,), torch.float32, dev)
     _call(where, B.load().moe_ovl_clip_grads, GradsArgs, dev, len(grads), 0, _host(at), 0 if to is None else _host(to), _host(sizes), _host(dtypes), norm.data_ptr(),
           max_norm, eps, 0, 0, _stream(dev, stream, *grads, norm, *(out or ())))
