@@ -571,6 +571,9 @@ def test_clip_grads_of_many_sizes(max_norm):
     sizes = [0, 1, 2, 3, 7, 8, 9, 31, 255, 256, 257, 8191, 8192, 8193, 16384, 100001]
     check_clip([normal(g, (n,), (BF16, F16, F32)[i % 3], 0.1) for i, n in enumerate(sizes * 3)], max_norm)
     check_clip([normal(g, (5,), F32)], max_norm)
+    for n in (131072, 131073, 262144, 262145):      # eight and sixteen chunks, and one value more
+        check_clip([normal(g, (n,), F32)], max_norm)
+        check_clip([normal(g, (n - 40000,), BF16), normal(g, (40000,), F16)], max_norm)
     check_clip([normal(g, (3, 0), F32)], max_norm)
     check_clip([], max_norm)
 
