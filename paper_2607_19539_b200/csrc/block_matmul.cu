@@ -49,12 +49,12 @@ template <int CTAS> __device__ __forceinline__ void multiply_step(uint32_t on, u
 
 template <int CTAS, int CHANNELS, int SPLITS_, typename Out> struct BlockRows {
     static constexpr int SPLITS = SPLITS_, PITCH = TILE_CHANNELS + 4, TOKENS = CTAS * TILE_CHANNELS, PARTS = CHANNELS / 128, SHARE = 128 / CTAS, COLS = 128 * PARTS / 2;     // SHARE: of a part's channels, per CTA
-    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 168 * 1024, 4, 128, 8, 1, PARTS>;
-    static constexpr int STAGE_OUT = 32 * 128;
+    using Shape = TileShape<CTAS, BM_M_BYTES + PARTS * SHARE * STAGE_ROW, 136 * 1024, 4, 128, 8, 1, PARTS>;
+    static constexpr int STAGE_OUT = 2 * 32 * 128;        // per finishing warp
     using Schedule = TileSchedule<CHANNELS, TOKENS>;
     using Tile = typename Schedule::Tile;
     const BmP &p;
-    const CUtensorMap *map_a, *map_b;
+    const CUtensorMap *map_a, *map_b, *map_out;
     int *tile_start, *row_start;
     uint8_t *stage;                          // [finishing warps][STAGE_OUT]
     float *part;                             // SPLITS > 1: [TOKENS][PITCH], where the operands were: a part is written when the last of them has been read
@@ -121,23 +121,30 @@ template <int CTAS, int CHANNELS, int SPLITS_, typename Out> struct BlockRows {
             for (int i = 0; i < COLS; i += 4) *reinterpret_cast<float4 *>(own + i) = make_float4(acc[i / 2].x, acc[i / 2].y, acc[i / 2 + 1].x, acc[i / 2 + 1].y);
             return true;
         }
-        store(t, acc, rank * TILE_CHANNELS + quarter * 32, ch0, stage + warp * STAGE_OUT, lane);
+        if (t.rows > rank * TILE_CHANNELS + quarter * 32) store(t, acc, rank * TILE_CHANNELS + quarter * 32, ch0, stage + warp * STAGE_OUT, lane);
         return true;
     }
     __device__ __forceinline__ void join(const Tile &t) const
     {
         join_parts<SPLITS, PITCH>(part, static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride, p.out_stride, t.channel0, p.n, t.rows, split, false);
     }
-    // A warp's 32 rows of COLS sums: 128 bytes of each row go through shared memory, 16 bytes of them in turn, so that a store's lanes lie next to each other.  A thread's own
-    // row straight from its registers is 32 lines of memory per store, which took as long as nine steps of K.
+    // A warp's 32 rows of COLS sums, 128 bytes of each row at a time: they are laid down in shared memory as a tile copy wants them, which takes them away while the warp goes on
+    // with its next tile (7919 x 28672 x 4096 757 -> 731 us against the warp's own stores).  Rows that end inside the 32 (the next expert's follow) and outputs that a tile copy does not take are stored
+    // by the warp, neighbours by neighbouring lanes.  A thread's own row straight from its registers would be 32 lines of memory per store, which took as long as nine steps of K.
     __device__ __forceinline__ void store(const Tile &t, const float2 (&acc)[COLS / 2], int row0, int ch0, uint8_t *own, int lane) const
     {
         constexpr int VEC = 16 / (int)sizeof(Out), WIDE = 128 / (int)sizeof(Out);
         const int rows = min(t.rows - row0, 32);
-        Out *out = static_cast<Out *>(p.out) + (long long)(t.row0 + row0) * p.out_stride + ch0;
 #pragma unroll
         for (int c0 = 0; c0 < COLS; c0 += WIDE) {
             const int left = p.n - ch0 - c0;
+            uint8_t *buffer = own + c0 / WIDE % 2 * (STAGE_OUT / 2);
+            // of the two buffers' copies the older one is this buffer's; where a row is one piece there is one buffer
+            if (lane == 0) {
+                if (COLS > WIDE) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 Pack<Out, VEC> pack;
@@ -146,27 +153,34 @@ template <int CTAS, int CHANNELS, int SPLITS_, typename Out> struct BlockRows {
                     const int c = c0 + i * VEC + j;
                     pack.v[j] = from_f32<Out>(c & 1 ? acc[c / 2].y : acc[c / 2].x);
                 }
-                *reinterpret_cast<uint4 *>(own + lane * 128 + (i ^ (lane & 7)) * 16) = *reinterpret_cast<const uint4 *>(&pack);
+                *reinterpret_cast<uint4 *>(buffer + lane * 128 + (i ^ (lane & 7)) * 16) = *reinterpret_cast<const uint4 *>(&pack);
             }
-            __syncwarp();
-            if (p.wide && left >= WIDE) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = i * 4 + lane / 8;
-                    const uint4 piece = *reinterpret_cast<const uint4 *>(own + row * 128 + ((lane ^ row) & 7) * 16);
-                    if (row < rows) *reinterpret_cast<uint4 *>(out + (long long)row * p.out_stride + c0 + lane % 8 * VEC) = piece;
-                }
+            if (p.wide && rows == 32 && left >= WIDE) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0)
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map_out), "r"(ch0 + c0), "r"(t.row0 + row0), "r"(smem_u32(buffer))
+                                 : "memory");
             } else {
+                __syncwarp();
+                Out *out = static_cast<Out *>(p.out) + (long long)(t.row0 + row0) * p.out_stride + ch0 + c0;
                 for (int row = 0; row < rows; ++row)
 #pragma unroll
                     for (int c = 0; c < WIDE; c += 32) {
                         const int col = c + lane;
-                        const Out v = *reinterpret_cast<const Out *>(own + row * 128 + ((col / VEC ^ row) & 7) * 16 + col % VEC * (int)sizeof(Out));
-                        if (col < left) out[(long long)row * p.out_stride + c0 + col] = v;
+                        const Out v = *reinterpret_cast<const Out *>(buffer + row * 128 + ((col / VEC ^ row) & 7) * 16 + col % VEC * (int)sizeof(Out));
+                        if (col < left) out[(long long)row * p.out_stride + col] = v;
                     }
             }
+            // a group for each buffer, empty or not
+            if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             __syncwarp();
         }
+    }
+    __device__ __forceinline__ void close(int lane) const
+    {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
 };
 
@@ -293,26 +307,27 @@ template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
         }
         return true;
     }
+    __device__ __forceinline__ void close(int) const {}
     __device__ __forceinline__ void join(const Tile &t) const
     {
         join_parts<SPLITS>(part, static_cast<Out *>(p.out) + (long long)t.row0 * p.out_stride, p.out_stride, t.channel0, p.n, t.rows, split, false);
     }
 };
 
-// Bound by the finishing warps' steps: about 700 clocks for a wait, 128 columns read and added, and giving them back, where the tensor cores need 512 (7919 x 28672 x 4096: 748-778 us, 2.4-2.5 PFLOP/s, the
+// Bound by the finishing warps' steps: about 700 clocks for a wait, 128 columns read and added, and giving them back, where the tensor cores need 512 (7919 x 28672 x 4096: 731-750 us, 2.5 PFLOP/s, the
 // tensor pipe at work for 70 % of the time).  A pair's tile of 256 x 256 takes all tensor memory for two steps, as four accumulators of 128 columns, each with four warps that add it up; wider ones would be
 // given back later, more warps have too few registers for their sums.
 template <int CTAS, int CHANNELS, int SPLITS, typename Out>
 __global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, SPLITS, Out>::Shape::THREADS, 1)
-block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ BmP p)
+block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ BmP p)
 {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ int s_tile_start[1025], s_row_start[1025];
     using Work = BlockRows<CTAS, CHANNELS, SPLITS, Out>;
     static_assert(SPLITS == 1 || (CTAS == 1 && CHANNELS == TILE_CHANNELS && Work::TOKENS * Work::PITCH * 4 <= Work::Shape::STAGES * Work::Shape::STAGE_BYTES), "room for the parts");
-    float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    __shared__ __align__(16) uint8_t s_out[Work::Shape::FINISHERS * Work::STAGE_OUT];
-    run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_out, part, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    float *part = reinterpret_cast<float *>(ring);
+    run_tiles(Work{p, &map_a, &map_b, &map_out, s_tile_start, s_row_start, ring + Work::Shape::STAGES * Work::Shape::STAGE_BYTES, part, {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
 // Bound by the weights' way from HBM (1 x 28672 x 4096: 20.5-21.5 us, 5.5-5.7 TB/s); with few tiles by their steps one after the other, which clusters share then (1 x 512 x 4096: 4.8 us, 9.1 unshared).
@@ -327,7 +342,7 @@ block_matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_
     run_tiles(Work{p, &map_a, &map_b, s_tile_start, s_row_start, s_factors, reinterpret_cast<float *>(smem_raw + Work::Shape::SMEM), {s_tile_start, s_row_start, p.row_tiles}}, p, smem_raw);
 }
 
-struct BmOperands { const void *a, *b; long long a_stride, b_stride, b_far; };
+struct BmOperands { const void *a, *b; long long a_stride, b_stride, b_far, out_bytes; };       // out_bytes: between rows of the output
 
 bool encode_operands(const BmP &p, const BmOperands &o, int a_rows, int b_rows, CUtensorMap *a, CUtensorMap *b)
 {
@@ -338,15 +353,20 @@ bool encode_operands(const BmP &p, const BmOperands &o, int a_rows, int b_rows, 
 template <int CTAS, int CHANNELS, int SPLITS, typename Out>
 int launch_rows(BmP p, const BmOperands &o, long long tiles, int device, cudaStream_t stream)
 {
-    using Shape = typename BlockRows<CTAS, CHANNELS, SPLITS, Out>::Shape;
-    CUtensorMap a, b;
+    using Work = BlockRows<CTAS, CHANNELS, SPLITS, Out>;
+    using Shape = typename Work::Shape;
+    constexpr int SMEM = Shape::SMEM + Shape::FINISHERS * Work::STAGE_OUT;
+    CUtensorMap a, b, out;
     p.row_tiles = (p.n - 1) / CHANNELS + 1;
     if (!encode_operands(p, o, TILE_CHANNELS, 128 / CTAS, &a, &b)) return MOE_OVL_ERR_CUDA;
+    const CUtensorMapDataType type = sizeof(Out) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;       // moved, not looked at
+    if (!p.wide) out = a;                    // not used
+    else if (!encode_tiles(&out, type, sizeof(Out), p.out, p.n, p.rows, o.out_bytes, 0, 0, 32)) return MOE_OVL_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
     const auto kernel = block_matmul_kernel<CTAS, CHANNELS, SPLITS, Out>;
-    if (!allow_smem(kernel, Shape::SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
+    if (!allow_smem(kernel, SMEM, device, allowed)) return MOE_OVL_ERR_CUDA;
     const unsigned blocks = SPLITS > 1 ? (unsigned)(tiles * SPLITS) : (unsigned)(sm_count(device) / CTAS * CTAS);
-    return launch_behind(kernel, blocks, dim3(Shape::THREADS), Shape::SMEM, CTAS * SPLITS, stream, a, b, p);
+    return launch_behind(kernel, blocks, dim3(Shape::THREADS), SMEM, CTAS * SPLITS, stream, a, b, out, p);
 }
 
 template <int TOKENS, int SPLITS, typename Out>
@@ -426,7 +446,8 @@ extern "C" int moe_ovl_block_matmul(const moe_ovl_block_matmul_args *a)
     p.timeout_ns = a->wait_timeout_us > 0 ? a->wait_timeout_us * 1000ull : TILE_TIMEOUT_NS;
     p.no_loads = (a->flags & MOE_OVL_MATMUL_TEST_NO_LOADS) != 0;
     p.wide = aligned(a->out, 16) && (a->rows == 1 || a->out_stride * es % 16 == 0);
-    const BmOperands o = {a->a, a->b, sa, sb, far};
+    // a single row's stride is never used: one that holds the row
+    const BmOperands o = {a->a, a->b, sa, sb, far, a->rows > 1 ? a->out_stride * es : ((long long)a->n * es + 15) / 16 * 16};
     const BmChoice c = choose(p);
     const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
     return with_dtype(a->out_dtype, [&](auto t) {

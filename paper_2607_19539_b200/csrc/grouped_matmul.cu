@@ -181,6 +181,7 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
         for (int i = 0; i < GM_K / 16; ++i)
             umma_f16<CTAS>(on, d, dm + (uint64_t)(i * STEP_M), dn + (uint64_t)(i * STEP_N), idesc, first && i == 0 ? 0u : 1u);
     }
+    __device__ __forceinline__ void close(int) const {}
     __device__ __forceinline__ void join(const Tile &t) const
     {
         Out *out = static_cast<Out *>(p.out) + (FORM == FORM_COLUMNS ? t.expert * p.out_far : 0) + (long long)t.row0 * p.out_stride;

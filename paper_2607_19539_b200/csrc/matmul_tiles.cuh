@@ -300,7 +300,7 @@ template <typename Shape> __device__ void await_copies(uint32_t bar_full, uint32
 // elected lane issues: copies and matrix instructions take their operands from uniform registers.
 // `Work` says what a tile is: begin(lane) fills the tables, by one warp; total(); at(t); steps(tile) of K, 0 for a tile that nothing is loaded for;
 // load(on, tile's operands, shared address, barrier, step); instruction(tile); multiply(on, accumulator, stage's address / 16, instruction, first, part);
-// finish(tile, accumulators, warp, lane), false when a wait gave up.  With SPLITS > 1 a cluster of that many CTAs works on one tile, each on its `split` of the steps; finish()
+// finish(tile, accumulators, warp, lane), false when a wait gave up; close(lane), when a finishing warp has done its last tile.  With SPLITS > 1 a cluster of that many CTAs works on one tile, each on its `split` of the steps; finish()
 // leaves the part in shared memory and join(tile), called by all threads when the parts of all are there, adds them up.
 template <typename Work, typename P> __device__ __forceinline__ void run_tiles(Work work, const P &p, uint8_t *smem_raw)
 {
@@ -355,6 +355,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
         for (long long t = first; t < total; t += step)
             if (!work.finish(work.at(t), accs, p, warp - Shape::CONTROL, lane)) break;         // a warp leaves the loop as one
         __syncwarp();
+        work.close(lane);
     } else if (warp == 0) {
         int stage = 0;
         uint32_t phase = 0, issued = 0;
