@@ -315,7 +315,7 @@ template <int TOKENS_, int SPLITS_, typename Out> struct BlockFew {
 };
 
 // Bound by the finishing warps' steps: about 700 clocks for a wait, 128 columns read and added, and giving them back, where the tensor cores need 512 (7919 x 28672 x 4096: 731-750 us, 2.5 PFLOP/s, the
-// tensor pipe at work for 70 % of the time).  A pair's tile of 256 x 256 takes all tensor memory for two steps, as four accumulators of 128 columns, each with four warps that add it up; wider ones would be
+// tensor pipe at work for 74 % of the time).  A pair's tile of 256 x 256 takes all tensor memory for two steps, as four accumulators of 128 columns, each with four warps that add it up; wider ones would be
 // given back later, more warps have too few registers for their sums.
 template <int CTAS, int CHANNELS, int SPLITS, typename Out>
 __global__ void __launch_bounds__(BlockRows<CTAS, CHANNELS, SPLITS, Out>::Shape::THREADS, 1)
