@@ -14,6 +14,7 @@ from __future__ import annotations
 from dataclasses import dataclass
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B, ops
 
@@ -138,14 +139,16 @@ class ExpertProduct(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, rows, weight, counts, status):
-        ctx.save_for_backward(rows, weight, counts, status)
+        ctx.save_for_backward(rows, weight, counts)
+        ctx.status = status             # not saved: the caller may clear it in between
         out = torch.zeros((rows.shape[0], weight.shape[1]), dtype=rows.dtype, device=rows.device)
         ops.moe_ovl_grouped_matmul(a=rows, b=weight, out=out, expert_counts=counts, status=status)
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
-        rows, weight, counts, status = ctx.saved_tensors
+        (rows, weight, counts), status = ctx.saved_tensors, ctx.status
         dout = dout.contiguous()
         drows = dweight = None
         if ctx.needs_input_grad[0]:
@@ -160,7 +163,8 @@ class ExpertProduct(torch.autograd.Function):
 
 def expert_ffn(rows, w1, w2, counts, status):
     """Rows grouped by expert ([n, d], counts [experts] int32) through their experts, for training: w1 [experts, 2F, d] (gate rows, then up rows), w2 [experts, d, F].
-    `status`: 4 int32 that the caller clears once; look at it after a synchronize of your own."""
+    d and F have to be multiples of 8.  `status`: 4 int32 that the caller clears once; look at it after a synchronize of your own.  Gradients of gradients are refused.  Where a
+    step is captured into a graph, no eager step's result may live any more: torch would tie the leaves' gradients to that step's stream, which no capture can wait for."""
     counts = counts.clone()             # the router's buffer may hold the next batch's by the time of the backward pass
     gate, up = ExpertProduct.apply(rows, w1, counts, status).float().chunk(2, dim=1)
     hidden = (torch.nn.functional.silu(gate) * up).to(rows.dtype)
@@ -168,7 +172,8 @@ def expert_ffn(rows, w1, w2, counts, status):
 
 
 def clip_gradients(parameters, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
-    """Scales the gradients of the parameters that have one, so that their norm is max_norm at most; returns the norm before, on the device."""
+    """Scales the gradients of the parameters (or of one) that have one, so that their norm is max_norm at most; returns the norm before, on the device."""
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else parameters
     grads = [p.grad for p in parameters if p.grad is not None]
     if not grads:
         return torch.zeros(1)

@@ -91,3 +91,92 @@ def test_expert_product_asks_for_the_gradients_that_are_wanted():
 
 def test_clip_gradients_without_any():
     assert L.clip_gradients([torch.nn.Parameter(torch.zeros(3))], 1.0).tolist() == [0.0]
+
+
+def test_clip_gradients_of_one_parameter():
+    class Seen(Exception):
+        pass
+
+    def norm_of(n):
+        raise Seen(n)
+
+    p, real = torch.nn.Parameter(torch.zeros(3, 5)), ops.moe_ovl_grad_norm_workspace_bytes
+    p.grad = torch.ones(3, 5)
+    ops.moe_ovl_grad_norm_workspace_bytes = norm_of
+    try:
+        for parameters in (p, [p], iter([p])):
+            with pytest.raises(Seen) as e:
+                L.clip_gradients(parameters, 1.0)
+            assert e.value.args == (1,)                            # one gradient, not one per row
+    finally:
+        ops.moe_ovl_grad_norm_workspace_bytes = real
+
+
+def training_leaves(n, d, f, experts, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *s, scale=1.0: (torch.randn(s, generator=g, device="cuda") * scale).to(torch.bfloat16)  # noqa: E731
+    leaves = [normal(n, d).requires_grad_(), normal(experts, 2 * f, d, scale=d ** -0.5).requires_grad_(), normal(experts, d, f, scale=f ** -0.5).requires_grad_()]
+    return leaves, normal(n, d), torch.zeros(4, dtype=torch.int32, device="cuda")
+
+
+@gpu
+def test_status_may_be_cleared_between_the_passes():
+    leaves, dout, status = training_leaves(40, 64, 32, 2, 5)
+    counts = torch.tensor([15, 25], dtype=torch.int32, device="cuda")
+    out = L.expert_ffn(*leaves, counts, status)
+    want = torch.autograd.grad(out, leaves, dout, retain_graph=True)
+    status.zero_()
+    counts.fill_(7)                                                # the next batch's: the gradients are of this one
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, leaves, dout), want))
+
+
+@gpu
+def test_gradients_of_gradients_are_refused():
+    leaves, dout, status = training_leaves(40, 64, 32, 2, 6)
+    counts = torch.tensor([15, 25], dtype=torch.int32, device="cuda")
+    for i in range(2):
+        got, = torch.autograd.grad(L.ExpertProduct.apply(*leaves[:2], counts, status).float().square().sum(), leaves[i], create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            got.float().sum().backward()
+
+
+@gpu
+def test_training_without_rows():
+    leaves, dout, status = training_leaves(0, 64, 32, 2, 7)
+    out = L.expert_ffn(*leaves, torch.zeros(2, dtype=torch.int32, device="cuda"), status)
+    out.backward(dout)
+    assert out.shape == (0, 64) and leaves[0].grad.shape == (0, 64) and not leaves[1].grad.any() and not leaves[2].grad.any() and not status.any()
+    assert float(L.clip_gradients(leaves, 1.0)) == 0.0 and not leaves[1].grad.any()
+
+
+@gpu
+def test_training_step_in_a_graph():
+    leaves, dout, status = training_leaves(230, 136, 72, 4, 8)
+    counts = torch.tensor([50, 0, 130, 20], dtype=torch.int32, device="cuda")
+
+    def step():
+        for t in leaves:
+            t.grad = None
+        out = L.expert_ffn(*leaves, counts, status)
+        out.backward(dout)
+        return out.detach(), L.clip_gradients(leaves, 0.25)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    kept = [*captured, *(t.grad for t in leaves)]
+    for now in ([50, 0, 130, 20], [0, 229, 0, 1], [0, 0, 0, 0]):
+        counts.copy_(torch.tensor(now, dtype=torch.int32))
+        for t in kept:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in kept]
+        eager = step()
+        assert all(torch.equal(a, b) for a, b in zip(got, [*eager, *(t.grad for t in leaves)])) and not status.any()
