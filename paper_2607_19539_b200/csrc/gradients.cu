@@ -79,14 +79,15 @@ template <typename T> __device__ __forceinline__ double chunk_sum(const T *x, lo
     constexpr int VEC = 16 / sizeof(T);
     const int head = head_of(x + begin);
     float2 sum = make_float2(0.0f, 0.0f);
-    unsigned bits = 0;                       // of anything but zeros
+    unsigned bits = 0;                       // of anything but zeros, of either sign
+    constexpr unsigned UNSIGNED = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
     constexpr int AT_ONCE = 4;               // 8: 146 us instead of 121 for 0.84 GB
     for_values<VEC, AT_ONCE>(begin, end, head, [&](long long i, int n) {
         const Packs<T, AT_ONCE> a = load_packs<AT_ONCE>(x + i, n);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const uint4 raw = *reinterpret_cast<const uint4 *>(&a.pack[k]);
-            bits |= raw.x | raw.y | raw.z | raw.w;
+            bits |= (raw.x | raw.y | raw.z | raw.w) & UNSIGNED;
 #pragma unroll
             for (int e = 0; e < VEC; e += 2) {
                 const float2 v = to_f32x2(&a.pack[k].v[e]);
@@ -96,13 +97,19 @@ template <typename T> __device__ __forceinline__ double chunk_sum(const T *x, lo
     }, [&](long long i) {
         const float v = to_f32(x[i]);
         sum.x = fmaf(v, v, sum.x);
-        bits |= __float_as_uint(v);
+        bits |= __float_as_uint(v) & 0x7fffffffu;
     });
     const float both_sums = sum.x + sum.y;
     if (both_sums >= 1e-30f && both_sums <= 1e38f) return (double)both_sums;
     if (bits == 0) return 0.0;
+    // the same values once more: each thread decides for itself, so its second sum has to be over its own share
     double wide = 0.0;
-    for_each(begin, end, [&](long long i) { wide += (double)to_f32(x[i]) * (double)to_f32(x[i]); });
+    auto add = [&](float v) { wide += (double)v * (double)v; };
+    for_values<VEC, 1>(begin, end, head, [&](long long i, int) {
+        const Pack<T, VEC> a = load_pack<T, VEC>(x + i);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) add(to_f32(a.v[e]));
+    }, [&](long long i) { add(to_f32(x[i])); });
     return wide;
 }
 

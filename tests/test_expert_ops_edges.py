@@ -1,0 +1,75 @@
+"""Edges of the operators for training experts and for experts in 8-bit floats: values that do not fit among their neighbours, the longest sums, gates far below
+zero, gradients that begin anywhere.  Tolerances are derived at each test; U is half a unit in the last place."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2607_19539_b200 import ops  # noqa: E402
+
+from tests.test_expert_ops import F8, INF, NAN, norm_of, status  # noqa: E402
+from tests.test_ops import BF16, F16, F32, U, close, gen, normal  # noqa: E402
+
+gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ norm of gradients
+
+# 32 positive terms in 32 bits and one more addition, the rest in 64, then a root (half of that) and a rounding
+NORM_OFF = (33 / 2 + 1) * 2.0 ** -24 * 1.01
+
+
+def gradient_lists(g, t):
+    """The tensor in lists of one block's run, of a cluster, of two kernels, and of more tensors than a short list holds."""
+    yield [t]
+    yield [normal(g, (40000,), F32), t]
+    yield [normal(g, (300001,), BF16), t, normal(g, (7,), F16)]
+    yield [normal(g, (i,), F32) for i in range(40)] + [t]
+
+
+def norm64(grads):
+    return math.sqrt(sum(float((t.double() ** 2).sum()) for t in grads))
+
+
+def starting(g, n, dtype, shift):
+    """n normal values that begin `shift` values behind a boundary of 16 bytes."""
+    return normal(g, (n + shift,), dtype)[shift:]
+
+
+@gpu
+@pytest.mark.parametrize("value", [NAN, INF, -INF, 1e20, 1e-25])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_grad_norm_of_one_value_unlike_the_others(dtype, value):
+    """One NaN, infinity, large or small value among ordinary ones: only the thread whose share it is leaves the range of 32 bits.  The clipped gradients are what the norm says."""
+    if dtype is F16 and abs(value) == 1e20:
+        value = 65504.0
+    g = gen(3)
+    for n in (2048, 16384, 100001):
+        for shift in (0, 1):
+            base = starting(g, n, dtype, shift)
+            for at in (0, 1, 5, 9, 257, 1000, n // 2, n - 1):
+                t = base.clone() if shift == 0 else torch.cat([base[:1], base])[1:]
+                t[at] = value
+                for grads in gradient_lists(g, t):
+                    norm, want = norm_of(grads), norm64(grads)
+                    if math.isfinite(want):
+                        assert abs(float(norm) - want) <= NORM_OFF * want, (n, shift, at, len(grads), float(norm), want)
+                        continue
+                    assert math.isnan(want) == math.isnan(float(norm)) and (math.isnan(want) or float(norm) == INF), (n, shift, at, len(grads), float(norm))
+                    out = [torch.full_like(x, 7.5) for x in grads]
+                    ops.moe_ovl_clip_grads(grads=grads, norm=norm, max_norm=1.0, out=out)
+                    for x, o in zip(grads, out):
+                        assert bool(o.isnan().all()) if math.isnan(want) else torch.equal(o.isnan(), x.isinf()) and not o.nan_to_num().any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,small,large", [(BF16, 1e-17, 1e-2), (F32, 1e-17, 1e-2), (F32, 1e-30, 1.0), (BF16, 1.0, 1e20), (F32, 1.0, 1e20), (BF16, -0.0, 1.0), (F16, -0.0, 1.0), (F32, -0.0, 1.0)])
+def test_grad_norm_of_columns_unlike_each_other(dtype, small, large):
+    """Whole columns of another magnitude, as experts and channels that are hardly used have: some threads' shares leave the range of 32 bits, their neighbours' do not."""
+    for rows, cols in ((16, 1024), (8, 2048), (100, 264), (33, 1001)):
+        for first in (cols // 2, 8, cols - 3):
+            t = torch.full((rows, cols), large, dtype=dtype, device="cuda")
+            t[:, :first] = small
+            for grads in gradient_lists(gen(5), t):
+                norm, want = float(norm_of(grads)), norm64(grads)
+                assert abs(norm - want) <= NORM_OFF * want, (rows, cols, first, len(grads), norm, want)
