@@ -22,9 +22,9 @@ constexpr int GM_BOX = STAGE_ROW * GM_K;     // bytes of 64 columns x 64 rows, K
 constexpr int GM_M_BYTES = TILE_CHANNELS * STAGE_ROW;
 
 // The tensor cores cut a sum off where they add to it, instead of rounding: its error grows with the number of steps, 8.4e-6 of a gradient over 6000 rows where 32-bit
-// sums are off by 9e-7.  For 32-bit outputs a sum ends after 512 of K, and the finishing warps add the pieces up in registers.  16-bit outputs do not see the difference; gradients
-// in 16 bits, whose sums have no end, are cut after 4096, so that no wait for one is long.
-constexpr int segment_of(bool wide, bool gradient) { return (wide ? 512 : gradient ? 4096 : 0) / GM_K; }
+// sums are off by 9e-7, and 1.4e-2 of 2^21 terms of one sign, many times the rounding of 16 bits.  So a sum ends after 512 of K for 32-bit outputs and after 4096 for 16-bit ones, and the finishing
+// warps add the pieces up in registers; a gradient's sums have no other end, so that no wait for one is long.
+constexpr int segment_of(bool wide) { return (wide ? 512 : 4096) / GM_K; }
 
 // What K runs along: rows of both operands; columns of the M side's; columns of both
 enum { FORM_ROWS = 0, FORM_MIXED = 1, FORM_COLUMNS = 2 };
@@ -55,7 +55,9 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
     static constexpr int SPLITS = SPLITS_;
     static constexpr int SHARE = TOKENS / CTAS;                              // of the N side, per CTA
     static constexpr int COLS = TOKENS < 32 ? 32 : TOKENS;                   // of tensor memory
-    static constexpr int SEGMENT = segment_of(sizeof(Out) == 4, FORM == FORM_COLUMNS);
+    static constexpr int SEGMENT = segment_of(sizeof(Out) == 4);
+    // Wide tiles whose sum is one piece go out as they are read, 32 columns at a time (96 rows of 16 experts, 8192 x 2048: 80.3 us, through the sums' registers 80.9)
+    static constexpr bool ONE_PIECE = FORM != FORM_COLUMNS && sizeof(Out) == 2 && TOKENS >= 128;
     static constexpr int RING_BYTES = (SPLITS == 1 ? 200 : TOKENS > 64 ? 128 : 72) * 1024;
     static constexpr int PER_SM = SPLITS > 1 && TOKENS <= 64 ? 2 : 1;        // blocks: a cluster finds its place where there is room for another one
     using Shape = TileShape<CTAS, GM_M_BYTES + SHARE * STAGE_ROW, RING_BYTES, 2, COLS, 8, SEGMENT>;
@@ -214,42 +216,7 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
         const int ch = t.channel0 + rank * TILE_CHANNELS + quarter * 32 + lane;
         const bool in = (unsigned)ch < (unsigned)p.n, none = steps(t) == 0;
         if (none && p.accumulate && SPLITS == 1) return true;
-        if constexpr (SEGMENT > 0) {
-            constexpr int MINE = TOKENS <= 32 ? 32 : TOKENS / 2;
-            float acc[MINE] = {};
-            if (half * 32 < COLS) {
-                if (FORM == FORM_COLUMNS && SPLITS == 1 && p.accumulate) {
-                    // what is added to comes while the first segment is multiplied.  Lanes and rows outside the output read its last ones, so that no load waits behind a branch
-                    const Out *old = static_cast<const Out *>(p.out) + t.expert * p.out_far + (long long)t.row0 * p.out_stride + min(ch, p.n - 1);
-#pragma unroll
-                    for (int c = 0; c < MINE; ++c) acc[c] = to_f32(old[(long long)min(half * 32 + c % 32 + c / 32 * 64, t.rows - 1) * p.out_stride]);
-                }
-                for (int k = 0; k < steps(t); k += SEGMENT) {
-                    if (!accs.wait(p, t.row0)) return false;
-                    const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 32);
-#pragma unroll
-                    for (int c = 0; c < MINE; c += 8) {
-                        uint32_t v[8];
-                        tmem_ld8(from + c % 32 + c / 32 * 64, v);
-                        tmem_ld_wait(v);
-#pragma unroll
-                        for (int j = 0; j < 8; j += 2) {
-                            const float2 sum = add2(make_float2(acc[c + j], acc[c + j + 1]), make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])));
-                            acc[c + j] = sum.x, acc[c + j + 1] = sum.y;
-                        }
-                    }
-                    accs.release();
-                }
-#pragma unroll
-                for (int c = 0; c < MINE; c += 32) store(t, &acc[c], half * 32 + c * 2, ch, in);
-            } else {
-                for (int k = 0; k < steps(t); k += SEGMENT) {
-                    if (!accs.wait(p, t.row0)) return false;
-                    accs.release();
-                }
-            }
-            return true;
-        } else {
+        if (ONE_PIECE && steps(t) <= SEGMENT) {
             if (!none && !accs.wait(p, t.row0)) return false;
             for (int c = half * 32; c < t.rows; c += 64) {
                 uint32_t v[32] = {};
@@ -262,6 +229,40 @@ template <int CTAS, int TOKENS, int FORM, int SPLITS_, typename Out> struct GmWo
             if (!none) accs.release();
             return true;
         }
+        constexpr int MINE = TOKENS <= 32 ? 32 : TOKENS / 2;
+        float acc[MINE] = {};
+        if (half * 32 < COLS) {
+            if (FORM == FORM_COLUMNS && SPLITS == 1 && p.accumulate) {
+                // what is added to comes while the first segment is multiplied.  Lanes and rows outside the output read its last ones, so that no load waits behind a branch
+                const Out *old = static_cast<const Out *>(p.out) + t.expert * p.out_far + (long long)t.row0 * p.out_stride + min(ch, p.n - 1);
+#pragma unroll
+                for (int c = 0; c < MINE; ++c) acc[c] = to_f32(old[(long long)min(half * 32 + c % 32 + c / 32 * 64, t.rows - 1) * p.out_stride]);
+            }
+            for (int k = 0; k < steps(t); k += SEGMENT) {
+                if (!accs.wait(p, t.row0)) return false;
+                const uint32_t from = accs.columns() + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 32);
+#pragma unroll
+                for (int c = 0; c < MINE; c += 8) {
+                    uint32_t v[8];
+                    tmem_ld8(from + c % 32 + c / 32 * 64, v);
+                    tmem_ld_wait(v);
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float2 sum = add2(make_float2(acc[c + j], acc[c + j + 1]), make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])));
+                        acc[c + j] = sum.x, acc[c + j + 1] = sum.y;
+                    }
+                }
+                accs.release();
+            }
+#pragma unroll
+            for (int c = 0; c < MINE; c += 32) store(t, &acc[c], half * 32 + c * 2, ch, in);
+        } else {
+            for (int k = 0; k < steps(t); k += SEGMENT) {
+                if (!accs.wait(p, t.row0)) return false;
+                accs.release();
+            }
+        }
+        return true;
     }
 };
 

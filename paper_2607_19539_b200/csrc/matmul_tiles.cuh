@@ -232,14 +232,13 @@ __device__ __forceinline__ float4 ld_shared_cluster_f32x4(uint32_t addr)
 // ------------------------------------------------------------------ persistent tiles in three roles
 
 // CTAS CTAs (one, or a pair that shares every matrix instruction) work on a tile; STAGE_BYTES are one CTA's operands of one step of K.  ACCS accumulators of
-// ACC_COLS columns of tensor memory go round.  SEGMENT 0: a tile has one accumulator, for all of its steps.  Otherwise every SEGMENT steps have PARTS of them, side by side
-// in the tile, which a share of the finishing warps each adds up.  TURNS > 1: that many groups of them take the accumulators in turn.
+// ACC_COLS columns of tensor memory go round.  Every SEGMENT steps have PARTS of them, side by side in the tile, which a share of the finishing warps each adds up.  TURNS > 1: that many groups of them take the accumulators in turn.
 template <int CTAS_, int STAGE_BYTES_, int SMEM_BYTES_, int ACCS_, int ACC_COLS_, int FINISHERS_, int SEGMENT_, int PARTS_ = 1, int TURNS_ = 1> struct TileShape {
     static constexpr int CTAS = CTAS_, STAGE_BYTES = STAGE_BYTES_, ACCS = ACCS_, ACC_COLS = ACC_COLS_, FINISHERS = FINISHERS_, SEGMENT = SEGMENT_, PARTS = PARTS_, GROUPS = PARTS_ * TURNS_;
     static constexpr int STAGES = SMEM_BYTES_ / STAGE_BYTES_;
     static constexpr int CONTROL = 2, THREADS = 32 * (CONTROL + FINISHERS);      // the load and the matrix warp
     static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
-    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32 && ACCS % GROUPS == 0 && FINISHERS % GROUPS == 0, "tensor memory");
+    static_assert(ACCS * ACC_COLS <= 512 && ACC_COLS >= 32 && ACCS % GROUPS == 0 && FINISHERS % GROUPS == 0 && SEGMENT > 0, "tensor memory");
 };
 
 // Arrival of a reader of tensor memory, on a barrier that may be the peer CTA's.  What it gives back has been read (tcgen05.wait, and the fence
@@ -393,8 +392,7 @@ template <typename Work, typename P> __device__ __forceinline__ void run_tiles(W
                 const uint32_t idesc = uniform(work.instruction(tile));
                 const int steps = uniform(work.steps(tile));
                 for (int k = 0; k < steps; ++k) {
-                    const bool begins = Shape::SEGMENT ? k % max(Shape::SEGMENT, 1) == 0 : k == 0;
-                    const bool ends = k == steps - 1 || (Shape::SEGMENT && k % max(Shape::SEGMENT, 1) == Shape::SEGMENT - 1);
+                    const bool begins = k % Shape::SEGMENT == 0, ends = k == steps - 1 || k % Shape::SEGMENT == Shape::SEGMENT - 1;
                     ok = warp_wait(bar_full + 8 * stage, phase, p, SITE_TILE_FULL, k);
                     if (!ok) break;
 #pragma unroll

@@ -73,3 +73,25 @@ def test_grad_norm_of_columns_unlike_each_other(dtype, small, large):
             for grads in gradient_lists(gen(5), t):
                 norm, want = float(norm_of(grads)), norm64(grads)
                 assert abs(norm - want) <= NORM_OFF * want, (rows, cols, first, len(grads), norm, want)
+
+
+# ------------------------------------------------------------------------------------------------ 16-bit products
+
+@gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("m", [1, 20, 64, 129, 300])
+def test_longest_sums_in_16_bits(m, dtype, transposed):
+    """The longest k, all terms of one sign.  A matrix instruction cuts its 16 products and the sum so far to 24 bits of the largest, 33 * 2^-23 of the magnitudes at most; a sum ends after 4096
+    of k, 256 instructions, and the up to 4096 of them are added in 32 bits, 2^-24 each (and as many parts as a cluster has CTAs): 1.25e-3, and the output's rounding."""
+    k, n, period = 1 << 24, 8, 1 << 20
+    g = gen(m)
+    pattern = lambda rows: (0.5 + 0.5 * torch.rand((rows, period), generator=g, device="cuda")).mul_(2.0 ** -6).to(dtype)  # noqa: E731
+    pa, pb = pattern(m), pattern(n)
+    a, b = pa.repeat(1, k // period), pb.repeat(1, k // period)
+    b = b.t().contiguous() if transposed else b
+    out, st = torch.empty((m, n), dtype=dtype, device="cuda"), status()
+    ops.moe_ovl_grouped_matmul(a=a, b=b, out=out, transposed=transposed, status=st)
+    want = sum(pa[:, c:c + 65536].double() @ pb[:, c:c + 65536].double().t() for c in range(0, period, 65536)) * (k // period)
+    assert not st.any()
+    close(out, want, ((256 * 33 * 2.0 ** -23) + (4096 + 8) * 2.0 ** -24 + U[dtype]) * want)
