@@ -220,7 +220,7 @@ clip_grads_kernel(const __grid_constant__ TensorList<N> list, const float *norm,
     after_previous();
     may_follow();
     const float whole = *norm + eps, ratio = __fdiv_rn(max_norm, whole);
-    const float factor = ratio >= 1.0f || whole == 0.0f ? 1.0f : ratio;          // NaN stays
+    const float factor = isinf(whole) ? 0.0f : ratio >= 1.0f || whole == 0.0f ? 1.0f : ratio;        // infinity by infinity too; NaN stays
     if (in_place && factor == 1.0f) return;
     const unsigned first = (unsigned)((unsigned long long)list.chunks * blockIdx.x / gridDim.x);
     const unsigned last = (unsigned)((unsigned long long)list.chunks * (blockIdx.x + 1) / gridDim.x);

@@ -75,6 +75,18 @@ def test_grad_norm_of_columns_unlike_each_other(dtype, small, large):
                 assert abs(norm - want) <= NORM_OFF * want, (rows, cols, first, len(grads), norm, want)
 
 
+@gpu
+def test_clip_grads_without_a_limit():
+    """max_norm may be infinite: the gradients stay as they are, but for a norm that is infinite (factor 0) or NaN."""
+    for values, want in (([1.0, 2.0], [1.0, 2.0]), ([1.0, INF, -2.0], [0.0, NAN, 0.0]), ([1.0, NAN], [NAN, NAN]), ([0.0, 0.0], [0.0, 0.0])):
+        for eps in (0.0, 1e-6):
+            t, w = torch.tensor(values, device="cuda"), torch.tensor(want, device="cuda")
+            norm, out = norm_of([t]), torch.full_like(t, 7.5)
+            ops.moe_ovl_clip_grads(grads=[t], norm=norm, max_norm=INF, eps=eps, out=[out])
+            ops.moe_ovl_clip_grads(grads=[t], norm=norm, max_norm=INF, eps=eps)
+            assert all(torch.equal(o.isnan(), w.isnan()) and torch.equal(o.nan_to_num(), w.nan_to_num()) for o in (out, t))
+
+
 # ------------------------------------------------------------------------------------------------ 16-bit products
 
 @gpu
