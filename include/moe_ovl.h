@@ -601,6 +601,7 @@ int moe_ovl_grouped_matmul_backward(const moe_ovl_grouped_matmul_backward_args *
  *   v = x, or with `gated` g / (1 + exp(-g)) * u of x [rows, 2k] = g | u;
  *   scale = max|v| / 448 of the block, q = v * 448 / max|v| divided in 32 bits, then to the nearest of e4m3, ties to even: v ~ q * scale.
  * A block is 128 neighbours of a row (activations), or with `tiles` 128 x 128 values of a matrix (weights); the last ones may be shorter.
+ * The gated v is formed in 32 bits, to a relative 2^-20 + |g| 2^-23 wherever it is 2^-100 or more; -inf as a gate gives NaN.
  * A block whose max|v| is below 2^-100 gives zeros; one that holds a NaN or an infinity gives a NaN scale and q = 0. */
 typedef struct {
     uint32_t struct_size;

@@ -8,6 +8,7 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "opcommon.cuh"
 
@@ -122,17 +123,67 @@ template <typename T, int VEC> __device__ __forceinline__ void floats(const Pack
     for (int e = 0; e < VEC; e += 2) v[e / 2] = VEC == 1 ? make_float2(to_f32(a.v[0]), 0.0f) : to_f32x2(&a.v[e]);
 }
 
+// Below this gate() loses what a large value leaves of itself: 1 / (1 + exp(-g)) ends as a normal number at -87.3.  Of f16 no value is large enough to matter.
+constexpr float BQ_FAR = -86.0f;
+// The smallest of a pack's gates and `low`.
+template <typename T, int VEC> __device__ __forceinline__ T lowest(T low, const Pack<T, VEC> &g)
+{
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        if constexpr (std::is_same<T, float>::value) low = fminf(low, g.v[e]);
+        else low = __hmin(low, g.v[e]);
+    }
+    return low;
+}
+template <int VEC> __device__ __forceinline__ __nv_bfloat162 lowest(__nv_bfloat162 low, const Pack<__nv_bfloat16, VEC> &g)
+{
+#pragma unroll
+    for (int e = 0; e < VEC; e += 2) low = __hmin2(low, *reinterpret_cast<const __nv_bfloat162 *>(&g.v[e]));
+    return low;
+}
+
 constexpr int BQ_THREADS = 256, BQ_RESIDENT = 8;     // blocks per SM
 
 // Blocks of 1 x 128.  LANES lanes work on a block, PER packs of VEC values each; a group of lanes has the loads of AHEAD neighbouring blocks under way.
 template <typename T, int VEC, bool GATED> struct BqShape {
     static constexpr int LANES = VEC == 1 ? 32 : BQ_BLOCK / VEC / 2, PER = BQ_BLOCK / VEC / LANES, AHEAD = VEC == 1 ? 1 : 2;
 };
-// Bound by HBM (8192 x 14336, bf16: 58 us, 6.1 TB/s; with the gate, whose instructions come next, 98-101 us, 5.9 TB/s).  Eight lanes for a block of 128 values, not sixteen with a pack each: the maximum's shuffles and what a block
+// What a gate leaves of a value, from far below zero too: there 1 + exp(-g) is exp(-g), and g * 2^(126 + g / ln 2) * u * 2^-126 is taken in an order in which nothing overflows and nothing that a block keeps
+// falls below the normal numbers.
+__device__ __forceinline__ float any_gate(float g, float u)
+{
+    if (!(g < BQ_FAR)) return gate(make_float2(g, g), make_float2(u, u)).x;
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(g, 1.4426950408889634f, 126.0f)));
+    return g * e * (u * 5.4210108624275222e-20f) * 2.1684043449710089e-19f;      // 2^-64, 2^-62
+}
+// Gated blocks that have such gates, once more and value by value: `count` of them from `u` on, by LANES lanes.  Out of the way of the others, which would pay for it with registers (8192 x 14336, bf16: 130 us
+// with the choice inside their loop, 98 with a vote at its end and 98 without any).
+template <typename T, int LANES> __device__ __noinline__ void far_blocks(const BqP &p, unsigned u, int count, int lane)
+{
+    __syncwarp();                            // behind what the lanes have stored
+    for (; count > 0; --count, ++u) {
+        const unsigned row = p.blocks == 1 ? u : (unsigned)__umul64hi(p.magic, u);
+        const int col = (int)(u - row * (unsigned)p.blocks) * BQ_BLOCK, end = u < p.units ? min(col + BQ_BLOCK, p.k) : 0;
+        const T *x = static_cast<const T *>(p.x) + (long long)row * p.x_stride;
+        float most = 0.0f;
+        for (int c = col + lane; c < end; c += LANES) most = max_abs(most, any_gate(to_f32(x[c]), to_f32(x[c + p.k])));
+        for (int o = LANES / 2; o > 0; o >>= 1) most = max_abs(most, __shfl_xor_sync(0xffffffffu, most, o));
+        if (end == 0) continue;
+        const Divisor d = divisor_of(most);
+        if (lane == 0) p.scale[u] = d.scale;
+        uint8_t *q = p.q + (long long)row * p.q_stride;
+        for (int c = col + lane; c < end; c += LANES) {
+            const float v = any_gate(to_f32(x[c]), to_f32(x[c + p.k]));
+            q[c] = d.none ? 0 : (uint8_t)rounded(divided<T>(make_float2(v, 0.0f), d));
+        }
+    }
+}
+// Bound by HBM (8192 x 14336, bf16: 58 us, 6.1 TB/s; with the gate, whose instructions come next, 98-101 us, 5.9 TB/s; f16 94, f32 159).  Eight lanes for a block of 128 values, not sixteen with a pack each: the maximum's shuffles and what a block
 // costs besides its values weigh half as much (96 -> 58 us).  Rows that begin anywhere go element by element (8192 x 14335: 153 us).
 template <typename T, int VEC, bool GATED, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
-block_quant_kernel(const BqP p)
+block_quant_kernel(const __grid_constant__ BqP p)
 {
     using Shape = BqShape<T, VEC, GATED>;
     constexpr int LANES = Shape::LANES, PER = Shape::PER, AHEAD = Shape::AHEAD, HALF = (VEC + 1) / 2;
@@ -145,6 +196,9 @@ block_quant_kernel(const BqP p)
     for (unsigned done = 0; first + done < p.units; done += step) {
         const unsigned u = own + done, row0 = p.blocks == 1 ? u : (unsigned)__umul64hi(p.magic, u), block0 = u - row0 * (unsigned)p.blocks;
         Pack<T, VEC> a[AHEAD][PER], b[GATED ? AHEAD : 1][PER];
+        constexpr bool FAR = GATED && !std::is_same<T, __half>::value;
+        using Low = std::conditional_t<std::is_same<T, __nv_bfloat16>::value && VEC % 2 == 0, __nv_bfloat162, T>;
+        Low low = {};
         unsigned row = row0, block = block0;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
@@ -166,6 +220,7 @@ block_quant_kernel(const BqP p)
             for (int j = 0; j < PER; ++j) {
                 floats(a[i][j], v[j]);
                 if (GATED) {
+                    if constexpr (FAR) low = lowest(low, a[i][j]);
                     float2 up[HALF];
                     floats(b[i][j], up);
 #pragma unroll
@@ -185,6 +240,12 @@ block_quant_kernel(const BqP p)
                 for (int j = 0; j < PER; ++j) store_rounded<T, VEC, EVEN>(q + j * LANES * VEC, v[j], d, p.k - col - j * LANES * VEC);
             }
             if (++block == (unsigned)p.blocks) block = 0, ++row;
+        }
+        if constexpr (FAR) {
+            float least;
+            if constexpr (std::is_same<Low, __nv_bfloat162>::value) least = fminf(__low2float(low), __high2float(low));
+            else least = to_f32(low);
+            if (__any_sync(0xffffffffu, least < BQ_FAR)) far_blocks<T, LANES>(p, u, AHEAD, lane);
         }
     }
 }

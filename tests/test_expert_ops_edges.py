@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 from paper_2607_19539_b200 import ops  # noqa: E402
 
-from tests.test_expert_ops import F8, INF, NAN, norm_of, status  # noqa: E402
+from tests.test_expert_ops import F8, INF, NAN, e4m3, norm_of, status  # noqa: E402
 from tests.test_ops import BF16, F16, F32, U, close, gen, normal  # noqa: E402
 
 gpu = pytest.mark.gpu
@@ -107,3 +107,35 @@ def test_longest_sums_in_16_bits(m, dtype, transposed):
     want = sum(pa[:, c:c + 65536].double() @ pb[:, c:c + 65536].double().t() for c in range(0, period, 65536)) * (k // period)
     assert not st.any()
     close(out, want, ((256 * 33 * 2.0 ** -23) + (4096 + 8) * 2.0 ** -24 + U[dtype]) * want)
+
+
+# ------------------------------------------------------------------------------------------------ quantiser
+
+@gpu
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_block_quant_gates_far_below_zero(dtype, shift):
+    """A gate far below zero leaves little of a value, but of a large one enough: exp(-87.4) is the last one whose reciprocal is a normal number.  Gate and value in 32 bits: the exponent is off by
+    |g| / ln 2 * 2^-24 twice (its factor and its rounding), the rest by 2^-20."""
+    k = 256
+    gates = [-1.0, -80.0, -86.5, -87.0, -87.5, -88.0, -88.5, -89.0, -90.0, -95.0, -100.0, -120.0, -140.0, -155.0, -160.0, -250.0, -1000.0, -1e30]
+    ups = [1.0, -1e-3, 1e30, 1e36, -3e38]
+    rows = len(gates) * len(ups)
+    x = torch.zeros((rows, 2 * k + 8), dtype=dtype, device="cuda")[:, shift:2 * k + shift]
+    g = torch.tensor(gates).repeat_interleave(len(ups))[:, None]
+    u = torch.tensor(ups).repeat(len(gates))[:, None]
+    spread = torch.linspace(0.25, 1.0, k)[None]
+    x[:, :k], x[:, k:] = (g * torch.where(torch.arange(k) % 3 == 0, 1.0, 0.99)).to("cuda"), (u * spread).to("cuda")
+    x[:, 5] = 0.0
+    x[1::2, 40:60], x[1::2, k + 40:k + 60] = 2.0, 3.0                      # ordinary ones beside them
+    q, scale = torch.empty((rows, k), dtype=F8, device="cuda"), torch.empty((rows, 2), device="cuda")
+    ops.moe_ovl_block_quant(x=x, q=q, scale=scale, gated=True)
+    gate, up = x[:, :k].double(), x[:, k:].double()
+    v = gate * torch.exp(gate.clamp_max(0)) / (1 + torch.exp(-gate.abs())) * up
+    most = v.abs().unflatten(1, (2, 128)).amax(2)
+    off = gate.abs().amax(1, keepdim=True).clamp_max(250.0) * 2.0 ** -23 + 2.0 ** -20
+    sure, none = most >= 2.0 ** -100 * (1 + off), most < 2.0 ** -100 * (1 - off)
+    assert not scale[none].any() and bool(((scale.double() - most / 448).abs() <= (2 * off + 2.0 ** -23) * most / 448)[sure].all())
+    t = (v.unflatten(1, (2, 128)) * 448 / most.clamp_min(1e-300)[..., None]).flatten(1)
+    got, whole = q.double(), sure.repeat_interleave(128, 1)
+    assert bool(((got >= e4m3(t - 2 * off * t.abs())) & (got <= e4m3(t + 2 * off * t.abs())))[whole].all()) and not got[none.repeat_interleave(128, 1)].any()
