@@ -172,11 +172,12 @@ def expert_ffn(rows, w1, w2, counts, status):
 
 
 def clip_gradients(parameters, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
-    """Scales the gradients of the parameters (or of one) that have one, so that their norm is max_norm at most; returns the norm before, on the device."""
-    parameters = [parameters] if isinstance(parameters, torch.Tensor) else parameters
+    """Scales the gradients of the parameters (or of one) that have one, so that their norm is max_norm at most; returns the norm before, on the gradients' device (where
+    there are none, 0 on the first parameter's)."""
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
     grads = [p.grad for p in parameters if p.grad is not None]
     if not grads:
-        return torch.zeros(1)
+        return torch.zeros(1, device=parameters[0].device if parameters else None)
     norm = torch.empty(1, device=grads[0].device)
     workspace = torch.empty(ops.moe_ovl_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device=norm.device)
     ops.moe_ovl_grad_norm(grads=grads, norm=norm, workspace=workspace)
