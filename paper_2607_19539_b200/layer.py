@@ -150,6 +150,8 @@ class ExpertProduct(torch.autograd.Function):
     def backward(ctx, dout):
         (rows, weight, counts), status = ctx.saved_tensors, ctx.status
         dout = dout.contiguous()
+        if dout.data_ptr() % 16:
+            dout = dout.clone()         # a piece of another tensor's gradient begins anywhere
         drows = dweight = None
         if ctx.needs_input_grad[0]:
             drows = torch.zeros_like(rows)
@@ -163,7 +165,7 @@ class ExpertProduct(torch.autograd.Function):
 
 def expert_ffn(rows, w1, w2, counts, status):
     """Rows grouped by expert ([n, d], counts [experts] int32) through their experts, for training: w1 [experts, 2F, d] (gate rows, then up rows), w2 [experts, d, F].
-    d and F have to be multiples of 8.  `status`: 4 int32 that the caller clears once; look at it after a synchronize of your own.  Gradients of gradients are refused.  Where a
+    d and F have to be multiples of 8, and rows and weights begin on 16 bytes.  `status`: 4 int32 that the caller clears once; look at it after a synchronize of your own.  Gradients of gradients are refused.  Where a
     step is captured into a graph, no eager step's result may live any more: torch would tie the leaves' gradients to that step's stream, which no capture can wait for."""
     counts = counts.clone()             # the router's buffer may hold the next batch's by the time of the backward pass
     gate, up = ExpertProduct.apply(rows, w1, counts, status).float().chunk(2, dim=1)

@@ -16,3 +16,17 @@ def test_clip_gradients_without_any_is_on_the_parameters_device():
         norm = L.clip_gradients(parameters, 1.0)
         assert norm.device == p.device and norm.dtype is torch.float32 and norm.tolist() == [0.0]
     assert L.clip_gradients([], 1.0).tolist() == [0.0]
+
+
+@gpu
+@pytest.mark.parametrize("product", [False, True])
+def test_gradients_that_begin_anywhere(product):
+    """What arrives on the way back is a piece of another tensor's gradient, contiguous, behind one value: not on 16 bytes.  The gradients are those of the same values on a boundary."""
+    leaves, dout, status = training_leaves(40, 64, 32, 2, 9)
+    counts = torch.tensor([15, 25], dtype=torch.int32, device="cuda")
+    out = L.ExpertProduct.apply(*leaves[:2], counts, status) if product else L.expert_ffn(*leaves, counts, status)
+    used = leaves[:2] if product else leaves
+    want = torch.autograd.grad(out, used, dout, retain_graph=True)
+    first = torch.zeros(1, dtype=out.dtype, device="cuda")
+    got = torch.autograd.grad(torch.cat([first, out.flatten()]), used, torch.cat([first, dout.flatten()]))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and not status.any()
