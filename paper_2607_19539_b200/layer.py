@@ -47,6 +47,8 @@ class QuantExpertLayer:
     Buffers are sized for `max_tokens` and reused by every call on the current stream; `status[0]` is not 0 when a bounded wait inside a product
     gave up, and the outputs since then are not to be used (nothing waits for it here: look after a synchronize of your own)."""
 
+    eight = torch.int8              # what rows and weights are held in
+
     def __init__(self, norm_weight, router, w1, w2, *, top_k: int, max_tokens: int, eps: float = 1e-6, score: int = ops.SCORE_SOFTMAX, bias=None,
                  num_groups: int = 1, top_groups: int = 1, group_best: int = 1, renormalise: bool = True, gate_scale: float = 1.0):
         self.norm_weight, self.router, self.eps, self.k = norm_weight, router, eps, top_k
@@ -58,22 +60,31 @@ class QuantExpertLayer:
                            gate_scale=gate_scale)
         dev, t, rows = w1.device, max_tokens, max_tokens * top_k
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
-        self.y, self.q, self.scale = new(t, self.d, dtype=w1.dtype), new(t, self.d, dtype=torch.int8), new(t)
+        self.y, self.q, self.scale = new(t, self.d, dtype=w1.dtype), new(t, self.d, dtype=self.eight), new(*self.scales(t, self.d))
         self.expert, self.gate, self.counts = new(t, top_k, dtype=torch.int32), new(t, top_k), new(self.experts, dtype=torch.int32)
-        self.gate_up, self.hidden, self.hidden_scale = new(rows, 2 * self.f, dtype=w1.dtype), new(rows, self.f, dtype=torch.int8), new(rows)
+        self.gate_up, self.hidden, self.hidden_scale = new(rows, 2 * self.f, dtype=w1.dtype), new(rows, self.f, dtype=self.eight), new(*self.scales(rows, self.f))
         self.rows_out = new(rows, self.d, dtype=w1.dtype)
         self.status = torch.zeros(4, dtype=torch.int32, device=dev)
+
+    def scales(self, rows: int, k: int) -> tuple:
+        """The shape of the scales of rows of k values."""
+        return (rows,)
 
     def hold(self, w1, w2) -> None:
         """Keeps the experts' weights in 8 bits."""
         self.w1, self.s1 = quantise_channels(w1)
         self.w2, self.s2 = quantise_channels(w2)
 
-    def route(self, x, residual=None, residual_out=None) -> RoutedRows:
-        """Norm (bf16 for the router, 8 bits for the experts) and choice; self.y, self.q and self.scale hold the normed rows."""
+    def norm(self, x, residual, residual_out) -> None:
+        """The normed rows, as they are and in 8 bits, into self.y, self.q and self.scale."""
         t = x.shape[0]
         ops.moe_ovl_add_norm(x=x, residual=residual, weight=self.norm_weight, eps=self.eps, residual_out=residual_out, y=self.y[:t], q=self.q[:t],
                              scale=self.scale[:t])
+
+    def route(self, x, residual=None, residual_out=None) -> RoutedRows:
+        """Norm (bf16 for the router, 8 bits for the experts) and choice; self.y, self.q and self.scale hold the normed rows."""
+        t = x.shape[0]
+        self.norm(x, residual, residual_out)
         logits = self.y[:t] @ self.router.t()
         ops.moe_ovl_route(logits=logits, expert=self.expert[:t], gate=self.gate[:t], counts=self.counts, **self.choice)
         return routed_rows(self.expert[:t], self.gate[:t], self.counts)
@@ -112,24 +123,29 @@ def quantise_blocks(w: torch.Tensor):
 class BlockExpertLayer(QuantExpertLayer):
     """The same layer with its experts in 8-bit floats: a scale per 128 values of a row and per 128 x 128 weights.  d and F have to be multiples of 16."""
 
+    eight = ops.FLOAT8
+
+    def scales(self, rows: int, k: int) -> tuple:
+        return (rows, -(-k // ops.BLOCK))
+
     def hold(self, w1, w2) -> None:
         if self.d % 16 or self.f % 16:
             raise B.MoeOvlError(B.ERR_UNSUPPORTED, "BlockExpertLayer: d and F have to be multiples of 16")
         self.w1, self.s1 = quantise_blocks(w1)
         self.w2, self.s2 = quantise_blocks(w2)
 
+    def norm(self, x, residual, residual_out) -> None:
+        t = x.shape[0]
+        ops.moe_ovl_add_norm(x=x, residual=residual, weight=self.norm_weight, eps=self.eps, residual_out=residual_out, y=self.y[:t])
+        ops.moe_ovl_block_quant(x=self.y[:t], q=self.q[:t], scale=self.scale[:t])
+
     def experts_of(self, r: RoutedRows):
-        n, token, dev = r.token.shape[0], r.token, r.token.device
-        t = n // self.k
-        q = torch.empty((t, self.d), dtype=ops.FLOAT8, device=dev)
-        scale = torch.empty((t, self.s1.shape[-1]), device=dev)
-        ops.moe_ovl_block_quant(x=self.y[:t], q=q, scale=scale)
-        hidden = torch.empty((n, self.f), dtype=ops.FLOAT8, device=dev)
-        hidden_scale = torch.empty((n, self.s2.shape[-1]), device=dev)
-        rows = q.view(torch.uint8)[token].view(ops.FLOAT8)          # torch gathers bytes
-        ops.moe_ovl_block_matmul(a=rows, a_scale=scale[token], b=self.w1, b_scale=self.s1, out=self.gate_up[:n], expert_counts=r.counts, status=self.status)
-        ops.moe_ovl_block_quant(x=self.gate_up[:n], q=hidden, scale=hidden_scale, gated=True)
-        ops.moe_ovl_block_matmul(a=hidden, a_scale=hidden_scale, b=self.w2, b_scale=self.s2, out=self.rows_out[:n], expert_counts=r.counts, status=self.status)
+        n, token = r.token.shape[0], r.token
+        rows = self.q.view(torch.uint8)[token].view(ops.FLOAT8)     # torch gathers bytes
+        ops.moe_ovl_block_matmul(a=rows, a_scale=self.scale[token], b=self.w1, b_scale=self.s1, out=self.gate_up[:n], expert_counts=r.counts, status=self.status)
+        ops.moe_ovl_block_quant(x=self.gate_up[:n], q=self.hidden[:n], scale=self.hidden_scale[:n], gated=True)
+        ops.moe_ovl_block_matmul(a=self.hidden[:n], a_scale=self.hidden_scale[:n], b=self.w2, b_scale=self.s2, out=self.rows_out[:n], expert_counts=r.counts,
+                                 status=self.status)
         return self.rows_out[:n]
 
 
