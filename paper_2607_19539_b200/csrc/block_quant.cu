@@ -159,7 +159,7 @@ __device__ __forceinline__ float any_gate(float g, float u)
 }
 // Gated blocks that have such gates, once more and value by value: `count` of them from `u` on, by LANES lanes.  Out of the way of the others, which would pay for it with registers (8192 x 14336, bf16: 130 us
 // with the choice inside their loop, 98 with a vote at its end and 98 without any).
-template <typename T, int LANES> __device__ __noinline__ void far_blocks(const BqP &p, unsigned u, int count, int lane)
+template <typename T, int LANES> __device__ __noinline__ void far_blocks(BqP p, unsigned u, int count, int lane)
 {
     __syncwarp();                            // behind what the lanes have stored
     for (; count > 0; --count, ++u) {
@@ -179,11 +179,11 @@ template <typename T, int LANES> __device__ __noinline__ void far_blocks(const B
         }
     }
 }
-// Bound by HBM (8192 x 14336, bf16: 58 us, 6.1 TB/s; with the gate, whose instructions come next, 98-101 us, 5.9 TB/s; f16 94, f32 159).  Eight lanes for a block of 128 values, not sixteen with a pack each: the maximum's shuffles and what a block
+// Bound by HBM (8192 x 14336, bf16: 58 us, 6.1 TB/s; with the gate, whose instructions come next, 98-101 us, 5.9 TB/s; f32 159).  Eight lanes for a block of 128 values, not sixteen with a pack each: the maximum's shuffles and what a block
 // costs besides its values weigh half as much (96 -> 58 us).  Rows that begin anywhere go element by element (8192 x 14335: 153 us).
 template <typename T, int VEC, bool GATED, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
-block_quant_kernel(const __grid_constant__ BqP p)
+block_quant_kernel(const BqP p)
 {
     using Shape = BqShape<T, VEC, GATED>;
     constexpr int LANES = Shape::LANES, PER = Shape::PER, AHEAD = Shape::AHEAD, HALF = (VEC + 1) / 2;
