@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 from paper_2607_19539_b200 import ops  # noqa: E402
 
-from tests.test_expert_ops import F8, INF, NAN, e4m3, norm_of, status  # noqa: E402
+from tests.test_expert_ops import F8, INF, NAN, check_grouped, e4m3, norm_of, status, whole  # noqa: E402
 from tests.test_ops import BF16, F16, F32, U, close, gen, normal  # noqa: E402
 
 gpu = pytest.mark.gpu
@@ -107,6 +107,22 @@ def test_longest_sums_in_16_bits(m, dtype, transposed):
     want = sum(pa[:, c:c + 65536].double() @ pb[:, c:c + 65536].double().t() for c in range(0, period, 65536)) * (k // period)
     assert not st.any()
     close(out, want, ((256 * 33 * 2.0 ** -23) + (4096 + 8) * 2.0 ** -24 + U[dtype]) * want)
+
+
+@gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("k", [4088, 4096, 4104, 8192, 8200, 12352])
+def test_sums_of_some_pieces(k, transposed):
+    """Whole numbers, whose sums are exact however they are cut: one piece of 4096, two, three, and a little more, on tiles of every width."""
+    g = gen(k)
+    for counts in ([1], [13], [30, 0, 2], [64], [130], [100, 0, 129, 1], [300, 700], [40] * 9):
+        m, n = sum(counts), 264
+        for dtype in (BF16, F16):
+            a, b = whole(g, (m, k), dtype, 2), whole(g, (len(counts), k, n) if transposed else (len(counts), n, k), dtype, 2)
+            check_grouped(a, b, counts, transposed, dtype)
+    a, b = whole(g, (33, k), BF16, 2), whole(g, (k, 20000) if transposed else (20000, k), BF16, 2)        # more tiles than SMs
+    check_grouped(a[:13], b, None, transposed, BF16)
+    check_grouped(a, b, None, transposed, BF16)
 
 
 # ------------------------------------------------------------------------------------------------ quantiser
