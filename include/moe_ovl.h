@@ -570,8 +570,8 @@ typedef struct {
 } moe_ovl_grouped_matmul_args;
 int moe_ovl_grouped_matmul(const moe_ovl_grouped_matmul_args *args);
 
-/* Gradient of its weights:  dweight[e][n][k] (+)= sum over the rows m of expert e of dy[m][n] * x[m][k], in 32 bits, each value by one
- * thread in the order of the rows (the same call gives the same bits).  An expert without rows gets zeros, or with `accumulate` keeps what it has; rows behind
+/* Gradient of its weights:  dweight[e][n][k] (+)= sum over the rows m of expert e of dy[m][n] * x[m][k], in 32 bits.  The order is fixed for
+ * given sizes: pieces of an expert's rows, the pieces one after the other, and where a cluster shares them its CTAs' parts in their order (the same call gives the same bits).  An expert without rows gets zeros, or with `accumulate` keeps what it has; rows behind
  * the last expert's are not looked at.  For b [num_experts, k, n] pass x as dy and dy as x. */
 typedef struct {
     uint32_t struct_size;
@@ -606,8 +606,8 @@ int moe_ovl_grouped_matmul_backward(const moe_ovl_grouped_matmul_backward_args *
 typedef struct {
     uint32_t struct_size;
     int32_t device;
-    int32_t depth;                /* matrices; 1 without `tiles` */
-    int32_t rows, k;              /* of q */
+    int32_t depth;                /* matrices, at most 65535; 1 without `tiles` */
+    int32_t rows, k;              /* of q; with `tiles` at most 65535 * 128 rows */
     int32_t dtype;                /* of x: MOE_OVL_BF16 ... */
     int32_t gated, tiles;         /* 0 or 1, not both */
     uint32_t flags;               /* 0 */
@@ -622,7 +622,8 @@ int moe_ovl_block_quant(const moe_ovl_block_quant_args *args);
 
 /* Product of 8-bit floats with a scale for each block of 128, dense or per expert as moe_ovl_quant_matmul:
  *   out[m][n] = sum over the blocks B of K of a_scale[m][B] * b_scale[e][n / 128][B] * (sum over k in B of a[m][k] * b[e][n][k])
- * in 32 bits, rounded once.  Operands as moe_ovl_block_quant writes them, b with `tiles`. */
+ * in 32 bits, rounded once; the two scales are multiplied with each other first, so their product has to be in the range of 32 bits.  Operands as moe_ovl_block_quant
+ * writes them, b with `tiles`. */
 typedef struct {
     uint32_t struct_size;
     int32_t device;

@@ -180,7 +180,7 @@ template <typename T, int LANES> __device__ __noinline__ void far_blocks(BqP p, 
     }
 }
 // Bound by HBM (8192 x 14336, bf16: 58 us, 6.1 TB/s; with the gate, whose instructions come next, 98-101 us, 5.9 TB/s; f32 159).  Eight lanes for a block of 128 values, not sixteen with a pack each: the maximum's shuffles and what a block
-// costs besides its values weigh half as much (96 -> 58 us).  Rows that begin anywhere go element by element (8192 x 14335: 153 us).
+// costs besides its values weigh half as much (96 -> 58 us).  Rows that begin anywhere go element by element (8192 x 14335: 153 us, gated 219-230).
 template <typename T, int VEC, bool GATED, bool EVEN>
 __global__ void __launch_bounds__(BQ_THREADS)
 block_quant_kernel(const BqP p)

@@ -3,7 +3,7 @@
 // A list goes to the kernel as a parameter, up to LIST_LONG tensors per launch, so no table has to be copied or kept on the device.  The
 // elements of all its tensors are dealt out in chunks, a contiguous run of them to each block, which finds its first tensor by bisection
 // and walks on from there.  Squares are summed in 32 bits over a thread's share of a chunk (64 values at most, two sums of 32) and in 64 bits beyond; a share whose 32-bit
-// sum overflows, or is so small that squares may have vanished, is summed again in 64.  Every block's sum has its place in the workspace (or, of a small
+// sum overflows, is not a number, or is so small that squares may have vanished, is summed again in 64, over the same values.  Every block's sum has its place in the workspace (or, of a small
 // list, in its shared memory) and one block adds them up in order: the same call gives the same bits.
 #include <algorithm>
 
@@ -155,7 +155,7 @@ grad_norm_kernel(const __grid_constant__ TensorList<N> list, double *partial)
 }
 
 // Small lists: one cluster, whose first block adds up the blocks' sums: one launch less, 1.7 us of the caller's time.  Bound by latency: 3.9 us on the device for
-// eight chunks and 4.3 in two kernels, 5.7 and 4.7 for ten, whose blocks take two in a row; with 24 the second kernel is the better one in every respect.
+// eight chunks and 4.3 in two kernels, 5.7 and 4.7 for ten, whose blocks take two in a row, less than the caller's time that they save (in a captured step two kernels would be the faster); with 24 the second kernel is the better one in every respect.
 constexpr int GN_CLUSTER = 8, GN_SMALL = 16;         // blocks; most chunks
 template <int N>
 __global__ void __launch_bounds__(GN_THREADS)
